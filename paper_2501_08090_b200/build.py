@@ -10,7 +10,7 @@ _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = [os.path.join(CSRC, "ckv_api.cu"), os.path.join(CSRC, "ckv_autoscaler.cc"),
            os.path.join(CSRC, "ckv_global_sim.cc")]
-HEADERS = [os.path.join(CSRC, "ckv_device.cuh"), os.path.join(_ROOT, "include", "chiron_kv.h"),
+HEADERS = [os.path.join(CSRC, "ckv_common.cuh"), os.path.join(CSRC, "ckv_device.cuh"), os.path.join(CSRC, "ckv_host.cuh"), os.path.join(_ROOT, "include", "chiron_kv.h"),
            os.path.join(_ROOT, "include", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
 

@@ -5,35 +5,21 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
 
 #include "ckv_device.cuh"
+#include "ckv_host.cuh"
+
+using ckv::aligned16;
+using ckv::check_call;
+using ckv::check_device;
+using ckv::fail;
+using ckv::WorkspaceLayout;
 
 namespace {
-
-thread_local char g_error[512] = "";
-
-int32_t fail(int32_t code, const char *fmt, ...)
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_error, sizeof g_error, fmt, ap);
-    va_end(ap);
-    return code;
-}
-
-#define CKV_CUDA(call)                                                                        \
-    do {                                                                                      \
-        cudaError_t e_ = (call);                                                              \
-        if (e_ != cudaSuccess)                                                                \
-            return fail(CKV_ECUDA, "%s failed: %s (%s:%d)", #call, cudaGetErrorString(e_),    \
-                        __FILE__, __LINE__);                                                  \
-    } while (0)
 
 // Attention kernel shapes: warps per CTA (one CTA per SM) and ring stages per warp.
 #ifndef CKV_WARPS128
@@ -77,12 +63,6 @@ bool config_ok(const ckv_config *c, const char **why)
     if (tiles >= (1ll << 31)) { *why = "max_batch * max context has 2^31 or more tiles"; return false; }
     return true;
 }
-
-struct WorkspaceLayout {
-    size_t status, header, span_start, part, arrivals, trace;
-    size_t st_tables, st_lens, st_q, st_k, st_v, st_out;
-    size_t total;
-};
 
 WorkspaceLayout carve(const ckv_config &c)
 {
@@ -148,27 +128,6 @@ int32_t encode_pool_map(const ckv_config *cfg, const void *d_pool, CUtensorMap *
 
 }  // namespace
 
-struct ckv_pool {
-    ckv_config cfg;
-    int device;
-    int num_sms;
-    int num_spans;                   // partition width: one span per warp of the attention kernel
-    uint8_t *d_pool;
-    uint8_t *d_ws;
-    WorkspaceLayout ws;
-    CUtensorMap tmap;
-    int64_t launches;
-    bool profile;
-    bool overlap;                    // launch kernels with programmatic stream serialization
-    bool pool_written;               // a kernel other than the fused step wrote the pool since the last attention launch
-    bool inputs_from_predecessor;    // the next attention launch reads tables and lengths its predecessor in the stream writes
-    int host_route;                  // decode_step_host: CKV_HOST_ROUTE_*
-    std::vector<cudaEvent_t> ev;     // pairs (start, stop)
-    int ev_used;
-
-    template <typename T> T *wsp(size_t off) const { return reinterpret_cast<T *>(d_ws + off); }
-};
-
 namespace {
 
 template <int D, int W, int S, bool kMulti>
@@ -195,27 +154,6 @@ int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t
     CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, ap));
     return CKV_OK;
 }
-
-int32_t check_device(const ckv_pool *pool, const char *fn)
-{
-    if (!pool) return fail(CKV_EINVAL, "%s: pool is NULL", fn);
-    int current = -1;
-    if (cudaGetDevice(&current) != cudaSuccess || current != pool->device)
-        return fail(CKV_EINVAL, "%s: the pool lives on device %d but device %d is current", fn, pool->device, current);
-    return CKV_OK;
-}
-
-int32_t check_call(ckv_pool *pool, int32_t layer, int32_t batch, const char *fn)
-{
-    if (int32_t rc = check_device(pool, fn)) return rc;
-    if (layer < 0 || layer >= pool->cfg.num_layers)
-        return fail(CKV_EINVAL, "%s: layer %d outside [0, %d)", fn, layer, pool->cfg.num_layers);
-    if (batch < 1 || batch > pool->cfg.max_batch)
-        return fail(CKV_EINVAL, "%s: batch %d outside [1, %d]", fn, batch, pool->cfg.max_batch);
-    return CKV_OK;
-}
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int32_t launch_plan(ckv_pool *pool, int32_t batch, const int32_t *d_seq_lens, cudaStream_t stream)
 {
@@ -291,7 +229,7 @@ int32_t launch_read_probe(ckv_pool *pool, const ckv::ProbeParams &pp, cudaStream
 
 extern "C" {
 
-const char *ckv_last_error(void) { return g_error; }
+const char *ckv_last_error(void) { return ckv::g_error; }
 
 size_t kv_pool_bytes(const ckv_config *cfg)
 {

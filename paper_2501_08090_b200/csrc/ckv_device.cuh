@@ -5,28 +5,9 @@
 // contiguous block of 32 rows (16 key rows, then 16 value rows) of d elements.
 #pragma once
 
-#include <cuda.h>            // CUtensorMap (type only; the driver library is not linked)
-#include <cuda_runtime.h>
-#include <stdint.h>
+#include "ckv_common.cuh"
 
 namespace ckv {
-
-constexpr int kPageSize = 16;        // tokens per page
-#ifndef CKV_PAGES_PER_TILE
-#define CKV_PAGES_PER_TILE 2
-#endif
-constexpr int kPagesPerTile = CKV_PAGES_PER_TILE;   // a tile is the scheduling unit: 32 tokens of one (request, kv head)
-constexpr int kTileTokens = kPageSize * kPagesPerTile;
-constexpr int kMaxGroup = 8;         // query heads per KV head handled by one MMA column block
-constexpr int kMaxSpans = 2048;      // upper bound on the partition width (one span per warp)
-constexpr int kMaxBatch = 8192;
-constexpr int kTreeFrom = 24;        // pairs cut into more partials than this are merged in two levels
-
-constexpr uint32_t kStatusBadLength = 1u;
-constexpr uint32_t kStatusBadPage = 2u;
-constexpr uint32_t kStatusWaitLimit = 4u;
-
-constexpr unsigned long long kWaitLimitNs = 1000000000ull;   // bound of every device-side wait
 
 // The split-KV partition.  Work is laid out on one axis of "units", request-major, then kv head:
 // every (request, kv head) contributes kPieceCostTiles overhead units (the fixed cost of starting,
@@ -52,14 +33,6 @@ struct PlanHeader {
     int32_t num_spans;
     int32_t spans_with_units;
 };
-
-// A context length is usable if min_len <= L <= table capacity (min_len = the number of new
-// tokens of the step, 1 for plain decode); otherwise the request has no tiles.
-__host__ __device__ __forceinline__ int tiles_of_length(int L, int max_pages_per_req, int min_len = 1)
-{
-    if (L < min_len || (long long)L > (long long)max_pages_per_req * kPageSize) return 0;
-    return (L + kTileTokens - 1) / kTileTokens;
-}
 
 // ------------------------------------------------------------------------------------------
 // K1: KV append.  One thread moves one 16-byte piece of one new key or value row.
@@ -311,168 +284,6 @@ __global__ void splitkv_plan_kernel(const PlanParams p)
             }
         }
     }
-}
-
-// ------------------------------------------------------------------------------------------
-// PTX wrappers
-// ------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t smem_u32(const void *ptr)
-{
-    return (uint32_t)__cvta_generic_to_shared(ptr);
-}
-
-__device__ __forceinline__ unsigned long long global_timer_ns()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-
-__device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done;
-}
-
-// Wait for a phase of an mbarrier, giving up after kWaitLimitNs.  Returns false when it gave up;
-// the status word is flagged and the caller stops working.
-__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, uint32_t *status,
-                                                  unsigned long long limit_ns = kWaitLimitNs)
-{
-    if (mbar_try_wait(bar, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
-    for (;;) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (global_timer_ns() - t0 > limit_ns) {
-            atomicOr(status, kStatusWaitLimit);
-            return false;
-        }
-    }
-}
-
-// L2 policy for data that is read once: such lines are the first to be evicted, so the stream of KV
-// tiles does not push tables, queries and partial results out of the cache.
-__device__ __forceinline__ uint64_t l2_evict_first_policy()
-{
-    uint64_t policy;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    return policy;
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar, uint64_t policy)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "l"(policy) : "memory");
-}
-
-// Programmatic dependent launch: a kernel launched with the stream-serialization attribute may
-// start while its predecessor in the stream still runs.  grid_dependency_wait() blocks until the
-// predecessor has completed and its writes are visible; without the attribute it returns at once.
-// Start fetching a tensor map (a kernel parameter) so that the first tile load does not wait for it.
-__device__ __forceinline__ void prefetch_tensormap(const CUtensorMap *map)
-{
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
-}
-
-__device__ __forceinline__ void grid_dependency_wait()
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-
-__device__ __forceinline__ void grid_launch_dependents()
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-
-// 1-D bulk copy global -> shared, completion counted in bytes on an mbarrier (16-byte aligned, size % 16 == 0)
-__device__ __forceinline__ void bulk_load_1d(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-
-__device__ __forceinline__ float4 ld_shared_f32x4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ void fence_proxy_async()
-{
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-
-// D(16x8, fp32) += A(16x16, bf16, row) * B(16x8, bf16, col)
-__device__ __forceinline__ void mma_bf16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
-{
-    uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
-    return d;
-}
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
-{
-    uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ float ld_cg_f32(const float *p)
-{
-    float v;
-    asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p));
-    return v;
-}
-
-__device__ __forceinline__ float4 ld_cg_f32x4(const float *p)
-{
-    float4 v;
-    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
-    return v;
 }
 
 // ------------------------------------------------------------------------------------------
