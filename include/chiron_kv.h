@@ -159,6 +159,131 @@ int32_t decode_attention_multi(ckv_pool *pool, int32_t layer, int32_t batch, int
                                const void *d_q, void *d_out, void *stream);
 
 /*
+ * Append with rotation (rotary position embedding): the queries and keys of a step's new tokens are
+ * turned by their positions, the turned keys and the values go to their pages and the turned queries
+ * to d_q_out -- what stands between an instance's projections and its attention, in one kernel, for
+ * decode steps, drafted tokens and prompts alike (Section 2.1 "Inference Primer").
+ *
+ * Pair j of a head (j < rotary_dim / 2) of a token at position t becomes
+ *   x' = scale * (x cos a - y sin a),  y' = scale * (y cos a + x sin a),   a = t * d_inv_freq[j],
+ * where (x, y) are elements (j, j + rotary_dim/2), or (2j, 2j + 1) if `interleaved` is not 0;
+ * elements from rotary_dim on are copied, and so are the values, bit-exactly.  The angle is formed in
+ * 64 bits; each result is rounded once to bf16.  scale is 1 unless a scheme for extended contexts
+ * asks for another factor (it applies to queries and keys).
+ *
+ *   d_new_start   int32 [batch + 1], not decreasing: request r's new tokens are rows new_start[r] ..
+ *                 new_start[r+1] - 1 of q, k_new, v_new and q_out (none is fine), at positions
+ *                 seq_lens[r] - n_r .. seq_lens[r] - 1, n_r their number.  Rows before new_start[0] and
+ *                 from new_start[batch] on (padding, up to n_tokens) are neither read for the cache
+ *                 nor written.  NULL: n_tokens / batch tokens each.
+ *   d_seq_lens    lengths AFTER the append, as everywhere.  A request with new tokens and a length
+ *                 below their number or beyond the table is unusable: status bit, its rows of q_out
+ *                 zero-filled, nothing appended.  A page id outside the pool: status bit, that row is not
+ *                 appended.
+ *   d_q, d_k_new, d_v_new, d_q_out   bf16 rows [n_tokens][heads][head_dim], 16-byte aligned, each with its
+ *                 own stride between tokens in elements (a multiple of 8, at least heads * head_dim), so
+ *                 that they may lie side by side in one projection's output.  d_q_out may be d_q (same
+ *                 stride); it must not overlap the others' rows.  d_q and d_q_out may both be NULL.
+ *   d_inv_freq    fp32 [rotary_dim / 2];  rotary_dim: a multiple of 16, 16 .. head_dim.
+ * n_tokens = 0 does nothing.  Errors: CKV_EINVAL, CKV_ECUDA.
+ */
+int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens,
+                       const int32_t *d_block_tables, const int32_t *d_seq_lens,
+                       const int32_t *d_new_start, const float *d_inv_freq, int32_t rotary_dim,
+                       int32_t interleaved, float scale, const void *d_q, int64_t q_stride,
+                       const void *d_k_new, int64_t k_stride, const void *d_v_new, int64_t v_stride,
+                       void *d_q_out, int64_t q_out_stride, void *stream);
+
+/*
+ * Page-sparse decode attention: for long contexts, each (request, KV head) attends to the `budget`
+ * pages whose keys can matter most to its new token, instead of to all of them; the iteration's time then stops
+ * growing with the context (the "self-attention computation" of Section 2.3).  It reads an index of the
+ * cache that is 1/30 of its size, and `budget` pages.
+ *
+ * The index (caller-owned, kv_index_bytes(), 16-byte aligned) holds for every (layer, page, KV head)
+ * lower and upper bounds of the page's keys, channel by channel, as 8-bit whole numbers of steps of a
+ * power of two:  int8 records[layers][pages][Hkv][2 (lo, hi)][head_dim], then float
+ * steps[layers][pages][Hkv], with lo * step <= k <= hi * step.  With m the largest |k| of the page and
+ * head (2^-100 if smaller), step = 2^(floor(log2 m) - 6), doubled if ceil(m / step) > 127; lo is rounded
+ * down, hi up.  A page with an infinity or a NaN in its keys gets lo = -127, hi = 127, step = 2^121.
+ * Its bits depend on the keys alone.
+ *
+ *   kv_index_update   (re)computes the records of the pages that hold the last `last_tokens` tokens of
+ *                     each request (0: all its pages), from the pool.  Call it after an append, with the
+ *                     appended count, or at least before a page leaves the `recent` ones: those
+ *                     are attended to without being looked up.  A page that requests share must be full
+ *                     in all of them.  Unusable lengths and page ids: status bit, skipped.
+ *   kv_index_values   the bounds of a layer as numbers (lo * step, hi * step, exact): bf16
+ *                     [num_pages][Hkv][2][head_dim], 16-byte aligned.
+ *   decode_select_pages   chooses pages for the batch's new queries (d_q bf16 [batch][Hq][head_dim],
+ *                     16-byte aligned).  A request of n > budget pages keeps its first `sink` and last
+ *                     `recent` pages and, of the others, the budget - sink - recent with the highest scores,
+ *                     equal ones from the front.  A page's score for a KV head is the largest over the group's
+ *                     query heads of  qstep * step * sum_x max(q8[x] lo[x], q8[x] hi[x]),  q8 = q in whole
+ *                     steps (nearest, ties to even, within 127) of qstep = 2^(floor(log2 max|q|) - 6).  Scores
+ *                     are compared exactly, except that fp32 rounds one that is below 2^-104 of
+ *                     what the group's largest query step and a page step of 1 give.  Infinities and NaN in q count as 0 here.  Requests of at most `budget` pages keep
+ *                     all of them.
+ *                       d_pages  int32 [batch][Hkv][budget]: page ids in context order, then -1s
+ *                       d_lens   int32 [batch]: tokens in the chosen pages (0 for an unusable length)
+ *   decode_attention_pages   decode_attention over such a list: d_pages and d_lens take the places of block
+ *                     tables and lengths, with a row of `budget` pages per (request, KV head).  It may
+ *                     directly follow the kernel that writes them.
+ *   decode_attention_sparse  both, in two launches.
+ * 1 <= recent, 0 <= sink, sink + recent <= budget; max_pages_per_req <= 49152 for selection.
+ * Errors: CKV_EINVAL, CKV_ENOMEM (index too small), CKV_ECUDA.
+ */
+size_t kv_index_bytes(const ckv_config *cfg);
+int32_t kv_index_update(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
+                        const int32_t *d_seq_lens, int32_t last_tokens, void *d_index,
+                        size_t index_bytes, void *stream);
+int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size_t index_bytes,
+                        void *d_out, void *stream);
+int32_t decode_select_pages(ckv_pool *pool, int32_t layer, int32_t batch,
+                            const int32_t *d_block_tables, const int32_t *d_seq_lens, const void *d_q,
+                            const void *d_index, size_t index_bytes, int32_t budget, int32_t sink,
+                            int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream);
+int32_t decode_attention_pages(ckv_pool *pool, int32_t layer, int32_t batch, int32_t budget,
+                               const int32_t *d_pages, const int32_t *d_lens, const void *d_q,
+                               void *d_out, void *stream);
+int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch,
+                                const int32_t *d_block_tables, const int32_t *d_seq_lens,
+                                const void *d_q, const void *d_index, size_t index_bytes,
+                                int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages,
+                                int32_t *d_lens, void *d_out, void *stream);
+
+/*
+ * Verification of drafted tokens (speculative decoding, the multi-token step's purpose): which of a
+ * request's drafted tokens stand, and the token that follows them, so that the result is
+ * distributed as the target model's own tokens are.  With p_j, q_j the target's and the draft's
+ * probabilities at draft j and u in [0, 1) given:
+ *   draft j is accepted while  u_accept[j] * q_j(x_j) < p_j(x_j);
+ *   at the first refusal j the next token is drawn from the weights max(p_j - q_j, 0) (from p_j where
+ *   they are all 0); after n acceptances it is drawn from p_n;
+ *   drawn: the first token whose running sum of weights exceeds u_sample * (sum of the weights).
+ * Products, differences and sums are in fp64.  A NaN weight counts as 0; a row without any weight
+ * gives token -1.  A drafted token outside the vocabulary is refused.  Runs on the current device and needs no pool.
+ *   dtype            CKV_PROBS_F32 or CKV_PROBS_BF16, of both probability arrays
+ *   d_draft_tokens   int32 [batch][max_draft]
+ *   d_draft_lens     int32 [batch], drafts of each request (clamped to 0 .. max_draft); NULL: max_draft
+ *   d_target_probs   [batch][max_draft + 1] rows of `vocab`, target_stride (>= vocab) elements apart
+ *   d_draft_probs    [batch][max_draft] rows, draft_stride apart; NULL: each draft is a point mass (a
+ *                    lookup), so it is accepted with p_j(x_j), and refusal draws from p_j without x_j
+ *   d_u_accept       fp32 [batch][max_draft];  d_u_sample fp32 [batch]
+ *   d_tokens         int32 [batch][max_draft + 1]: the accepted drafts, the drawn token, then -1s
+ *   d_accepted       int32 [batch]: number of accepted drafts
+ * Rows are read where they decide something; the rest of the arrays is not touched.
+ * Errors: CKV_EINVAL, CKV_ECUDA.
+ */
+#define CKV_PROBS_F32  0
+#define CKV_PROBS_BF16 1
+int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dtype,
+                     const int32_t *d_draft_tokens, const int32_t *d_draft_lens,
+                     const void *d_target_probs, int64_t target_stride, const void *d_draft_probs,
+                     int64_t draft_stride, const float *d_u_accept, const float *d_u_sample,
+                     int32_t *d_tokens, int32_t *d_accepted, void *stream);
+
+/*
  * The split-KV partition decode_attention uses for these lengths, copied to the host for
  * inspection (runs a small kernel and synchronises `stream`; decode_attention itself derives the
  * same partition inside its attention kernel and launches no plan kernel).  A "tile" is 32

@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
 
 CKV_OK, CKV_EINVAL, CKV_ENOMEM, CKV_ECUDA, CKV_EBOUNDS, CKV_ETIMEOUT = 0, -1, -2, -3, -4, -5
+PROBS_F32, PROBS_BF16 = 0, 1
 STATUS_BAD_LENGTH, STATUS_BAD_PAGE, STATUS_WAIT_LIMIT = 1, 2, 4
 HOST_ROUTE_AUTO, HOST_ROUTE_STAGED, HOST_ROUTE_DIRECT, HOST_ROUTE_COPY = 0, 1, 2, 3
 TILE_TOKENS, PIECE_COST_TILES = 32, 3      # the plan's tile size and per-piece overhead units
@@ -28,6 +29,8 @@ EXPORTS = (
     "ckv_launch_count", "ckv_last_error", "ckv_read_span_trace", "ckv_set_overlap",
     "decode_attention_noalloc", "decode_step", "kv_swap_out", "kv_swap_in",
     "kv_append_multi", "decode_attention_multi", "kv_read_probe", "ckv_wait_limit_selftest", "ckv_set_host_route",
+    "kv_append_rope", "kv_index_bytes", "kv_index_update", "kv_index_values", "decode_select_pages",
+    "decode_attention_pages", "decode_attention_sparse", "draft_verify",
     "local_autoscaler_instance_slo", "local_autoscaler_create", "local_autoscaler_destroy",
     "local_autoscaler_update", "local_autoscaler_get", "local_autoscaler_simulate",
     "global_request_groups", "global_waiting_time", "global_batch_backpressure", "global_batch_autoscale",
@@ -97,6 +100,19 @@ def _load() -> ctypes.CDLL:
     lib.decode_attention_multi.restype = i32; lib.decode_attention_multi.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.kv_read_probe.restype = i32; lib.kv_read_probe.argtypes = [vp, i32, i32, vp, vp, vp]
     lib.ckv_wait_limit_selftest.restype = i32; lib.ckv_wait_limit_selftest.argtypes = [vp, ctypes.c_uint64, vp]
+    f32 = ctypes.c_float
+    lib.kv_append_rope.restype = i32
+    lib.kv_append_rope.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, i32, i32, f32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.kv_index_bytes.restype = sz; lib.kv_index_bytes.argtypes = [cfgp]
+    lib.kv_index_update.restype = i32; lib.kv_index_update.argtypes = [vp, i32, i32, vp, vp, i32, vp, sz, vp]
+    lib.kv_index_values.restype = i32; lib.kv_index_values.argtypes = [vp, i32, vp, sz, vp, vp]
+    lib.decode_select_pages.restype = i32
+    lib.decode_select_pages.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, i32, i32, vp, vp, vp]
+    lib.decode_attention_pages.restype = i32; lib.decode_attention_pages.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.decode_attention_sparse.restype = i32
+    lib.decode_attention_sparse.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, i32, i32, vp, vp, vp, vp]
+    lib.draft_verify.restype = i32
+    lib.draft_verify.argtypes = [i32, i32, i32, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]
     lib.decode_plan.restype = i32; lib.decode_plan.argtypes = [vp, i32, vp, vp, vp, vp]
     lib.ckv_set_partition.restype = i32; lib.ckv_set_partition.argtypes = [vp, i32]
     lib.ckv_set_overlap.restype = i32; lib.ckv_set_overlap.argtypes = [vp, i32]
@@ -173,6 +189,27 @@ def _dev_ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
     return t.data_ptr()
 
 
+def kv_index_bytes(cfg: Config) -> int:
+    return int(lib.kv_index_bytes(ctypes.byref(cfg)))
+
+
+def _on(device: int, t: torch.Tensor, dtype: torch.dtype, what: str, *shape: int) -> int:
+    """The address of a contiguous tensor of this type and shape on this device."""
+    if t.dtype != dtype or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s %s on %s%s"
+                         % (what, dtype, shape, device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
+    return t.data_ptr()
+
+
+def _rows_on(device: int, t: torch.Tensor, what: str, *shape: int):
+    """(address, stride between tokens) of bf16 rows [tokens][heads][d] whose tokens may lie apart."""
+    if t.dtype != torch.bfloat16 or t.get_device() != device or tuple(t.shape) != shape or \
+            (t.stride(2) != 1 and shape[2] > 1) or (t.stride(1) != shape[2] and shape[1] > 1):
+        raise ValueError("%s must be bfloat16 rows of shape %s on cuda:%d, contiguous within a token, got %s %s (strides %s) on %s"
+                         % (what, shape, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.data_ptr(), t.stride(0)
+
+
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
@@ -198,6 +235,7 @@ class KvPool:
         self.pool, self.workspace = pool, workspace
         self._h = ctypes.c_void_p()
         index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._index, self._index_bytes = index, kv_index_bytes(cfg)
         _check(lib.kv_pool_create(ctypes.byref(cfg), _dev_ptr(pool), pool.numel() * pool.element_size(),
                                   _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
                                   index, ctypes.byref(self._h)))
@@ -271,6 +309,92 @@ class KvPool:
         _check(lib.decode_attention_multi(self._h, layer, int(seq_lens.shape[0]), int(q_len),
                                           _dev_ptr(block_tables, torch.int32), _dev_ptr(seq_lens, torch.int32),
                                           _dev_ptr(q, torch.bfloat16), _dev_ptr(out, torch.bfloat16), _stream_ptr(stream)))
+
+    # -- around a long decode step
+    def _tables_of(self, block_tables, seq_lens) -> int:
+        """The batch of these lengths; both on the pool's device, the table as wide as the configuration says."""
+        batch = int(seq_lens.shape[0])
+        _on(self._index, seq_lens, torch.int32, "seq_lens", batch)
+        _on(self._index, block_tables, torch.int32, "block_tables", batch, self.cfg.max_pages_per_req)
+        return batch
+
+    def kv_append_rope(self, layer: int, block_tables, seq_lens, q, k_new, v_new, q_out, inv_freq, *, new_start=None,
+                       interleaved: bool = False, scale: float = 1.0, stream=None) -> None:
+        """Rotate the new tokens' queries (into q_out) and keys by their positions, append keys and values.
+
+        q, q_out [tokens][Hq][d] (both may be None; q_out may be q), k_new, v_new [tokens][Hkv][d]: bf16, tokens may lie apart (slices of one
+        projection's output).  new_start int32 [batch + 1]: each request's first token; without it
+        every request has the same number.  inv_freq fp32 [rotary_dim / 2]."""
+        c, dev = self.cfg, self._index
+        batch, tokens = self._tables_of(block_tables, seq_lens), int(k_new.shape[0])
+        q_ptr = out_ptr = None
+        q_stride = out_stride = 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q is not None:
+            q_ptr, q_stride = _rows_on(dev, q, "q", tokens, c.num_q_heads, c.head_dim)
+            out_ptr, out_stride = _rows_on(dev, q_out, "q_out", tokens, c.num_q_heads, c.head_dim)
+        k_ptr, k_stride = _rows_on(dev, k_new, "k_new", tokens, c.num_kv_heads, c.head_dim)
+        v_ptr, v_stride = _rows_on(dev, v_new, "v_new", tokens, c.num_kv_heads, c.head_dim)
+        half = int(inv_freq.shape[0])
+        _check(lib.kv_append_rope(self._h, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
+                                  None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
+                                  _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half, 1 if interleaved else 0, scale,
+                                  q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride, _stream_ptr(stream)))
+
+    def make_index(self) -> torch.Tensor:
+        """An empty index of the pool's keys (uint8, kv_index_bytes), for kv_index_update and the sparse calls."""
+        return torch.zeros(kv_index_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+
+    def _index_on(self, index) -> int:
+        return _on(self._index, index, torch.uint8, "index", self._index_bytes)
+
+    def kv_index_update(self, layer: int, block_tables, seq_lens, index, *, last_tokens: int = 0, stream=None) -> None:
+        """Recompute the key bounds of the pages that hold each request's last `last_tokens` tokens (0: all)."""
+        batch = self._tables_of(block_tables, seq_lens)
+        _check(lib.kv_index_update(self._h, layer, batch, block_tables.data_ptr(), seq_lens.data_ptr(), int(last_tokens),
+                                   self._index_on(index), self._index_bytes, _stream_ptr(stream)))
+
+    def kv_index_values(self, layer: int, index, out, stream=None) -> None:
+        """The key bounds of a layer as numbers: out bf16 [pages][Hkv][2][d]."""
+        c = self.cfg
+        _check(lib.kv_index_values(self._h, layer, self._index_on(index), self._index_bytes,
+                                   _on(self._index, out, torch.bfloat16, "out", c.num_pages, c.num_kv_heads, 2, c.head_dim),
+                                   _stream_ptr(stream)))
+
+    def _select_args(self, block_tables, seq_lens, q, index, pages, lens):
+        c, dev = self.cfg, self._index
+        batch, budget = self._tables_of(block_tables, seq_lens), int(pages.shape[-1])
+        return batch, budget, (block_tables.data_ptr(), seq_lens.data_ptr(),
+                               _on(dev, q, torch.bfloat16, "q", batch, c.num_q_heads, c.head_dim),
+                               self._index_on(index), self._index_bytes), \
+            (_on(dev, pages, torch.int32, "pages", batch, c.num_kv_heads, budget), _on(dev, lens, torch.int32, "lens", batch))
+
+    def decode_select_pages(self, layer: int, block_tables, seq_lens, q, index, pages, lens, *, sink: int = 1, recent: int = 2,
+                            stream=None) -> None:
+        """Choose pages.shape[2] pages per (request, kv head) for the new queries; writes pages and lens."""
+        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
+        _check(lib.decode_select_pages(self._h, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream)))
+
+    def decode_attention_pages(self, layer: int, pages, lens, q, out, stream=None) -> None:
+        """decode_attention over a list of pages per (request, kv head): pages [batch][Hkv][budget], lens [batch]."""
+        c, dev = self.cfg, self._index
+        batch, budget = int(lens.shape[0]), int(pages.shape[-1])
+        _check(lib.decode_attention_pages(self._h, layer, batch, budget,
+                                          _on(dev, pages, torch.int32, "pages", batch, c.num_kv_heads, budget),
+                                          _on(dev, lens, torch.int32, "lens", batch),
+                                          _on(dev, q, torch.bfloat16, "q", batch, c.num_q_heads, c.head_dim),
+                                          _on(dev, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
+                                          _stream_ptr(stream)))
+
+    def decode_attention_sparse(self, layer: int, block_tables, seq_lens, q, index, pages, lens, out, *, sink: int = 1,
+                                recent: int = 2, stream=None) -> None:
+        """decode_select_pages, then decode_attention_pages over what it chose."""
+        c = self.cfg
+        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
+        _check(lib.decode_attention_sparse(self._h, layer, batch, *ins, budget, sink, recent, *outs,
+                                           _on(self._index, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
+                                           _stream_ptr(stream)))
 
     def swap_image_bytes(self, n_pages: int) -> int:
         c = self.cfg
@@ -427,6 +551,37 @@ def decode_attention_noalloc(cfg: Config, pool: torch.Tensor, layer: int, block_
                                       _stream_ptr(stream), ctypes.byref(bits) if sync else None)
     _check(rc)
     return int(bits.value)
+
+
+def draft_verify(draft_tokens, target_probs, draft_probs, u_accept, u_sample, tokens, accepted, *, draft_lens=None,
+                 stream=None) -> None:
+    """Accept drafted tokens or replace the first refused one, on the current device.
+
+    draft_tokens int32 [batch][n]; target_probs [batch][n + 1][vocab] and draft_probs [batch][n][vocab] (or
+    None: point masses), fp32 or bf16, rows evenly spaced; u_accept fp32 [batch][n], u_sample fp32
+    [batch]; writes tokens int32 [batch][n + 1] and accepted int32 [batch]."""
+    dev = torch.cuda.current_device()
+    batch, n = draft_tokens.shape
+    vocab, dtype = int(target_probs.shape[2]), target_probs.dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("probabilities must be float32 or bfloat16, got %s" % dtype)
+
+    def rows(t, what, count):
+        if t.dtype != dtype or t.get_device() != dev or tuple(t.shape) != (batch, count, vocab) or \
+                (t.stride(2) != 1 and vocab > 1) or (batch > 1 and count > 0 and t.stride(0) != count * t.stride(1)):
+            raise ValueError("%s must be %s rows [%d][%d][%d], evenly spaced, on cuda:%d, got %s %s (strides %s) on %s"
+                             % (what, dtype, batch, count, vocab, dev, t.dtype, tuple(t.shape), t.stride(), t.device))
+        return t.data_ptr(), t.stride(1)
+
+    p_ptr, p_stride = rows(target_probs, "target_probs", n + 1)
+    q_ptr, q_stride = rows(draft_probs, "draft_probs", n) if draft_probs is not None else (None, 0)
+    _check(lib.draft_verify(batch, n, vocab, PROBS_F32 if dtype == torch.float32 else PROBS_BF16,
+                            _on(dev, draft_tokens, torch.int32, "draft_tokens", batch, n),
+                            None if draft_lens is None else _on(dev, draft_lens, torch.int32, "draft_lens", batch),
+                            p_ptr, p_stride, q_ptr, q_stride, _on(dev, u_accept, torch.float32, "u_accept", batch, n),
+                            _on(dev, u_sample, torch.float32, "u_sample", batch),
+                            _on(dev, tokens, torch.int32, "tokens", batch, n + 1),
+                            _on(dev, accepted, torch.int32, "accepted", batch), _stream_ptr(stream)))
 
 
 class LocalAutoscaler:

@@ -8,10 +8,10 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
-SOURCES = [os.path.join(CSRC, "ckv_api.cu"), os.path.join(CSRC, "ckv_autoscaler.cc"),
-           os.path.join(CSRC, "ckv_global_sim.cc")]
-HEADERS = [os.path.join(CSRC, "ckv_common.cuh"), os.path.join(CSRC, "ckv_device.cuh"), os.path.join(CSRC, "ckv_host.cuh"), os.path.join(_ROOT, "include", "chiron_kv.h"),
-           os.path.join(_ROOT, "include", "chiron_autoscaler.h")]
+SOURCES = [os.path.join(CSRC, n) for n in ("ckv_api.cu", "ckv_ops.cu", "ckv_autoscaler.cc", "ckv_global_sim.cc")]
+HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "ckv_host.cuh", "ckv_rope.cuh",
+                                          "ckv_sparse.cuh", "ckv_verify.cuh")] + \
+          [os.path.join(_ROOT, "include", n) for n in ("chiron_kv.h", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
 
 NVCC_FLAGS = [

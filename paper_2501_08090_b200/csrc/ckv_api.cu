@@ -130,12 +130,12 @@ int32_t encode_pool_map(const ckv_config *cfg, const void *d_pool, CUtensorMap *
 
 namespace {
 
-template <int D, int W, int S, bool kMulti>
+template <int D, int W, int S, bool kMulti, bool kHeadTables = false>
 int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t stream)
 {
     using Lay = ckv::AttnLayout<D, W, S>;
     static thread_local int configured_device = -1;
-    auto kernel = ckv::paged_decode_attn_kernel<D, W, S, kMulti>;
+    auto kernel = ckv::paged_decode_attn_kernel<D, W, S, kMulti, kHeadTables>;
     if (configured_device != pool->device) {
         CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes));
         configured_device = pool->device;
@@ -388,10 +388,12 @@ int32_t kv_append_multi(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_
                          stream);
 }
 
-// Attention for one layer, optionally with the KV append folded into the same kernel.
+// Attention for one layer, optionally with the KV append folded into the same kernel.  head_pages > 0:
+// the tables hold a row of that many pages per (request, kv head).
 static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, int32_t q_len,
                                 const int32_t *d_block_tables, const int32_t *d_seq_lens, const void *d_q,
-                                const void *d_k_new, const void *d_v_new, void *d_out, void *stream)
+                                const void *d_k_new, const void *d_v_new, void *d_out, void *stream,
+                                int32_t head_pages = 0)
 {
     if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
     if (q_len < 1 || q_len > ckv::kMaxGroup) return fail(CKV_EINVAL, "%s: q_len %d outside [1, %d]", fn, q_len, ckv::kMaxGroup);
@@ -418,7 +420,7 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
     ap.trace = pool->wsp<unsigned long long>(pool->ws.trace);
     ap.status = pool->wsp<uint32_t>(pool->ws.status);
     ap.batch = batch;
-    ap.max_pages_per_req = c.max_pages_per_req;
+    ap.max_pages_per_req = head_pages > 0 ? head_pages : c.max_pages_per_req;
     ap.num_pages = c.num_pages;
     ap.num_kv_heads = c.num_kv_heads;
     ap.num_q_heads = c.num_q_heads;
@@ -460,7 +462,10 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
         ap.q_base = base;
         ap.q_pass = std::min(per_pass, q_len - base);
         int32_t rc;
-        if (c.head_dim == 128)
+        if (head_pages > 0)
+            rc = c.head_dim == 128 ? launch_attention<128, kWarps128, kStages128, false, true>(pool, ap, s)
+                                   : launch_attention<64, kWarps64, kStages64, false, true>(pool, ap, s);
+        else if (c.head_dim == 128)
             rc = q_len > 1 ? launch_attention<128, kWarps128, kStages128, true>(pool, ap, s)
                            : launch_attention<128, kWarps128, kStages128, false>(pool, ap, s);
         else
@@ -495,6 +500,18 @@ int32_t decode_step(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t 
     if (!d_k_new || !d_v_new) return fail(CKV_EINVAL, "decode_step: NULL k_new/v_new");
     return attention_launch(pool, "decode_step", layer, batch, 1, d_block_tables, d_seq_lens, d_q, d_k_new, d_v_new,
                             d_out, stream);
+}
+
+int32_t decode_attention_pages(ckv_pool *pool, int32_t layer, int32_t batch, int32_t budget,
+                               const int32_t *d_pages, const int32_t *d_lens, const void *d_q, void *d_out,
+                               void *stream)
+{
+    if (int32_t rc = check_call(pool, layer, batch, "decode_attention_pages")) return rc;
+    if (int32_t rc = ckv::check_budget(pool, batch, budget, "decode_attention_pages")) return rc;
+    // the preceding kernel may be the selection that writes the tables: this one waits before its plan
+    if (d_pages && d_lens && d_q && d_out && aligned16(d_q) && aligned16(d_out)) pool->inputs_from_predecessor = true;
+    return attention_launch(pool, "decode_attention_pages", layer, batch, 1, d_pages, d_lens, d_q, nullptr, nullptr, d_out,
+                            stream, budget);
 }
 
 int32_t kv_read_probe(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,

@@ -598,7 +598,9 @@ struct SpanCursor {
 
 // kMulti = false: one new token per request (every live column sees the whole context);
 // kMulti = true:  q_len > 1 new tokens, each column with its own causal limit.
-template <int D, int W, int NS, bool kMulti>
+// kHeadTables = true: block_tables is [batch][Hkv][max_pages_per_req], a row per (request, kv head)
+//                 (the pages that a selection chose for it); everything else is the same.
+template <int D, int W, int NS, bool kMulti, bool kHeadTables = false>
 __global__ void __launch_bounds__(W * 32, 1)
 paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p)
 {
@@ -661,17 +663,20 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     bool more_to_issue = true;                   // the issue cursor still points at a tile of this span
     int issued = 0, i_slot = 0;                  // i_slot = issued % NS
     bool alive = true;
-    auto table_row = [&](int r) { return p.block_tables + (size_t)r * p.max_pages_per_req; };
-    auto load_chunk = [&](int r, int chunk) -> int {
+    const int table_rows = kHeadTables ? p.batch * p.num_kv_heads : p.batch;
+    auto row_at = [&](int r, int h) { return kHeadTables ? r * p.num_kv_heads + h : r; };
+    auto row_after = [&](int r, int h) { return kHeadTables ? r * p.num_kv_heads + h + 1 : (h + 1 < p.num_kv_heads ? r : r + 1); };
+    auto table_row = [&](int row) { return p.block_tables + (size_t)row * p.max_pages_per_req; };
+    auto load_chunk = [&](int row, int chunk) -> int {
         const int idx = chunk * 32 + lane;
-        return (r < p.batch && idx < p.max_pages_per_req) ? __ldg(table_row(r) + idx) : -1;
+        return (row < table_rows && idx < p.max_pages_per_req) ? __ldg(table_row(row) + idx) : -1;
     };
     constexpr int kTilesPerChunk = 32 / kPagesPerTile;
     int cur_chunk = ic.tile / kTilesPerChunk;
-    int cur_val = load_chunk(ic.r, cur_chunk);
-    int nxt_val = load_chunk(ic.r, cur_chunk + 1);
-    // chunk 0 of the row the NEXT (request, kv head) will read: this row again, or the next request's
-    int pf_row = (ic.h + 1 < p.num_kv_heads) ? ic.r : ic.r + 1;
+    int cur_val = load_chunk(row_at(ic.r, ic.h), cur_chunk);
+    int nxt_val = load_chunk(row_at(ic.r, ic.h), cur_chunk + 1);
+    // chunk 0 of the row the NEXT (request, kv head) will read: this row again, or the next one
+    int pf_row = row_after(ic.r, ic.h);
     int pf_val = load_chunk(pf_row, 0);
 
     // query fragments of a (request, kv head), fetched when the issue cursor enters it
@@ -712,7 +717,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
         if (ck != cur_chunk) {
             cur_chunk = ck;
             cur_val = nxt_val;
-            nxt_val = load_chunk(ic.r, ck + 1);
+            nxt_val = load_chunk(row_at(ic.r, ic.h), ck + 1);
         }
         const int n_pages = (ic.L + kPageSize - 1) / kPageSize;
         const int np = min(kPagesPerTile, n_pages - ic.tile * kPagesPerTile);
@@ -747,10 +752,11 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             if (ic.tile == 0) {
                 // entered a new (request, kv head): its first table chunk was fetched ahead
                 cur_chunk = 0;
-                cur_val = (pf_row == ic.r) ? pf_val : load_chunk(ic.r, 0);
-                nxt_val = load_chunk(ic.r, 1);
-                pf_row = (ic.h + 1 < p.num_kv_heads) ? ic.r : ic.r + 1;
-                pf_val = (pf_row == ic.r) ? cur_val : load_chunk(pf_row, 0);
+                const int row = row_at(ic.r, ic.h);
+                cur_val = (pf_row == row) ? pf_val : load_chunk(row, 0);
+                nxt_val = load_chunk(row, 1);
+                pf_row = row_after(ic.r, ic.h);
+                pf_val = (pf_row == row) ? cur_val : load_chunk(pf_row, 0);
                 if (qn_r < 0 && inputs_ready) {
                     load_q(qn, ic.r, ic.h);
                     qn_r = ic.r; qn_h = ic.h;

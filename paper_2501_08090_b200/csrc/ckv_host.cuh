@@ -81,6 +81,15 @@ inline int32_t check_call(ckv_pool *pool, int32_t layer, int32_t batch, const ch
     return CKV_OK;
 }
 
+// A row of `budget` pages per (request, kv head): tile counts are int32, as for whole contexts.
+inline int32_t check_budget(const ckv_pool *pool, int32_t batch, int32_t budget, const char *fn)
+{
+    constexpr int kOverhead = 4;                 // more than the plan's units per (request, kv head), rounding included
+    if (budget < 1 || (long long)batch * pool->cfg.num_kv_heads * (budget / kPagesPerTile + kOverhead) >= (1ll << 31))
+        return fail(CKV_EINVAL, "%s: budget %d out of range", fn, budget);
+    return CKV_OK;
+}
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace ckv
