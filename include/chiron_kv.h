@@ -229,7 +229,7 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *   decode_attention_pages   decode_attention over such a list: d_pages and d_lens take the places of block
  *                     tables and lengths, with a row of `budget` pages per (request, KV head).  It may
  *                     directly follow the kernel that writes them.
- *   decode_attention_sparse  both, in two launches.
+ *   decode_attention_sparse  both.
  * 1 <= recent, 0 <= sink, sink + recent <= budget; max_pages_per_req <= 49152 for selection.
  * Errors: CKV_EINVAL, CKV_ENOMEM (index too small), CKV_ECUDA.
  */

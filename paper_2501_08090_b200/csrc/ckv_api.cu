@@ -82,6 +82,7 @@ WorkspaceLayout carve(const ckv_config &c)
     w.st_k = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_v = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_out = take((size_t)c.max_batch * c.num_q_heads * d2);
+    w.sel_keys = take(sizeof(uint32_t) * (size_t)std::min((long long)c.max_batch * c.num_kv_heads * ckv::key_stride(c), ckv::kMaxSelectKeys));
     w.total = at;
     return w;
 }

@@ -31,9 +31,16 @@ inline int32_t fail(int32_t code, const char *fmt, ...)
                         __FILE__, __LINE__);                                                  \
     } while (0)
 
+// Scores that one selection may hold in the workspace: every page of every table, up to this many.
+constexpr long long kMaxSelectKeys = 64ll << 20;
+
+// Scores of a (request, kv head), the number rounded up for 16-byte loads.
+inline int32_t key_stride(const ckv_config &c) { return (c.max_pages_per_req + 3) & ~3; }
+
 struct WorkspaceLayout {
     size_t status, header, span_start, part, arrivals, trace;
     size_t st_tables, st_lens, st_q, st_k, st_v, st_out;
+    size_t sel_keys;
     size_t total;
 };
 

@@ -53,16 +53,33 @@ cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
 // Pages that one request may hold where pages are selected: their scores fit an SM's shared memory.
 constexpr int kMaxSelectPages = 49152;
 
+// score_pages_kernel over all candidate pages, then select_pages_kernel; cand: the most a request can have.
 template <int D>
-int32_t launch_select(ckv_pool *pool, const ckv::SelectParams &sp, size_t smem, unsigned cluster, void *stream)
+int32_t launch_select(ckv_pool *pool, const ckv::SelectParams &sp, int cand, void *stream)
 {
     static thread_local int configured_device = -1;
-    auto kernel = ckv::select_pages_kernel<D>;
+    auto score = ckv::score_pages_kernel<D>;
+    auto select = ckv::select_pages_kernel<true>;
+    auto select_many = ckv::select_pages_kernel<false>;
+    constexpr size_t score_smem = ckv::ScoreLayout<D>::kSmemBytes;
     if (configured_device != pool->device) {
-        CKV_CUDA(allow(kernel, true, (size_t)kMaxSelectPages * 4));
+        CKV_CUDA(allow(score, false, score_smem));
+        CKV_CUDA(allow(select_many, false, (size_t)kMaxSelectPages * 4));
         configured_device = pool->device;
     }
-    CKV_CUDA(enqueue(kernel, sp, (unsigned)sp.batch * sp.num_kv_heads * cluster, ckv::kSelectThreads, smem, pool->overlap, cluster, stream));
+    const long long pairs = (long long)sp.batch * sp.num_kv_heads;
+    if (cand > 0) {
+        const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
+        const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, 2ll * pool->num_sms);
+        CKV_CUDA(enqueue(score, sp, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream));
+        pool->launches += 1;
+    }
+    const int needed = std::max(cand, 1);
+    const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (needed + ckv::kKeysPerThread * 32 - 1) / (ckv::kKeysPerThread * 32) * 32));
+    if (needed <= threads * ckv::kKeysPerThread)
+        CKV_CUDA(enqueue(select, sp, (unsigned)pairs, threads, 0, pool->overlap, 0, stream));
+    else
+        CKV_CUDA(enqueue(select_many, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream));
     pool->launches += 1;
     return CKV_OK;
 }
@@ -279,13 +296,14 @@ static int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int3
     sp.budget = budget;
     sp.sink = sink;
     sp.recent = recent;
-    const int cand = std::max(0, c.max_pages_per_req > budget ? c.max_pages_per_req - sink - recent : 0);
-    // enough CTAs to fill the GPU four times over, each with at least 64 pages to score
-    const long long pairs = (long long)batch * c.num_kv_heads;
-    const long long fill = (4ll * pool->num_sms + pairs - 1) / pairs;
-    const unsigned cluster = cluster_of(std::min<long long>(fill, cand / 64));
-    return c.head_dim == 128 ? launch_select<128>(pool, sp, (size_t)cand * 4, cluster, stream)
-                             : launch_select<64>(pool, sp, (size_t)cand * 4, cluster, stream);
+    sp.key_stride = ckv::key_stride(c);
+    const long long keys = (long long)batch * c.num_kv_heads * sp.key_stride;
+    if (keys > ckv::kMaxSelectKeys)
+        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need room for %lld scores, the workspace holds %lld", fn, batch,
+                    c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
+    sp.keys = pool->wsp<uint32_t>(pool->ws.sel_keys);
+    const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
+    return c.head_dim == 128 ? launch_select<128>(pool, sp, cand, stream) : launch_select<64>(pool, sp, cand, stream);
 }
 
 int32_t decode_select_pages(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,

@@ -247,11 +247,16 @@ __global__ void kv_index_values_kernel(const IndexValuesParams p)
 // small beside the group's largest that fp32 holds it as a denormal) does not depend on the order of
 // summation, and the selection is the same whichever way the work is split.
 //
-// A cluster works on one (request, kv head): its CTAs score a share of the candidate pages each
-// and store the scores, as ordered 32-bit keys, into the first CTA's shared memory; that CTA then
-// finds the threshold by counting (2048 bins over the range of the keys that are still in question,
-// then within the bin that holds the threshold) and writes the chosen pages in context order.
-// The first `sink` and the last `recent` pages are always taken; equal scores go to the earlier page.
+// Two kernels.  score_pages_kernel: candidate pages are scored in tiles of 16 (the rows of an MMA).  The
+// tiles of all (request, kv head) pairs lie on one axis that is cut evenly over the warps of a grid
+// that fills the GPU, so that contexts of very different lengths balance.  A warp copies the records
+// of the tiles ahead of the one it multiplies into a ring of its own in shared memory (asynchronous
+// copies: no registers wait for them, and a new pair's queries are converted while they fly).
+// Bound by HBM: 2 d + 4 bytes per page and kv head, once.
+// select_pages_kernel: a CTA per pair finds the threshold by bisection of the range of its keys (the
+// scores as ordered 32-bit numbers, in registers), counting the keys at or above the middle each time
+// until exactly the wanted number is, and writes the chosen pages in context order.  The first `sink`
+// and the last `recent` pages are always taken; equal scores go to the earlier page.
 // ------------------------------------------------------------------------------------------
 struct SelectParams {
     const uint8_t *records;
@@ -261,13 +266,17 @@ struct SelectParams {
     const uint16_t *q;              // [batch][Hq][d]
     int32_t *sel_tables;            // [batch][Hkv][budget]
     int32_t *sel_lens;              // [batch]
+    uint32_t *keys;                 // [batch * Hkv][key_stride]
+    int32_t key_stride;             // a multiple of 4, at least max_pages_per_req
     uint32_t *status;
     int32_t batch, max_pages_per_req, num_pages, num_kv_heads, group;
     int32_t budget, sink, recent;
 };
 
-constexpr int kSelectThreads = 256;
-constexpr int kSelectBins = 2048;
+constexpr int kScoreWarps = 8;       // two CTAs an SM: 16 warps x 3 stages x 4 KB in flight (head_dim 128)
+constexpr int kScoreStages = 3;
+constexpr int kKeysPerThread = 16;   // of select_pages_kernel, in registers
+constexpr int kMaxSelectThreads = 1024;
 
 __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -276,81 +285,32 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
         : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Inclusive sum over the threads of the CTA (kSelectThreads of them); `total` gets the whole sum.
-__device__ __forceinline__ int cta_inclusive_sum(int v, int *s_warp, int &total)
+// Candidate pages of a request: those that neither fit the budget with all others nor are kept anyway.
+__device__ __forceinline__ int candidates(const SelectParams &p, int L)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += up;
-    }
-    __syncthreads();                             // s_warp may still be read from the call before
-    if (lane == 31) s_warp[warp] = v;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kSelectThreads / 32; ++w) {
-        const int x = s_warp[w];
-        if (w < warp) before += x;
-        total += x;
-    }
-    return v + before;
+    if (tiles_of_length(L, p.max_pages_per_req) == 0) return 0;
+    const int n = (L + kPageSize - 1) / kPageSize;
+    return n > p.budget && p.budget > p.sink + p.recent ? n - p.sink - p.recent : 0;
 }
 
+// The group's queries as B fragments: column = lane / 4, this lane's bytes of each piece; step0 and
+// step1 are those of the two columns whose sums this lane receives (-1: no such head).
 template <int D>
-__global__ void __launch_bounds__(kSelectThreads)
-select_pages_kernel(const SelectParams p)
-{
-    constexpr int P = 2 * D / 64;                // 16-byte pieces of a record that one lane reads
-    extern __shared__ uint32_t s_keys[];         // [max candidates] in the first CTA of the cluster
-    __shared__ int s_hist[kSelectBins];
-    __shared__ int s_warp[kSelectThreads / 32];
-    __shared__ uint32_t s_range[2];
-    __shared__ int s_found[3];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
-    const int pair = blockIdx.x / ctas;          // (request, kv head)
-    const int r = pair / p.num_kv_heads, h = pair % p.num_kv_heads;
-    grid_dependency_wait();
-    grid_launch_dependents();
+struct QueryFragments {
+    static constexpr int kPieces = D / 64;       // 16-byte pieces of 8-bit channels that one lane holds
+    uint32_t neg[kPieces][4], pos[kPieces][4];
+    float step0, step1;
 
-    const int L = __ldg(p.seq_lens + r);
-    const bool usable = tiles_of_length(L, p.max_pages_per_req) != 0;
-    const int n = usable ? (L + kPageSize - 1) / kPageSize : 0;
-    const int32_t *table = p.block_tables + (size_t)r * p.max_pages_per_req;
-    int32_t *out = p.sel_tables + (size_t)pair * p.budget;
-    if (rank == 0 && threadIdx.x == 0) {
-        if (!usable) atomicOr(p.status, kStatusBadLength);
-        if (h == 0) p.sel_lens[r] = n > p.budget ? L - (n - p.budget) * kPageSize : (usable ? L : 0);
-    }
-    if (n <= p.budget) {                         // the whole context fits (the same for every CTA of the cluster)
-        if (rank == 0)
-            for (int i = threadIdx.x; i < p.budget; i += kSelectThreads) out[i] = i < n ? __ldg(table + i) : -1;
-        return;
-    }
-    const int cand = n - p.sink - p.recent;      // pages sink .. sink + cand - 1 compete for `want` places
-    const int want = p.budget - p.sink - p.recent;
-    if (rank == 0) {
-        for (int i = threadIdx.x; i < p.sink; i += kSelectThreads) out[i] = __ldg(table + i);
-        for (int i = threadIdx.x; i < p.recent; i += kSelectThreads) out[p.budget - p.recent + i] = __ldg(table + n - p.recent + i);
-    }
-    if (want == 0) return;
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this CTA runs: others may reach its memory
-
-    // ---- the group's queries as B fragments: column = lane / 4, this lane's bytes of each piece
-    const int g = lane >> 2, t = lane & 3;
-    uint32_t qneg[P / 2][4], qpos[P / 2][4];
-    float qstep = 0.f;
+    __device__ __forceinline__ void load(const uint16_t *q, int group, int lane)
     {
-        uint4 raw[P / 2][2];
+        const int g = lane >> 2, t = lane & 3;
+        uint4 raw[kPieces][2];
         float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < P / 2; ++i) {
+        for (int i = 0; i < kPieces; ++i) {
             raw[i][0] = raw[i][1] = make_uint4(0u, 0u, 0u, 0u);
-            if (g < p.group) {
-                const uint4 *src = (const uint4 *)(p.q + ((size_t)r * p.num_kv_heads * p.group + h * p.group + g) * D + i * 64 + t * 16);
+            if (g < group) {
+                const uint4 *src = (const uint4 *)(q + g * D + i * 64 + t * 16);
                 raw[i][0] = __ldg(src);
                 raw[i][1] = __ldg(src + 1);
             }
@@ -371,139 +331,302 @@ select_pages_kernel(const SelectParams p)
         int e_max = e;
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) e_max = max(e_max, __shfl_xor_sync(0xffffffffu, e_max, x));
-        qstep = ldexpf(1.f, e - e_max);
+        const float step = g < group ? ldexpf(1.f, e - e_max) : -1.f;
         auto whole = [&](float x) { return fabsf(x) < INFINITY ? (int)fminf(fmaxf(rintf(x * inv), -127.f), 127.f) : 0; };
 #pragma unroll
-        for (int i = 0; i < P / 2; ++i) {
+        for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                uint32_t neg = 0u, pos = 0u;
+                uint32_t n8 = 0u, p8 = 0u;
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const uint32_t w = ((const uint32_t *)raw[i])[2 * x + y];
                     const int a = whole(__uint_as_float(w << 16)), b = whole(__uint_as_float(w & 0xffff0000u));
-                    neg |= ((uint32_t)(min(a, 0) & 0xff) | (uint32_t)(min(b, 0) & 0xff) << 8) << (16 * y);
-                    pos |= ((uint32_t)max(a, 0) | (uint32_t)max(b, 0) << 8) << (16 * y);
+                    n8 |= ((uint32_t)(min(a, 0) & 0xff) | (uint32_t)(min(b, 0) & 0xff) << 8) << (16 * y);
+                    p8 |= ((uint32_t)max(a, 0) | (uint32_t)max(b, 0) << 8) << (16 * y);
                 }
-                qneg[i][x] = neg;
-                qpos[i][x] = pos;
+                neg[i][x] = n8;
+                pos[i][x] = p8;
             }
         }
+        step0 = __shfl_sync(0xffffffffu, step, (2 * t) * 4);
+        step1 = __shfl_sync(0xffffffffu, step, (2 * t + 1) * 4);
     }
-    // steps of the two columns whose sums this lane receives
-    const float step0 = __shfl_sync(0xffffffffu, qstep, (2 * t) * 4), step1 = __shfl_sync(0xffffffffu, qstep, (2 * t + 1) * 4);
-    const bool live0 = 2 * t < p.group, live1 = 2 * t + 1 < p.group;
+};
 
-    // ---- scores of this CTA's share, 16 pages per warp and turn
-    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    const uint32_t keys0 = cluster_map(smem_u32(s_keys), 0);
-    const int tiles = (cand + 15) / 16;
-    const int per = (tiles + ctas - 1) / ctas;
-    const int tile_end = min(tiles, (rank + 1) * per);
-    for (int tile = rank * per + warp; tile < tile_end; tile += kSelectThreads / 32) {
-        const int c0 = tile * 16 + g, c1 = c0 + 8;
-        int page0 = c0 < cand ? __ldg(table + p.sink + c0) : 0, page1 = c1 < cand ? __ldg(table + p.sink + c1) : 0;
-        if (page0 < 0 || page0 >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page0 = 0; }
-        if (page1 < 0 || page1 >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page1 = 0; }
-        const size_t at0 = (size_t)page0 * p.num_kv_heads + h, at1 = (size_t)page1 * p.num_kv_heads + h;
-        uint4 a[P], b[P];
+template <int D>
+struct ScoreLayout {
+    static constexpr int kPieces = 2 * D / 64;                   // 16-byte pieces of a record that one lane reads
+    static constexpr int kStepsOff = 16 * 2 * D;                 // a stage: 16 records, then their 16 steps
+    static constexpr int kStageBytes = kStepsOff + 64;
+    static constexpr int kSmemBytes = kScoreWarps * kScoreStages * kStageBytes;
+};
+
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A place on the axis of tiles: request, kv head, tile of that pair.
+struct TileCursor {
+    int r, h, tile, cand, tiles;
+
+    __device__ __forceinline__ void next(const SelectParams &p)
+    {
+        if (++tile < tiles) return;
+        tile = 0;
+        if (++h < p.num_kv_heads) return;
+        h = 0;
+        do {
+            if (++r >= p.batch) { cand = tiles = 0; return; }
+            cand = candidates(p, __ldg(p.seq_lens + r));
+        } while (cand == 0);
+        tiles = (cand + 15) / 16;
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kScoreWarps * 32, 2)
+score_pages_kernel(const SelectParams p)
+{
+    using Lay = ScoreLayout<D>;
+    constexpr int P = Lay::kPieces;
+    extern __shared__ __align__(16) uint8_t s_ring[];
+    const int lane = threadIdx.x & 31;
+    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, warps = gridDim.x * kScoreWarps;
+    const int g = lane >> 2, t = lane & 3;
+    const uint32_t ring = smem_u32(s_ring) + (threadIdx.x >> 5) * kScoreStages * Lay::kStageBytes;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    // ---- this warp's stretch of the axis
+    long long tiles = 0;
+    for (int base = 0; base < p.batch; base += 32)
+        if (base + lane < p.batch) tiles += (candidates(p, __ldg(p.seq_lens + base + lane)) + 15) / 16;
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            a[i] = __ldg((const uint4 *)(p.records + at0 * 2 * D) + i * 4 + t);
-            b[i] = __ldg((const uint4 *)(p.records + at1 * 2 * D) + i * 4 + t);
+    for (int x = 16; x > 0; x >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, x);
+    const long long total = tiles * p.num_kv_heads;
+    const long long per = (total + warps - 1) / warps;
+    const long long begin = warp * per;
+    const int n_tiles = (int)(min(begin + per, total) - begin);
+    if (n_tiles <= 0) return;
+    TileCursor ic;
+    {
+        long long before = 0;                    // tiles of the requests before
+        ic.r = ic.cand = 0;
+        for (int base = 0; base < p.batch; base += 32) {
+            const int c = base + lane < p.batch ? candidates(p, __ldg(p.seq_lens + base + lane)) : 0;
+            long long upto = (c + 15) / 16;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            upto = before + upto * p.num_kv_heads;
+            const unsigned hit = __ballot_sync(0xffffffffu, upto > begin);
+            if (hit) {
+                const int src = __ffs(hit) - 1;
+                ic.r = base + src;
+                ic.cand = __shfl_sync(0xffffffffu, c, src);
+                before = __shfl_sync(0xffffffffu, upto, src) - (long long)((ic.cand + 15) / 16) * p.num_kv_heads;
+                break;
+            }
+            before = __shfl_sync(0xffffffffu, upto, 31);
         }
-        const float s0 = __ldg(p.steps + at0), s1 = __ldg(p.steps + at1);
+        ic.tiles = (ic.cand + 15) / 16;
+        ic.h = (int)((begin - before) / ic.tiles);
+        ic.tile = (int)((begin - before) % ic.tiles);
+    }
+    TileCursor cc = ic;
+
+    // ---- issue side: lane (g, t) copies its quarter of the records of rows g and g + 8; the table entries
+    // of the tile after are on their way already
+    int ids[2];
+    auto fetch_ids = [&]() {
+        const int32_t *table = p.block_tables + (size_t)ic.r * p.max_pages_per_req + p.sink;
+        const int c = ic.tile * 16 + g;
+        ids[0] = c < ic.cand ? __ldg(table + c) : 0;
+        ids[1] = c + 8 < ic.cand ? __ldg(table + c + 8) : 0;
+    };
+    int issued = 0;
+    auto issue = [&]() {
+        if (issued < n_tiles) {
+            const uint32_t stage = ring + (issued % kScoreStages) * Lay::kStageBytes;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                int page = ids[x];
+                if (page < 0 || page >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page = 0; }
+                const size_t at = (size_t)page * p.num_kv_heads + ic.h;
+                const uint8_t *src = p.records + at * 2 * D + t * 16;
+#pragma unroll
+                for (int i = 0; i < P; ++i) cp_async_16(stage + (x * P + i) * 512 + lane * 16, src + i * 64);
+                if (t == x) cp_async_4(stage + Lay::kStepsOff + (x * 8 + g) * 4, p.steps + at);
+            }
+            if (++issued < n_tiles) { ic.next(p); fetch_ids(); }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    fetch_ids();
+#pragma unroll
+    for (int s = 0; s < kScoreStages; ++s) issue();
+
+    // ---- compute side
+    QueryFragments<D> q;
+    int q_pair = -1;
+    for (int done = 0; done < n_tiles; ++done) {
+        const int pair = cc.r * p.num_kv_heads + cc.h;
+        if (pair != q_pair) {
+            q.load(p.q + (size_t)pair * p.group * D, p.group, lane);
+            q_pair = pair;
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kScoreStages - 1) : "memory");
+        __syncwarp();
+        const uint8_t *stage = s_ring + ((threadIdx.x >> 5) * kScoreStages + done % kScoreStages) * Lay::kStageBytes;
         int acc[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const uint32_t *q8 = i < P / 2 ? qneg[i] : qpos[i - P / 2];
-            mma_s8_16832(acc, a[i].x, b[i].x, a[i].y, b[i].y, q8[0], q8[1]);
-            mma_s8_16832(acc, a[i].z, b[i].z, a[i].w, b[i].w, q8[2], q8[3]);
+            const uint4 a = *(const uint4 *)(stage + i * 512 + lane * 16), b = *(const uint4 *)(stage + (P + i) * 512 + lane * 16);
+            const uint32_t *q8 = i < P / 2 ? q.neg[i] : q.pos[i - P / 2];
+            mma_s8_16832(acc, a.x, b.x, a.y, b.y, q8[0], q8[1]);
+            mma_s8_16832(acc, a.z, b.z, a.w, b.w, q8[2], q8[3]);
         }
-        float x0 = fmaxf(live0 ? (float)acc[0] * step0 : -INFINITY, live1 ? (float)acc[1] * step1 : -INFINITY);
-        float x1 = fmaxf(live0 ? (float)acc[2] * step0 : -INFINITY, live1 ? (float)acc[3] * step1 : -INFINITY);
+        const float row_step = *(const float *)(stage + Lay::kStepsOff + ((t & 1) * 8 + g) * 4);
+        __syncwarp();                            // the stage has been read
+        issue();
+        float x0 = fmaxf(q.step0 >= 0.f ? (float)acc[0] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[1] * q.step1 : -INFINITY);
+        float x1 = fmaxf(q.step0 >= 0.f ? (float)acc[2] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[3] * q.step1 : -INFINITY);
         x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
         x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
         x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
         x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
-        const int c = t == 0 ? c0 : c1;
-        if (t < 2 && c < cand) {
+        const int c = cc.tile * 16 + g + (t == 0 ? 0 : 8);
+        if (t < 2 && c < cc.cand) {
             // 2^-22: sums stay below 2^21, steps below 2^123; + 0 makes a negative zero positive
-            const float s = (t == 0 ? x0 * (s0 * 0x1p-22f) : x1 * (s1 * 0x1p-22f)) + 0.f;
+            const float s = (t == 0 ? x0 : x1) * (row_step * 0x1p-22f) + 0.f;
             const uint32_t bits = __float_as_uint(s);
-            const uint32_t key = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys0 + 4 * c), "r"(key) : "memory");
+            p.keys[(size_t)pair * p.key_stride + c] = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
+        }
+        cc.next(p);
+    }
+}
+
+// kInRegisters: at most kKeysPerThread keys a thread; otherwise they are read from shared memory.
+template <bool kInRegisters>
+__global__ void __launch_bounds__(kMaxSelectThreads)
+select_pages_kernel(const SelectParams p)
+{
+    constexpr int K = kInRegisters ? kKeysPerThread : 1;
+    extern __shared__ uint32_t s_keys[];         // [candidates] unless kInRegisters
+    __shared__ int s_count[2][32];
+    __shared__ uint32_t s_range[2][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int pair = blockIdx.x, r = pair / p.num_kv_heads;
+    const int32_t *table = p.block_tables + (size_t)r * p.max_pages_per_req;
+    int32_t *out = p.sel_tables + (size_t)pair * p.budget;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    const int L = __ldg(p.seq_lens + r);
+    const bool usable = tiles_of_length(L, p.max_pages_per_req) != 0;
+    const int n = usable ? (L + kPageSize - 1) / kPageSize : 0;
+    if (threadIdx.x == 0) {
+        if (!usable) atomicOr(p.status, kStatusBadLength);
+        if (pair % p.num_kv_heads == 0) p.sel_lens[r] = n > p.budget ? L - (n - p.budget) * kPageSize : (usable ? L : 0);
+    }
+    if (n <= p.budget) {                         // the whole context fits
+        for (int i = threadIdx.x; i < p.budget; i += blockDim.x) out[i] = i < n ? __ldg(table + i) : -1;
+        return;
+    }
+    for (int i = threadIdx.x; i < p.sink; i += blockDim.x) out[i] = __ldg(table + i);
+    for (int i = threadIdx.x; i < p.recent; i += blockDim.x) out[p.budget - p.recent + i] = __ldg(table + n - p.recent + i);
+    const int cand = n - p.sink - p.recent;      // pages sink .. sink + cand - 1 compete for `want` places
+    const int want = p.budget - p.sink - p.recent;
+    if (want == 0) return;
+    table += p.sink;
+    out += p.sink;
+
+    // thread x owns the keys first .. last - 1 (contiguous, so that context order is thread order)
+    const uint32_t *keys = p.keys + (size_t)pair * p.key_stride;
+    const int share = kInRegisters ? K : ((cand + blockDim.x - 1) / blockDim.x) | 1;     // odd: no bank conflicts
+    const int first = min(cand, (int)threadIdx.x * share), last = min(cand, first + share);
+    uint32_t own[K];
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    if constexpr (kInRegisters) {
+#pragma unroll
+        for (int x = 0; x < K; x += 4) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (first + x < cand) v = __ldg((const uint4 *)(keys + first + x));          // the stride is a multiple of 4
+            own[x] = v.x; own[x + 1] = v.y; own[x + 2] = v.z; own[x + 3] = v.w;
+        }
+#pragma unroll
+        for (int x = 0; x < K; ++x) {
+            if (first + x < last) { lo = min(lo, own[x]); hi = max(hi, own[x]); }
+            else own[x] = 0u;                    // below every score's key
+        }
+    } else {
+        for (int i = threadIdx.x; i < cand; i += blockDim.x) {
+            const uint32_t k = __ldg(keys + i);
+            s_keys[i] = k;
+            lo = min(lo, k);
+            hi = max(hi, k);
         }
     }
-    cluster_barrier();
-    if (rank != 0) return;
-
-    // ---- the threshold: the want-th largest key.  [lo, hi] always holds it; `left` of the places are
-    // still to be filled from the keys in that range (all keys above hi are in).
-    const int share = ((cand + kSelectThreads - 1) / kSelectThreads) | 1;        // odd: no bank conflicts
-    const int first = min(cand, (int)threadIdx.x * share), last = min(cand, first + share);
-    if (threadIdx.x == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0u; }
-    __syncthreads();
-    uint32_t lo = 0xffffffffu, hi = 0u;
-    for (int i = first; i < last; ++i) { lo = min(lo, s_keys[i]); hi = max(hi, s_keys[i]); }
+    // calls f(key, index) on this thread's keys
+    auto each = [&](auto f) {
+        if constexpr (kInRegisters) {
+#pragma unroll
+            for (int x = 0; x < K; ++x) f(own[x], first + x);
+        } else {
+            for (int i = first; i < last; ++i) f(s_keys[i], i);
+        }
+    };
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    if (lane == 0) { atomicMin(&s_range[0], lo); atomicMax(&s_range[1], hi); }
+    if (lane == 0) { s_range[0][warp] = lo; s_range[1][warp] = hi; }
     __syncthreads();
-    lo = s_range[0];
-    hi = s_range[1];
-    int left = want;
-    for (;;) {
-        const int shift = max(0, 21 - __clz((int)(hi - lo)));              // (hi - lo) >> shift < 2048
-        for (int i = threadIdx.x; i < kSelectBins; i += kSelectThreads) s_hist[i] = 0;
+    lo = __reduce_min_sync(0xffffffffu, lane < warps ? s_range[0][lane] : 0xffffffffu);
+    hi = __reduce_max_sync(0xffffffffu, lane < warps ? s_range[1][lane] : 0u);
+
+    // at least `want` keys are >= lo, fewer are > hi
+    int turn = 0;
+    for (; lo < hi; ++turn) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        int count = 0;
+        each([&](uint32_t k, int) { count += k >= mid; });
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (lane == 0) s_count[turn & 1][warp] = count;          // two sets: one barrier a turn
         __syncthreads();
-        for (int i = first; i < last; ++i) {
-            const uint32_t k = s_keys[i];
-            if (k >= lo && k <= hi) atomicAdd(&s_hist[(k - lo) >> shift], 1);
-        }
-        __syncthreads();
-        // thread x holds bins from the top: 2047 - 8 x down to 2040 - 8 x
-        constexpr int kOwn = kSelectBins / kSelectThreads;
-        int own = 0;
+        count = __reduce_add_sync(0xffffffffu, lane < warps ? s_count[turn & 1][lane] : 0);
+        if (count >= want) lo = mid;
+        else hi = mid - 1;
+        if (count == want) break;
+    }
+    // keys above lo are in; of the keys equal to lo the first ones in context order fill what is left
+    unsigned mine = 0;                           // above lo in the upper half, equal in the lower
+    each([&](uint32_t k, int) { mine += k > lo ? 0x10000u : k == lo ? 1u : 0u; });
+    unsigned upto = mine;
 #pragma unroll
-        for (int x = 0; x < kOwn; ++x) own += s_hist[kSelectBins - 1 - (int)threadIdx.x * kOwn - x];
-        int total;
-        const int upto = cta_inclusive_sum(own, s_warp, total);
-        if (upto >= left && upto - own < left) {                            // exactly one thread
-            int above = upto - own;
-            int bin = kSelectBins - 1 - (int)threadIdx.x * kOwn;
-            while (above + s_hist[bin] < left) above += s_hist[bin--];
-            s_found[0] = bin;
-            s_found[1] = left - above;
-            s_found[2] = s_hist[bin];
-        }
-        __syncthreads();
-        lo += (uint32_t)s_found[0] << shift;
-        hi = min(hi, lo + ((1u << shift) - 1u));
-        left = s_found[1];
-        const int held = s_found[2];
-        __syncthreads();
-        if (shift == 0 || held == left) break;
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
     }
-    // keys above lo are in; of the keys equal to lo the first `left` in context order (all of them
-    // if the whole bin was taken)
-    int above = 0, equal = 0;
-    for (int i = first; i < last; ++i) {
-        above += s_keys[i] > lo;
-        equal += s_keys[i] == lo;
-    }
-    int n_above, n_equal;
-    int above_before = cta_inclusive_sum(above, s_warp, n_above) - above;
-    int equal_before = cta_inclusive_sum(equal, s_warp, n_equal) - equal;
-    const int equal_places = want - n_above;
-    for (int i = first; i < last; ++i) {
-        const uint32_t k = s_keys[i];
-        const bool eq = k == lo;
-        if (k > lo || (eq && equal_before < equal_places))
-            out[p.sink + above_before + min(equal_before, equal_places)] = __ldg(table + p.sink + i);
-        above_before += k > lo;
-        equal_before += eq;
-    }
+    if (lane == 31) s_range[0][warp] = upto;
+    __syncthreads();
+    const unsigned w = lane < warps ? s_range[0][lane] : 0u;
+    const unsigned whole = __reduce_add_sync(0xffffffffu, w);
+    const unsigned before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - mine;
+    const int equal_places = want - (int)(whole >> 16);
+    int above = (int)(before >> 16), equal = (int)(before & 0xffffu);
+    each([&](uint32_t k, int i) {
+        if (k > lo || (k == lo && equal < equal_places)) out[above + min(equal, equal_places)] = __ldg(table + i);
+        above += k > lo;
+        equal += k == lo;
+    });
 }
 
 }  // namespace ckv
