@@ -390,11 +390,12 @@ int32_t kv_append_multi(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_
 }
 
 // Attention for one layer, optionally with the KV append folded into the same kernel.  head_pages > 0:
-// the tables hold a row of that many pages per (request, kv head).
+// the tables hold a row of that many pages per (request, kv head); context_pages > 0: they are what the
+// selection just launched writes, and the lengths are the whole contexts'.
 static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, int32_t q_len,
                                 const int32_t *d_block_tables, const int32_t *d_seq_lens, const void *d_q,
                                 const void *d_k_new, const void *d_v_new, void *d_out, void *stream,
-                                int32_t head_pages = 0)
+                                int32_t head_pages = 0, int32_t context_pages = 0)
 {
     if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
     if (q_len < 1 || q_len > ckv::kMaxGroup) return fail(CKV_EINVAL, "%s: q_len %d outside [1, %d]", fn, q_len, ckv::kMaxGroup);
@@ -431,6 +432,7 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
     ap.q_len = q_len;
     ap.q_base = 0;
     ap.q_pass = q_len;
+    ap.context_pages = context_pages;
     // A fused step may start loading tiles under its predecessor's tail -- unless that predecessor
     // may be a kernel of this library that writes the pool (an append or a swap-in).
     ap.early_loads = pool->inputs_from_predecessor ? -1 : pool->pool_written ? 0 : 1;
@@ -509,10 +511,23 @@ int32_t decode_attention_pages(ckv_pool *pool, int32_t layer, int32_t batch, int
 {
     if (int32_t rc = check_call(pool, layer, batch, "decode_attention_pages")) return rc;
     if (int32_t rc = ckv::check_budget(pool, batch, budget, "decode_attention_pages")) return rc;
-    // the preceding kernel may be the selection that writes the tables: this one waits before its plan
+    // the preceding kernel may be the one that writes the lists: this one waits before its plan
     if (d_pages && d_lens && d_q && d_out && aligned16(d_q) && aligned16(d_out)) pool->inputs_from_predecessor = true;
     return attention_launch(pool, "decode_attention_pages", layer, batch, 1, d_pages, d_lens, d_q, nullptr, nullptr, d_out,
                             stream, budget);
+}
+
+int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
+                                const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
+                                int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens,
+                                void *d_out, void *stream)
+{
+    if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "decode_attention_sparse: out is NULL or not 16-byte aligned");
+    if (int32_t rc = ckv::select_launch(pool, "decode_attention_sparse", layer, batch, d_block_tables, d_seq_lens, d_q, d_index,
+                                        index_bytes, budget, sink, recent, d_pages, d_lens, stream))
+        return rc;
+    return attention_launch(pool, "decode_attention_sparse", layer, batch, 1, d_pages, d_seq_lens, d_q, nullptr, nullptr, d_out,
+                            stream, budget, pool->cfg.max_pages_per_req);
 }
 
 int32_t kv_read_probe(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,

@@ -33,6 +33,15 @@ __host__ __device__ __forceinline__ int tiles_of_length(int L, int max_pages_per
     return (L + kTileTokens - 1) / kTileTokens;
 }
 
+// Tokens in the pages that a selection of at most `budget` pages keeps of a context of length L: whole pages
+// but for the last one.  0 for an unusable length.
+__host__ __device__ __forceinline__ int attended_length(int L, int max_pages_per_req, int budget)
+{
+    if (tiles_of_length(L, max_pages_per_req) == 0) return 0;
+    const int n = (L + kPageSize - 1) / kPageSize;
+    return n > budget ? L - (n - budget) * kPageSize : L;
+}
+
 // ------------------------------------------------------------------------------------------
 // PTX wrappers
 // ------------------------------------------------------------------------------------------

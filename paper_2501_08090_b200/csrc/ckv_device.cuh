@@ -185,14 +185,15 @@ struct SpanStart {
 };
 
 // Requests with an unusable length get their output rows cleared and the status word flagged.
-// Executed by one warp of the grid.
-__device__ __forceinline__ void flag_unusable_requests(const int32_t *__restrict__ seq_lens, int batch,
+// Executed by one warp of the grid.  length_of(r): the context length of request r.
+template <typename LengthOf>
+__device__ __forceinline__ void flag_unusable_requests(LengthOf length_of, int batch,
                                                        int max_pages_per_req, int min_len, int lane, uint16_t *out,
                                                        int out_row_elems, uint32_t *status)
 {
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        const bool bad = r < batch && tiles_of_length(__ldg(seq_lens + r), max_pages_per_req, min_len) == 0;
+        const bool bad = r < batch && tiles_of_length(length_of(r), max_pages_per_req, min_len) == 0;
         unsigned todo = __ballot_sync(0xffffffffu, bad);
         if (todo && lane == 0) atomicOr(status, kStatusBadLength);
         while (todo) {                                   // the whole warp clears one row at a time
@@ -209,14 +210,15 @@ __device__ __forceinline__ int units_of_tiles(int t) { return t > 0 ? t + kPiece
 
 // Executed by one whole warp.  Two passes over seq_lens: the total number of units, then the
 // (request, kv head) that holds unit span*q and the first tile at or after it.
-__device__ __forceinline__ SpanStart warp_plan(const int32_t *__restrict__ seq_lens, int batch, int max_pages_per_req,
+template <typename LengthOf>
+__device__ __forceinline__ SpanStart warp_plan(LengthOf length_of, int batch, int max_pages_per_req,
                                                int num_kv_heads, int num_spans, int span, int lane, int min_len = 1)
 {
     SpanStart s;
     int sum = 0;
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        if (r < batch) sum += units_of_tiles(tiles_of_length(__ldg(seq_lens + r), max_pages_per_req, min_len));
+        if (r < batch) sum += units_of_tiles(tiles_of_length(length_of(r), max_pages_per_req, min_len));
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
@@ -231,7 +233,7 @@ __device__ __forceinline__ SpanStart warp_plan(const int32_t *__restrict__ seq_l
     long long running = 0;                               // units (all heads) before request `base`
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        const int L = r < batch ? __ldg(seq_lens + r) : 0;
+        const int L = r < batch ? length_of(r) : 0;
         const int t = r < batch ? tiles_of_length(L, max_pages_per_req, min_len) : 0;
         int incl = units_of_tiles(t);
 #pragma unroll
@@ -273,7 +275,8 @@ __global__ void splitkv_plan_kernel(const PlanParams p)
     const int lane = threadIdx.x & 31;
     const int warps = (gridDim.x * blockDim.x) >> 5;
     for (int span = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; span < p.num_spans; span += warps) {
-        const SpanStart s = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane);
+        const SpanStart s = warp_plan([&](int r) { return __ldg(p.seq_lens + r); }, p.batch, p.max_pages_per_req, p.num_kv_heads,
+                                      p.num_spans, span, lane);
         if (lane == 0) {
             p.span_start[span] = s.r < 0 ? make_int4(-1, -1, -1, -1) : make_int4(s.r, s.h, s.tile, (int)s.v);
             if (span == 0) {
@@ -341,7 +344,20 @@ struct AttnParams {
                                     // < 0: even seq_lens and the tables come from the preceding kernel: wait before the plan
     int32_t q_base, q_pass;         // this launch computes new tokens q_base .. q_base + q_pass - 1; q_pass*group <= 8
     float scale_log2;               // log2(e) / sqrt(d)
+    int32_t context_pages;          // page lists that a selection of whole contexts wrote: seq_lens are the contexts', over
+                                    // tables of this many pages; 0: seq_lens are the lists' own
 };
+
+// The length that attention of request r covers.  Lists of a selection hold max_pages_per_req pages of a longer
+// context, the last of them its last page; their length follows from the context's, so that the plan
+// need not wait for the selection.
+template <bool kHeadTables>
+__device__ __forceinline__ int attended_length(const AttnParams &p, int r)
+{
+    const int L = __ldg(p.seq_lens + r);
+    if (!kHeadTables || p.context_pages == 0) return L;
+    return attended_length(L, p.context_pages, p.max_pages_per_req);
+}
 
 // Columns.  The 8 columns of the MMA hold (new token, head of the group) pairs: column c is new
 // token q_base + c / G and head c % G, ncols = q_pass * G <= 8 of them are live.  A step with more
@@ -579,6 +595,7 @@ struct SpanCursor {
     long long v;          // unit index of that tile on the plan's axis
 
     // step to the next tile; returns false when it left the last request
+    template <bool kHeadTables = false>
     __device__ __forceinline__ bool next(const AttnParams &p)
     {
         ++v;
@@ -589,7 +606,7 @@ struct SpanCursor {
         h = 0;
         do {
             if (++r >= p.batch) return false;
-            L = __ldg(p.seq_lens + r);
+            L = attended_length<kHeadTables>(p, r);
             tiles = tiles_of_length(L, p.max_pages_per_req, p.q_len);
         } while (tiles == 0);
         return true;
@@ -633,13 +650,15 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     // ---- plan: where does this warp's span start?
     // Nothing read up to the dependency wait below is written by the preceding kernel of a decode
     // step (the KV append writes only the pool), so this prologue overlaps that kernel's tail.
-    const SpanStart st = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane,
+    auto length_of = [&](int r) { return attended_length<kHeadTables>(p, r); };
+    const SpanStart st = warp_plan(length_of, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane,
                                    p.q_len);
+    if (kHeadTables) grid_dependency_wait();     // the selection before this kernel writes the tables
     if (st.r < 0 || span == 0) {
         grid_dependency_wait();
         grid_launch_dependents();
         if (span == 0)
-            flag_unusable_requests(p.seq_lens, p.batch, p.max_pages_per_req, p.q_len, lane, p.out,
+            flag_unusable_requests(length_of, p.batch, p.max_pages_per_req, p.q_len, lane, p.out,
                                    p.q_len * p.num_q_heads * D, p.status);
     }
     if (st.r < 0) {
@@ -747,7 +766,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             an_r = ic.r; an_h = ic.h;
         }
         ++issued;
-        more_to_issue = ic.next(p) && ic.v < v_end;
+        more_to_issue = ic.template next<kHeadTables>(p) && ic.v < v_end;
         if (more_to_issue) {
             if (ic.tile == 0) {
                 // entered a new (request, kv head): its first table chunk was fetched ahead
@@ -1070,7 +1089,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
         // move the compute cursor past the piece: to the next (request, kv head) or out of the span
         cc.tile += n - 1;
         cc.v += n - 1;
-        more_to_compute = cc.next(p) && cc.v < v_end;
+        more_to_compute = cc.template next<kHeadTables>(p) && cc.v < v_end;
     }
 
     if (lane == 0) p.trace[span * 8 + 2] = global_timer_ns();
@@ -1341,7 +1360,8 @@ pool_read_probe_kernel(const __grid_constant__ CUtensorMap tmap, const ProbePara
         fence_proxy_async();
     }
     __syncwarp();
-    const SpanStart st = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane);
+    const SpanStart st = warp_plan([&](int r) { return __ldg(p.seq_lens + r); }, p.batch, p.max_pages_per_req, p.num_kv_heads,
+                                   p.num_spans, span, lane);
     if (st.r < 0) return;
     AttnParams ap{};                              // the cursor reads only these
     ap.seq_lens = p.seq_lens; ap.batch = p.batch; ap.max_pages_per_req = p.max_pages_per_req;

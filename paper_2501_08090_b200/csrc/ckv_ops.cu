@@ -55,7 +55,7 @@ constexpr int kMaxSelectPages = 49152;
 
 // score_pages_kernel over all candidate pages, then select_pages_kernel; cand: the most a request can have.
 template <int D>
-int32_t launch_select(ckv_pool *pool, const ckv::SelectParams &sp, int cand, void *stream)
+int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stream)
 {
     static thread_local int configured_device = -1;
     auto score = ckv::score_pages_kernel<D>;
@@ -64,6 +64,7 @@ int32_t launch_select(ckv_pool *pool, const ckv::SelectParams &sp, int cand, voi
     constexpr size_t score_smem = ckv::ScoreLayout<D>::kSmemBytes;
     if (configured_device != pool->device) {
         CKV_CUDA(allow(score, false, score_smem));
+        CKV_CUDA(allow(select, false, (size_t)ckv::kMaxSelectThreads * ckv::kKeysPerThread * 4));
         CKV_CUDA(allow(select_many, false, (size_t)kMaxSelectPages * 4));
         configured_device = pool->device;
     }
@@ -72,12 +73,13 @@ int32_t launch_select(ckv_pool *pool, const ckv::SelectParams &sp, int cand, voi
         const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
         const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, 2ll * pool->num_sms);
         CKV_CUDA(enqueue(score, sp, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream));
+        sp.after_scores = 1;
         pool->launches += 1;
     }
     const int needed = std::max(cand, 1);
     const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (needed + ckv::kKeysPerThread * 32 - 1) / (ckv::kKeysPerThread * 32) * 32));
     if (needed <= threads * ckv::kKeysPerThread)
-        CKV_CUDA(enqueue(select, sp, (unsigned)pairs, threads, 0, pool->overlap, 0, stream));
+        CKV_CUDA(enqueue(select, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream));
     else
         CKV_CUDA(enqueue(select_many, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream));
     pool->launches += 1;
@@ -136,6 +138,51 @@ uint16_t *layer_pool(const ckv_pool *pool, int32_t layer)
 }
 
 }  // namespace
+
+namespace ckv {
+
+int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, const int32_t *d_block_tables,
+                             const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
+                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream)
+{
+    if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
+    if (!d_block_tables || !d_seq_lens || !d_q || !d_pages || !d_lens) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (!aligned16(d_q)) return fail(CKV_EINVAL, "%s: q not 16-byte aligned", fn);
+    if (sink < 0 || recent < 1 || budget < 1 || (long long)sink + recent > budget)
+        return fail(CKV_EINVAL, "%s: budget %d must hold sink %d >= 0 and recent %d >= 1 pages", fn, budget, sink, recent);
+    if (int32_t rc = ckv::check_budget(pool, batch, budget, fn)) return rc;
+    const ckv_config &c = pool->cfg;
+    if (c.max_pages_per_req > kMaxSelectPages)
+        return fail(CKV_EINVAL, "%s: selection holds at most %d pages of a request, the tables have %d", fn, kMaxSelectPages, c.max_pages_per_req);
+    if (int32_t rc = check_index(pool, fn, d_index, index_bytes)) return rc;
+    ckv::SelectParams sp{};
+    sp.records = layer_records(pool, d_index, layer);
+    sp.steps = layer_steps(pool, d_index, layer);
+    sp.block_tables = d_block_tables;
+    sp.seq_lens = d_seq_lens;
+    sp.q = static_cast<const uint16_t *>(d_q);
+    sp.sel_tables = d_pages;
+    sp.sel_lens = d_lens;
+    sp.status = pool->wsp<uint32_t>(pool->ws.status);
+    sp.batch = batch;
+    sp.max_pages_per_req = c.max_pages_per_req;
+    sp.num_pages = c.num_pages;
+    sp.num_kv_heads = c.num_kv_heads;
+    sp.group = c.num_q_heads / c.num_kv_heads;
+    sp.budget = budget;
+    sp.sink = sink;
+    sp.recent = recent;
+    sp.key_stride = ckv::key_stride(c);
+    const long long keys = (long long)batch * c.num_kv_heads * sp.key_stride;
+    if (keys > ckv::kMaxSelectKeys)
+        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need room for %lld scores, the workspace holds %lld", fn, batch,
+                    c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
+    sp.keys = pool->wsp<uint32_t>(pool->ws.sel_keys);
+    const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
+    return c.head_dim == 128 ? launch_select<128>(pool, sp, cand, stream) : launch_select<64>(pool, sp, cand, stream);
+}
+
+}  // namespace ckv
 
 extern "C" {
 
@@ -265,65 +312,12 @@ int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size
     return CKV_OK;
 }
 
-static int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, const int32_t *d_block_tables,
-                             const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
-                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream)
-{
-    if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
-    if (!d_block_tables || !d_seq_lens || !d_q || !d_pages || !d_lens) return fail(CKV_EINVAL, "%s: NULL argument", fn);
-    if (!aligned16(d_q)) return fail(CKV_EINVAL, "%s: q not 16-byte aligned", fn);
-    if (sink < 0 || recent < 1 || budget < 1 || (long long)sink + recent > budget)
-        return fail(CKV_EINVAL, "%s: budget %d must hold sink %d >= 0 and recent %d >= 1 pages", fn, budget, sink, recent);
-    if (int32_t rc = ckv::check_budget(pool, batch, budget, fn)) return rc;
-    const ckv_config &c = pool->cfg;
-    if (c.max_pages_per_req > kMaxSelectPages)
-        return fail(CKV_EINVAL, "%s: selection holds at most %d pages of a request, the tables have %d", fn, kMaxSelectPages, c.max_pages_per_req);
-    if (int32_t rc = check_index(pool, fn, d_index, index_bytes)) return rc;
-    ckv::SelectParams sp{};
-    sp.records = layer_records(pool, d_index, layer);
-    sp.steps = layer_steps(pool, d_index, layer);
-    sp.block_tables = d_block_tables;
-    sp.seq_lens = d_seq_lens;
-    sp.q = static_cast<const uint16_t *>(d_q);
-    sp.sel_tables = d_pages;
-    sp.sel_lens = d_lens;
-    sp.status = pool->wsp<uint32_t>(pool->ws.status);
-    sp.batch = batch;
-    sp.max_pages_per_req = c.max_pages_per_req;
-    sp.num_pages = c.num_pages;
-    sp.num_kv_heads = c.num_kv_heads;
-    sp.group = c.num_q_heads / c.num_kv_heads;
-    sp.budget = budget;
-    sp.sink = sink;
-    sp.recent = recent;
-    sp.key_stride = ckv::key_stride(c);
-    const long long keys = (long long)batch * c.num_kv_heads * sp.key_stride;
-    if (keys > ckv::kMaxSelectKeys)
-        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need room for %lld scores, the workspace holds %lld", fn, batch,
-                    c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
-    sp.keys = pool->wsp<uint32_t>(pool->ws.sel_keys);
-    const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
-    return c.head_dim == 128 ? launch_select<128>(pool, sp, cand, stream) : launch_select<64>(pool, sp, cand, stream);
-}
-
 int32_t decode_select_pages(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
                             const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream)
 {
-    return select_launch(pool, "decode_select_pages", layer, batch, d_block_tables, d_seq_lens, d_q, d_index, index_bytes,
+    return ckv::select_launch(pool, "decode_select_pages", layer, batch, d_block_tables, d_seq_lens, d_q, d_index, index_bytes,
                          budget, sink, recent, d_pages, d_lens, stream);
-}
-
-int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
-                                const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
-                                int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens,
-                                void *d_out, void *stream)
-{
-    if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "decode_attention_sparse: out is NULL or not 16-byte aligned");
-    if (int32_t rc = select_launch(pool, "decode_attention_sparse", layer, batch, d_block_tables, d_seq_lens, d_q, d_index,
-                                   index_bytes, budget, sink, recent, d_pages, d_lens, stream))
-        return rc;
-    return decode_attention_pages(pool, layer, batch, budget, d_pages, d_lens, d_q, d_out, stream);
 }
 
 int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dtype, const int32_t *d_draft_tokens,

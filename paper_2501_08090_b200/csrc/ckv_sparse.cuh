@@ -253,10 +253,12 @@ __global__ void kv_index_values_kernel(const IndexValuesParams p)
 // of the tiles ahead of the one it multiplies into a ring of its own in shared memory (asynchronous
 // copies: no registers wait for them, and a new pair's queries are converted while they fly).
 // Bound by HBM: 2 d + 4 bytes per page and kv head, once.
-// select_pages_kernel: a CTA per pair finds the threshold by bisection of the range of its keys (the
-// scores as ordered 32-bit numbers, in registers), counting the keys at or above the middle each time
-// until exactly the wanted number is, and writes the chosen pages in context order.  The first `sink`
-// and the last `recent` pages are always taken; equal scores go to the earlier page.
+// select_pages_kernel: a CTA per pair finds the threshold among its keys (the scores as ordered 32-bit
+// numbers, in registers) by counting them in 256 bins over the range still in question, then over
+// the bin that holds the threshold, until that bin is wanted whole (usually the second time; bisection,
+// one bit a turn, took 2-3 times as long), and writes the chosen pages in context order.  It copies
+// the table to shared memory while the scores are still being computed.  The first `sink` and the last `recent`
+// pages are always taken; equal scores go to the earlier page.
 // ------------------------------------------------------------------------------------------
 struct SelectParams {
     const uint8_t *records;
@@ -271,6 +273,7 @@ struct SelectParams {
     uint32_t *status;
     int32_t batch, max_pages_per_req, num_pages, num_kv_heads, group;
     int32_t budget, sink, recent;
+    int32_t after_scores;           // select_pages_kernel directly follows score_pages_kernel
 };
 
 constexpr int kScoreWarps = 8;       // two CTAs an SM: 16 warps x 3 stages x 4 KB in flight (head_dim 128)
@@ -515,40 +518,61 @@ score_pages_kernel(const SelectParams p)
     }
 }
 
-// kInRegisters: at most kKeysPerThread keys a thread; otherwise they are read from shared memory.
+constexpr int kSelectBins = 256;
+constexpr int kSelectRounds = 4;     // 8 bits of the keys' range each
+
+// kInRegisters: at most kKeysPerThread keys a thread, the table in shared memory; otherwise the keys are
+// in shared memory.
 template <bool kInRegisters>
 __global__ void __launch_bounds__(kMaxSelectThreads)
 select_pages_kernel(const SelectParams p)
 {
     constexpr int K = kInRegisters ? kKeysPerThread : 1;
-    extern __shared__ uint32_t s_keys[];         // [candidates] unless kInRegisters
-    __shared__ int s_count[2][32];
-    __shared__ uint32_t s_range[2][32];
+    extern __shared__ uint32_t s_words[];        // [candidates] page ids or keys
+    __shared__ __align__(16) int s_hist[kSelectRounds][kSelectBins];
+    __shared__ uint32_t s_range[3][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int pair = blockIdx.x, r = pair / p.num_kv_heads;
     const int32_t *table = p.block_tables + (size_t)r * p.max_pages_per_req;
     int32_t *out = p.sel_tables + (size_t)pair * p.budget;
-    grid_dependency_wait();
-    grid_launch_dependents();
-
+    // Right behind score_pages_kernel, the lengths and tables may be read before the wait: that kernel
+    // released this one after its own wait, so whatever wrote them has completed.
+    if (!p.after_scores) grid_dependency_wait();
     const int L = __ldg(p.seq_lens + r);
     const bool usable = tiles_of_length(L, p.max_pages_per_req) != 0;
     const int n = usable ? (L + kPageSize - 1) / kPageSize : 0;
-    if (threadIdx.x == 0) {
-        if (!usable) atomicOr(p.status, kStatusBadLength);
-        if (pair % p.num_kv_heads == 0) p.sel_lens[r] = n > p.budget ? L - (n - p.budget) * kPageSize : (usable ? L : 0);
-    }
-    if (n <= p.budget) {                         // the whole context fits
-        for (int i = threadIdx.x; i < p.budget; i += blockDim.x) out[i] = i < n ? __ldg(table + i) : -1;
-        return;
-    }
-    for (int i = threadIdx.x; i < p.sink; i += blockDim.x) out[i] = __ldg(table + i);
-    for (int i = threadIdx.x; i < p.recent; i += blockDim.x) out[p.budget - p.recent + i] = __ldg(table + n - p.recent + i);
     const int cand = n - p.sink - p.recent;      // pages sink .. sink + cand - 1 compete for `want` places
     const int want = p.budget - p.sink - p.recent;
-    if (want == 0) return;
-    table += p.sink;
-    out += p.sink;
+    const bool chosen = n > p.budget && want > 0;
+    // the pages that are always taken: the first ones and the last ones, or all
+    const int ends = n > p.budget ? p.sink + p.recent : p.budget;
+    auto end_page = [&](int i, int &place) -> int32_t {
+        if (n <= p.budget) { place = i; return i < n ? __ldg(table + i) : -1; }
+        const bool head = i < p.sink;
+        place = head ? i : p.budget - p.recent + i - p.sink;
+        return __ldg(table + (head ? i : n - p.recent + i - p.sink));
+    };
+    int place0 = 0;
+    const int32_t end0 = (int)threadIdx.x < ends ? end_page(threadIdx.x, place0) : 0;
+    if (chosen) {
+        for (int i = threadIdx.x; i < kSelectRounds * kSelectBins; i += blockDim.x) (&s_hist[0][0])[i] = 0;
+        if constexpr (kInRegisters)
+            for (int i = threadIdx.x; i < cand; i += blockDim.x) s_words[i] = (uint32_t)__ldg(table + p.sink + i);
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    if (threadIdx.x == 0) {
+        if (!usable) atomicOr(p.status, kStatusBadLength);
+        if (pair % p.num_kv_heads == 0) p.sel_lens[r] = attended_length(L, p.max_pages_per_req, p.budget);
+    }
+    if ((int)threadIdx.x < ends) out[place0] = end0;
+    for (int i = threadIdx.x + blockDim.x; i < ends; i += blockDim.x) {
+        int place;
+        const int32_t id = end_page(i, place);
+        out[place] = id;
+    }
+    if (!chosen) return;
 
     // thread x owns the keys first .. last - 1 (contiguous, so that context order is thread order)
     const uint32_t *keys = p.keys + (size_t)pair * p.key_stride;
@@ -571,18 +595,18 @@ select_pages_kernel(const SelectParams p)
     } else {
         for (int i = threadIdx.x; i < cand; i += blockDim.x) {
             const uint32_t k = __ldg(keys + i);
-            s_keys[i] = k;
+            s_words[i] = k;
             lo = min(lo, k);
             hi = max(hi, k);
         }
     }
-    // calls f(key, index) on this thread's keys
+    // calls f(key) on this thread's keys
     auto each = [&](auto f) {
         if constexpr (kInRegisters) {
 #pragma unroll
-            for (int x = 0; x < K; ++x) f(own[x], first + x);
+            for (int x = 0; x < K; ++x) f(own[x]);
         } else {
-            for (int i = first; i < last; ++i) f(s_keys[i], i);
+            for (int i = first; i < last; ++i) f(s_words[i]);
         }
     };
     lo = __reduce_min_sync(0xffffffffu, lo);
@@ -592,40 +616,65 @@ select_pages_kernel(const SelectParams p)
     lo = __reduce_min_sync(0xffffffffu, lane < warps ? s_range[0][lane] : 0xffffffffu);
     hi = __reduce_max_sync(0xffffffffu, lane < warps ? s_range[1][lane] : 0u);
 
-    // at least `want` keys are >= lo, fewer are > hi
-    int turn = 0;
-    for (; lo < hi; ++turn) {
-        const uint32_t mid = lo + (hi - lo) / 2 + 1;
-        int count = 0;
-        each([&](uint32_t k, int) { count += k >= mid; });
-        count = __reduce_add_sync(0xffffffffu, count);
-        if (lane == 0) s_count[turn & 1][warp] = count;          // two sets: one barrier a turn
+    // The want-th largest key lies in [lo, hi]; `left` places remain for the keys of that range.  Every
+    // warp reads the bins and comes to the same conclusion, so a round has one barrier.
+    int left = want;
+    for (int round = 0; round < kSelectRounds; ++round) {
+        const int shift = max(0, 24 - __clz((int)(hi - lo)));              // (hi - lo) >> shift < 256
+        int *hist = s_hist[round];
+        each([&](uint32_t k) {
+            if (k >= lo && k <= hi) atomicAdd(hist + ((k - lo) >> shift), 1);
+        });
         __syncthreads();
-        count = __reduce_add_sync(0xffffffffu, lane < warps ? s_count[turn & 1][lane] : 0);
-        if (count >= want) lo = mid;
-        else hi = mid - 1;
-        if (count == want) break;
+        // lane x holds the bins 255 - 8 x down to 248 - 8 x
+        const int4 b1 = *(const int4 *)(hist + 252 - 8 * lane), b0 = *(const int4 *)(hist + 248 - 8 * lane);
+        const int bins[8] = {b1.w, b1.z, b1.y, b1.x, b0.w, b0.z, b0.y, b0.x};
+        int sum = 0;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum += bins[x];
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const int src = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;      // the lane whose bins reach `left`
+        int above = upto - sum, bin = 0, held = 0;
+        bool found = false;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            if (!found && above + bins[x] >= left) { found = true; bin = 255 - 8 * lane - x; held = bins[x]; }
+            if (!found) above += bins[x];
+        }
+        bin = __shfl_sync(0xffffffffu, bin, src);
+        held = __shfl_sync(0xffffffffu, held, src);
+        left -= __shfl_sync(0xffffffffu, above, src);
+        lo += (uint32_t)bin << shift;
+        hi = min(hi, lo + ((1u << shift) - 1u));
+        if (shift == 0 || held == left) break;
     }
     // keys above lo are in; of the keys equal to lo the first ones in context order fill what is left
     unsigned mine = 0;                           // above lo in the upper half, equal in the lower
-    each([&](uint32_t k, int) { mine += k > lo ? 0x10000u : k == lo ? 1u : 0u; });
+    each([&](uint32_t k) { mine += k > lo ? 0x10000u : k == lo ? 1u : 0u; });
     unsigned upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
         if (lane >= o) upto += v;
     }
-    if (lane == 31) s_range[0][warp] = upto;
+    if (lane == 31) s_range[2][warp] = upto;
     __syncthreads();
-    const unsigned w = lane < warps ? s_range[0][lane] : 0u;
+    const unsigned w = lane < warps ? s_range[2][lane] : 0u;
     const unsigned whole = __reduce_add_sync(0xffffffffu, w);
     const unsigned before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - mine;
     const int equal_places = want - (int)(whole >> 16);
-    int above = (int)(before >> 16), equal = (int)(before & 0xffffu);
-    each([&](uint32_t k, int i) {
-        if (k > lo || (k == lo && equal < equal_places)) out[above + min(equal, equal_places)] = __ldg(table + i);
+    int above = (int)(before >> 16), equal = (int)(before & 0xffffu), i = first;
+    each([&](uint32_t k) {
+        if (k > lo || (k == lo && equal < equal_places))
+            out[p.sink + above + min(equal, equal_places)] = kInRegisters ? (int32_t)s_words[i] : __ldg(table + p.sink + i);
         above += k > lo;
         equal += k == lo;
+        ++i;
     });
 }
 
