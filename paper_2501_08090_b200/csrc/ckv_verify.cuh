@@ -13,13 +13,16 @@ namespace ckv {
 // whose running sum of weights exceeds u * (sum of all weights).  Without draft rows q_j is a point
 // mass at x_j.  If the differences leave nothing (p_j <= q_j everywhere), the weights are p_j.
 //
-// Products, differences and sums are in 64 bits: over 10^5 tokens a sum in 32 bits moves the borders
-// between tokens by more than many tokens' probability.
+// Products are formed in 64 bits, differences and sums to 48 bits or more (fp32 pairs whose rounding
+// errors are kept, added up in fp64): over 10^5 tokens a sum in 32 bits moves the borders between
+// tokens by more than many tokens' probability.
 //
 // Bound by reading the one or two rows that decide (4 V bytes each in fp32).  A cluster works on a
 // request; every warp owns a contiguous segment of the vocabulary and adds up its weights, the
 // segments' sums tell which warp holds the crossing, and that warp walks its segment once more
-// (from the cache) to find the token.  All sums are taken in a fixed order.
+// (from the cache) to find the token.  Loads are issued in batches before anything is added, in
+// the walk too: one stripe at a time, each waited for, the walk alone took 15 us of a 128256-token row
+// split over 32 warps.  All sums are taken in a fixed order.
 struct VerifyParams {
     const int32_t *draft_tokens;    // [batch][max_draft]
     const int32_t *draft_lens;      // [batch] or NULL: max_draft each
@@ -33,7 +36,7 @@ struct VerifyParams {
     int32_t batch, max_draft, vocab;
 };
 
-constexpr int kVerifyThreads = 512;
+constexpr int kVerifyThreads = 256;
 constexpr int kMaxCluster = 16;
 
 __device__ __forceinline__ float prob_of(const float *p) { return __ldg(p); }
@@ -42,35 +45,229 @@ __device__ __forceinline__ float prob_of(const __nv_bfloat16 *p)
     return __uint_as_float((uint32_t)__ldg((const unsigned short *)p) << 16);
 }
 
-template <typename T, int kVec>
-__device__ __forceinline__ void load_probs(const T *p, float (&out)[kVec])
-{
-    if constexpr (kVec == 1) {
-        out[0] = prob_of(p);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 v = __ldg((const float4 *)p);
-        out[0] = v.x; out[1] = v.y; out[2] = v.z; out[3] = v.w;
-    } else {
-        const uint2 v = __ldg((const uint2 *)p);
-        out[0] = __uint_as_float(v.x << 16); out[1] = __uint_as_float(v.x & 0xffff0000u);
-        out[2] = __uint_as_float(v.y << 16); out[3] = __uint_as_float(v.y & 0xffff0000u);
+// 16 bytes of a row: kVec probabilities.
+template <typename T>
+struct ProbVec {
+    static constexpr int kVec = 16 / sizeof(T);
+    uint32_t w[4];
+
+    __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
+    __device__ __forceinline__ void load(const void *p)          // 16-byte aligned
+    {
+        const uint4 v = __ldg((const uint4 *)p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     }
-}
+    __device__ __forceinline__ float get(int x) const
+    {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(x & 1 ? w[x / 2] & 0xffff0000u : w[x / 2] << 16);
+        else return __uint_as_float(w[x]);
+    }
+    __device__ __forceinline__ void drop(int x)
+    {
+        if constexpr (sizeof(T) == 2) w[x / 2] &= x & 1 ? 0x0000ffffu : 0xffff0000u;
+        else w[x] = 0u;
+    }
+    // bytes `by` .. `by` + 15 of this piece followed by `next` (by: a multiple of the type's size below 16)
+    __device__ __forceinline__ void shift(const ProbVec &next, int by)
+    {
+        uint32_t v[8] = {w[0], w[1], w[2], w[3], next.w[0], next.w[1], next.w[2], next.w[3]};
+        if (by & 8) {
+#pragma unroll
+            for (int x = 0; x < 6; ++x) v[x] = v[x + 2];
+        }
+        if (by & 4) {
+#pragma unroll
+            for (int x = 0; x < 5; ++x) v[x] = v[x + 1];
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] = sizeof(T) == 2 ? __funnelshift_r(v[x], v[x + 1], (by & 2) * 8) : v[x];
+    }
+};
 
-// max(p - q, 0) in 64 bits; a NaN counts as nothing.
-__device__ __forceinline__ double weight_of(float p, float q)
-{
-    const double w = (double)p - (double)q;
-    return w > 0.0 ? w : 0.0;
-}
+// A sum of weights: fp64, and the rounding errors of the fp32 sums that went into it.
+struct WeightSum {
+    double hi = 0.0;
+    float lo = 0.f;
 
-template <typename T, int kVec>
-__global__ void __launch_bounds__(kVerifyThreads)
+    // a + b, both >= 0: one conversion to fp64 for two values (conversions, 16 a clock and SM, are what
+    // limits a sum in fp64 here; the two-term sum's error is exact)
+    __device__ __forceinline__ void add(float a, float b)
+    {
+        const float s = a + b, bb = s - a;
+        lo += (a - (s - bb)) + (b - bb);
+        hi += (double)s;
+    }
+    __device__ __forceinline__ double total() const { return hi + (double)lo; }
+};
+
+// A row's weights: max(p - q, 0), with q = 0 where there is no draft row; 0 for the token `hole` and for a
+// NaN.  Rows may start anywhere.  A warp reads stripes of 32 pieces that are aligned in the target's
+// row (token 0 lies `skip` tokens into stripe 0); the draft's piece is put together from two where
+// its row starts at another offset.  A piece is read if it holds a token of the row; what else
+// it holds is dropped.
+template <typename T, bool kDraft>
+struct Weights {
+    using Vec = ProbVec<T>;
+    static constexpr int kVec = Vec::kVec;
+    static constexpr int kStripe = 32 * kVec;
+    static constexpr int kBatch = kDraft ? 2 : 8;                // stripes whose loads are in flight together
+    const T *p, *q;
+    int vocab, hole, lane, skip;
+
+    __device__ __forceinline__ Weights(const T *p_, const T *q_, int vocab_, int hole_, int lane_)
+        : p(p_), q(q_), vocab(vocab_), hole(hole_), lane(lane_), skip((int)(((uintptr_t)p_ & 15u) / sizeof(T)))
+    {
+    }
+    __device__ __forceinline__ int stripes() const { return (vocab + skip + kStripe - 1) / kStripe; }
+    __device__ __forceinline__ int token(int stripe) const { return stripe * kStripe + lane * kVec - skip; }
+    __device__ __forceinline__ bool holds(int first) const { return first + kVec > 0 && first < vocab; }
+
+    struct Batch { Vec p[kBatch], q[kDraft ? kBatch : 1]; };
+    // the loads of stripes at .. at + kBatch - 1, as far as they lie before `end`
+    __device__ __forceinline__ void load(Batch &b, int at, int end) const
+    {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int first = token(at + k);
+            b.p[k].clear();
+            if (at + k < end && holds(first)) b.p[k].load(p + first);
+        }
+        if constexpr (kDraft) {
+            const int by = (int)((uintptr_t)(q - skip) & 15u);   // the same for every piece
+            Vec next[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int first = token(at + k), before = first - by / (int)sizeof(T);
+                const bool live = at + k < end;
+                b.q[k].clear();
+                next[k].clear();
+                if (live && holds(before)) b.q[k].load(q + before);
+                if (live && by != 0 && holds(before + kVec)) next[k].load(q + before + kVec);
+            }
+            if (by != 0) {
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) b.q[k].shift(next[k], by);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int first = token(at + k);
+            const bool edge = first < 0 || first + kVec > vocab, holed = !kDraft && (unsigned)(hole - first) < (unsigned)kVec;
+            if (edge || holed) {
+#pragma unroll
+                for (int x = 0; x < kVec; ++x)
+                    if ((unsigned)(first + x) >= (unsigned)vocab || (!kDraft && first + x == hole)) {
+                        b.p[k].drop(x);
+                        if constexpr (kDraft) b.q[k].drop(x);
+                    }
+            }
+        }
+    }
+    // weight = hi + lo exactly (lo = 0 without a draft row)
+    __device__ __forceinline__ float weight(const Batch &b, int k, int x, float &lo) const
+    {
+        const float pv = b.p[k].get(x);
+        if constexpr (kDraft) {
+            const float qv = b.q[k].get(x);
+            const bool more = pv > qv;           // false for a NaN
+            const float w = more ? pv - qv : 0.f;
+            lo = more ? (pv - w) - qv : 0.f;
+            return w;
+        } else {
+            lo = 0.f;
+            return fmaxf(pv, 0.f);
+        }
+    }
+    __device__ __forceinline__ void add(WeightSum &sum, const Batch &b, int k) const
+    {
+#pragma unroll
+        for (int x = 0; x < kVec; x += 2) {
+            float l0, l1;
+            const float w0 = weight(b, k, x, l0), w1 = weight(b, k, x + 1, l1);
+            sum.add(w0, w1);
+            if constexpr (kDraft) sum.lo += l0 + l1;
+        }
+    }
+    __device__ double segment_sum(int from, int to) const
+    {
+        WeightSum sum[2];                        // two chains of additions
+        Batch b;
+        for (int at = from; at < to; at += kBatch) {
+            load(b, at, to);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) add(sum[k & 1], b, k);
+        }
+        double all = sum[0].total() + sum[1].total();
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        return all;
+    }
+    // The first token of the segment whose running sum, `run` before the segment, exceeds `goal`; if
+    // rounding leaves none, the last one with any weight.
+    __device__ int walk(int from, int to, double run, double goal) const
+    {
+        constexpr int kAt = kDraft ? 2 : 4;      // stripes at a time: their sums stay in registers
+        Batch b;
+        int last = -1;                           // last stripe with any weight
+        for (int at = from; at < to; at += kAt) {
+            load(b, at, min(to, at + kAt));
+            double sum[kAt];
+#pragma unroll
+            for (int k = 0; k < kAt; ++k) {
+                WeightSum own;
+                add(own, b, k);
+                sum[k] = own.total();
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                for (int k = 0; k < kAt; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
+#pragma unroll
+            for (int k = 0; k < kAt; ++k) {
+                if (sum[k] > 0.0) {
+                    last = at + k;
+                    if (run + sum[k] > goal) return in_stripe(at + k, run, goal);
+                }
+                run += sum[k];
+            }
+        }
+        return last < 0 ? -1 : in_stripe(last, run, INFINITY);
+    }
+    __device__ int in_stripe(int stripe, double run, double goal) const
+    {
+        Batch b;
+        load(b, stripe, stripe + 1);
+        WeightSum sum;
+        add(sum, b, 0);
+        const double own = sum.total();
+        double upto = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const unsigned any = __ballot_sync(0xffffffffu, own > 0.0);
+        const unsigned over = __ballot_sync(0xffffffffu, own > 0.0 && run + upto > goal);
+        const int src = over ? __ffs(over) - 1 : 31 - __clz(any);        // some lane has weight
+        int pick = 0;
+        bool found = false;
+        double at = run + (upto - own);
+#pragma unroll
+        for (int x = 0; x < kVec; ++x) {
+            float lo;
+            const float hi = weight(b, 0, x, lo);
+            if (hi > 0.f && !(found && at > goal)) { pick = x; found = true; }
+            at += (double)hi + (double)lo;
+        }
+        return __shfl_sync(0xffffffffu, token(stripe) + pick, src);
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads, 4)
 draft_verify_kernel(const VerifyParams p)
 {
     constexpr int kWarps = kVerifyThreads / 32;
-    constexpr int kStripe = 32 * kVec;           // tokens a warp reads at once
-    constexpr int kUnroll = 8;
     __shared__ int s_taken;
     __shared__ double s_warp[kWarps];
     __shared__ double s_cta[2][kMaxCluster];     // every CTA's sum, in every CTA; one set per round
@@ -113,50 +310,25 @@ draft_verify_kernel(const VerifyParams p)
     const bool refused = taken < n;
     const T *p_row = target + ((size_t)r * (p.max_draft + 1) + taken) * p.target_stride;
     const T *q_row = refused && draft != nullptr ? draft + ((size_t)r * p.max_draft + taken) * p.draft_stride : nullptr;
-    int hole = refused && draft == nullptr ? __ldg(p.draft_tokens + (size_t)r * p.max_draft + taken) : -1;
+    const int hole = refused && draft == nullptr ? __ldg(p.draft_tokens + (size_t)r * p.max_draft + taken) : -1;
     int32_t *out = p.tokens + (size_t)r * (p.max_draft + 1) + taken;
+    const Weights<T, true> differences(p_row, q_row, p.vocab, -1, lane);
+    Weights<T, false> plain(p_row, nullptr, p.vocab, hole, lane);
 
-    // this warp's segment of the vocabulary
+    // this warp's segment of the vocabulary, in stripes
     const int segments = ctas * kWarps;
-    const int stripes = (p.vocab + kStripe - 1) / kStripe;
+    const int stripes = plain.stripes();
     const int per = (stripes + segments - 1) / segments;
     const int from = min((rank * kWarps + warp) * per, stripes), to = min(from + per, stripes);
-    auto weights = [&](int stripe, double (&w)[kVec]) {
-        const int at = stripe * kStripe + lane * kVec;
-        float pv[kVec], qv[kVec];
-#pragma unroll
-        for (int x = 0; x < kVec; ++x) pv[x] = qv[x] = 0.f;
-        if (at < p.vocab) {                      // kVec > 1 only if it divides the vocabulary
-            load_probs<T, kVec>(p_row + at, pv);
-            if (q_row != nullptr) load_probs<T, kVec>(q_row + at, qv);
-        }
-#pragma unroll
-        for (int x = 0; x < kVec; ++x) w[x] = at + x == hole ? 0.0 : weight_of(pv[x], qv[x]);
-    };
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");                // every CTA runs: its memory may be written
     for (int round = 0; round < 2; ++round) {
-        double sum = 0.0;
-        for (int stripe = from; stripe < to; stripe += kUnroll) {
-            double part[kUnroll];
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                double w[kVec];
-                part[k] = 0.0;
-                if (stripe + k < to) {
-                    weights(stripe + k, w);
-#pragma unroll
-                    for (int x = 0; x < kVec; ++x) part[k] += w[x];
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) sum += part[k];
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const bool by_difference = q_row != nullptr && round == 0;
+        const double sum = by_difference ? differences.segment_sum(from, to) : plain.segment_sum(from, to);
         if (lane == 0) s_warp[warp] = sum;
         __syncthreads();
         if (warp == 0) {
             double mine = 0.0;
+#pragma unroll
             for (int w = 0; w < kWarps; ++w) mine += s_warp[w];
             if (lane < ctas) {
                 const uint32_t dst = cluster_map(smem_u32(&s_cta[round][rank]), lane);
@@ -167,9 +339,8 @@ draft_verify_kernel(const VerifyParams p)
         double total = 0.0;
         for (int c = 0; c < ctas; ++c) total += s_cta[round][c];
         if (!(total > 0.0)) {                    // the same in every CTA
-            if (round == 0 && (q_row != nullptr || hole >= 0)) {
-                q_row = nullptr;
-                hole = -1;
+            if (round == 0 && (by_difference || hole >= 0)) {
+                plain.hole = -1;
                 continue;
             }
             if (rank == 0 && threadIdx.x == 0) *out = -1;      // a row without any weight
@@ -194,36 +365,7 @@ draft_verify_kernel(const VerifyParams p)
             run += v;
         }
         if (owner != warp) return;
-        run = before;
-        int token = -1;
-        for (int stripe = from; stripe < to; ++stripe) {
-            double w[kVec], own = 0.0;
-            weights(stripe, w);
-#pragma unroll
-            for (int x = 0; x < kVec; ++x) own += w[x];
-            double upto = own;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double v = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += v;
-            }
-            const unsigned any = __ballot_sync(0xffffffffu, own > 0.0);
-            const unsigned over = __ballot_sync(0xffffffffu, own > 0.0 && run + upto > goal);
-            if (any) {
-                // the lane that crosses, else (so far) the last lane with any weight
-                const int src = over ? __ffs(over) - 1 : 31 - __clz(any);
-                int pick = -1;
-                double at = run + (upto - own);
-#pragma unroll
-                for (int x = 0; x < kVec; ++x) {
-                    if (w[x] > 0.0 && !(pick >= 0 && at > goal)) pick = x;
-                    at += w[x];
-                }
-                token = stripe * kStripe + src * kVec + __shfl_sync(0xffffffffu, pick, src);
-            }
-            if (over) break;
-            run += __shfl_sync(0xffffffffu, upto, 31);
-        }
+        const int token = by_difference ? differences.walk(from, to, before, goal) : plain.walk(from, to, before, goal);
         if (lane == 0) *out = token;
         return;
     }
