@@ -86,6 +86,21 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
     return CKV_OK;
 }
 
+template <int D>
+int32_t launch_index_update(ckv_pool *pool, const ckv::IndexParams &ip, unsigned blocks, void *stream)
+{
+    static thread_local int configured_device = -1;
+    auto kernel = ckv::kv_index_update_kernel<D>;
+    constexpr size_t smem = ckv::IndexLayout<D>::kSmemBytes;
+    if (configured_device != pool->device) {
+        CKV_CUDA(allow(kernel, false, smem));
+        configured_device = pool->device;
+    }
+    CKV_CUDA(enqueue(kernel, ip, blocks, ckv::kIndexWarps * 32, smem, pool->overlap, 0, stream));
+    pool->launches += 1;
+    return CKV_OK;
+}
+
 template <typename T>
 int32_t launch_verify(const ckv::VerifyParams &vp, unsigned cluster, void *stream)
 {
@@ -285,12 +300,9 @@ int32_t kv_index_update(ckv_pool *pool, int32_t layer, int32_t batch, const int3
     ip.last = last_tokens;
     // no more warps than there can be units
     const long long pages = last_tokens > 0 ? std::min<long long>(c.max_pages_per_req, last_tokens / c.page_size + 2) : c.max_pages_per_req;
-    const long long ctas = (pages * batch * c.num_kv_heads + 7) / 8;
-    const unsigned blocks = (unsigned)std::min<long long>(ctas, (long long)pool->num_sms * 4);
-    CKV_CUDA(c.head_dim == 128 ? enqueue(ckv::kv_index_update_kernel<128>, ip, blocks, 256, 0, pool->overlap, 0, stream)
-                               : enqueue(ckv::kv_index_update_kernel<64>, ip, blocks, 256, 0, pool->overlap, 0, stream));
-    pool->launches += 1;
-    return CKV_OK;
+    const long long ctas = (pages * batch * c.num_kv_heads + ckv::kIndexWarps - 1) / ckv::kIndexWarps;
+    const unsigned blocks = (unsigned)std::min<long long>(ctas, 2ll * pool->num_sms);
+    return c.head_dim == 128 ? launch_index_update<128>(pool, ip, blocks, stream) : launch_index_update<64>(pool, ip, blocks, stream);
 }
 
 int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size_t index_bytes, void *d_out, void *stream)

@@ -48,21 +48,61 @@ __device__ __forceinline__ int index_pages(const IndexParams &p, int L, int &fir
     return (L + kPageSize - 1) / kPageSize - first;
 }
 
-// A warp takes one (page, kv head) at a time: 16 key rows, contiguous in the pool, one 16-byte piece
-// of 32 / (D/8) rows per load.  The units of all requests lie on one axis that is cut evenly over
-// the warps of the grid, so long and short requests balance; neighbouring units are neighbours in
-// memory (kv heads of a page first).  Bound by HBM: it reads the key half of the pool once, and the
-// next unit's rows are on their way while one is reduced.
+constexpr int kIndexWarps = 8;       // two CTAs an SM: 16 warps x 3 stages x 4 KB in flight (head_dim 128)
+constexpr int kIndexStages = 3;
+
 template <int D>
-__global__ void __launch_bounds__(256)
+struct IndexLayout {
+    static constexpr int kStageBytes = kPageSize * D * 2;        // the key rows of one (page, kv head)
+    static constexpr int kBarOff = kIndexWarps * kIndexStages * kStageBytes;
+    static constexpr int kSmemBytes = kBarOff + kIndexWarps * kIndexStages * 8;
+};
+
+// A place among the units (request, page, kv head) of an update, kv heads of a page first: neighbouring
+// units are neighbours in memory.
+struct IndexCursor {
+    int r, page_at, page_end, h, L;
+
+    __device__ __forceinline__ void next(const IndexParams &p)
+    {
+        if (++h < p.num_kv_heads) return;
+        h = 0;
+        if (++page_at < page_end) return;
+        int n = 0;
+        do {
+            if (++r >= p.batch) return;
+            L = __ldg(p.seq_lens + r);
+            n = index_pages(p, L, page_at);
+        } while (n == 0);
+        page_end = page_at + n;
+    }
+};
+
+// A warp takes one (page, kv head) at a time: 16 key rows, contiguous in the pool, one bulk copy.  The
+// units of all requests lie on one axis that is cut evenly over the warps of the grid, so long and
+// short requests balance; the copies of the units ahead fill a ring of the warp's own.  Bound by
+// HBM: it reads the key half of the pool once.  (With the rows loaded to registers, one unit ahead, 96
+// registers left 16 warps an SM and 4 KB each in flight: 75 us for 8 requests of 4001 to 32768 tokens.)
+template <int D>
+__global__ void __launch_bounds__(kIndexWarps * 32, 2)
 kv_index_update_kernel(const IndexParams p)
 {
+    using Lay = IndexLayout<D>;
     constexpr int kVecs = D / 8;                 // 16-byte pieces of a row
-    constexpr int kRows = 32 / kVecs;            // rows of one load
+    constexpr int kRows = 32 / kVecs;            // rows that a warp reads at once
     constexpr int NV = kPageSize / kRows;
+    extern __shared__ __align__(128) uint8_t s_ring[];
     const int lane = threadIdx.x & 31;
-    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, warps = (gridDim.x * blockDim.x) >> 5;
-    const int vec = lane % kVecs, row0 = lane / kVecs;
+    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, warps = gridDim.x * kIndexWarps;
+    const int row0 = lane / kVecs;
+    const uint32_t ring = smem_u32(s_ring) + (threadIdx.x >> 5) * kIndexStages * Lay::kStageBytes;
+    const uint32_t bars = smem_u32(s_ring) + Lay::kBarOff + (threadIdx.x >> 5) * kIndexStages * 8;
+    if (lane == 0) {
+        for (int s = 0; s < kIndexStages; ++s) mbar_init(bars + s * 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    __syncwarp();
     grid_dependency_wait();
     grid_launch_dependents();
 
@@ -78,134 +118,146 @@ kv_index_update_kernel(const IndexParams p)
     for (int x = 16; x > 0; x >>= 1) pages += __shfl_xor_sync(0xffffffffu, pages, x);
     const long long total = pages * p.num_kv_heads;
     const long long per = (total + warps - 1) / warps;
-    const long long begin = warp * per, end = min(begin + per, total);
-    if (begin >= end) return;
+    const long long begin = warp * per;
+    const int units = (int)(min(begin + per, total) - begin);
+    if (units <= 0) return;
 
     // the request that holds unit `begin`
-    int r = 0, page_at = 0, page_end = 0, L = 0;
-    long long running = 0;
-    for (int base = 0; base < p.batch; base += 32) {
-        const int rr = base + lane;
-        int first = 0;
-        const int len = rr < p.batch ? __ldg(p.seq_lens + rr) : 0;
-        const int n = rr < p.batch ? index_pages(p, len, first) : 0;
-        long long upto = n;
+    IndexCursor ic = {};
+    {
+        long long before = 0;
+        for (int base = 0; base < p.batch; base += 32) {
+            const int rr = base + lane;
+            int first = 0;
+            const int len = rr < p.batch ? __ldg(p.seq_lens + rr) : 0;
+            const int n = rr < p.batch ? index_pages(p, len, first) : 0;
+            long long upto = n;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += v;
+            }
+            upto = before + upto * p.num_kv_heads;
+            const unsigned hit = __ballot_sync(0xffffffffu, upto > begin);
+            if (hit) {
+                const int src = __ffs(hit) - 1;
+                ic.r = base + src;
+                ic.L = __shfl_sync(0xffffffffu, len, src);
+                const int n_r = __shfl_sync(0xffffffffu, n, src);
+                before = __shfl_sync(0xffffffffu, upto, src) - (long long)n_r * p.num_kv_heads;
+                ic.page_at = __shfl_sync(0xffffffffu, first, src) + (int)((begin - before) / p.num_kv_heads);
+                ic.page_end = (ic.L + kPageSize - 1) / kPageSize;
+                break;
+            }
+            before = __shfl_sync(0xffffffffu, upto, 31);
         }
-        upto = running + upto * p.num_kv_heads;
-        const unsigned hit = __ballot_sync(0xffffffffu, upto > begin);
-        if (hit) {
-            const int src = __ffs(hit) - 1;
-            r = base + src;
-            L = __shfl_sync(0xffffffffu, len, src);
-            const int n_r = __shfl_sync(0xffffffffu, n, src);
-            const long long before = __shfl_sync(0xffffffffu, upto, src) - (long long)n_r * p.num_kv_heads;
-            page_at = __shfl_sync(0xffffffffu, first, src) + (int)((begin - before) / p.num_kv_heads);
-            page_end = (L + kPageSize - 1) / kPageSize;
-            running = before;
-            break;
-        }
-        running = __shfl_sync(0xffffffffu, upto, 31);
+        ic.h = (int)((begin - before) % p.num_kv_heads);
     }
-    int h = (int)((begin - running) % p.num_kv_heads);
 
-    uint4 rows[NV], next_rows[NV];
-    int page, next_page = -1;
-    auto fetch = [&](uint4 (&dst)[NV], int &pg) {
-        pg = __ldg(p.block_tables + (size_t)r * p.max_pages_per_req + page_at);
-        if (pg < 0 || pg >= p.num_pages) {
-            if (lane == 0) atomicOr(p.status, kStatusBadPage);
-            pg = -1;
-            return;
+    // what the compute side needs of the units in flight, oldest first
+    int f_page[kIndexStages], f_head[kIndexStages], f_tokens[kIndexStages];
+    int next_id = __ldg(p.block_tables + (size_t)ic.r * p.max_pages_per_req + ic.page_at);
+    int issued = 0;
+    auto issue = [&](int &f_pg, int &f_h, int &f_t) {
+        if (issued >= units) return;
+        const int slot = issued % kIndexStages;
+        f_pg = next_id;
+        f_h = ic.h;
+        f_t = min(kPageSize, ic.L - ic.page_at * kPageSize);
+        if (f_pg < 0 || f_pg >= p.num_pages) {
+            if (lane == 0) {
+                atomicOr(p.status, kStatusBadPage);
+                mbar_arrive_expect_tx(bars + slot * 8, 0);       // nothing to wait for
+            }
+            f_pg = -1;
+        } else if (lane == 0) {
+            const uint32_t bytes = f_t * D * 2;
+            mbar_arrive_expect_tx(bars + slot * 8, bytes);
+            bulk_load_1d(ring + slot * Lay::kStageBytes, p.pool_layer + ((size_t)f_pg * p.num_kv_heads + f_h) * 2 * kPageSize * D, bytes, bars + slot * 8);
         }
-        const int tokens = min(kPageSize, L - page_at * kPageSize);
-        const uint4 *src = (const uint4 *)(p.pool_layer + ((size_t)pg * p.num_kv_heads + h) * 2 * kPageSize * D);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (k * kRows + row0 < tokens) dst[k] = __ldg(src + (k * kRows + row0) * kVecs + vec);
+        if (++issued < units) {
+            ic.next(p);
+            if (ic.h == 0) next_id = __ldg(p.block_tables + (size_t)ic.r * p.max_pages_per_req + ic.page_at);
+        }
     };
-    fetch(rows, page);
-    int tokens = min(kPageSize, L - page_at * kPageSize), head = h;
-    for (long long unit = begin; unit < end; ++unit) {
-        // step to the next unit and start its loads
-        int next_tokens = 0, next_head = 0;
-        if (unit + 1 < end) {
-            if (++h == p.num_kv_heads) {
-                h = 0;
-                if (++page_at == page_end) {
-                    int n, first;
-                    do { L = __ldg(p.seq_lens + ++r); n = index_pages(p, L, first); } while (n == 0);
-                    page_at = first;
-                    page_end = first + n;
-                }
-            }
-            fetch(next_rows, next_page);
-            next_tokens = min(kPageSize, L - page_at * kPageSize);
-            next_head = h;
-        }
-        if (page >= 0) {
-            const __nv_bfloat162 top = __nv_bfloat162(__ushort_as_bfloat16(0x7f80), __ushort_as_bfloat16(0x7f80));
-            const __nv_bfloat162 bottom = __nv_bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80));
-            __nv_bfloat162 lo[4] = {top, top, top, top}, hi[4] = {bottom, bottom, bottom, bottom};
-            bool invalid = false;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                if (k * kRows + row0 < tokens) {
-                    const uint32_t w[4] = {rows[k].x, rows[k].y, rows[k].z, rows[k].w};
+    for (int s = 0; s < kIndexStages; ++s) issue(f_page[s], f_head[s], f_tokens[s]);
+
+    bool alive = true;
+    int landed = 0;
+    for (int done = 0; done < units; ++done) {
+        const int slot = done % kIndexStages;
+        alive = __all_sync(0xffffffffu, mbar_wait_bounded(bars + slot * 8, (done / kIndexStages) & 1, p.status));
+        if (!alive) break;
+        ++landed;
+        const int page = f_page[0], head = f_head[0], tokens = f_tokens[0];
+        // minimum and maximum over the rows; a NaN propagates, an infinity is an end of its own
+        const __nv_bfloat162 top = __nv_bfloat162(__ushort_as_bfloat16(0x7f80), __ushort_as_bfloat16(0x7f80));
+        const __nv_bfloat162 bottom = __nv_bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80));
+        __nv_bfloat162 lo[4] = {top, top, top, top}, hi[4] = {bottom, bottom, bottom, bottom};
+        const uint8_t *stage = s_ring + ((threadIdx.x >> 5) * kIndexStages + slot) * Lay::kStageBytes;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162 *>(&w[x]);
-                        invalid |= (w[x] & 0x7f80u) == 0x7f80u || (w[x] & 0x7f800000u) == 0x7f800000u;
-                        lo[x] = __hmin2(lo[x], v);
-                        hi[x] = __hmax2(hi[x], v);
-                    }
-                }
-            }
-#pragma unroll
-            for (int o = kVecs; o < 32; o <<= 1) {
+        for (int k = 0; k < NV; ++k) {
+            if (k * kRows + row0 < tokens) {
+                const uint4 v = *(const uint4 *)(stage + (k * 32 + lane) * 16);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    lo[x] = __hmin2(lo[x], __shfl_xor_sync(0xffffffffu, lo[x], o));
-                    hi[x] = __hmax2(hi[x], __shfl_xor_sync(0xffffffffu, hi[x], o));
+                    const __nv_bfloat162 e = *reinterpret_cast<const __nv_bfloat162 *>(&w[x]);
+                    lo[x] = __hmin2_nan(lo[x], e);
+                    hi[x] = __hmax2_nan(hi[x], e);
                 }
             }
-            invalid = __any_sync(0xffffffffu, invalid);
-            float m = 0.f;
+        }
+        __syncwarp();                            // the stage has been read
+#pragma unroll
+        for (int s = 0; s + 1 < kIndexStages; ++s) { f_page[s] = f_page[s + 1]; f_head[s] = f_head[s + 1]; f_tokens[s] = f_tokens[s + 1]; }
+        issue(f_page[kIndexStages - 1], f_head[kIndexStages - 1], f_tokens[kIndexStages - 1]);
+        if (page < 0) continue;
+#pragma unroll
+        for (int o = kVecs; o < 32; o <<= 1) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const float2 a = __bfloat1622float2(lo[x]), b = __bfloat1622float2(hi[x]);
-                m = fmaxf(m, fmaxf(fmaxf(fabsf(a.x), fabsf(a.y)), fmaxf(fabsf(b.x), fabsf(b.y))));
+                lo[x] = __hmin2_nan(lo[x], __shfl_xor_sync(0xffffffffu, lo[x], o));
+                hi[x] = __hmax2_nan(hi[x], __shfl_xor_sync(0xffffffffu, hi[x], o));
             }
+        }
+        float a[8], b[8], m = 0.f;
+        bool finite = true;
 #pragma unroll
-            for (int o = 1; o < kVecs; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            float inv;
-            int e = step_exponent(m, inv);
-            if (ceilf(m * inv) > 127.f) { ++e; inv *= 0.5f; }
-            uint32_t lo8[2] = {0u, 0u}, hi8[2] = {0u, 0u};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float2 a = __bfloat1622float2(lo[x]), b = __bfloat1622float2(hi[x]);
-                const int a0 = invalid ? -127 : (int)floorf(a.x * inv), a1 = invalid ? -127 : (int)floorf(a.y * inv);
-                const int b0 = invalid ? 127 : (int)ceilf(b.x * inv), b1 = invalid ? 127 : (int)ceilf(b.y * inv);
-                lo8[x / 2] |= ((uint32_t)(a0 & 0xff) | (uint32_t)(a1 & 0xff) << 8) << (16 * (x & 1));
-                hi8[x / 2] |= ((uint32_t)(b0 & 0xff) | (uint32_t)(b1 & 0xff) << 8) << (16 * (x & 1));
-            }
-            const size_t at = (size_t)page * p.num_kv_heads + head;
-            if (lane < kVecs) {
-                *(uint2 *)(p.records + at * 2 * D + 8 * lane) = make_uint2(lo8[0], lo8[1]);
-                *(uint2 *)(p.records + at * 2 * D + D + 8 * lane) = make_uint2(hi8[0], hi8[1]);
-            }
-            if (lane == 0) p.steps[at] = invalid ? kIndexStepOfInvalid : __uint_as_float((uint32_t)(e + 127) << 23);
+        for (int x = 0; x < 4; ++x) {
+            const float2 l = __bfloat1622float2(lo[x]), u = __bfloat1622float2(hi[x]);
+            a[2 * x] = l.x; a[2 * x + 1] = l.y; b[2 * x] = u.x; b[2 * x + 1] = u.y;
         }
 #pragma unroll
-        for (int k = 0; k < NV; ++k) rows[k] = next_rows[k];
-        page = next_page;
-        tokens = next_tokens;
-        head = next_head;
+        for (int x = 0; x < 8; ++x) {
+            const float most = fmaxf(fabsf(a[x]), fabsf(b[x]));
+            finite = finite && a[x] > -INFINITY && b[x] < INFINITY;      // false for a NaN
+            m = fmaxf(m, most);
+        }
+        const bool invalid = __any_sync(0xffffffffu, !finite);
+#pragma unroll
+        for (int o = 1; o < kVecs; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        float inv;
+        int e = step_exponent(m, inv);
+        if (ceilf(m * inv) > 127.f) { ++e; inv *= 0.5f; }
+        uint32_t lo8[2] = {0u, 0u}, hi8[2] = {0u, 0u};
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int l = invalid ? -127 : (int)floorf(a[x] * inv), u = invalid ? 127 : (int)ceilf(b[x] * inv);
+            lo8[x / 4] |= (uint32_t)(l & 0xff) << (8 * (x & 3));
+            hi8[x / 4] |= (uint32_t)(u & 0xff) << (8 * (x & 3));
+        }
+        const size_t at = (size_t)page * p.num_kv_heads + head;
+        if (lane < kVecs) {
+            *(uint2 *)(p.records + at * 2 * D + 8 * lane) = make_uint2(lo8[0], lo8[1]);
+            *(uint2 *)(p.records + at * 2 * D + D + 8 * lane) = make_uint2(hi8[0], hi8[1]);
+        }
+        if (lane == 0) p.steps[at] = invalid ? kIndexStepOfInvalid : __uint_as_float((uint32_t)(e + 127) << 23);
     }
+    // Do not leave while copies into this warp's ring may still be in flight (only after a wait gave up).
+    if (!alive)
+        for (int k = landed; k < issued; ++k) mbar_wait_bounded(bars + (k % kIndexStages) * 8, (k / kIndexStages) & 1, p.status);
 }
 
 // The bounds as numbers: bf16 [pages][kv heads][2][d] (exact: 7 bits times a power of two).
