@@ -249,20 +249,26 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
     rp.num_q_heads = c.num_q_heads;
     rp.num_kv_heads = c.num_kv_heads;
     rp.rotary = rotary_dim;
-    rp.interleaved = interleaved;
+    rp.n_tokens = n_tokens;
     rp.scale = scale;
-    // a CTA per token, as many rows at a time as make equal turns of at most 256 threads
+    // as many rows at a time as make equal turns of at most 256 threads; four tokens a CTA where that leaves
+    // every SM eight CTAs
     const int units = c.head_dim / 16, row_count = (d_q ? c.num_q_heads : 0) + 2 * c.num_kv_heads;
     const int turns = (row_count * units + 255) / 256;
     const int rows_per_turn = (row_count + turns - 1) / turns;
-    const unsigned threads = (unsigned)((rows_per_turn * units + 31) / 32 * 32);
+    const int several = (long long)pool->num_sms * 8 * 4 <= n_tokens ? 4 : 1;
+    const unsigned threads = (unsigned)std::max(32 * several, (rows_per_turn * units + 31) / 32 * 32), blocks = (unsigned)((n_tokens + several - 1) / several);
+    const auto launch = [&](auto one, auto four) {
+        return several == 1 ? enqueue(one, rp, blocks, threads, 0, pool->overlap, 0, stream)
+                            : enqueue(four, rp, blocks, threads, 0, pool->overlap, 0, stream);
+    };
     cudaError_t e;
     if (c.head_dim == 128)
-        e = interleaved ? enqueue(ckv::kv_append_rope_kernel<128, true>, rp, n_tokens, threads, 0, pool->overlap, 0, stream)
-                        : enqueue(ckv::kv_append_rope_kernel<128, false>, rp, n_tokens, threads, 0, pool->overlap, 0, stream);
+        e = interleaved ? launch(ckv::kv_append_rope_kernel<128, true, 1>, ckv::kv_append_rope_kernel<128, true, 4>)
+                        : launch(ckv::kv_append_rope_kernel<128, false, 1>, ckv::kv_append_rope_kernel<128, false, 4>);
     else
-        e = interleaved ? enqueue(ckv::kv_append_rope_kernel<64, true>, rp, n_tokens, threads, 0, pool->overlap, 0, stream)
-                        : enqueue(ckv::kv_append_rope_kernel<64, false>, rp, n_tokens, threads, 0, pool->overlap, 0, stream);
+        e = interleaved ? launch(ckv::kv_append_rope_kernel<64, true, 1>, ckv::kv_append_rope_kernel<64, true, 4>)
+                        : launch(ckv::kv_append_rope_kernel<64, false, 1>, ckv::kv_append_rope_kernel<64, false, 4>);
     CKV_CUDA(e);
     pool->launches += 1;
     pool->pool_written = true;

@@ -104,6 +104,15 @@ def test_many_requests_are_searched_in_rounds():
     run([20] * 33, 0, 2, 1, 64, 64, True, seed=7, new=[1] * 32 + [4])
 
 
+@pytest.mark.parametrize("interleaved,in_place", [(False, True), (True, False)])
+def test_long_prompts_take_several_tokens_a_cta(interleaved, in_place):
+    """Enough tokens for four a CTA: requests that begin and end inside a CTA, empty ones, padding, a ragged end."""
+    new = [0, 2501, 1, 0, 2, 2, 1801, 0, 450]
+    run([n + extra for n, extra in zip(new, (5, 0, 40, 1, 0, 700, 3, 9, 0))], 0, 3, 1, 64, 32, interleaved, seed=11, new=new,
+        packed=True, in_place=in_place, pad=6)
+    run([1201] * 4, 1201, 2, 2, 64, 64, interleaved, seed=12)
+
+
 def test_far_positions_keep_their_angle():
     for L in (131072, 1000003):
         run([L], 1, 4, 1, 64, 64, False, seed=8)
