@@ -195,23 +195,25 @@ def kv_index_bytes(cfg: Config) -> int:
 
 def _on(device: int, t: torch.Tensor, dtype: torch.dtype, what: str, *shape: int) -> int:
     """The address of a contiguous tensor of this type and shape on this device."""
-    if t.dtype != dtype or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s %s on %s%s"
-                         % (what, dtype, shape, device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s %s on %s%s"
+                     % (what, dtype, shape, device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
 
 
 def _rows_on(device: int, t: torch.Tensor, what: str, *shape: int):
     """(address, stride between tokens) of bf16 rows [tokens][heads][d] whose tokens may lie apart."""
-    if t.dtype != torch.bfloat16 or t.get_device() != device or tuple(t.shape) != shape or \
-            (t.stride(2) != 1 and shape[2] > 1) or (t.stride(1) != shape[2] and shape[1] > 1):
-        raise ValueError("%s must be bfloat16 rows of shape %s on cuda:%d, contiguous within a token, got %s %s (strides %s) on %s"
-                         % (what, shape, device, t.dtype, tuple(t.shape), t.stride(), t.device))
-    return t.data_ptr(), t.stride(0)
+    if t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device:
+        token, head, element = t.stride()
+        if element == 1 and (head == shape[2] or shape[1] == 1):
+            return t.data_ptr(), token
+    raise ValueError("%s must be bfloat16 rows of shape %s on cuda:%d, contiguous within a token, got %s %s (strides %s) on %s"
+                     % (what, shape, device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
-    return (stream or torch.cuda.current_stream()).cuda_stream
+    # the raw handle: building the current stream's Python object takes 3 us, as long as a launch
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class KvPool:

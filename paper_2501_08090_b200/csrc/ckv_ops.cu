@@ -71,7 +71,7 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
     const long long pairs = (long long)sp.batch * sp.num_kv_heads;
     if (cand > 0) {
         const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
-        const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, 2ll * pool->num_sms);
+        const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, (long long)ckv::kScoreCtas * pool->num_sms);
         CKV_CUDA(enqueue(score, sp, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream));
         sp.after_scores = 1;
         pool->launches += 1;

@@ -328,8 +328,11 @@ struct SelectParams {
     int32_t after_scores;           // select_pages_kernel directly follows score_pages_kernel
 };
 
-constexpr int kScoreWarps = 8;       // two CTAs an SM: 16 warps x 3 stages x 4 KB in flight (head_dim 128)
-constexpr int kScoreStages = 3;
+// Four CTAs an SM: 24 warps x 2 stages x 4 KB in flight (head_dim 128).  Other splits of the same shared
+// memory are within 2 % (16 warps x 3, 26 x 2, 18 x 3), 8 warps x 6 is 18 % slower, 48 x 1 50 %.
+constexpr int kScoreWarps = 6;
+constexpr int kScoreStages = 2;
+constexpr int kScoreCtas = 4;
 constexpr int kKeysPerThread = 16;   // of select_pages_kernel, in registers
 constexpr int kMaxSelectThreads = 1024;
 
@@ -446,7 +449,7 @@ struct TileCursor {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kScoreWarps * 32, 2)
+__global__ void __launch_bounds__(kScoreWarps * 32, kScoreCtas)
 score_pages_kernel(const SelectParams p)
 {
     using Lay = ScoreLayout<D>;
