@@ -175,7 +175,8 @@ int32_t decode_attention_multi(ckv_pool *pool, int32_t layer, int32_t batch, int
  *                 new_start[r+1] - 1 of q, k_new, v_new and q_out (none is fine), at positions
  *                 seq_lens[r] - n_r .. seq_lens[r] - 1, n_r their number.  Rows before new_start[0] and
  *                 from new_start[batch] on (padding, up to n_tokens) are neither read for the cache
- *                 nor written.  NULL: n_tokens / batch tokens each.
+ *                 nor written; tokens from n_tokens on are not processed, whatever the list says.
+ *                 NULL: n_tokens / batch tokens each.
  *   d_seq_lens    lengths AFTER the append, as everywhere.  A request with new tokens and a length
  *                 below their number or beyond the table is unusable: status bit, its rows of q_out
  *                 zero-filled, nothing appended.  A page id outside the pool: status bit, that row is not
@@ -185,7 +186,8 @@ int32_t decode_attention_multi(ckv_pool *pool, int32_t layer, int32_t batch, int
  *                 that they may lie side by side in one projection's output.  d_q_out may be d_q (same
  *                 stride); it must not overlap the others' rows.  d_q and d_q_out may both be NULL.
  *   d_inv_freq    fp32 [rotary_dim / 2];  rotary_dim: a multiple of 16, 16 .. head_dim.
- * n_tokens = 0 does nothing.  Errors: CKV_EINVAL, CKV_ECUDA.
+ * n_tokens = 0 does nothing.  All inputs, the lists and lengths among them, may come from the kernel
+ * that directly precedes the call.  Errors: CKV_EINVAL, CKV_ECUDA.
  */
 int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens,
                        const int32_t *d_block_tables, const int32_t *d_seq_lens,
@@ -222,16 +224,20 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *                     query heads of  qstep * step * sum_x max(q8[x] lo[x], q8[x] hi[x]),  q8 = q in whole
  *                     steps (nearest, ties to even, within 127) of qstep = 2^(floor(log2 max|q|) - 6).  Scores
  *                     are compared exactly, except that fp32 rounds one that is below 2^-104 of
- *                     what the group's largest query step and a page step of 1 give.  Infinities and NaN in q count as 0 here.  Requests of at most `budget` pages keep
- *                     all of them.
+ *                     what the group's largest query step and a page step of 1 give.  Infinities
+ *                     and NaN in q count as 0 here.  Requests of at most `budget` pages keep all.
  *                       d_pages  int32 [batch][Hkv][budget]: page ids in context order, then -1s
  *                       d_lens   int32 [batch]: tokens in the chosen pages (0 for an unusable length)
  *   decode_attention_pages   decode_attention over such a list: d_pages and d_lens take the places of block
  *                     tables and lengths, with a row of `budget` pages per (request, KV head).  It may
  *                     directly follow the kernel that writes them.
  *   decode_attention_sparse  both.
- * 1 <= recent, 0 <= sink, sink + recent <= budget; max_pages_per_req <= 49152 for selection.
- * Errors: CKV_EINVAL, CKV_ENOMEM (index too small), CKV_ECUDA.
+ * 1 <= recent, 0 <= sink, sink + recent <= budget.  For selection max_pages_per_req <= 49152 and
+ * batch * Hkv * max_pages_per_req (rounded up to 4) <= 2^26.  Scores live in the handle's workspace: as
+ * with every attention call, two calls on one handle must not overlap on the GPU.  All inputs may
+ * come from the kernel that directly precedes the call.  The other appends and kv_swap_in do not
+ * touch an index: update it after them.
+ * Errors: CKV_EINVAL, CKV_ENOMEM (index too small, too many scores), CKV_ECUDA.
  */
 size_t kv_index_bytes(const ckv_config *cfg);
 int32_t kv_index_update(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
@@ -261,8 +267,9 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch,
  *   at the first refusal j the next token is drawn from the weights max(p_j - q_j, 0) (from p_j where
  *   they are all 0); after n acceptances it is drawn from p_n;
  *   drawn: the first token whose running sum of weights exceeds u_sample * (sum of the weights).
- * Products, differences and sums are in fp64.  A NaN weight counts as 0; a row without any weight
- * gives token -1.  A drafted token outside the vocabulary is refused.  Runs on the current device and needs no pool.
+ * Products are formed in fp64, differences and sums to 48 bits or more.  A NaN weight counts as 0; a
+ * row without any weight, or with an infinite one, gives token -1.  A drafted token outside the
+ * vocabulary is refused.  Runs on the current device and needs no pool.
  *   dtype            CKV_PROBS_F32 or CKV_PROBS_BF16, of both probability arrays
  *   d_draft_tokens   int32 [batch][max_draft]
  *   d_draft_lens     int32 [batch], drafts of each request (clamped to 0 .. max_draft); NULL: max_draft

@@ -230,6 +230,8 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
             return fail(CKV_EINVAL, "%s: %s's stride between tokens, %lld, is below a token's %lld elements or no multiple of 8", fn, x.name,
                         (long long)x.stride, (long long)x.row);
     }
+    if (d_q && d_q_out == d_q && n_tokens > 1 && q_out_stride != q_stride)
+        return fail(CKV_EINVAL, "%s: q_out in place of q must have its stride", fn);
     ckv::RopeParams rp{};
     rp.q = static_cast<const uint16_t *>(d_q);
     rp.k = static_cast<const uint16_t *>(d_k_new);

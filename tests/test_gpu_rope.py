@@ -168,6 +168,46 @@ def test_a_second_layer_and_a_captured_call():
     kp.close()
 
 
+def test_rows_far_apart():
+    """Tokens 2^30 elements apart: offsets beyond 32 bits."""
+    kp, lens, bt, pool, btd, sld = setup([20, 33, 7], 4, 2, 64, 15)
+    q, k, v = rows(3, 4, 64, 15, 2), rows(3, 2, 64, 15, 3), rows(3, 2, 64, 15, 4)
+    freq = inv_freq(64)
+    want, tol, ref, ptol = expect(q, k, v, pool, bt, lens, freq, False)
+    far = torch.empty(2 * 2 ** 30 + 4096, dtype=torch.bfloat16, device="cuda")
+    at = lambda heads, off: far[off:].as_strided((3, heads, 64), (2 ** 30, 64, 1))
+    qd, kd, vd, out = at(4, 0), at(2, 256), at(2, 384), at(4, 512)
+    qd.copy_(bits_to_dev(q)); kd.copy_(bits_to_dev(k)); vd.copy_(bits_to_dev(v))
+    kp.kv_append_rope(0, btd, sld, qd, kd, vd, out, torch.from_numpy(freq).cuda())
+    assert kp.check_status() == 0
+    assert np.all(np.abs(widen(dev_to_bits(out)) - want) <= tol)
+    assert np.all(np.abs(widen(dev_to_bits(kp.pool)).reshape(ref.shape) - ref) <= ptol)
+    kp.close()
+
+
+def test_inputs_written_by_the_kernel_just_before():
+    """Queries, lists and lengths come from the kernel that directly precedes each call, many times over."""
+    kp, lens, bt, pool, btd, sld = setup([300, 77], 8, 2, 128, 16)
+    freq = torch.from_numpy(inv_freq(128)).cuda()
+    q0, k0, v0 = (torch.randn(6, h, 128, device="cuda").to(torch.bfloat16) for h in (8, 2, 2))
+    start0 = torch.tensor([0, 4, 6], dtype=torch.int32, device="cuda")
+    want = torch.empty_like(q0)
+    kp.kv_append_rope(0, btd, sld, q0, k0, v0, want, freq, new_start=start0)
+    pool0 = kp.pool.clone()
+    q, start, out, lens_d = torch.empty_like(q0), torch.empty_like(start0), torch.empty_like(want), torch.empty_like(sld)
+    for i in range(200):
+        q.zero_(); start.zero_(); lens_d.fill_(1)
+        lens_d.copy_(sld)
+        start.copy_(start0)
+        torch.add(q0, 0, out=q)
+        kp.kv_append_rope(0, btd, lens_d, q, k0, v0, out, freq, new_start=start)
+        if i % 20 == 0:
+            assert torch.equal(out, want) and torch.equal(kp.pool, pool0)
+        out.zero_()
+    assert kp.check_status() == 0
+    kp.close()
+
+
 def test_unusable_requests_and_pages_are_flagged():
     from paper_2501_08090_b200 import binding as b
     kp, lens, bt, pool, btd, sld = setup([20, 20, 20, 20, 20], 4, 2, 64, 12)
@@ -223,6 +263,8 @@ def test_refusals():
         kp.kv_append_rope(0, btd, sld, odd[1:1 + 512].view(2, 4, 64), k, v, out, freq)
     with pytest.raises(b.CkvError):                                      # stride not a multiple of 8
         kp.kv_append_rope(0, btd, sld, odd.as_strided((2, 4, 64), (260, 64, 1)), k, v, out, freq)
+    with pytest.raises(b.CkvError):                                      # in place with another stride
+        kp.kv_append_rope(0, btd, sld, odd[:512].view(2, 4, 64), k, v, odd.as_strided((2, 4, 64), (264, 64, 1)), freq)
     for wrong in (q.float(), q[:, :3], q.transpose(1, 2).contiguous().transpose(1, 2), q.cpu()):
         with pytest.raises(ValueError):
             kp.kv_append_rope(0, btd, sld, wrong, k, v, out, freq)

@@ -176,8 +176,8 @@ def test_equal_scores_go_to_the_earlier_page(distinct):
     c.close()
 
 
-def test_a_long_context_over_a_whole_cluster():
-    """8192 pages of one request: 16 CTAs score, one selects; also with nearly all and with hardly any taken."""
+def test_one_long_context():
+    """8192 pages of one request; also with nearly all and with hardly any taken."""
     c = Case([131072 - 5], 8, 2, 64, seed=6)
     c.update()
     for budget, sink, recent in ((128, 1, 2), (8191, 4, 4), (3, 1, 1)):
@@ -185,7 +185,7 @@ def test_a_long_context_over_a_whole_cluster():
     c.close()
 
 
-def test_many_requests_of_one_cta_each():
+def test_many_requests():
     rng = np.random.default_rng(8)
     c = Case(rng.integers(1, 900, size=150), 4, 4, 64, seed=7)
     c.update()
@@ -267,6 +267,55 @@ def test_attention_over_lists_of_the_callers_own():
                 live = [int(x) for x in lists[r, h] if x >= 0]
                 ref = ref_ops.attend(pool, live, int(tokens[r]), q[r, 4 * h:4 * h + 4], h)
                 assert_close(dev_to_bits(out[r, 4 * h:4 * h + 4]), ref, "part %s request %d head %d" % (part, r, h))
+    c.close()
+
+
+def test_lists_longer_than_their_rows_are_flagged():
+    c = Case([700, 90], 8, 2, 128, seed=15)
+    pages, lens, out = c.out(4)
+    pages.copy_(torch.from_numpy(np.stack([c.bt[:, :4]] * 2, 1)).cuda())
+    lens.copy_(torch.tensor([65, 64], dtype=torch.int32))                  # 4 pages hold 64 tokens
+    c.kp.decode_attention_pages(0, pages, lens, c.qd, out)
+    assert c.kp.check_status(raise_on_error=False) == c.b.STATUS_BAD_LENGTH
+    assert not out[0].any() and out[1].all()
+    c.close()
+
+
+def test_layers_have_their_own_pages_and_bounds():
+    c = Case([1000, 333], 8, 2, 128, seed=16, layers=3)
+    c.update()
+    c.check(9, 1, 2)
+    c.close()
+
+
+def test_plain_stream_order():
+    """With kernel overlap off, and with inputs that the kernel just before writes, results are the same."""
+    c = Case([3000, 517, 90, 2048], 32, 8, 128, seed=17)
+    c.update()
+    pages, lens, out = c.out(20)
+    c.kp.decode_attention_sparse(0, c.btd, c.sld, c.qd, c.index, pages, lens, out)
+    want = [t.clone() for t in (pages, lens, out)]
+    q, sl, bt = torch.empty_like(c.qd), torch.empty_like(c.sld), torch.empty_like(c.btd)
+    for overlap in (False, True):
+        c.kp.set_overlap(overlap)
+        for order in range(3):
+            for _ in range(30):
+                q.zero_(); sl.fill_(1); bt.fill_(0)
+                moves = [lambda: q.copy_(c.qd), lambda: sl.copy_(c.sld), lambda: bt.copy_(c.btd)]
+                for k in range(3):
+                    moves[(order + k) % 3]()
+                c.kp.decode_attention_sparse(0, bt, sl, q, c.index, pages, lens, out)
+            assert all(torch.equal(a, b) for a, b in zip(want, (pages, lens, out)))
+    assert c.kp.check_status() == 0
+    c.close()
+
+
+def test_contexts_wider_than_the_registers_hold():
+    """Tables of more than 16384 pages select from shared memory: ties, few and nearly all pages."""
+    c = Case([300007, 262144 + 16 * 700], 2, 1, 64, seed=18, distinct=300)
+    c.update()
+    for budget, sink, recent in ((64, 1, 2), (17000, 5, 7)):
+        c.check(budget, sink, recent, requests=[0, 1])
     c.close()
 
 

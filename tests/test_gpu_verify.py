@@ -70,6 +70,62 @@ def test_rows_apart(dtype, pad):
     check(*make(9, 4, 6000, seed=pad, dtype=dtype, pad=pad))
 
 
+def test_rows_far_apart():
+    """Rows 2^29 elements apart: offsets beyond 32 bits."""
+    target, q, x, ua, us = make(2, 2, 300, seed=21, dtype=torch.bfloat16)
+    far = torch.empty(5 * 2 ** 29 + 2 ** 10, dtype=torch.bfloat16, device="cuda")
+    p_far = far.as_strided((2, 3, 300), (3 * 2 ** 29, 2 ** 29, 1))
+    q_far = far[512:].as_strided((2, 2, 300), (2 * 2 ** 29, 2 ** 29, 1))
+    p_far.copy_(target); q_far.copy_(q)
+    from paper_2501_08090_b200 import binding as b
+    for u in (ua, torch.zeros_like(ua), torch.ones_like(ua)):
+        tokens, accepted = torch.empty(2, 3, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+        b.draft_verify(x.cuda(), p_far, q_far, u.cuda(), us.cuda(), tokens, accepted)
+        want = check(target, q, x, u, us)
+        assert tokens.tolist() == want[0] and accepted.tolist() == want[1]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [7, 8, 33, 256, 2049, 9000])
+def test_rows_of_every_alignment(V, dtype):
+    """Target and draft rows that start at every offset within 16 bytes, each against each."""
+    target, q, x, ua, us = make(3, 2, V, seed=V, dtype=dtype)
+    from paper_2501_08090_b200 import binding as b
+    want = check(target, q, x, ua, us)
+    step = 16 // target.element_size()
+    dev = [t.cuda() for t in (x, ua, us)]
+    stride = (V + 2 * step - 1) // step * step                             # every row at the same offset
+
+    def place(t, off):
+        base = torch.full((t.shape[0] * t.shape[1] * stride + 2 * step,), float("nan"), dtype=dtype, device="cuda")
+        rows = base[off:].as_strided(t.shape, (t.shape[1] * stride, stride, 1))
+        rows.copy_(t)
+        return rows
+
+    for i in range(step):
+        for j in range(step):
+            tokens, accepted = torch.empty(3, 3, dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda")
+            b.draft_verify(dev[0], place(target, i), place(q, j), dev[1], dev[2], tokens, accepted)
+            assert tokens.tolist() == want[0] and accepted.tolist() == want[1], (i, j)
+
+
+def test_infinite_weights():
+    """An infinity in the deciding row gives -1; in the draft's row it only refuses its own token."""
+    V = 500
+    p, q = torch.full((3, 2, V), 1.0 / V), torch.full((3, 1, V), 0.5 / V)
+    x = torch.full((3, 1), 4, dtype=torch.int32)
+    ua = torch.tensor([[0.5], [0.999999], [0.5]])
+    p[0, 1, 77] = float("inf")                                             # accepted; the next row decides
+    p[1, 0, 77] = float("inf")
+    q[1, 0, 4] = 1.0                                                       # refused
+    q[2, 0, 4] = float("inf")
+    q[2, 0, 5:] = 1.0                                                      # refused; tokens 0 .. 3 remain
+    from paper_2501_08090_b200 import binding as b
+    tokens, accepted = torch.empty(3, 2, dtype=torch.int32, device="cuda"), torch.empty(3, dtype=torch.int32, device="cuda")
+    b.draft_verify(x.cuda(), p.cuda(), q.cuda(), ua.cuda(), torch.tensor([0.5, 0.5, 0.6]).cuda(), tokens, accepted)
+    assert tokens.tolist() == [[4, -1], [-1, -1], [2, -1]] and accepted.tolist() == [1, 0, 0]
+
+
 def test_every_border_of_a_small_distribution():
     """Eighths: each draw's goal falls on a border exactly, or half a step beside it."""
     V = 8
