@@ -59,13 +59,11 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
 {
     static thread_local int configured_device = -1;
     auto score = ckv::score_pages_kernel<D>;
-    auto select = ckv::select_pages_kernel<true>;
-    auto select_many = ckv::select_pages_kernel<false>;
     constexpr size_t score_smem = ckv::ScoreLayout<D>::kSmemBytes;
     if (configured_device != pool->device) {
         CKV_CUDA(allow(score, false, score_smem));
-        CKV_CUDA(allow(select, false, (size_t)ckv::kMaxSelectThreads * ckv::kKeysPerThread * 4));
-        CKV_CUDA(allow(select_many, false, (size_t)kMaxSelectPages * 4));
+        CKV_CUDA(allow(ckv::select_pages_kernel<16>, false, (size_t)ckv::kMaxSelectThreads * 16 * 4));
+        CKV_CUDA(allow(ckv::select_pages_kernel<0>, false, (size_t)kMaxSelectPages * 4));
         configured_device = pool->device;
     }
     const long long pairs = (long long)sp.batch * sp.num_kv_heads;
@@ -76,12 +74,14 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
         sp.after_scores = 1;
         pool->launches += 1;
     }
-    const int needed = std::max(cand, 1);
-    const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (needed + ckv::kKeysPerThread * 32 - 1) / (ckv::kKeysPerThread * 32) * 32));
-    if (needed <= threads * ckv::kKeysPerThread)
-        CKV_CUDA(enqueue(select, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream));
-    else
-        CKV_CUDA(enqueue(select_many, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream));
+    const auto select = [&](auto kernel, int keys) {             // `keys` a thread
+        const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (cand + keys * 32 - 1) / (keys * 32) * 32));
+        return enqueue(kernel, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream);
+    };
+    CKV_CUDA(cand <= 4 * ckv::kMaxSelectThreads    ? select(ckv::select_pages_kernel<4>, 4)
+             : cand <= 8 * ckv::kMaxSelectThreads  ? select(ckv::select_pages_kernel<8>, 8)
+             : cand <= 16 * ckv::kMaxSelectThreads ? select(ckv::select_pages_kernel<16>, 16)
+                                                   : select(ckv::select_pages_kernel<0>, 16));
     pool->launches += 1;
     return CKV_OK;
 }

@@ -333,7 +333,6 @@ struct SelectParams {
 constexpr int kScoreWarps = 6;
 constexpr int kScoreStages = 2;
 constexpr int kScoreCtas = 4;
-constexpr int kKeysPerThread = 16;   // of select_pages_kernel, in registers
 constexpr int kMaxSelectThreads = 1024;
 
 __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -576,13 +575,17 @@ score_pages_kernel(const SelectParams p)
 constexpr int kSelectBins = 256;
 constexpr int kSelectRounds = 4;     // 8 bits of the keys' range each
 
-// kInRegisters: at most kKeysPerThread keys a thread, the table in shared memory; otherwise the keys are
-// in shared memory.
-template <bool kInRegisters>
+// kKeys > 0: at most that many keys a thread, in registers, and the table in shared memory; 0: the keys
+// are in shared memory.  Few keys a thread and many threads are best, as the code runs once, from a cold
+// instruction cache: over 2048 pages 4 keys a thread make sparse_b64's selection 41.5 us with the scores,
+// 8 keys 43, 16 keys 45.5, the keys in shared memory 44-51.
+template <int kKeys>
 __global__ void __launch_bounds__(kMaxSelectThreads)
 select_pages_kernel(const SelectParams p)
 {
-    constexpr int K = kInRegisters ? kKeysPerThread : 1;
+    constexpr bool kInRegisters = kKeys > 0;
+    constexpr int K = kInRegisters ? kKeys : 1;
+    static_assert(K == 1 || K % 4 == 0, "keys are loaded four at a time");
     extern __shared__ uint32_t s_words[];        // [candidates] page ids or keys
     __shared__ __align__(16) int s_hist[kSelectRounds][kSelectBins];
     __shared__ uint32_t s_range[3][32];

@@ -177,12 +177,13 @@ def test_equal_scores_go_to_the_earlier_page(distinct):
 
 
 def test_one_long_context():
-    """8192 pages of one request; also with nearly all and with hardly any taken."""
-    c = Case([131072 - 5], 8, 2, 64, seed=6)
-    c.update()
-    for budget, sink, recent in ((128, 1, 2), (8191, 4, 4), (3, 1, 1)):
-        c.check(budget, sink, recent)
-    c.close()
+    """8192 and 11004 pages of one request; also with nearly all and with hardly any taken."""
+    for length in (131072 - 5, 16 * 11003 + 9):
+        c = Case([length], 8, 2, 64, seed=6)
+        c.update()
+        for budget, sink, recent in ((128, 1, 2), (-(-length // 16) - 1, 4, 4), (3, 1, 1)):
+            c.check(budget, sink, recent)
+        c.close()
 
 
 def test_many_requests():
