@@ -53,6 +53,11 @@ cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
 // Pages that one request may hold where pages are selected: their scores fit an SM's shared memory.
 constexpr int kMaxSelectPages = 49152;
 
+// Up to this many pages and (request, kv head) pairs one kernel scores and selects.  8 and 32 pairs of at most
+// 94 pages: 5.1 and 5.3 us against 6.1 and 6.4 with two kernels, and a launch less; of 250 pages 6.5 and
+// 6.7 against 6.2 and 6.6; 256 pairs of 94 pages make attention start later (31.1 us in all against 30.2).
+constexpr int kFusedPages = 256, kFusedPairs = 128;
+
 // score_pages_kernel over all candidate pages, then select_pages_kernel; cand: the most a request can have.
 template <int D>
 int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stream)
@@ -67,6 +72,11 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
         configured_device = pool->device;
     }
     const long long pairs = (long long)sp.batch * sp.num_kv_heads;
+    if (cand > 0 && cand <= kFusedPages && pairs <= kFusedPairs) {
+        CKV_CUDA(enqueue(ckv::select_pages_kernel<4, D>, sp, (unsigned)pairs, ckv::kFusedThreads, (size_t)(cand + 3) / 4 * 4 * 8, pool->overlap, 0, stream));
+        pool->launches += 1;
+        return CKV_OK;
+    }
     if (cand > 0) {
         const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
         const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, (long long)ckv::kScoreCtas * pool->num_sms);

@@ -334,6 +334,7 @@ constexpr int kScoreWarps = 6;
 constexpr int kScoreStages = 2;
 constexpr int kScoreCtas = 4;
 constexpr int kMaxSelectThreads = 1024;
+constexpr int kFusedThreads = 256;
 
 __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -410,6 +411,31 @@ struct QueryFragments {
         step1 = __shfl_sync(0xffffffffu, step, (2 * t + 1) * 4);
     }
 };
+
+// One tile: the keys (ordered scores) of rows g and g + 8 from lane (g, t)'s pieces a and b of their records.
+// Lane t = 0 of a row of four gets row g's, t = 1 row g + 8's; row_step is the step of that lane's row.
+template <int D>
+__device__ __forceinline__ uint32_t tile_key(const uint4 (&a)[2 * D / 64], const uint4 (&b)[2 * D / 64], const QueryFragments<D> &q, float row_step, int t)
+{
+    constexpr int P = 2 * D / 64;
+    int acc[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const uint32_t *q8 = i < P / 2 ? q.neg[i] : q.pos[i - P / 2];
+        mma_s8_16832(acc, a[i].x, b[i].x, a[i].y, b[i].y, q8[0], q8[1]);
+        mma_s8_16832(acc, a[i].z, b[i].z, a[i].w, b[i].w, q8[2], q8[3]);
+    }
+    float x0 = fmaxf(q.step0 >= 0.f ? (float)acc[0] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[1] * q.step1 : -INFINITY);
+    float x1 = fmaxf(q.step0 >= 0.f ? (float)acc[2] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[3] * q.step1 : -INFINITY);
+    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
+    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
+    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
+    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
+    // 2^-22: sums stay below 2^21, steps below 2^123; + 0 makes a negative zero positive
+    const float s = (t == 0 ? x0 : x1) * (row_step * 0x1p-22f) + 0.f;
+    const uint32_t bits = __float_as_uint(s);
+    return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
+}
 
 template <int D>
 struct ScoreLayout {
@@ -544,30 +570,17 @@ score_pages_kernel(const SelectParams p)
         asm volatile("cp.async.wait_group %0;" ::"n"(kScoreStages - 1) : "memory");
         __syncwarp();
         const uint8_t *stage = s_ring + ((threadIdx.x >> 5) * kScoreStages + done % kScoreStages) * Lay::kStageBytes;
-        int acc[4] = {0, 0, 0, 0};
+        uint4 a[P], b[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const uint4 a = *(const uint4 *)(stage + i * 512 + lane * 16), b = *(const uint4 *)(stage + (P + i) * 512 + lane * 16);
-            const uint32_t *q8 = i < P / 2 ? q.neg[i] : q.pos[i - P / 2];
-            mma_s8_16832(acc, a.x, b.x, a.y, b.y, q8[0], q8[1]);
-            mma_s8_16832(acc, a.z, b.z, a.w, b.w, q8[2], q8[3]);
+            a[i] = *(const uint4 *)(stage + i * 512 + lane * 16);
+            b[i] = *(const uint4 *)(stage + (P + i) * 512 + lane * 16);
         }
-        const float row_step = *(const float *)(stage + Lay::kStepsOff + ((t & 1) * 8 + g) * 4);
+        const uint32_t key = tile_key<D>(a, b, q, *(const float *)(stage + Lay::kStepsOff + ((t & 1) * 8 + g) * 4), t);
         __syncwarp();                            // the stage has been read
         issue();
-        float x0 = fmaxf(q.step0 >= 0.f ? (float)acc[0] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[1] * q.step1 : -INFINITY);
-        float x1 = fmaxf(q.step0 >= 0.f ? (float)acc[2] * q.step0 : -INFINITY, q.step1 >= 0.f ? (float)acc[3] * q.step1 : -INFINITY);
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 1));
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 1));
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, 2));
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, 2));
         const int c = cc.tile * 16 + g + (t == 0 ? 0 : 8);
-        if (t < 2 && c < cc.cand) {
-            // 2^-22: sums stay below 2^21, steps below 2^123; + 0 makes a negative zero positive
-            const float s = (t == 0 ? x0 : x1) * (row_step * 0x1p-22f) + 0.f;
-            const uint32_t bits = __float_as_uint(s);
-            p.keys[(size_t)pair * p.key_stride + c] = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
-        }
+        if (t < 2 && c < cc.cand) p.keys[(size_t)pair * p.key_stride + c] = key;
         cc.next(p);
     }
 }
@@ -579,14 +592,16 @@ constexpr int kSelectRounds = 4;     // 8 bits of the keys' range each
 // are in shared memory.  Few keys a thread and many threads are best, as the code runs once, from a cold
 // instruction cache: over 2048 pages 4 keys a thread make sparse_b64's selection 41.5 us with the scores,
 // 8 keys 43, 16 keys 45.5, the keys in shared memory 44-51.
-template <int kKeys>
-__global__ void __launch_bounds__(kMaxSelectThreads)
+// kScoreD > 0: few pairs with short tables; the CTA scores its pair's pages itself (head_dim kScoreD), one
+// launch in place of two.
+template <int kKeys, int kScoreD = 0>
+__global__ void __launch_bounds__(kScoreD > 0 ? kFusedThreads : kMaxSelectThreads)
 select_pages_kernel(const SelectParams p)
 {
     constexpr bool kInRegisters = kKeys > 0;
     constexpr int K = kInRegisters ? kKeys : 1;
     static_assert(K == 1 || K % 4 == 0, "keys are loaded four at a time");
-    extern __shared__ uint32_t s_words[];        // [candidates] page ids or keys
+    extern __shared__ __align__(16) uint32_t s_words[];          // [candidates] page ids or keys; kScoreD: ids, then keys
     __shared__ __align__(16) int s_hist[kSelectRounds][kSelectBins];
     __shared__ uint32_t s_range[3][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -612,7 +627,7 @@ select_pages_kernel(const SelectParams p)
     };
     int place0 = 0;
     const int32_t end0 = (int)threadIdx.x < ends ? end_page(threadIdx.x, place0) : 0;
-    if (chosen) {
+    if (kScoreD == 0 && chosen) {
         for (int i = threadIdx.x; i < kSelectRounds * kSelectBins; i += blockDim.x) (&s_hist[0][0])[i] = 0;
         if constexpr (kInRegisters)
             for (int i = threadIdx.x; i < cand; i += blockDim.x) s_words[i] = (uint32_t)__ldg(table + p.sink + i);
@@ -632,6 +647,36 @@ select_pages_kernel(const SelectParams p)
     }
     if (!chosen) return;
 
+    if constexpr (kScoreD > 0) {
+        constexpr int P = 2 * kScoreD / 64;
+        const int g = lane >> 2, t = lane & 3, h = pair % p.num_kv_heads;
+        uint32_t *s_keys = s_words + ((cand + 3) & ~3);
+        QueryFragments<kScoreD> q;
+        for (int base = warp * 16; base < cand; base += warps * 16) {
+            const int c0 = base + g, c1 = c0 + 8;
+            int page[2] = {c0 < cand ? __ldg(table + p.sink + c0) : 0, c1 < cand ? __ldg(table + p.sink + c1) : 0};
+            if (t < 2 && base + g + 8 * t < cand) s_words[base + g + 8 * t] = (uint32_t)(t == 0 ? page[0] : page[1]);
+            size_t at[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (page[x] < 0 || page[x] >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page[x] = 0; }
+                at[x] = (size_t)page[x] * p.num_kv_heads + h;
+            }
+            uint4 a[P], b[P];
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                a[i] = __ldg((const uint4 *)(p.records + at[0] * 2 * kScoreD) + i * 4 + t);
+                b[i] = __ldg((const uint4 *)(p.records + at[1] * 2 * kScoreD) + i * 4 + t);
+            }
+            const float row_step = __ldg(p.steps + (t & 1 ? at[1] : at[0]));
+            if (base == warp * 16) q.load(p.q + (size_t)pair * p.group * kScoreD, p.group, lane);
+            const uint32_t key = tile_key<kScoreD>(a, b, q, row_step, t);
+            if (t < 2 && base + g + 8 * t < cand) s_keys[base + g + 8 * t] = key;
+        }
+        for (int i = threadIdx.x; i < kSelectRounds * kSelectBins; i += blockDim.x) (&s_hist[0][0])[i] = 0;
+        __syncthreads();
+    }
+
     // thread x owns the keys first .. last - 1 (contiguous, so that context order is thread order)
     const uint32_t *keys = p.keys + (size_t)pair * p.key_stride;
     const int share = kInRegisters ? K : ((cand + blockDim.x - 1) / blockDim.x) | 1;     // odd: no bank conflicts
@@ -642,7 +687,8 @@ select_pages_kernel(const SelectParams p)
 #pragma unroll
         for (int x = 0; x < K; x += 4) {
             uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (first + x < cand) v = __ldg((const uint4 *)(keys + first + x));          // the stride is a multiple of 4
+            if (first + x < cand)                                            // the stride is a multiple of 4
+                v = kScoreD > 0 ? *(const uint4 *)(s_words + ((cand + 3) & ~3) + first + x) : __ldg((const uint4 *)(keys + first + x));
             own[x] = v.x; own[x + 1] = v.y; own[x + 2] = v.z; own[x + 3] = v.w;
         }
 #pragma unroll

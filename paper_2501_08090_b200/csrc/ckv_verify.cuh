@@ -110,7 +110,7 @@ struct Weights {
     using Vec = ProbVec<T>;
     static constexpr int kVec = Vec::kVec;
     static constexpr int kStripe = 32 * kVec;
-    static constexpr int kBatch = kDraft ? 2 : 8;                // stripes whose loads are in flight together
+    static constexpr int kBatch = kDraft ? 2 : sizeof(T) == 2 ? 4 : 8;      // stripes whose loads are in flight together
     const T *p, *q;
     int vocab, hole, lane, skip;
 
@@ -208,8 +208,10 @@ struct Weights {
     {
         constexpr int kAt = kDraft ? 2 : 4;      // stripes at a time: their sums stay in registers
         Batch b;
-        int last = -1;                           // last stripe with any weight
-        for (int at = from; at < to; at += kAt) {
+        int hit = -1;                            // the crossing stripe, or so far the last one with any weight
+        double hit_run = run;
+        bool found = false;
+        for (int at = from; at < to && !found; at += kAt) {
             load(b, at, min(to, at + kAt));
             double sum[kAt];
 #pragma unroll
@@ -224,14 +226,15 @@ struct Weights {
                 for (int k = 0; k < kAt; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
 #pragma unroll
             for (int k = 0; k < kAt; ++k) {
-                if (sum[k] > 0.0) {
-                    last = at + k;
-                    if (run + sum[k] > goal) return in_stripe(at + k, run, goal);
+                if (sum[k] > 0.0 && !found) {
+                    hit = at + k;
+                    hit_run = run;
+                    found = run + sum[k] > goal;
                 }
                 run += sum[k];
             }
         }
-        return last < 0 ? -1 : in_stripe(last, run, INFINITY);
+        return hit < 0 ? -1 : in_stripe(hit, hit_run, found ? goal : INFINITY);
     }
     __device__ int in_stripe(int stripe, double run, double goal) const
     {

@@ -161,16 +161,18 @@ def test_bounds_balance_over_very_uneven_requests():
 
 @pytest.mark.parametrize("Hq,Hkv,d", LAYOUTS)
 @pytest.mark.parametrize("budget,sink,recent", [(6, 1, 2), (9, 0, 1), (4, 2, 2), (40, 3, 5), (1, 0, 1)])
-def test_selection_and_attention(Hq, Hkv, d, budget, sink, recent):
-    c = Case([1, 16 * budget, 16 * budget + 1, 17, 1000, 333, 16 * 70], Hq, Hkv, d, seed=Hq * 7 + d + budget)
+@pytest.mark.parametrize("width", [None, 300, 5000])                       # one kernel scores and selects, or two
+def test_selection_and_attention(Hq, Hkv, d, budget, sink, recent, width):
+    c = Case([1, 16 * budget, 16 * budget + 1, 17, 1000, 333, 16 * 70], Hq, Hkv, d, seed=Hq * 7 + d + budget, width=width)
     c.update()
     c.check(budget, sink, recent)
     c.close()
 
 
 @pytest.mark.parametrize("distinct", [1, 2, 5])
-def test_equal_scores_go_to_the_earlier_page(distinct):
-    c = Case([1600, 3217, 48], 8, 2, 128, seed=distinct, distinct=distinct)
+@pytest.mark.parametrize("width", [None, 260, 4200, 9000])
+def test_equal_scores_go_to_the_earlier_page(distinct, width):
+    c = Case([1600, 3217, 48], 8, 2, 128, seed=distinct, distinct=distinct, width=width)
     c.update()
     c.check(17, 1, 2)
     c.close()
@@ -289,9 +291,10 @@ def test_layers_have_their_own_pages_and_bounds():
     c.close()
 
 
-def test_plain_stream_order():
+@pytest.mark.parametrize("width", [None, 600])
+def test_plain_stream_order(width):
     """With kernel overlap off, and with inputs that the kernel just before writes, results are the same."""
-    c = Case([3000, 517, 90, 2048], 32, 8, 128, seed=17)
+    c = Case([3000, 517, 90, 2048], 32, 8, 128, seed=17, width=width)
     c.update()
     pages, lens, out = c.out(20)
     c.kp.decode_attention_sparse(0, c.btd, c.sld, c.qd, c.index, pages, lens, out)
@@ -331,9 +334,10 @@ def test_a_budget_beyond_the_context_is_whole_attention():
     c.close()
 
 
-def test_streams_graphs_and_repetition():
+@pytest.mark.parametrize("width", [None, 600])
+def test_streams_graphs_and_repetition(width):
     """The same bits eagerly, on another stream, captured and replayed after the inputs changed and back."""
-    c = Case([3000, 517, 90, 2048], 32, 8, 128, seed=13)
+    c = Case([3000, 517, 90, 2048], 32, 8, 128, seed=13, width=width)
     c.update()
     pages, lens, out = c.out(20)
     args = (0, c.btd, c.sld, c.qd, c.index, pages, lens, out)
