@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = [os.path.join(CSRC, n) for n in ("ckv_api.cu", "ckv_ops.cu", "ckv_autoscaler.cc", "ckv_global_sim.cc")]
-HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "ckv_host.cuh", "ckv_rope.cuh",
+HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "ckv_host.cuh", "ckv_pagelist.cuh", "ckv_rope.cuh",
                                           "ckv_sparse.cuh", "ckv_verify.cuh")] + \
           [os.path.join(_ROOT, "include", n) for n in ("chiron_kv.h", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")

@@ -12,6 +12,7 @@
 
 #include "ckv_device.cuh"
 #include "ckv_host.cuh"
+#include "ckv_pagelist.cuh"
 
 using ckv::aligned16;
 using ckv::check_call;
@@ -37,6 +38,7 @@ namespace {
 constexpr int kWarps128 = CKV_WARPS128, kStages128 = CKV_STAGES128;   // head_dim 128: 4 warps x 3 stages x 16 KB = 192 KB per SM
 constexpr int kWarps64 = CKV_WARPS64, kStages64 = CKV_STAGES64;       // head_dim 64:  4 warps x 4 stages x 8 KB
 constexpr int kMaxProfile = 4096;
+constexpr int kListTurns = 2;                                         // page_list_attn_kernel: tiles a warp takes at most
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -152,6 +154,42 @@ int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t
     attr[0].val.programmaticStreamSerializationAllowed = pool->overlap ? 1 : 0;
     lc.attrs = attr;
     lc.numAttrs = 1;
+    CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, ap));
+    return CKV_OK;
+}
+
+// CTAs of page_list_attn_kernel's clusters for lists of up to `pages` pages; 0: paged_decode_attn_kernel is used.
+unsigned list_cluster(const ckv_pool *pool, long long pairs, int pages)
+{
+    const long long tiles = (pages + ckv::kPagesPerTile - 1) / ckv::kPagesPerTile;
+    unsigned c = 1;
+    while (c < 8 && c * 8 < tiles && 2 * c * pairs <= pool->num_sms) c *= 2;
+    return pairs * c <= pool->num_sms && tiles <= (long long)kListTurns * 8 * c ? c : 0;
+}
+
+template <int D>
+int32_t launch_list_attention(ckv_pool *pool, const ckv::AttnParams &ap, unsigned cluster, cudaStream_t stream)
+{
+    using Lay = ckv::ListLayout<D>;
+    static thread_local int configured_device = -1;
+    auto kernel = ckv::page_list_attn_kernel<D>;
+    if (configured_device != pool->device) {
+        CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes));
+        configured_device = pool->device;
+    }
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)(ap.batch * ap.num_kv_heads) * cluster);
+    lc.blockDim = dim3(Lay::kWarps * 32);
+    lc.dynamicSmemBytes = Lay::kSmemBytes;
+    lc.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pool->overlap ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
     CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, ap));
     return CKV_OK;
 }
@@ -465,7 +503,10 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
         ap.q_base = base;
         ap.q_pass = std::min(per_pass, q_len - base);
         int32_t rc;
-        if (head_pages > 0)
+        const unsigned cluster = head_pages > 0 ? list_cluster(pool, (long long)batch * c.num_kv_heads, head_pages) : 0;
+        if (cluster > 0)
+            rc = c.head_dim == 128 ? launch_list_attention<128>(pool, ap, cluster, s) : launch_list_attention<64>(pool, ap, cluster, s);
+        else if (head_pages > 0)
             rc = c.head_dim == 128 ? launch_attention<128, kWarps128, kStages128, false, true>(pool, ap, s)
                                    : launch_attention<64, kWarps64, kStages64, false, true>(pool, ap, s);
         else if (c.head_dim == 128)

@@ -1,0 +1,284 @@
+// Attention over short lists of pages, for few (request, kv head) pairs: the form of
+// paged_decode_attn_kernel for launches that are all latency.
+#pragma once
+
+#include "ckv_device.cuh"
+
+namespace ckv {
+
+// A cluster of CTAs per (request, kv head), a tile of 32 tokens per warp and turn.  The arithmetic of a
+// tile is paged_decode_attn_kernel's (S^T = K Q^T, softmax in the log2 domain, O^T += V^T P^T on
+// mma.sync); the difference is how partials meet.  There the warps' spans cross pairs, and partials of
+// different CTAs meet in global memory: a chain of publish, fence, count, fetch and fold that takes
+// 4 to 8 us, which a long stream hides and a short list does not.  Here a pair's partials never
+// leave the cluster: they are folded in the CTA's shared memory, a warp per column, then across the
+// cluster through distributed shared memory, a CTA per column, in a fixed order.
+//
+//   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i   over warps, then over CTAs.
+template <int D>
+struct ListLayout {
+    static constexpr int kWarps = 8;
+    static constexpr int kHalves = D / 64;
+    static constexpr int kHalfBytes = 32 * 128;                  // one TMA box: 32 rows x 128 B
+    static constexpr int kPageBytes = kHalves * kHalfBytes;
+    static constexpr int kStageBytes = kPagesPerTile * kPageBytes;
+    static constexpr int kPitch = D + 4;                         // floats per row of a partial (bank spread)
+    static constexpr int kPartFloats = kMaxGroup * kPitch + 2 * kMaxGroup;       // rows, then m[8], l[8]
+    static constexpr int kPartOff = kWarps * kStageBytes;
+    static constexpr int kBarOff = kPartOff + (kWarps + 1) * kPartFloats * 4;    // a partial per warp, and the CTA's
+    static constexpr int kSmemBytes = kBarOff + kWarps * 8 + 1024;
+};
+
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+
+template <int D>
+__global__ void __launch_bounds__(ListLayout<D>::kWarps * 32, 1)
+page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p)
+{
+    using Lay = ListLayout<D>;
+    constexpr int W = Lay::kWarps, kKSteps = D / 16, kDTiles = D / 16;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
+    const int pair = blockIdx.x / ctas, r = pair / p.num_kv_heads, h = pair % p.num_kv_heads;
+    const int G = p.group;
+    const uint32_t stage = smem_u32(smem) + warp * Lay::kStageBytes, bar = smem_u32(smem + Lay::kBarOff) + warp * 8;
+    float *part = (float *)(smem + Lay::kPartOff) + warp * Lay::kPartFloats;
+    if (lane == 0) {
+        prefetch_tensormap(&tmap);
+        mbar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+    }
+    __syncwarp();
+    // Behind a selection lengths and queries may be read before the wait, as in paged_decode_attn_kernel.
+    if (p.early_loads < 0) grid_dependency_wait();
+    const int L = attended_length<true>(p, r);
+    const int tiles = tiles_of_length(L, p.max_pages_per_req);
+    uint16_t *out_rows = p.out + ((size_t)r * p.num_q_heads + h * G) * D;
+    uint32_t qf[kKSteps][2];
+    {
+        const int c = lane >> 2;
+        const uint32_t *qrow = (const uint32_t *)(p.q + ((size_t)r * p.num_q_heads + h * G + c) * D);
+#pragma unroll
+        for (int ks = 0; ks < kKSteps; ++ks) {
+            qf[ks][0] = c < G ? __ldg(qrow + ks * 8 + (lane & 3)) : 0u;
+            qf[ks][1] = c < G ? __ldg(qrow + ks * 8 + 4 + (lane & 3)) : 0u;
+        }
+    }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (tiles == 0) {                            // unusable: the same for the whole cluster
+        if (rank == 0) {
+            for (int i = threadIdx.x; i < G * D / 8; i += W * 32) ((uint4 *)out_rows)[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
+        }
+        return;
+    }
+
+    const int32_t *list = p.block_tables + (size_t)pair * p.max_pages_per_req;
+    const uint64_t policy = l2_evict_first_policy();
+    auto tokens_of = [&](int tile) { return min(kTileTokens, L - tile * kTileTokens); };
+    auto issue = [&](int tile) {
+        const int np = (tokens_of(tile) + kPageSize - 1) / kPageSize;
+        if (lane == 0) mbar_arrive_expect_tx(bar, np * Lay::kPageBytes);
+        __syncwarp();
+        if (lane < np * Lay::kHalves) {
+            const int pg = lane / Lay::kHalves, hf = lane % Lay::kHalves;
+            int page = __ldg(list + tile * kPagesPerTile + pg);
+            if (page < 0 || page >= p.num_pages) {
+                atomicOr(p.status, kStatusBadPage);
+                page = 0;
+            }
+            const int y = ((p.layer_page_base + page) * p.num_kv_heads + h) * 32;
+            tma_load_2d(stage + pg * Lay::kPageBytes + hf * Lay::kHalfBytes, &tmap, hf * 64, y, bar, policy);
+        }
+    };
+    const int step = ctas * W;
+    int tile = rank * W + warp;
+    if (tile < tiles) issue(tile);
+
+    const int g0 = (lane & 3) * 2;               // first of the two columns this lane accumulates
+    uint32_t k_off[4], v_off[4];                 // ldmatrix lane offsets inside one page block
+    {
+        const int krow = (lane & 7) + ((lane >> 3) & 1) * 8, ksel = lane >> 4;
+        const int vrow = 16 + (lane & 7) + (lane >> 4) * 8, vsel = (lane >> 3) & 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            k_off[j] = krow * 128 + (((j * 2 + ksel) ^ (lane & 7)) << 4);
+            v_off[j] = vrow * 128 + (((j * 2 + vsel) ^ (lane & 7)) << 4);
+        }
+    }
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float o[kDTiles][4];
+#pragma unroll
+    for (int dt = 0; dt < kDTiles; ++dt) o[dt][0] = o[dt][1] = o[dt][2] = o[dt][3] = 0.f;
+    bool alive = true;
+    uint32_t phase = 0;
+#pragma unroll 1
+    for (; tile < tiles && alive; tile += step, phase ^= 1u) {
+        alive = __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase, p.status));
+        if (!alive) break;
+        const int ntok = tokens_of(tile), np = (ntok + kPageSize - 1) / kPageSize;
+        if (ntok & (kPageSize - 1)) {
+            // value rows past the context's end may hold anything; their weights are zero, 0 * NaN is not
+            const int row0 = ntok - (np - 1) * kPageSize, pieces = (kPageSize - row0) * 8 * Lay::kHalves;
+            for (int i = lane; i < pieces; i += 32) {
+                const int hf = i / ((kPageSize - row0) * 8), rem = i % ((kPageSize - row0) * 8);
+                const uint32_t at = stage + (np - 1) * Lay::kPageBytes + hf * Lay::kHalfBytes + (16 + row0 + rem / 8) * 128 + (rem % 8) * 16;
+                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0u) : "memory");
+            }
+            fence_proxy_async();                  // these writes precede the stage's next fill
+            __syncwarp();
+        }
+        float s[kPagesPerTile][4];
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) s[mt][0] = s[mt][1] = s[mt][2] = s[mt][3] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < kKSteps; ++ks) {
+#pragma unroll
+            for (int mt = 0; mt < kPagesPerTile; ++mt) {
+                if (mt < np) {
+                    uint32_t a[4];
+                    ldmatrix_x4(a, stage + mt * Lay::kPageBytes + (ks / 4) * Lay::kHalfBytes + k_off[ks % 4]);
+                    mma_bf16_16816(s[mt], a, qf[ks][0], qf[ks][1]);
+                }
+            }
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (mt * kPageSize + (lane >> 2) + (i >= 2 ? 8 : 0) >= ntok) s[mt][i] = -INFINITY;      // selected, never multiplied
+            mx0 = fmaxf(mx0, fmaxf(s[mt][0], s[mt][2]));
+            mx1 = fmaxf(mx1, fmaxf(s[mt][1], s[mt][3]));
+        }
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, x));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, x));
+        }
+        const float mn0 = fmaxf(m0, mx0 * p.scale_log2), mn1 = fmaxf(m1, mx1 * p.scale_log2);
+        const float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);
+        m0 = mn0; m1 = mn1;
+        l0 *= al0; l1 *= al1;
+#pragma unroll
+        for (int dt = 0; dt < kDTiles; ++dt) { o[dt][0] *= al0; o[dt][2] *= al0; o[dt][1] *= al1; o[dt][3] *= al1; }
+        uint32_t pb[kPagesPerTile][2];
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+            const float p0 = fast_exp2(fmaf(s[mt][0], p.scale_log2, -mn0)), p1 = fast_exp2(fmaf(s[mt][1], p.scale_log2, -mn1));
+            const float p2 = fast_exp2(fmaf(s[mt][2], p.scale_log2, -mn0)), p3 = fast_exp2(fmaf(s[mt][3], p.scale_log2, -mn1));
+            l0 += p0 + p2;
+            l1 += p1 + p3;
+            pb[mt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
+            pb[mt][1] = movmatrix_trans(pack_bf16x2(p2, p3));
+        }
+#pragma unroll
+        for (int dt = 0; dt < kDTiles; ++dt) {
+#pragma unroll
+            for (int mt = 0; mt < kPagesPerTile; ++mt) {
+                if (mt < np) {
+                    uint32_t a[4];
+                    ldmatrix_x4_trans(a, stage + mt * Lay::kPageBytes + (dt / 4) * Lay::kHalfBytes + v_off[dt % 4]);
+                    mma_bf16_16816(o[dt], a, pb[mt][0], pb[mt][1]);
+                }
+            }
+        }
+        if (tile + step < tiles) issue(tile + step);              // the stage's reads have been consumed
+    }
+
+    // Do not go on while a copy into this warp's stage may still be in flight (only after a wait gave up).
+    if (!alive) mbar_wait_bounded(bar, phase, p.status);
+
+    // ---- this warp's partial (m = -inf, l = 0 if it had no tile)
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) {
+        l0 += __shfl_xor_sync(0xffffffffu, l0, x);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+    }
+#pragma unroll
+    for (int dt = 0; dt < kDTiles; ++dt) {
+        const int d = dt * 16 + (lane >> 2);
+        part[g0 * Lay::kPitch + d] = o[dt][0];
+        part[(g0 + 1) * Lay::kPitch + d] = o[dt][1];
+        part[g0 * Lay::kPitch + d + 8] = o[dt][2];
+        part[(g0 + 1) * Lay::kPitch + d + 8] = o[dt][3];
+    }
+    if (lane < 4) {
+        float *ml = part + kMaxGroup * Lay::kPitch;
+        ml[g0] = m0; ml[g0 + 1] = m1;
+        ml[kMaxGroup + g0] = l0; ml[kMaxGroup + g0 + 1] = l1;
+    }
+    __syncthreads();
+
+    // ---- the CTA's fold: warp g takes column g, a lane four elements of its row
+    const float *parts = (const float *)(smem + Lay::kPartOff);
+    float *mine = (float *)(smem + Lay::kPartOff) + W * Lay::kPartFloats;
+    auto store = [&](int g, float4 acc, float l) {
+        const float inv = 1.f / l;
+        uint2 packed;
+        packed.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+        packed.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+        *(uint2 *)(out_rows + g * D + lane * 4) = packed;
+    };
+    if (warp < G) {
+        float M = -INFINITY, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, parts[w * Lay::kPartFloats + kMaxGroup * Lay::kPitch + warp]);
+        const float ref = M == -INFINITY ? 0.f : M;              // no warp of this CTA had a tile
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float *src = parts + w * Lay::kPartFloats;
+            const float f = fast_exp2(src[kMaxGroup * Lay::kPitch + warp] - ref);
+            l += f * src[kMaxGroup * Lay::kPitch + kMaxGroup + warp];
+            if (lane * 4 < D) {
+                const float4 a = *(const float4 *)(src + warp * Lay::kPitch + lane * 4);
+                acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
+            }
+        }
+        if (ctas == 1) {
+            if (lane * 4 < D && alive) store(warp, acc, l);
+        } else {
+            if (lane * 4 < D) *(float4 *)(mine + warp * Lay::kPitch + lane * 4) = acc;
+            if (lane == 0) { mine[kMaxGroup * Lay::kPitch + warp] = M; mine[kMaxGroup * Lay::kPitch + kMaxGroup + warp] = l; }
+        }
+    }
+    if (ctas == 1) return;
+    cluster_barrier();
+    // ---- the cluster's fold: CTA c takes columns c, c + ctas, ...
+    for (int g = rank + warp * ctas; g < G; g += W * ctas) {
+        const uint32_t row = smem_u32(mine) + (g * Lay::kPitch + lane * 4) * 4, ml = smem_u32(mine) + (kMaxGroup * Lay::kPitch + g) * 4;
+        float M = -INFINITY, l = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = 0; c < ctas; ++c) M = fmaxf(M, ld_cluster_f32(cluster_map(ml, c)));
+        const float ref = M == -INFINITY ? 0.f : M;              // only after a wait gave up everywhere
+        for (int c = 0; c < ctas; ++c) {
+            const float f = fast_exp2(ld_cluster_f32(cluster_map(ml, c)) - ref);
+            l += f * ld_cluster_f32(cluster_map(ml + 4 * kMaxGroup, c));
+            if (lane * 4 < D) {
+                const float4 a = ld_cluster_f32x4(cluster_map(row, c));
+                acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
+            }
+        }
+        if (lane * 4 < D) store(g, acc, l);
+    }
+    cluster_barrier();                            // nobody leaves while others read its partial
+}
+
+}  // namespace ckv

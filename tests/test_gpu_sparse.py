@@ -188,11 +188,36 @@ def test_one_long_context():
         c.close()
 
 
-def test_many_requests():
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 4, 64), (8, 4, 128), (28, 4, 128), (16, 2, 64)])
+@pytest.mark.parametrize("part", [None, 5, 2048])
+def test_many_requests(Hq, Hkv, d, part):
+    """More pairs than SMs: attention streams over spans that cross pairs, whatever the partition."""
     rng = np.random.default_rng(8)
-    c = Case(rng.integers(1, 900, size=150), 4, 4, 64, seed=7)
+    c = Case(rng.integers(1, 900, size=150), Hq, Hkv, d, seed=7)
     c.update()
-    c.check(12, 1, 3, requests=range(0, 150, 7))
+    if part:
+        c.kp.set_partition(part)
+    c.check(12, 1, 3, requests=range(0, 150, 17))
+    c.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 1, 64), (32, 8, 128), (14, 2, 128)])
+@pytest.mark.parametrize("budget", [1, 2, 15, 16, 17, 31, 33, 64, 127, 200])
+def test_few_pairs_of_every_list_length(Hq, Hkv, d, budget):
+    """One request alone: one CTA to a cluster of 8 a pair, one or two tiles a warp, lists beyond that."""
+    c = Case([16 * 230 + 3], Hq, Hkv, d, seed=budget)
+    c.update()
+    c.check(budget, 0, 1)
+    for tokens in {1, 16 * budget, 16 * budget - 15, max(1, 8 * budget)}:
+        lists = torch.from_numpy(np.stack([c.bt[:, 10:10 + budget]] * Hkv, 1)).cuda()
+        out = c.out(budget)[2]
+        c.kp.decode_attention_pages(0, lists, torch.tensor([tokens], dtype=torch.int32, device="cuda"), c.qd, out)
+        assert c.kp.check_status() == 0
+        pool, q = widen(c.pool), widen(c.q)
+        for h in range(Hkv):
+            G = Hq // Hkv
+            ref = ref_ops.attend(pool, [int(x) for x in c.bt[0][10:10 + budget]], tokens, q[0, h * G:h * G + G], h)
+            assert_close(dev_to_bits(out[0, h * G:h * G + G]), ref, "tokens %d kv head %d" % (tokens, h))
     c.close()
 
 
@@ -323,14 +348,19 @@ def test_contexts_wider_than_the_registers_hold():
     c.close()
 
 
-def test_a_budget_beyond_the_context_is_whole_attention():
-    c = Case([700, 33, 1], 8, 2, 128, seed=12)
+@pytest.mark.parametrize("batch", [1, 40])
+def test_a_budget_beyond_the_context_is_whole_attention(batch):
+    c = Case([700, 33, 1] * batch, 8, 2, 128, seed=12)
     c.update()
     pages, lens, out = c.out(64)
-    whole = torch.empty_like(out)
     c.kp.decode_attention_sparse(0, c.btd, c.sld, c.qd, c.index, pages, lens, out)
-    c.kp.decode_attention(0, c.btd, c.sld, c.qd, whole)
-    assert lens.tolist() == [700, 33, 1] and torch.equal(out, whole)
+    assert lens.tolist() == [700, 33, 1] * batch
+    pool, q = widen(c.pool), widen(c.q)
+    for r in range(0, 3 * batch, 1 + 2 * (batch > 1)):
+        L = int(c.lens[r])
+        for h in range(2):
+            ref = ref_ops.attend(pool, [int(x) for x in c.bt[r][:-(-L // 16)]], L, q[r, 4 * h:4 * h + 4], h)
+            assert_close(dev_to_bits(out[r, 4 * h:4 * h + 4]), ref, "request %d head %d" % (r, h))
     c.close()
 
 
