@@ -228,9 +228,11 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *                     and NaN in q count as 0 here.  Requests of at most `budget` pages keep all.
  *                       d_pages  int32 [batch][Hkv][budget]: page ids in context order, then -1s
  *                       d_lens   int32 [batch]: tokens in the chosen pages (0 for an unusable length)
- *   decode_attention_pages   decode_attention over such a list: d_pages and d_lens take the places of block
- *                     tables and lengths, with a row of `budget` pages per (request, KV head).  It may
- *                     directly follow the kernel that writes them.
+ *   decode_attention_pages   attention as decode_attention's over such lists: d_pages and d_lens take the
+ *                     places of block tables and lengths, with a row of `budget` pages per (request,
+ *                     KV head).  It may directly follow the kernel that writes them.  A cluster of
+ *                     thread blocks owns a (request, KV head): ckv_set_partition and the span timeline
+ *                     do not apply, and results are bit-identical from run to run.
  *   decode_attention_sparse  both.
  * 1 <= recent, 0 <= sink, sink + recent <= budget.  For selection max_pages_per_req <= 49152 and
  * batch * Hkv * max_pages_per_req (rounded up to 4) <= 2^26.  Scores live in the handle's workspace: as

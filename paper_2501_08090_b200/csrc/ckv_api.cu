@@ -38,7 +38,6 @@ namespace {
 constexpr int kWarps128 = CKV_WARPS128, kStages128 = CKV_STAGES128;   // head_dim 128: 4 warps x 3 stages x 16 KB = 192 KB per SM
 constexpr int kWarps64 = CKV_WARPS64, kStages64 = CKV_STAGES64;       // head_dim 64:  4 warps x 4 stages x 8 KB
 constexpr int kMaxProfile = 4096;
-constexpr int kListTurns = 2;                                         // page_list_attn_kernel: tiles a warp takes at most
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -133,12 +132,12 @@ int32_t encode_pool_map(const ckv_config *cfg, const void *d_pool, CUtensorMap *
 
 namespace {
 
-template <int D, int W, int S, bool kMulti, bool kHeadTables = false>
+template <int D, int W, int S, bool kMulti>
 int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t stream)
 {
     using Lay = ckv::AttnLayout<D, W, S>;
     static thread_local int configured_device = -1;
-    auto kernel = ckv::paged_decode_attn_kernel<D, W, S, kMulti, kHeadTables>;
+    auto kernel = ckv::paged_decode_attn_kernel<D, W, S, kMulti>;
     if (configured_device != pool->device) {
         CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes));
         configured_device = pool->device;
@@ -158,27 +157,24 @@ int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t
     return CKV_OK;
 }
 
-// CTAs of page_list_attn_kernel's clusters for lists of up to `pages` pages; 0: paged_decode_attn_kernel is used.
-unsigned list_cluster(const ckv_pool *pool, long long pairs, int pages)
-{
-    const long long tiles = (pages + ckv::kPagesPerTile - 1) / ckv::kPagesPerTile;
-    unsigned c = 1;
-    while (c < 8 && c * 8 < tiles && 2 * c * pairs <= pool->num_sms) c *= 2;
-    return pairs * c <= pool->num_sms && tiles <= (long long)kListTurns * 8 * c ? c : 0;
-}
-
 template <int D>
-int32_t launch_list_attention(ckv_pool *pool, const ckv::AttnParams &ap, unsigned cluster, cudaStream_t stream)
+int32_t launch_list_attention(ckv_pool *pool, const ckv::ListParams &lp, cudaStream_t stream)
 {
     using Lay = ckv::ListLayout<D>;
     static thread_local int configured_device = -1;
     auto kernel = ckv::page_list_attn_kernel<D>;
     if (configured_device != pool->device) {
         CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes));
+        CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         configured_device = pool->device;
     }
+    // few pairs: clusters that together fit the GPU, with no more warps than a list has tiles
+    const long long pairs = (long long)lp.batch * lp.num_kv_heads;
+    const int tiles = (lp.budget + ckv::kPagesPerTile - 1) / ckv::kPagesPerTile;
+    unsigned cluster = 1;
+    while (cluster < 16 && (int)cluster * Lay::kWarps < tiles && 2 * cluster * pairs <= (long long)Lay::kCtas * pool->num_sms) cluster *= 2;
     cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((unsigned)(ap.batch * ap.num_kv_heads) * cluster);
+    lc.gridDim = dim3((unsigned)(pairs * cluster));
     lc.blockDim = dim3(Lay::kWarps * 32);
     lc.dynamicSmemBytes = Lay::kSmemBytes;
     lc.stream = stream;
@@ -190,7 +186,9 @@ int32_t launch_list_attention(ckv_pool *pool, const ckv::AttnParams &ap, unsigne
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
     lc.numAttrs = 2;
-    CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, ap));
+    CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, lp));
+    pool->launches += 1;
+    pool->pool_written = false;                  // whatever wrote the pool has completed before this kernel releases the next
     return CKV_OK;
 }
 
@@ -427,13 +425,10 @@ int32_t kv_append_multi(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_
                          stream);
 }
 
-// Attention for one layer, optionally with the KV append folded into the same kernel.  head_pages > 0:
-// the tables hold a row of that many pages per (request, kv head); context_pages > 0: they are what the
-// selection just launched writes, and the lengths are the whole contexts'.
+// Attention for one layer, optionally with the KV append folded into the same kernel.
 static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, int32_t q_len,
                                 const int32_t *d_block_tables, const int32_t *d_seq_lens, const void *d_q,
-                                const void *d_k_new, const void *d_v_new, void *d_out, void *stream,
-                                int32_t head_pages = 0, int32_t context_pages = 0)
+                                const void *d_k_new, const void *d_v_new, void *d_out, void *stream)
 {
     if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
     if (q_len < 1 || q_len > ckv::kMaxGroup) return fail(CKV_EINVAL, "%s: q_len %d outside [1, %d]", fn, q_len, ckv::kMaxGroup);
@@ -460,7 +455,7 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
     ap.trace = pool->wsp<unsigned long long>(pool->ws.trace);
     ap.status = pool->wsp<uint32_t>(pool->ws.status);
     ap.batch = batch;
-    ap.max_pages_per_req = head_pages > 0 ? head_pages : c.max_pages_per_req;
+    ap.max_pages_per_req = c.max_pages_per_req;
     ap.num_pages = c.num_pages;
     ap.num_kv_heads = c.num_kv_heads;
     ap.num_q_heads = c.num_q_heads;
@@ -470,7 +465,6 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
     ap.q_len = q_len;
     ap.q_base = 0;
     ap.q_pass = q_len;
-    ap.context_pages = context_pages;
     // A fused step may start loading tiles under its predecessor's tail -- unless that predecessor
     // may be a kernel of this library that writes the pool (an append or a swap-in).
     ap.early_loads = pool->inputs_from_predecessor ? -1 : pool->pool_written ? 0 : 1;
@@ -503,13 +497,7 @@ static int32_t attention_launch(ckv_pool *pool, const char *fn, int32_t layer, i
         ap.q_base = base;
         ap.q_pass = std::min(per_pass, q_len - base);
         int32_t rc;
-        const unsigned cluster = head_pages > 0 ? list_cluster(pool, (long long)batch * c.num_kv_heads, head_pages) : 0;
-        if (cluster > 0)
-            rc = c.head_dim == 128 ? launch_list_attention<128>(pool, ap, cluster, s) : launch_list_attention<64>(pool, ap, cluster, s);
-        else if (head_pages > 0)
-            rc = c.head_dim == 128 ? launch_attention<128, kWarps128, kStages128, false, true>(pool, ap, s)
-                                   : launch_attention<64, kWarps64, kStages64, false, true>(pool, ap, s);
-        else if (c.head_dim == 128)
+        if (c.head_dim == 128)
             rc = q_len > 1 ? launch_attention<128, kWarps128, kStages128, true>(pool, ap, s)
                            : launch_attention<128, kWarps128, kStages128, false>(pool, ap, s);
         else
@@ -546,16 +534,39 @@ int32_t decode_step(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t 
                             d_out, stream);
 }
 
+// Attention over lists of pages; context_pages > 0: the selection just launched writes them, and d_lens are the contexts'.
+static int32_t list_attention_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, int32_t budget,
+                                     const int32_t *d_pages, const int32_t *d_lens, const void *d_q, void *d_out,
+                                     void *stream, int32_t context_pages)
+{
+    if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
+    if (int32_t rc = ckv::check_budget(budget, fn)) return rc;
+    if (!d_pages || !d_lens || !d_q || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (!aligned16(d_q) || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: q/out not 16-byte aligned", fn);
+    const ckv_config &c = pool->cfg;
+    ckv::ListParams lp{};
+    lp.pages = d_pages;
+    lp.lens = d_lens;
+    lp.q = static_cast<const uint16_t *>(d_q);
+    lp.out = static_cast<uint16_t *>(d_out);
+    lp.status = pool->wsp<uint32_t>(pool->ws.status);
+    lp.batch = batch;
+    lp.budget = budget;
+    lp.num_pages = c.num_pages;
+    lp.num_kv_heads = c.num_kv_heads;
+    lp.group = c.num_q_heads / c.num_kv_heads;
+    lp.layer_page_base = layer * c.num_pages;
+    lp.context_pages = context_pages;
+    lp.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return c.head_dim == 128 ? launch_list_attention<128>(pool, lp, s) : launch_list_attention<64>(pool, lp, s);
+}
+
 int32_t decode_attention_pages(ckv_pool *pool, int32_t layer, int32_t batch, int32_t budget,
                                const int32_t *d_pages, const int32_t *d_lens, const void *d_q, void *d_out,
                                void *stream)
 {
-    if (int32_t rc = check_call(pool, layer, batch, "decode_attention_pages")) return rc;
-    if (int32_t rc = ckv::check_budget(pool, batch, budget, "decode_attention_pages")) return rc;
-    // the preceding kernel may be the one that writes the lists: this one waits before its plan
-    if (d_pages && d_lens && d_q && d_out && aligned16(d_q) && aligned16(d_out)) pool->inputs_from_predecessor = true;
-    return attention_launch(pool, "decode_attention_pages", layer, batch, 1, d_pages, d_lens, d_q, nullptr, nullptr, d_out,
-                            stream, budget);
+    return list_attention_launch(pool, "decode_attention_pages", layer, batch, budget, d_pages, d_lens, d_q, d_out, stream, 0);
 }
 
 int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
@@ -563,12 +574,12 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, co
                                 int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens,
                                 void *d_out, void *stream)
 {
-    if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "decode_attention_sparse: out is NULL or not 16-byte aligned");
-    if (int32_t rc = ckv::select_launch(pool, "decode_attention_sparse", layer, batch, d_block_tables, d_seq_lens, d_q, d_index,
-                                        index_bytes, budget, sink, recent, d_pages, d_lens, stream))
+    const char *fn = "decode_attention_sparse";
+    if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: out is NULL or not 16-byte aligned", fn);
+    if (int32_t rc = ckv::select_launch(pool, fn, layer, batch, d_block_tables, d_seq_lens, d_q, d_index, index_bytes, budget,
+                                        sink, recent, d_pages, d_lens, stream))
         return rc;
-    return attention_launch(pool, "decode_attention_sparse", layer, batch, 1, d_pages, d_seq_lens, d_q, nullptr, nullptr, d_out,
-                            stream, budget, pool->cfg.max_pages_per_req);
+    return list_attention_launch(pool, fn, layer, batch, budget, d_pages, d_seq_lens, d_q, d_out, stream, pool->cfg.max_pages_per_req);
 }
 
 int32_t kv_read_probe(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,

@@ -185,15 +185,14 @@ struct SpanStart {
 };
 
 // Requests with an unusable length get their output rows cleared and the status word flagged.
-// Executed by one warp of the grid.  length_of(r): the context length of request r.
-template <typename LengthOf>
-__device__ __forceinline__ void flag_unusable_requests(LengthOf length_of, int batch,
+// Executed by one warp of the grid.
+__device__ __forceinline__ void flag_unusable_requests(const int32_t *__restrict__ seq_lens, int batch,
                                                        int max_pages_per_req, int min_len, int lane, uint16_t *out,
                                                        int out_row_elems, uint32_t *status)
 {
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        const bool bad = r < batch && tiles_of_length(length_of(r), max_pages_per_req, min_len) == 0;
+        const bool bad = r < batch && tiles_of_length(__ldg(seq_lens + r), max_pages_per_req, min_len) == 0;
         unsigned todo = __ballot_sync(0xffffffffu, bad);
         if (todo && lane == 0) atomicOr(status, kStatusBadLength);
         while (todo) {                                   // the whole warp clears one row at a time
@@ -210,15 +209,14 @@ __device__ __forceinline__ int units_of_tiles(int t) { return t > 0 ? t + kPiece
 
 // Executed by one whole warp.  Two passes over seq_lens: the total number of units, then the
 // (request, kv head) that holds unit span*q and the first tile at or after it.
-template <typename LengthOf>
-__device__ __forceinline__ SpanStart warp_plan(LengthOf length_of, int batch, int max_pages_per_req,
+__device__ __forceinline__ SpanStart warp_plan(const int32_t *__restrict__ seq_lens, int batch, int max_pages_per_req,
                                                int num_kv_heads, int num_spans, int span, int lane, int min_len = 1)
 {
     SpanStart s;
     int sum = 0;
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        if (r < batch) sum += units_of_tiles(tiles_of_length(length_of(r), max_pages_per_req, min_len));
+        if (r < batch) sum += units_of_tiles(tiles_of_length(__ldg(seq_lens + r), max_pages_per_req, min_len));
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
@@ -233,7 +231,7 @@ __device__ __forceinline__ SpanStart warp_plan(LengthOf length_of, int batch, in
     long long running = 0;                               // units (all heads) before request `base`
     for (int base = 0; base < batch; base += 32) {
         const int r = base + lane;
-        const int L = r < batch ? length_of(r) : 0;
+        const int L = r < batch ? __ldg(seq_lens + r) : 0;
         const int t = r < batch ? tiles_of_length(L, max_pages_per_req, min_len) : 0;
         int incl = units_of_tiles(t);
 #pragma unroll
@@ -275,8 +273,7 @@ __global__ void splitkv_plan_kernel(const PlanParams p)
     const int lane = threadIdx.x & 31;
     const int warps = (gridDim.x * blockDim.x) >> 5;
     for (int span = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; span < p.num_spans; span += warps) {
-        const SpanStart s = warp_plan([&](int r) { return __ldg(p.seq_lens + r); }, p.batch, p.max_pages_per_req, p.num_kv_heads,
-                                      p.num_spans, span, lane);
+        const SpanStart s = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane);
         if (lane == 0) {
             p.span_start[span] = s.r < 0 ? make_int4(-1, -1, -1, -1) : make_int4(s.r, s.h, s.tile, (int)s.v);
             if (span == 0) {
@@ -344,20 +341,7 @@ struct AttnParams {
                                     // < 0: even seq_lens and the tables come from the preceding kernel: wait before the plan
     int32_t q_base, q_pass;         // this launch computes new tokens q_base .. q_base + q_pass - 1; q_pass*group <= 8
     float scale_log2;               // log2(e) / sqrt(d)
-    int32_t context_pages;          // page lists that a selection of whole contexts wrote: seq_lens are the contexts', over
-                                    // tables of this many pages; 0: seq_lens are the lists' own
 };
-
-// The length that attention of request r covers.  Lists of a selection hold max_pages_per_req pages of a longer
-// context, the last of them its last page; their length follows from the context's, so that the plan
-// need not wait for the selection.
-template <bool kHeadTables>
-__device__ __forceinline__ int attended_length(const AttnParams &p, int r)
-{
-    const int L = __ldg(p.seq_lens + r);
-    if (!kHeadTables || p.context_pages == 0) return L;
-    return attended_length(L, p.context_pages, p.max_pages_per_req);
-}
 
 // Columns.  The 8 columns of the MMA hold (new token, head of the group) pairs: column c is new
 // token q_base + c / G and head c % G, ncols = q_pass * G <= 8 of them are live.  A step with more
@@ -595,7 +579,6 @@ struct SpanCursor {
     long long v;          // unit index of that tile on the plan's axis
 
     // step to the next tile; returns false when it left the last request
-    template <bool kHeadTables = false>
     __device__ __forceinline__ bool next(const AttnParams &p)
     {
         ++v;
@@ -606,7 +589,7 @@ struct SpanCursor {
         h = 0;
         do {
             if (++r >= p.batch) return false;
-            L = attended_length<kHeadTables>(p, r);
+            L = __ldg(p.seq_lens + r);
             tiles = tiles_of_length(L, p.max_pages_per_req, p.q_len);
         } while (tiles == 0);
         return true;
@@ -615,9 +598,7 @@ struct SpanCursor {
 
 // kMulti = false: one new token per request (every live column sees the whole context);
 // kMulti = true:  q_len > 1 new tokens, each column with its own causal limit.
-// kHeadTables = true: block_tables is [batch][Hkv][max_pages_per_req], a row per (request, kv head)
-//                 (the pages that a selection chose for it); everything else is the same.
-template <int D, int W, int NS, bool kMulti, bool kHeadTables = false>
+template <int D, int W, int NS, bool kMulti>
 __global__ void __launch_bounds__(W * 32, 1)
 paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p)
 {
@@ -650,15 +631,13 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     // ---- plan: where does this warp's span start?
     // Nothing read up to the dependency wait below is written by the preceding kernel of a decode
     // step (the KV append writes only the pool), so this prologue overlaps that kernel's tail.
-    auto length_of = [&](int r) { return attended_length<kHeadTables>(p, r); };
-    const SpanStart st = warp_plan(length_of, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane,
+    const SpanStart st = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane,
                                    p.q_len);
-    if (kHeadTables) grid_dependency_wait();     // the selection before this kernel writes the tables
     if (st.r < 0 || span == 0) {
         grid_dependency_wait();
         grid_launch_dependents();
         if (span == 0)
-            flag_unusable_requests(length_of, p.batch, p.max_pages_per_req, p.q_len, lane, p.out,
+            flag_unusable_requests(p.seq_lens, p.batch, p.max_pages_per_req, p.q_len, lane, p.out,
                                    p.q_len * p.num_q_heads * D, p.status);
     }
     if (st.r < 0) {
@@ -682,20 +661,17 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
     bool more_to_issue = true;                   // the issue cursor still points at a tile of this span
     int issued = 0, i_slot = 0;                  // i_slot = issued % NS
     bool alive = true;
-    const int table_rows = kHeadTables ? p.batch * p.num_kv_heads : p.batch;
-    auto row_at = [&](int r, int h) { return kHeadTables ? r * p.num_kv_heads + h : r; };
-    auto row_after = [&](int r, int h) { return kHeadTables ? r * p.num_kv_heads + h + 1 : (h + 1 < p.num_kv_heads ? r : r + 1); };
-    auto table_row = [&](int row) { return p.block_tables + (size_t)row * p.max_pages_per_req; };
-    auto load_chunk = [&](int row, int chunk) -> int {
+    auto table_row = [&](int r) { return p.block_tables + (size_t)r * p.max_pages_per_req; };
+    auto load_chunk = [&](int r, int chunk) -> int {
         const int idx = chunk * 32 + lane;
-        return (row < table_rows && idx < p.max_pages_per_req) ? __ldg(table_row(row) + idx) : -1;
+        return (r < p.batch && idx < p.max_pages_per_req) ? __ldg(table_row(r) + idx) : -1;
     };
     constexpr int kTilesPerChunk = 32 / kPagesPerTile;
     int cur_chunk = ic.tile / kTilesPerChunk;
-    int cur_val = load_chunk(row_at(ic.r, ic.h), cur_chunk);
-    int nxt_val = load_chunk(row_at(ic.r, ic.h), cur_chunk + 1);
-    // chunk 0 of the row the NEXT (request, kv head) will read: this row again, or the next one
-    int pf_row = row_after(ic.r, ic.h);
+    int cur_val = load_chunk(ic.r, cur_chunk);
+    int nxt_val = load_chunk(ic.r, cur_chunk + 1);
+    // chunk 0 of the row the NEXT (request, kv head) will read: this row again, or the next request's
+    int pf_row = (ic.h + 1 < p.num_kv_heads) ? ic.r : ic.r + 1;
     int pf_val = load_chunk(pf_row, 0);
 
     // query fragments of a (request, kv head), fetched when the issue cursor enters it
@@ -736,7 +712,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
         if (ck != cur_chunk) {
             cur_chunk = ck;
             cur_val = nxt_val;
-            nxt_val = load_chunk(row_at(ic.r, ic.h), ck + 1);
+            nxt_val = load_chunk(ic.r, ck + 1);
         }
         const int n_pages = (ic.L + kPageSize - 1) / kPageSize;
         const int np = min(kPagesPerTile, n_pages - ic.tile * kPagesPerTile);
@@ -766,16 +742,15 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             an_r = ic.r; an_h = ic.h;
         }
         ++issued;
-        more_to_issue = ic.template next<kHeadTables>(p) && ic.v < v_end;
+        more_to_issue = ic.next(p) && ic.v < v_end;
         if (more_to_issue) {
             if (ic.tile == 0) {
                 // entered a new (request, kv head): its first table chunk was fetched ahead
                 cur_chunk = 0;
-                const int row = row_at(ic.r, ic.h);
-                cur_val = (pf_row == row) ? pf_val : load_chunk(row, 0);
-                nxt_val = load_chunk(row, 1);
-                pf_row = row_after(ic.r, ic.h);
-                pf_val = (pf_row == row) ? cur_val : load_chunk(pf_row, 0);
+                cur_val = (pf_row == ic.r) ? pf_val : load_chunk(ic.r, 0);
+                nxt_val = load_chunk(ic.r, 1);
+                pf_row = (ic.h + 1 < p.num_kv_heads) ? ic.r : ic.r + 1;
+                pf_val = (pf_row == ic.r) ? cur_val : load_chunk(pf_row, 0);
                 if (qn_r < 0 && inputs_ready) {
                     load_q(qn, ic.r, ic.h);
                     qn_r = ic.r; qn_h = ic.h;
@@ -1089,7 +1064,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
         // move the compute cursor past the piece: to the next (request, kv head) or out of the span
         cc.tile += n - 1;
         cc.v += n - 1;
-        more_to_compute = cc.template next<kHeadTables>(p) && cc.v < v_end;
+        more_to_compute = cc.next(p) && cc.v < v_end;
     }
 
     if (lane == 0) p.trace[span * 8 + 2] = global_timer_ns();
@@ -1360,8 +1335,7 @@ pool_read_probe_kernel(const __grid_constant__ CUtensorMap tmap, const ProbePara
         fence_proxy_async();
     }
     __syncwarp();
-    const SpanStart st = warp_plan([&](int r) { return __ldg(p.seq_lens + r); }, p.batch, p.max_pages_per_req, p.num_kv_heads,
-                                   p.num_spans, span, lane);
+    const SpanStart st = warp_plan(p.seq_lens, p.batch, p.max_pages_per_req, p.num_kv_heads, p.num_spans, span, lane);
     if (st.r < 0) return;
     AttnParams ap{};                              // the cursor reads only these
     ap.seq_lens = p.seq_lens; ap.batch = p.batch; ap.max_pages_per_req = p.max_pages_per_req;

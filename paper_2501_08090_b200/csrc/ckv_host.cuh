@@ -88,12 +88,10 @@ inline int32_t check_call(ckv_pool *pool, int32_t layer, int32_t batch, const ch
     return CKV_OK;
 }
 
-// A row of `budget` pages per (request, kv head): tile counts are int32, as for whole contexts.
-inline int32_t check_budget(const ckv_pool *pool, int32_t batch, int32_t budget, const char *fn)
+// Pages of a list; their tokens have to be countable in 32 bits.
+inline int32_t check_budget(int32_t budget, const char *fn)
 {
-    constexpr int kOverhead = 4;                 // more than the plan's units per (request, kv head), rounding included
-    if (budget < 1 || (long long)batch * pool->cfg.num_kv_heads * (budget / kPagesPerTile + kOverhead) >= (1ll << 31))
-        return fail(CKV_EINVAL, "%s: budget %d out of range", fn, budget);
+    if (budget < 1 || budget > 1 << 26) return fail(CKV_EINVAL, "%s: budget %d outside [1, 2^26]", fn, budget);
     return CKV_OK;
 }
 

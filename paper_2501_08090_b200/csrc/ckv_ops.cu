@@ -175,7 +175,7 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
     if (!aligned16(d_q)) return fail(CKV_EINVAL, "%s: q not 16-byte aligned", fn);
     if (sink < 0 || recent < 1 || budget < 1 || (long long)sink + recent > budget)
         return fail(CKV_EINVAL, "%s: budget %d must hold sink %d >= 0 and recent %d >= 1 pages", fn, budget, sink, recent);
-    if (int32_t rc = ckv::check_budget(pool, batch, budget, fn)) return rc;
+    if (int32_t rc = ckv::check_budget(budget, fn)) return rc;
     const ckv_config &c = pool->cfg;
     if (c.max_pages_per_req > kMaxSelectPages)
         return fail(CKV_EINVAL, "%s: selection holds at most %d pages of a request, the tables have %d", fn, kMaxSelectPages, c.max_pages_per_req);

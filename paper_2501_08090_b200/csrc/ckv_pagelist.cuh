@@ -1,31 +1,52 @@
-// Attention over short lists of pages, for few (request, kv head) pairs: the form of
-// paged_decode_attn_kernel for launches that are all latency.
+// Attention over a list of pages per (request, kv head): what a page selection is followed by.
 #pragma once
 
-#include "ckv_device.cuh"
+#include "ckv_common.cuh"
 
 namespace ckv {
 
-// A cluster of CTAs per (request, kv head), a tile of 32 tokens per warp and turn.  The arithmetic of a
-// tile is paged_decode_attn_kernel's (S^T = K Q^T, softmax in the log2 domain, O^T += V^T P^T on
-// mma.sync); the difference is how partials meet.  There the warps' spans cross pairs, and partials of
-// different CTAs meet in global memory: a chain of publish, fence, count, fetch and fold that takes
-// 4 to 8 us, which a long stream hides and a short list does not.  Here a pair's partials never
-// leave the cluster: they are folded in the CTA's shared memory, a warp per column, then across the
-// cluster through distributed shared memory, a CTA per column, in a fixed order.
+// A cluster of CTAs per (request, kv head), a tile of 32 tokens (2 pages) per warp and turn, each warp with a
+// stage of its own that it fills by TMA.  The arithmetic of a tile is paged_decode_attn_kernel's:
+//   S^T[tok 16 x g 8] = K[tok 16 x d] . Q^T[d x g 8],   O^T[d 16 x g 8] += V^T[d 16 x tok 16] . P^T[tok 16 x g 8]
+// on mma.sync with the softmax in the log2 domain.  That kernel cuts the tokens of all requests into even
+// spans, since contexts differ a thousandfold, and its spans' partials meet in global memory: publish,
+// fence, count, fetch, fold, 4 to 8 us.  Lists of a selection are of one length, or shorter, so here a CTA or
+// cluster owns a pair and its partials never leave the SMs: they are folded in the CTA's shared memory, a
+// warp per column, then across the cluster through distributed shared memory, a CTA per column, in a
+// fixed order.
 //
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i   over warps, then over CTAs.
+//
+// Bound by HBM where the pairs fill the GPU (512 pairs of 128 pages 80.8 us against 87 in even spans; 768
+// of 33 pages 37.8 against 44), by latency where they do not (5 pairs of 24 pages 4.0 us against 8.8).
+// Six warps and two CTAs an SM: 296 CTAs at a time.  Of the same 12 warps an SM, 4 x 3 leave 512 pairs a second
+// wave that is nearly empty (95 us), 2 x 6 too (91), 12 x 1 folds while nothing is loaded (88).
+struct ListParams {
+    const int32_t *pages;           // [batch][Hkv][budget]
+    const int32_t *lens;            // [batch] tokens in the lists, or (context_pages > 0) of the contexts they were chosen from
+    const uint16_t *q;
+    uint16_t *out;
+    uint32_t *status;
+    int32_t batch, budget, num_pages, num_kv_heads, group;
+    int32_t layer_page_base;        // layer * num_pages
+    int32_t context_pages;          // > 0: a selection over tables of this many pages wrote the lists just before
+    float scale_log2;               // log2(e) / sqrt(d)
+};
+
 template <int D>
 struct ListLayout {
-    static constexpr int kWarps = 8;
+    static constexpr int kWarps = 6;
+    static constexpr int kCtas = 2;              // resident on an SM
     static constexpr int kHalves = D / 64;
     static constexpr int kHalfBytes = 32 * 128;                  // one TMA box: 32 rows x 128 B
     static constexpr int kPageBytes = kHalves * kHalfBytes;
     static constexpr int kStageBytes = kPagesPerTile * kPageBytes;
     static constexpr int kPitch = D + 4;                         // floats per row of a partial (bank spread)
     static constexpr int kPartFloats = kMaxGroup * kPitch + 2 * kMaxGroup;       // rows, then m[8], l[8]
-    static constexpr int kPartOff = kWarps * kStageBytes;
-    static constexpr int kBarOff = kPartOff + (kWarps + 1) * kPartFloats * 4;    // a partial per warp, and the CTA's
+    // a warp's partial takes its stage's place once its last tile is done; the CTA's lies in warp 0's second half
+    static constexpr int kCtaPartOff = kStageBytes / 2;
+    static_assert(kPartFloats * 4 <= kStageBytes / 2, "two partials must fit a stage");
+    static constexpr int kBarOff = kWarps * kStageBytes;
     static constexpr int kSmemBytes = kBarOff + kWarps * 8 + 1024;
 };
 
@@ -44,8 +65,8 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
 }
 
 template <int D>
-__global__ void __launch_bounds__(ListLayout<D>::kWarps * 32, 1)
-page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams p)
+__global__ void __launch_bounds__(ListLayout<D>::kWarps * 32, ListLayout<D>::kCtas)
+page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams p)
 {
     using Lay = ListLayout<D>;
     constexpr int W = Lay::kWarps, kKSteps = D / 16, kDTiles = D / 16;
@@ -56,7 +77,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
     const int pair = blockIdx.x / ctas, r = pair / p.num_kv_heads, h = pair % p.num_kv_heads;
     const int G = p.group;
     const uint32_t stage = smem_u32(smem) + warp * Lay::kStageBytes, bar = smem_u32(smem + Lay::kBarOff) + warp * 8;
-    float *part = (float *)(smem + Lay::kPartOff) + warp * Lay::kPartFloats;
+    float *part = (float *)(smem + warp * Lay::kStageBytes);
     if (lane == 0) {
         prefetch_tensormap(&tmap);
         mbar_init(bar, 1);
@@ -64,15 +85,19 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
         fence_proxy_async();
     }
     __syncwarp();
-    // Behind a selection lengths and queries may be read before the wait, as in paged_decode_attn_kernel.
-    if (p.early_loads < 0) grid_dependency_wait();
-    const int L = attended_length<true>(p, r);
-    const int tiles = tiles_of_length(L, p.max_pages_per_req);
-    uint16_t *out_rows = p.out + ((size_t)r * p.num_q_heads + h * G) * D;
+    // Right behind a selection, lengths and queries may be read before the wait: the selection released this
+    // kernel after its own wait, so whatever wrote them has completed; the lists' length follows from
+    // the context's.
+    if (p.context_pages == 0) grid_dependency_wait();
+    const int len = __ldg(p.lens + r);
+    const int L = p.context_pages > 0 ? attended_length(len, p.context_pages, p.budget) : len;
+    const int tiles = tiles_of_length(L, p.budget);
+    const int heads = p.num_kv_heads * G;
+    uint16_t *out_rows = p.out + ((size_t)r * heads + h * G) * D;
     uint32_t qf[kKSteps][2];
     {
         const int c = lane >> 2;
-        const uint32_t *qrow = (const uint32_t *)(p.q + ((size_t)r * p.num_q_heads + h * G + c) * D);
+        const uint32_t *qrow = (const uint32_t *)(p.q + ((size_t)r * heads + h * G + c) * D);
 #pragma unroll
         for (int ks = 0; ks < kKSteps; ++ks) {
             qf[ks][0] = c < G ? __ldg(qrow + ks * 8 + (lane & 3)) : 0u;
@@ -89,7 +114,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
         return;
     }
 
-    const int32_t *list = p.block_tables + (size_t)pair * p.max_pages_per_req;
+    const int32_t *list = p.pages + (size_t)pair * p.budget;
     const uint64_t policy = l2_evict_first_policy();
     auto tokens_of = [&](int tile) { return min(kTileTokens, L - tile * kTileTokens); };
     auto issue = [&](int tile) {
@@ -205,6 +230,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
     // Do not go on while a copy into this warp's stage may still be in flight (only after a wait gave up).
     if (!alive) mbar_wait_bounded(bar, phase, p.status);
 
+    __syncwarp();
     // ---- this warp's partial (m = -inf, l = 0 if it had no tile)
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) {
@@ -226,9 +252,10 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
     }
     __syncthreads();
 
-    // ---- the CTA's fold: warp g takes column g, a lane four elements of its row
-    const float *parts = (const float *)(smem + Lay::kPartOff);
-    float *mine = (float *)(smem + Lay::kPartOff) + W * Lay::kPartFloats;
+    // ---- the CTA's fold: warp g takes column g, its lanes four elements of the row each
+    constexpr int kPartStride = Lay::kStageBytes / 4;
+    const float *parts = (const float *)smem;
+    float *mine = (float *)(smem + Lay::kCtaPartOff);
     auto store = [&](int g, float4 acc, float l) {
         const float inv = 1.f / l;
         uint2 packed;
@@ -236,27 +263,27 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnParams
         packed.y = pack_bf16x2(acc.z * inv, acc.w * inv);
         *(uint2 *)(out_rows + g * D + lane * 4) = packed;
     };
-    if (warp < G) {
+    for (int g = warp; g < G; g += W) {
         float M = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < W; ++w) M = fmaxf(M, parts[w * Lay::kPartFloats + kMaxGroup * Lay::kPitch + warp]);
+        for (int w = 0; w < W; ++w) M = fmaxf(M, parts[w * kPartStride + kMaxGroup * Lay::kPitch + g]);
         const float ref = M == -INFINITY ? 0.f : M;              // no warp of this CTA had a tile
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float *src = parts + w * Lay::kPartFloats;
-            const float f = fast_exp2(src[kMaxGroup * Lay::kPitch + warp] - ref);
-            l += f * src[kMaxGroup * Lay::kPitch + kMaxGroup + warp];
+            const float *src = parts + w * kPartStride;
+            const float f = fast_exp2(src[kMaxGroup * Lay::kPitch + g] - ref);
+            l += f * src[kMaxGroup * Lay::kPitch + kMaxGroup + g];
             if (lane * 4 < D) {
-                const float4 a = *(const float4 *)(src + warp * Lay::kPitch + lane * 4);
+                const float4 a = *(const float4 *)(src + g * Lay::kPitch + lane * 4);
                 acc.x += f * a.x; acc.y += f * a.y; acc.z += f * a.z; acc.w += f * a.w;
             }
         }
         if (ctas == 1) {
-            if (lane * 4 < D && alive) store(warp, acc, l);
+            if (lane * 4 < D && alive) store(g, acc, l);
         } else {
-            if (lane * 4 < D) *(float4 *)(mine + warp * Lay::kPitch + lane * 4) = acc;
-            if (lane == 0) { mine[kMaxGroup * Lay::kPitch + warp] = M; mine[kMaxGroup * Lay::kPitch + kMaxGroup + warp] = l; }
+            if (lane * 4 < D) *(float4 *)(mine + g * Lay::kPitch + lane * 4) = acc;
+            if (lane == 0) { mine[kMaxGroup * Lay::kPitch + g] = M; mine[kMaxGroup * Lay::kPitch + kMaxGroup + g] = l; }
         }
     }
     if (ctas == 1) return;
