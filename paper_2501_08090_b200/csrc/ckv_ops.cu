@@ -331,13 +331,14 @@ int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size
     if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: out is NULL or not 16-byte aligned", fn);
     const ckv_config &c = pool->cfg;
     ckv::IndexValuesParams vp{};
-    vp.records = reinterpret_cast<const uint4 *>(layer_records(pool, d_index, layer));
+    vp.records = reinterpret_cast<const uint2 *>(layer_records(pool, d_index, layer));
     vp.steps = layer_steps(pool, d_index, layer);
     vp.out = static_cast<uint4 *>(d_out);
-    vp.vecs_per_record = 2 * c.head_dim / 16;
-    vp.vecs = (long long)c.num_pages * c.num_kv_heads * vp.vecs_per_record;
-    const unsigned blocks = (unsigned)std::min<long long>((vp.vecs + 255) / 256, (long long)pool->num_sms * 16);
-    CKV_CUDA(enqueue(ckv::kv_index_values_kernel, vp, blocks, 256, 0, pool->overlap, 0, stream));
+    vp.records_n = (long long)c.num_pages * c.num_kv_heads;
+    const long long pieces = vp.records_n * (2 * c.head_dim / 8);
+    const unsigned blocks = (unsigned)((pieces + 1023) / 1024);
+    CKV_CUDA(c.head_dim == 128 ? enqueue(ckv::kv_index_values_kernel<128>, vp, blocks, 256, 0, pool->overlap, 0, stream)
+                               : enqueue(ckv::kv_index_values_kernel<64>, vp, blocks, 256, 0, pool->overlap, 0, stream));
     pool->launches += 1;
     return CKV_OK;
 }
