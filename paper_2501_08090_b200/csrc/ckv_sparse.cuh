@@ -48,6 +48,13 @@ __device__ __forceinline__ int index_pages(const IndexParams &p, int L, int &fir
     return (L + kPageSize - 1) / kPageSize - first;
 }
 
+// bulk_load_1d of data that is read once
+__device__ __forceinline__ void bulk_load_once(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar), "l"(policy) : "memory");
+}
+
 constexpr int kIndexWarps = 8;       // two CTAs an SM: 16 warps x 3 stages x 4 KB in flight (head_dim 128)
 constexpr int kIndexStages = 3;
 
@@ -154,6 +161,7 @@ kv_index_update_kernel(const IndexParams p)
         ic.h = (int)((begin - before) % p.num_kv_heads);
     }
 
+    const uint64_t policy = l2_evict_first_policy();             // keys are read once
     // what the compute side needs of the units in flight, oldest first
     int f_page[kIndexStages], f_head[kIndexStages], f_tokens[kIndexStages];
     int next_id = __ldg(p.block_tables + (size_t)ic.r * p.max_pages_per_req + ic.page_at);
@@ -173,7 +181,7 @@ kv_index_update_kernel(const IndexParams p)
         } else if (lane == 0) {
             const uint32_t bytes = f_t * D * 2;
             mbar_arrive_expect_tx(bars + slot * 8, bytes);
-            bulk_load_1d(ring + slot * Lay::kStageBytes, p.pool_layer + ((size_t)f_pg * p.num_kv_heads + f_h) * 2 * kPageSize * D, bytes, bars + slot * 8);
+            bulk_load_once(ring + slot * Lay::kStageBytes, p.pool_layer + ((size_t)f_pg * p.num_kv_heads + f_h) * 2 * kPageSize * D, bytes, bars + slot * 8, policy);
         }
         if (++issued < units) {
             ic.next(p);
