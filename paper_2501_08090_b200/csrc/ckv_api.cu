@@ -157,14 +157,14 @@ int32_t launch_attention(ckv_pool *pool, const ckv::AttnParams &ap, cudaStream_t
     return CKV_OK;
 }
 
-template <int D>
-int32_t launch_list_attention(ckv_pool *pool, const ckv::ListParams &lp, cudaStream_t stream)
+template <int D, bool kSelect>
+int32_t launch_list_attention(ckv_pool *pool, const ckv::ListParams &lp, const ckv::SelectParams &sp, cudaStream_t stream)
 {
     using Lay = ckv::ListLayout<D>;
     static thread_local int configured_device = -1;
-    auto kernel = ckv::page_list_attn_kernel<D>;
+    auto kernel = ckv::page_list_attn_kernel<D, kSelect>;
     if (configured_device != pool->device) {
-        CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes));
+        CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kSmemBytes + (kSelect ? ckv::kMaxListInKernel * 4 : 0)));
         CKV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         configured_device = pool->device;
     }
@@ -176,7 +176,7 @@ int32_t launch_list_attention(ckv_pool *pool, const ckv::ListParams &lp, cudaStr
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3((unsigned)(pairs * cluster));
     lc.blockDim = dim3(Lay::kWarps * 32);
-    lc.dynamicSmemBytes = Lay::kSmemBytes;
+    lc.dynamicSmemBytes = Lay::kSmemBytes + (kSelect ? (size_t)lp.budget * 4 : 0);
     lc.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -186,7 +186,7 @@ int32_t launch_list_attention(ckv_pool *pool, const ckv::ListParams &lp, cudaStr
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
     lc.numAttrs = 2;
-    CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, lp));
+    CKV_CUDA(cudaLaunchKernelEx(&lc, kernel, pool->tmap, lp, sp));
     pool->launches += 1;
     pool->pool_written = false;                  // whatever wrote the pool has completed before this kernel releases the next
     return CKV_OK;
@@ -534,15 +534,9 @@ int32_t decode_step(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t 
                             d_out, stream);
 }
 
-// Attention over lists of pages; context_pages > 0: the selection just launched writes them, and d_lens are the contexts'.
-static int32_t list_attention_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, int32_t budget,
-                                     const int32_t *d_pages, const int32_t *d_lens, const void *d_q, void *d_out,
-                                     void *stream, int32_t context_pages)
+static ckv::ListParams list_params(const ckv_pool *pool, int32_t layer, int32_t batch, int32_t budget, const int32_t *d_pages,
+                                   const int32_t *d_lens, const void *d_q, void *d_out)
 {
-    if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
-    if (int32_t rc = ckv::check_budget(budget, fn)) return rc;
-    if (!d_pages || !d_lens || !d_q || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
-    if (!aligned16(d_q) || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: q/out not 16-byte aligned", fn);
     const ckv_config &c = pool->cfg;
     ckv::ListParams lp{};
     lp.pages = d_pages;
@@ -556,17 +550,24 @@ static int32_t list_attention_launch(ckv_pool *pool, const char *fn, int32_t lay
     lp.num_kv_heads = c.num_kv_heads;
     lp.group = c.num_q_heads / c.num_kv_heads;
     lp.layer_page_base = layer * c.num_pages;
-    lp.context_pages = context_pages;
     lp.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return c.head_dim == 128 ? launch_list_attention<128>(pool, lp, s) : launch_list_attention<64>(pool, lp, s);
+    return lp;
 }
 
 int32_t decode_attention_pages(ckv_pool *pool, int32_t layer, int32_t batch, int32_t budget,
                                const int32_t *d_pages, const int32_t *d_lens, const void *d_q, void *d_out,
                                void *stream)
 {
-    return list_attention_launch(pool, "decode_attention_pages", layer, batch, budget, d_pages, d_lens, d_q, d_out, stream, 0);
+    const char *fn = "decode_attention_pages";
+    if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
+    if (int32_t rc = ckv::check_budget(budget, fn)) return rc;
+    if (!d_pages || !d_lens || !d_q || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (!aligned16(d_q) || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: q/out not 16-byte aligned", fn);
+    const ckv::ListParams lp = list_params(pool, layer, batch, budget, d_pages, d_lens, d_q, d_out);
+    const ckv::SelectParams none{};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return pool->cfg.head_dim == 128 ? launch_list_attention<128, false>(pool, lp, none, s)
+                                     : launch_list_attention<64, false>(pool, lp, none, s);
 }
 
 int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
@@ -576,10 +577,17 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch, co
 {
     const char *fn = "decode_attention_sparse";
     if (!d_out || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: out is NULL or not 16-byte aligned", fn);
+    ckv::SelectParams sp;
+    bool selected = false;
     if (int32_t rc = ckv::select_launch(pool, fn, layer, batch, d_block_tables, d_seq_lens, d_q, d_index, index_bytes, budget,
-                                        sink, recent, d_pages, d_lens, stream))
+                                        sink, recent, d_pages, d_lens, true, &sp, &selected, stream))
         return rc;
-    return list_attention_launch(pool, fn, layer, batch, budget, d_pages, d_seq_lens, d_q, d_out, stream, pool->cfg.max_pages_per_req);
+    ckv::ListParams lp = list_params(pool, layer, batch, budget, d_pages, d_seq_lens, d_q, d_out);
+    lp.context_pages = pool->cfg.max_pages_per_req;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (selected)
+        return pool->cfg.head_dim == 128 ? launch_list_attention<128, false>(pool, lp, sp, s) : launch_list_attention<64, false>(pool, lp, sp, s);
+    return pool->cfg.head_dim == 128 ? launch_list_attention<128, true>(pool, lp, sp, s) : launch_list_attention<64, true>(pool, lp, sp, s);
 }
 
 int32_t kv_read_probe(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,

@@ -95,10 +95,15 @@ inline int32_t check_budget(int32_t budget, const char *fn)
     return CKV_OK;
 }
 
-// Checks and launches of decode_select_pages (ckv_ops.cu), for it and for decode_attention_sparse.
+constexpr int kMaxListInKernel = 2048;           // pages of a list that the attention kernel selects itself
+
+// Checks and launches of decode_select_pages (ckv_ops.cu), for it and for decode_attention_sparse.  `attend`: the
+// attention kernel follows and may be left the whole selection; *selected says whether it was done.
+struct SelectParams;
 int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, const int32_t *d_block_tables,
                       const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
-                      int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream);
+                      int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, bool attend,
+                      SelectParams *out_params, bool *selected, void *stream);
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "ckv_host.cuh"
+#include "ckv_pagelist.cuh"
 #include "ckv_rope.cuh"
 #include "ckv_sparse.cuh"
 #include "ckv_verify.cuh"
@@ -53,14 +54,10 @@ cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
 // Pages that one request may hold where pages are selected: their scores fit an SM's shared memory.
 constexpr int kMaxSelectPages = 49152;
 
-// Up to this many pages and (request, kv head) pairs one kernel scores and selects.  8 and 32 pairs of at most
-// 94 pages: 5.1 and 5.3 us against 6.1 and 6.4 with two kernels, and a launch less; of 250 pages 6.5 and
-// 6.7 against 6.2 and 6.6; 256 pairs of 94 pages make attention start later (31.1 us in all against 30.2).
-constexpr int kFusedPages = 256, kFusedPairs = 128;
-
-// score_pages_kernel over all candidate pages, then select_pages_kernel; cand: the most a request can have.
+// score_pages_kernel over all candidate pages, then select_pages_kernel; cand: the most candidates a request
+// can have.
 template <int D>
-int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stream)
+int32_t launch_select(ckv_pool *pool, ckv::SelectParams &sp, int cand, void *stream)
 {
     static thread_local int configured_device = -1;
     auto score = ckv::score_pages_kernel<D>;
@@ -72,17 +69,12 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams sp, int cand, void *stre
         configured_device = pool->device;
     }
     const long long pairs = (long long)sp.batch * sp.num_kv_heads;
-    if (cand > 0 && cand <= kFusedPages && pairs <= kFusedPairs) {
-        CKV_CUDA(enqueue(ckv::select_pages_kernel<4, D>, sp, (unsigned)pairs, ckv::kFusedThreads, (size_t)(cand + 3) / 4 * 4 * 8, pool->overlap, 0, stream));
-        pool->launches += 1;
-        return CKV_OK;
-    }
     if (cand > 0) {
         const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
         const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, (long long)ckv::kScoreCtas * pool->num_sms);
         CKV_CUDA(enqueue(score, sp, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream));
-        sp.after_scores = 1;
         pool->launches += 1;
+        sp.after_scores = 1;
     }
     const auto select = [&](auto kernel, int keys) {             // `keys` a thread
         const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (cand + keys * 32 - 1) / (keys * 32) * 32));
@@ -168,7 +160,8 @@ namespace ckv {
 
 int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t batch, const int32_t *d_block_tables,
                              const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
-                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream)
+                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, bool attend,
+                      SelectParams *out_params, bool *selected, void *stream)
 {
     if (int32_t rc = check_call(pool, layer, batch, fn)) return rc;
     if (!d_block_tables || !d_seq_lens || !d_q || !d_pages || !d_lens) return fail(CKV_EINVAL, "%s: NULL argument", fn);
@@ -180,7 +173,8 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
     if (c.max_pages_per_req > kMaxSelectPages)
         return fail(CKV_EINVAL, "%s: selection holds at most %d pages of a request, the tables have %d", fn, kMaxSelectPages, c.max_pages_per_req);
     if (int32_t rc = check_index(pool, fn, d_index, index_bytes)) return rc;
-    ckv::SelectParams sp{};
+    SelectParams &sp = *out_params;
+    sp = SelectParams{};
     sp.records = layer_records(pool, d_index, layer);
     sp.steps = layer_steps(pool, d_index, layer);
     sp.block_tables = d_block_tables;
@@ -204,6 +198,9 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
                     c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
     sp.keys = pool->wsp<uint32_t>(pool->ws.sel_keys);
     const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
+    // 5 requests of up to 187 pages: 7.8 us in one launch, 8.1 in two, and a launch is 2.4 us of the caller's time
+    *selected = !(attend && cand <= kListSelectPages && (long long)batch * c.num_kv_heads <= kListSelectPairs && budget <= kMaxListInKernel);
+    if (!*selected) return CKV_OK;
     return c.head_dim == 128 ? launch_select<128>(pool, sp, cand, stream) : launch_select<64>(pool, sp, cand, stream);
 }
 
@@ -347,8 +344,10 @@ int32_t decode_select_pages(ckv_pool *pool, int32_t layer, int32_t batch, const 
                             const int32_t *d_seq_lens, const void *d_q, const void *d_index, size_t index_bytes,
                             int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, void *stream)
 {
+    ckv::SelectParams sp;
+    bool selected;
     return ckv::select_launch(pool, "decode_select_pages", layer, batch, d_block_tables, d_seq_lens, d_q, d_index, index_bytes,
-                         budget, sink, recent, d_pages, d_lens, stream);
+                              budget, sink, recent, d_pages, d_lens, false, &sp, &selected, stream);
 }
 
 int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dtype, const int32_t *d_draft_tokens,

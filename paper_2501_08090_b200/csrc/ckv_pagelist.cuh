@@ -2,6 +2,7 @@
 #pragma once
 
 #include "ckv_common.cuh"
+#include "ckv_sparse.cuh"
 
 namespace ckv {
 
@@ -18,7 +19,7 @@ namespace ckv {
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i   over warps, then over CTAs.
 //
 // Bound by HBM where the pairs fill the GPU (512 pairs of 128 pages 80.8 us against 87 in even spans; 768
-// of 33 pages 37.8 against 44), by latency where they do not (5 pairs of 24 pages 4.0 us against 8.8).
+// of 33 pages 37.8 against 44), by latency where they do not (5 pairs of 24 pages 3.8 us against 8.8).
 // Six warps and two CTAs an SM: 296 CTAs at a time.  Of the same 12 warps an SM, 4 x 3 leave 512 pairs a second
 // wave that is nearly empty (95 us), 2 x 6 too (91), 12 x 1 folds while nothing is loaded (88).
 struct ListParams {
@@ -47,7 +48,11 @@ struct ListLayout {
     static constexpr int kCtaPartOff = kStageBytes / 2;
     static_assert(kPartFloats * 4 <= kStageBytes / 2, "two partials must fit a stage");
     static constexpr int kBarOff = kWarps * kStageBytes;
-    static constexpr int kSmemBytes = kBarOff + kWarps * 8 + 1024;
+    static constexpr int kListOff = kBarOff + kWarps * 8;        // the list, where this kernel selects it
+    static constexpr int kSmemBytes = kListOff + 1024;           // and the list
+    // a selection's scratch lies where the stages will be
+    static constexpr int kHistOff = 16384, kRangeOff = kHistOff + kSelectRounds * kSelectBins * 4;
+    static_assert(kRangeOff + 3 * 32 * 4 <= kWarps * kStageBytes, "a selection's scratch must fit the stages");
 };
 
 __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr)
@@ -64,9 +69,15 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
     return v;
 }
 
-template <int D>
+// kSelect: the lists are not there yet.  Every CTA of a cluster scores and selects its pair's pages for
+// itself (few short tables: kListSelectPages), and the first one writes the list out: one launch in
+// place of three.  (Selecting here behind score_pages_kernel, for any table, was slower than
+// select_pages_kernel: 768 pairs 73 us in all against 70, since two CTAs an SM select while nothing is loaded.)
+constexpr int kListSelectKeys = 4;               // a thread
+constexpr int kListSelectPages = 256, kListSelectPairs = 128;
+template <int D, bool kSelect>
 __global__ void __launch_bounds__(ListLayout<D>::kWarps * 32, ListLayout<D>::kCtas)
-page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams p)
+page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams p, const __grid_constant__ SelectParams sp)
 {
     using Lay = ListLayout<D>;
     constexpr int W = Lay::kWarps, kKSteps = D / 16, kDTiles = D / 16;
@@ -85,17 +96,10 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
         fence_proxy_async();
     }
     __syncwarp();
-    // Right behind a selection, lengths and queries may be read before the wait: the selection released this
-    // kernel after its own wait, so whatever wrote them has completed; the lists' length follows from
-    // the context's.
-    if (p.context_pages == 0) grid_dependency_wait();
-    const int len = __ldg(p.lens + r);
-    const int L = p.context_pages > 0 ? attended_length(len, p.context_pages, p.budget) : len;
-    const int tiles = tiles_of_length(L, p.budget);
     const int heads = p.num_kv_heads * G;
     uint16_t *out_rows = p.out + ((size_t)r * heads + h * G) * D;
     uint32_t qf[kKSteps][2];
-    {
+    auto load_q = [&]() {
         const int c = lane >> 2;
         const uint32_t *qrow = (const uint32_t *)(p.q + ((size_t)r * heads + h * G + c) * D);
 #pragma unroll
@@ -103,13 +107,33 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
             qf[ks][0] = c < G ? __ldg(qrow + ks * 8 + (lane & 3)) : 0u;
             qf[ks][1] = c < G ? __ldg(qrow + ks * 8 + 4 + (lane & 3)) : 0u;
         }
+    };
+    // Right behind a selection, lengths and queries may be read before the wait: that kernel released this
+    // one after its own wait, so whatever wrote them has completed; the lists' length follows from the
+    // context's.
+    if (kSelect || p.context_pages == 0) grid_dependency_wait();
+    load_q();
+    const int len = __ldg(p.lens + r);
+    const int L = p.context_pages > 0 ? attended_length(len, p.context_pages, p.budget) : len;
+    const int tiles = tiles_of_length(L, p.budget);
+    int32_t *s_list = (int32_t *)(smem + Lay::kListOff);
+    if constexpr (kSelect) {
+        int32_t *out = sp.sel_tables + (size_t)pair * sp.budget;
+        const SelectScratch scratch = {(uint32_t *)smem, (int (*)[kSelectBins])(smem + Lay::kHistOff), (uint32_t (*)[32])(smem + Lay::kRangeOff)};
+        select_pair<kListSelectKeys, D>(sp, pair, scratch, rank == 0, [&](int place, int32_t id) {
+            s_list[place] = id;
+            if (rank == 0) out[place] = id;
+        });
+        fence_proxy_async();                     // the scratch was written here, the stages are filled by the copy engine
+        __syncthreads();
+    } else {
+        grid_dependency_wait();
+        grid_launch_dependents();
     }
-    grid_dependency_wait();
-    grid_launch_dependents();
     if (tiles == 0) {                            // unusable: the same for the whole cluster
         if (rank == 0) {
             for (int i = threadIdx.x; i < G * D / 8; i += W * 32) ((uint4 *)out_rows)[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
+            if (!kSelect && threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
         }
         return;
     }
@@ -123,7 +147,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
         __syncwarp();
         if (lane < np * Lay::kHalves) {
             const int pg = lane / Lay::kHalves, hf = lane % Lay::kHalves;
-            int page = __ldg(list + tile * kPagesPerTile + pg);
+            int page = kSelect ? s_list[tile * kPagesPerTile + pg] : __ldg(list + tile * kPagesPerTile + pg);
             if (page < 0 || page >= p.num_pages) {
                 atomicOr(p.status, kStatusBadPage);
                 page = 0;

@@ -321,14 +321,14 @@ kv_index_values_kernel(const IndexValuesParams p)
 // small beside the group's largest that fp32 holds it as a denormal) does not depend on the order of
 // summation, and the selection is the same whichever way the work is split.
 //
-// Two kernels.  score_pages_kernel: candidate pages are scored in tiles of 16 (the rows of an MMA).  The
+// score_pages_kernel: candidate pages are scored in tiles of 16 (the rows of an MMA).  The
 // tiles of all (request, kv head) pairs lie on one axis that is cut evenly over the warps of a grid
 // that fills the GPU, so that contexts of very different lengths balance.  A warp copies the records
 // of the tiles ahead of the one it multiplies into a ring of its own in shared memory (asynchronous
 // copies: no registers wait for them, and a new pair's queries are converted while they fly).
 // Bound by HBM: 2 d + 4 bytes per page and kv head, once.
-// select_pages_kernel: a CTA per pair finds the threshold among its keys (the scores as ordered 32-bit
-// numbers, in registers) by counting them in 256 bins over the range still in question, then over
+// select_pair: a CTA finds the threshold among its keys (the scores as ordered 32-bit
+// numbers, in registers) of its pair by counting them in 256 bins over the range still in question, then over
 // the bin that holds the threshold, until that bin is wanted whole (usually the second time; bisection,
 // one bit a turn, took 2-3 times as long), and writes the chosen pages in context order.  It copies
 // the table to shared memory while the scores are still being computed.  The first `sink` and the last `recent`
@@ -356,7 +356,6 @@ constexpr int kScoreWarps = 6;
 constexpr int kScoreStages = 2;
 constexpr int kScoreCtas = 4;
 constexpr int kMaxSelectThreads = 1024;
-constexpr int kFusedThreads = 256;
 
 __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -610,26 +609,33 @@ score_pages_kernel(const SelectParams p)
 constexpr int kSelectBins = 256;
 constexpr int kSelectRounds = 4;     // 8 bits of the keys' range each
 
+struct SelectScratch {
+    uint32_t *words;                // shared memory, 16-byte aligned: [candidates] page ids or keys; kScoreD: ids, then keys
+    int (*hist)[kSelectBins];       // [kSelectRounds], 16-byte aligned
+    uint32_t (*range)[32];          // [3]
+};
+
+// The selection of one (request, kv head) by a whole CTA, the waits for the preceding kernel included;
+// emit(place, page id) is called once for each place of its list.  `report`: this CTA writes the
+// request's length and flags an unusable one.
+//
 // kKeys > 0: at most that many keys a thread, in registers, and the table in shared memory; 0: the keys
 // are in shared memory.  Few keys a thread and many threads are best, as the code runs once, from a cold
 // instruction cache: over 2048 pages 4 keys a thread make sparse_b64's selection 41.5 us with the scores,
 // 8 keys 43, 16 keys 45.5, the keys in shared memory 44-51.
-// kScoreD > 0: few pairs with short tables; the CTA scores its pair's pages itself (head_dim kScoreD), one
-// launch in place of two.
-template <int kKeys, int kScoreD = 0>
-__global__ void __launch_bounds__(kScoreD > 0 ? kFusedThreads : kMaxSelectThreads)
-select_pages_kernel(const SelectParams p)
+// kScoreD > 0: the CTA scores its pair's pages itself (head_dim kScoreD); score_pages_kernel is not launched.
+template <int kKeys, int kScoreD, typename Emit>
+__device__ __forceinline__ void select_pair(const SelectParams &p, int pair, const SelectScratch scratch, bool report, Emit emit)
 {
     constexpr bool kInRegisters = kKeys > 0;
     constexpr int K = kInRegisters ? kKeys : 1;
     static_assert(K == 1 || K % 4 == 0, "keys are loaded four at a time");
-    extern __shared__ __align__(16) uint32_t s_words[];          // [candidates] page ids or keys; kScoreD: ids, then keys
-    __shared__ __align__(16) int s_hist[kSelectRounds][kSelectBins];
-    __shared__ uint32_t s_range[3][32];
+    uint32_t *s_words = scratch.words;
+    int (*s_hist)[kSelectBins] = scratch.hist;
+    uint32_t (*s_range)[32] = scratch.range;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int pair = blockIdx.x, r = pair / p.num_kv_heads;
+    const int r = pair / p.num_kv_heads;
     const int32_t *table = p.block_tables + (size_t)r * p.max_pages_per_req;
-    int32_t *out = p.sel_tables + (size_t)pair * p.budget;
     // Right behind score_pages_kernel, the lengths and tables may be read before the wait: that kernel
     // released this one after its own wait, so whatever wrote them has completed.
     if (!p.after_scores) grid_dependency_wait();
@@ -657,15 +663,15 @@ select_pages_kernel(const SelectParams p)
     grid_dependency_wait();
     grid_launch_dependents();
 
-    if (threadIdx.x == 0) {
+    if (report && threadIdx.x == 0) {
         if (!usable) atomicOr(p.status, kStatusBadLength);
         if (pair % p.num_kv_heads == 0) p.sel_lens[r] = attended_length(L, p.max_pages_per_req, p.budget);
     }
-    if ((int)threadIdx.x < ends) out[place0] = end0;
+    if ((int)threadIdx.x < ends) emit(place0, end0);
     for (int i = threadIdx.x + blockDim.x; i < ends; i += blockDim.x) {
         int place;
         const int32_t id = end_page(i, place);
-        out[place] = id;
+        emit(place, id);
     }
     if (!chosen) return;
 
@@ -797,11 +803,22 @@ select_pages_kernel(const SelectParams p)
     int above = (int)(before >> 16), equal = (int)(before & 0xffffu), i = first;
     each([&](uint32_t k) {
         if (k > lo || (k == lo && equal < equal_places))
-            out[p.sink + above + min(equal, equal_places)] = kInRegisters ? (int32_t)s_words[i] : __ldg(table + p.sink + i);
+            emit(p.sink + above + min(equal, equal_places), kInRegisters ? (int32_t)s_words[i] : __ldg(table + p.sink + i));
         above += k > lo;
         equal += k == lo;
         ++i;
     });
+}
+
+template <int kKeys>
+__global__ void __launch_bounds__(kMaxSelectThreads)
+select_pages_kernel(const SelectParams p)
+{
+    extern __shared__ __align__(16) uint32_t s_words[];
+    __shared__ __align__(16) int s_hist[kSelectRounds][kSelectBins];
+    __shared__ uint32_t s_range[3][32];
+    int32_t *out = p.sel_tables + (size_t)blockIdx.x * p.budget;
+    select_pair<kKeys, 0>(p, blockIdx.x, SelectScratch{s_words, s_hist, s_range}, true, [&](int place, int32_t id) { out[place] = id; });
 }
 
 }  // namespace ckv

@@ -64,7 +64,12 @@ class Case:
         """Selection exactly, lengths, and attention of every usable request."""
         pages, lens, out = self.out(budget)
         self.kp.decode_attention_sparse(self.layer, self.btd, self.sld, self.qd, self.index, pages, lens, out, sink=sink, recent=recent)
+        # the two halves of the call give the same lists and the same bits
+        pages2, lens2, out2 = self.out(budget)
+        self.kp.decode_select_pages(self.layer, self.btd, self.sld, self.qd, self.index, pages2, lens2, sink=sink, recent=recent)
+        self.kp.decode_attention_pages(self.layer, pages2, lens2, self.qd, out2)
         assert self.kp.check_status() == 0
+        assert torch.equal(pages, pages2) and torch.equal(lens, lens2) and torch.equal(out, out2)
         pages, lens = pages.cpu().numpy(), lens.cpu().numpy()
         rec, step = self.host_index()
         pool, q = widen(self.pool), widen(self.q)
