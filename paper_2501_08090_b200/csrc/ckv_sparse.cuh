@@ -29,6 +29,74 @@ __device__ __forceinline__ int step_exponent(float m, float &inv)
     return e;
 }
 
+// The stretch of work that each warp of a grid takes when the units of all requests lie on one axis that
+// is cut evenly.  Executed by whole CTAs of kThreads: the requests' units are summed once a CTA (once a warp,
+// every warp of an SM repeating it, it took 2.6 us of score_pages_kernel's 20).  units_of(r): the units of request
+// r.  T counts them.
+template <typename T>
+struct Stretch {
+    T begin, n;                     // first unit of the warp, their number (0: none)
+    T before;                       // units of the requests before r
+    int r;                          // the request that holds `begin`
+};
+
+template <int kThreads, typename T, typename UnitsOf>
+__device__ __forceinline__ Stretch<T> find_stretch(UnitsOf units_of, int batch)
+{
+    constexpr int kWarps = kThreads / 32;
+    __shared__ T s_upto[kThreads];
+    __shared__ T s_warp[kWarps];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const T warps = (T)gridDim.x * kWarps, warp = (T)blockIdx.x * kWarps + w;
+    Stretch<T> s = {0, 0, 0, -1};
+    T before = 0, total = 0;
+    if (batch > kThreads) {                      // more requests than threads: their sum first
+        for (int r = threadIdx.x; r < batch; r += kThreads) total += units_of(r);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) total += __shfl_xor_sync(0xffffffffu, total, x);
+        if (lane == 0) s_warp[w] = total;
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) total += s_warp[x];
+    }
+    for (int base = 0; base < batch; base += kThreads) {
+        const int r = base + threadIdx.x;
+        T upto = r < batch ? (T)units_of(r) : (T)0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const T v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        __syncthreads();                         // the shared arrays may still be read
+        if (lane == 31) s_warp[w] = upto;
+        __syncthreads();
+        T all = 0;
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) {
+            if (x < w) upto += s_warp[x];
+            all += s_warp[x];
+        }
+        s_upto[threadIdx.x] = upto;
+        __syncthreads();
+        if (batch <= kThreads) total = all;
+        if (base == 0) {
+            const T per = (total + warps - 1) / warps;
+            s.begin = warp * per;
+            s.n = s.begin < total ? min(per, total - s.begin) : (T)0;
+        }
+        if (s.n > 0 && s.r < 0 && s.begin < before + all) {
+            int at = 0;
+            while (s_upto[at + 31] <= s.begin - before) at += 32;
+            at += __ffs(__ballot_sync(0xffffffffu, s_upto[at + lane] > s.begin - before)) - 1;
+            s.r = base + at;
+            s.before = before + (at > 0 ? s_upto[at - 1] : (T)0);
+        }
+        before += all;
+    }
+    return s;
+}
+
 struct IndexParams {
     const uint16_t *pool_layer;
     const int32_t *block_tables;
@@ -100,7 +168,6 @@ kv_index_update_kernel(const IndexParams p)
     constexpr int NV = kPageSize / kRows;
     extern __shared__ __align__(128) uint8_t s_ring[];
     const int lane = threadIdx.x & 31;
-    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, warps = gridDim.x * kIndexWarps;
     const int row0 = lane / kVecs;
     const uint32_t ring = smem_u32(s_ring) + (threadIdx.x >> 5) * kIndexStages * Lay::kStageBytes;
     const uint32_t bars = smem_u32(s_ring) + Lay::kBarOff + (threadIdx.x >> 5) * kIndexStages * 8;
@@ -113,53 +180,21 @@ kv_index_update_kernel(const IndexParams p)
     grid_dependency_wait();
     grid_launch_dependents();
 
-    long long pages = 0;
-    for (int base = 0; base < p.batch; base += 32) {
-        const int r = base + lane;
+    const Stretch<long long> st = find_stretch<kIndexWarps * 32, long long>([&](int r) {
         int first;
-        const int n = r < p.batch ? index_pages(p, __ldg(p.seq_lens + r), first) : 1;
-        if (warp == 0 && n == 0) atomicOr(p.status, kStatusBadLength);
-        if (r < p.batch) pages += n;
-    }
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) pages += __shfl_xor_sync(0xffffffffu, pages, x);
-    const long long total = pages * p.num_kv_heads;
-    const long long per = (total + warps - 1) / warps;
-    const long long begin = warp * per;
-    const int units = (int)(min(begin + per, total) - begin);
+        const int n = index_pages(p, __ldg(p.seq_lens + r), first);
+        if (blockIdx.x == 0 && n == 0) atomicOr(p.status, kStatusBadLength);
+        return (long long)n * p.num_kv_heads;
+    }, p.batch);
+    const int units = (int)st.n;
     if (units <= 0) return;
-
-    // the request that holds unit `begin`
-    IndexCursor ic = {};
-    {
-        long long before = 0;
-        for (int base = 0; base < p.batch; base += 32) {
-            const int rr = base + lane;
-            int first = 0;
-            const int len = rr < p.batch ? __ldg(p.seq_lens + rr) : 0;
-            const int n = rr < p.batch ? index_pages(p, len, first) : 0;
-            long long upto = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += v;
-            }
-            upto = before + upto * p.num_kv_heads;
-            const unsigned hit = __ballot_sync(0xffffffffu, upto > begin);
-            if (hit) {
-                const int src = __ffs(hit) - 1;
-                ic.r = base + src;
-                ic.L = __shfl_sync(0xffffffffu, len, src);
-                const int n_r = __shfl_sync(0xffffffffu, n, src);
-                before = __shfl_sync(0xffffffffu, upto, src) - (long long)n_r * p.num_kv_heads;
-                ic.page_at = __shfl_sync(0xffffffffu, first, src) + (int)((begin - before) / p.num_kv_heads);
-                ic.page_end = (ic.L + kPageSize - 1) / kPageSize;
-                break;
-            }
-            before = __shfl_sync(0xffffffffu, upto, 31);
-        }
-        ic.h = (int)((begin - before) % p.num_kv_heads);
-    }
+    IndexCursor ic;
+    ic.r = st.r;
+    ic.L = __ldg(p.seq_lens + st.r);
+    index_pages(p, ic.L, ic.page_at);
+    ic.page_at += (int)((st.begin - st.before) / p.num_kv_heads);
+    ic.page_end = (ic.L + kPageSize - 1) / kPageSize;
+    ic.h = (int)((st.begin - st.before) % p.num_kv_heads);
 
     const uint64_t policy = l2_evict_first_policy();             // keys are read once
     // what the compute side needs of the units in flight, oldest first
@@ -383,24 +418,49 @@ struct QueryFragments {
     __device__ __forceinline__ void load(const uint16_t *q, int group, int lane)
     {
         const int g = lane >> 2, t = lane & 3;
-        uint4 raw[kPieces][2];
-        float m = 0.f;
+        uint32_t raw[kPieces][8];
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            raw[i][0] = raw[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
             if (g < group) {
                 const uint4 *src = (const uint4 *)(q + g * D + i * 64 + t * 16);
-                raw[i][0] = __ldg(src);
-                raw[i][1] = __ldg(src + 1);
+                a = __ldg(src);
+                b = __ldg(src + 1);
             }
+            raw[i][0] = a.x; raw[i][1] = a.y; raw[i][2] = a.z; raw[i][3] = a.w;
+            raw[i][4] = b.x; raw[i][5] = b.y; raw[i][6] = b.z; raw[i][7] = b.w;
+        }
+        // the largest magnitude, two at a time; a NaN would win, as an infinity does
+        __nv_bfloat162 most = __nv_bfloat162(__ushort_as_bfloat16(0), __ushort_as_bfloat16(0));
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i)
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                const uint32_t w = ((const uint32_t *)raw[i])[x];
-                const float a = fabsf(__uint_as_float(w << 16)), b = fabsf(__uint_as_float(w & 0xffff0000u));
-                if (a < INFINITY) m = fmaxf(m, a);               // infinities and NaN take no part in the selection
-                if (b < INFINITY) m = fmaxf(m, b);
+                const uint32_t w = raw[i][x] & 0x7fff7fffu;
+                most = __hmax2_nan(most, *reinterpret_cast<const __nv_bfloat162 *>(&w));
             }
+        const float2 two = __bfloat1622float2(most);
+        if (__any_sync(0xffffffffu, !(two.x < INFINITY && two.y < INFINITY))) {
+            // infinities and NaN take no part in the selection: they become zeros
+            float m = 0.f;
+#pragma unroll 1
+            for (int n = 0; n < kPieces * 16; ++n) {
+                uint32_t keep = 0u;
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        if (i * 16 + x * 2 == (n & ~1)) {
+                            const uint32_t half = n & 1 ? 0xffff0000u : 0x0000ffffu;
+                            if ((raw[i][x] & half & 0x7f807f80u) == (half & 0x7f807f80u)) raw[i][x] &= ~half;
+                            keep = raw[i][x] & half & 0x7fff7fffu;
+                        }
+                m = fmaxf(m, __uint_as_float(n & 1 ? keep : keep << 16));
+            }
+            most = __nv_bfloat162(__float2bfloat16(m), __float2bfloat16(m));
         }
+        const float2 pair = __bfloat1622float2(most);
+        float m = fmaxf(pair.x, pair.y);
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
         float inv;
@@ -411,21 +471,23 @@ struct QueryFragments {
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) e_max = max(e_max, __shfl_xor_sync(0xffffffffu, e_max, x));
         const float step = g < group ? ldexpf(1.f, e - e_max) : -1.f;
-        auto whole = [&](float x) { return fabsf(x) < INFINITY ? (int)fminf(fmaxf(rintf(x * inv), -127.f), 127.f) : 0; };
+        // x * inv is exact; added to 1.5 * 2^23 it is rounded to a whole number (ties to even), which is
+        // then the low byte of the sum
+        constexpr float kMagic = 12582912.f;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                uint32_t n8 = 0u, p8 = 0u;
+                uint32_t n8[4], p8[4];
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const uint32_t w = ((const uint32_t *)raw[i])[2 * x + y];
-                    const int a = whole(__uint_as_float(w << 16)), b = whole(__uint_as_float(w & 0xffff0000u));
-                    n8 |= ((uint32_t)(min(a, 0) & 0xff) | (uint32_t)(min(b, 0) & 0xff) << 8) << (16 * y);
-                    p8 |= ((uint32_t)max(a, 0) | (uint32_t)max(b, 0) << 8) << (16 * y);
+                for (int y = 0; y < 4; ++y) {
+                    const uint32_t w = raw[i][2 * x + y / 2];
+                    const float v = fmaf(__uint_as_float(y & 1 ? w & 0xffff0000u : w << 16), inv, kMagic);
+                    n8[y] = __float_as_uint(fmaxf(fminf(v, kMagic), kMagic - 127.f));
+                    p8[y] = __float_as_uint(fminf(fmaxf(v, kMagic), kMagic + 127.f));
                 }
-                neg[i][x] = n8;
-                pos[i][x] = p8;
+                neg[i][x] = __byte_perm(__byte_perm(n8[0], n8[1], 0x0040), __byte_perm(n8[2], n8[3], 0x0040), 0x5410);
+                pos[i][x] = __byte_perm(__byte_perm(p8[0], p8[1], 0x0040), __byte_perm(p8[2], p8[3], 0x0040), 0x5410);
             }
         }
         step0 = __shfl_sync(0xffffffffu, step, (2 * t) * 4);
@@ -502,80 +564,58 @@ score_pages_kernel(const SelectParams p)
     constexpr int P = Lay::kPieces;
     extern __shared__ __align__(16) uint8_t s_ring[];
     const int lane = threadIdx.x & 31;
-    const int warp = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, warps = gridDim.x * kScoreWarps;
     const int g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_u32(s_ring) + (threadIdx.x >> 5) * kScoreStages * Lay::kStageBytes;
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // ---- this warp's stretch of the axis
-    long long tiles = 0;
-    for (int base = 0; base < p.batch; base += 32)
-        if (base + lane < p.batch) tiles += (candidates(p, __ldg(p.seq_lens + base + lane)) + 15) / 16;
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, x);
-    const long long total = tiles * p.num_kv_heads;
-    const long long per = (total + warps - 1) / warps;
-    const long long begin = warp * per;
-    const int n_tiles = (int)(min(begin + per, total) - begin);
+    const Stretch<int> st = find_stretch<kScoreWarps * 32, int>(
+        [&](int r) { return (candidates(p, __ldg(p.seq_lens + r)) + 15) / 16 * p.num_kv_heads; }, p.batch);
+    const int n_tiles = st.n;
     if (n_tiles <= 0) return;
     TileCursor ic;
-    {
-        long long before = 0;                    // tiles of the requests before
-        ic.r = ic.cand = 0;
-        for (int base = 0; base < p.batch; base += 32) {
-            const int c = base + lane < p.batch ? candidates(p, __ldg(p.seq_lens + base + lane)) : 0;
-            long long upto = (c + 15) / 16;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += v;
-            }
-            upto = before + upto * p.num_kv_heads;
-            const unsigned hit = __ballot_sync(0xffffffffu, upto > begin);
-            if (hit) {
-                const int src = __ffs(hit) - 1;
-                ic.r = base + src;
-                ic.cand = __shfl_sync(0xffffffffu, c, src);
-                before = __shfl_sync(0xffffffffu, upto, src) - (long long)((ic.cand + 15) / 16) * p.num_kv_heads;
-                break;
-            }
-            before = __shfl_sync(0xffffffffu, upto, 31);
-        }
-        ic.tiles = (ic.cand + 15) / 16;
-        ic.h = (int)((begin - before) / ic.tiles);
-        ic.tile = (int)((begin - before) % ic.tiles);
-    }
+    ic.r = st.r;
+    ic.cand = candidates(p, __ldg(p.seq_lens + st.r));
+    ic.tiles = (ic.cand + 15) / 16;
+    ic.h = (st.begin - st.before) / ic.tiles;
+    ic.tile = (st.begin - st.before) % ic.tiles;
     TileCursor cc = ic;
 
     // ---- issue side: lane (g, t) copies its quarter of the records of rows g and g + 8; the table entries
-    // of the tile after are on their way already
-    int ids[2];
-    auto fetch_ids = [&]() {
+    // of the next two tiles are on their way already
+    int ids[2][2], ids_h[2];
+    int fetched = 0;
+    auto fetch_ids = [&](int (&id)[2], int &h) {
+        if (fetched >= n_tiles) return;
+        if (fetched++ > 0) ic.next(p);
         const int32_t *table = p.block_tables + (size_t)ic.r * p.max_pages_per_req + p.sink;
         const int c = ic.tile * 16 + g;
-        ids[0] = c < ic.cand ? __ldg(table + c) : 0;
-        ids[1] = c + 8 < ic.cand ? __ldg(table + c + 8) : 0;
+        id[0] = c < ic.cand ? __ldg(table + c) : 0;
+        id[1] = c + 8 < ic.cand ? __ldg(table + c + 8) : 0;
+        h = ic.h;
     };
     int issued = 0;
     auto issue = [&]() {
         if (issued < n_tiles) {
             const uint32_t stage = ring + (issued % kScoreStages) * Lay::kStageBytes;
+            ++issued;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                int page = ids[x];
+                int page = ids[0][x];
                 if (page < 0 || page >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page = 0; }
-                const size_t at = (size_t)page * p.num_kv_heads + ic.h;
+                const size_t at = (size_t)page * p.num_kv_heads + ids_h[0];
                 const uint8_t *src = p.records + at * 2 * D + t * 16;
 #pragma unroll
                 for (int i = 0; i < P; ++i) cp_async_16(stage + (x * P + i) * 512 + lane * 16, src + i * 64);
                 if (t == x) cp_async_4(stage + Lay::kStepsOff + (x * 8 + g) * 4, p.steps + at);
             }
-            if (++issued < n_tiles) { ic.next(p); fetch_ids(); }
+            ids[0][0] = ids[1][0]; ids[0][1] = ids[1][1]; ids_h[0] = ids_h[1];
+            fetch_ids(ids[1], ids_h[1]);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    fetch_ids();
+    fetch_ids(ids[0], ids_h[0]);
+    fetch_ids(ids[1], ids_h[1]);
 #pragma unroll
     for (int s = 0; s < kScoreStages; ++s) issue();
 

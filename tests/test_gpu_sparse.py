@@ -203,6 +203,21 @@ def test_many_requests(Hq, Hkv, d):
     c.close()
 
 
+@pytest.mark.parametrize("seed", [0, 1])
+def test_more_requests_than_a_block_has_threads(seed):
+    """The work is cut over the sums of all requests, in several turns of a block's threads."""
+    rng = np.random.default_rng(seed)
+    lens = np.where(rng.random(700) < 0.4, 1, rng.integers(1, 700, size=700))
+    lens[[0, 191, 192, 255, 256, 383, 384, 699]] = 640
+    c = Case(lens, 2, 1, 64, seed=20 + seed, width=80)
+    c.update()
+    rec, step = c.host_index()
+    for (page, h), (lo, hi, st) in ref_ops.index_of(widen(c.pool), c.bt, c.lens).items():
+        assert np.array_equal(rec[page, h], [lo, hi]) and step[page, h] == st
+    c.check(9, 1, 2, requests=[0, 191, 192, 255, 256, 383, 384, 699] + list(range(5, 700, 41)))
+    c.close()
+
+
 @pytest.mark.parametrize("Hq,Hkv,d", [(4, 1, 64), (32, 8, 128), (14, 2, 128)])
 @pytest.mark.parametrize("budget", [1, 2, 11, 12, 13, 25, 33, 64, 127, 200, 229])
 def test_few_pairs_of_every_list_length(Hq, Hkv, d, budget):
