@@ -281,7 +281,8 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch,
  *   d_u_accept       fp32 [batch][max_draft];  d_u_sample fp32 [batch]
  *   d_tokens         int32 [batch][max_draft + 1]: the accepted drafts, the drawn token, then -1s
  *   d_accepted       int32 [batch]: number of accepted drafts
- * Rows are read where they decide something; the rest of the arrays is not touched.
+ * Rows are read where they decide something, in aligned pieces of 16 bytes: up to 15 bytes beside a row
+ * may be read with it, and are not used.
  * Errors: CKV_EINVAL, CKV_ECUDA.
  */
 #define CKV_PROBS_F32  0

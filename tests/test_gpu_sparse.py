@@ -313,6 +313,48 @@ def test_attention_over_lists_of_the_callers_own():
     c.close()
 
 
+def test_requests_that_share_full_pages():
+    """A common prefix: the shared pages' bounds are written twice, with the same bits."""
+    c = Case([700, 700, 900], 8, 2, 64, seed=19)
+    c.bt[1][:30] = c.bt[0][:30]
+    c.bt[2][:43] = c.bt[0][:43]
+    c.btd.copy_(torch.from_numpy(c.bt))
+    c.update()
+    rec, step = c.host_index()
+    for (page, h), (lo, hi, st) in ref_ops.index_of(widen(c.pool), c.bt, c.lens).items():
+        assert np.array_equal(rec[page, h], [lo, hi]) and step[page, h] == st
+    c.check(9, 1, 2)
+    c.close()
+
+
+def test_two_handles_on_two_streams():
+    """Calls on two handles at once, of different kinds and sizes, do not touch each other's work."""
+    cases = [Case([3000, 517, 90, 2048] * 10, 8, 2, 128, seed=23, width=400), Case([1500, 33], 4, 1, 64, seed=24)]
+    streams, want, bufs = [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    for c in cases:
+        c.update()
+        bufs.append(c.out(20))
+        c.kp.decode_attention_sparse(0, c.btd, c.sld, c.qd, c.index, *bufs[-1])
+        want.append([t.clone() for t in bufs[-1]])
+    torch.cuda.synchronize()
+    for _ in range(60):
+        for c, s, b in zip(cases, streams, bufs):
+            c.kp.kv_index_update(0, c.btd, c.sld, c.index, stream=s)
+            c.kp.decode_attention_sparse(0, c.btd, c.sld, c.qd, c.index, *b, stream=s)
+    torch.cuda.synchronize()
+    for c, w, b in zip(cases, want, bufs):
+        assert all(torch.equal(x, y) for x, y in zip(w, b))
+        assert c.kp.check_status() == 0
+        c.close()
+
+
+def test_the_widest_table():
+    c = Case([3000, 17], 4, 1, 64, seed=25, width=49152)
+    c.update()
+    c.check(9, 1, 2)
+    c.close()
+
+
 def test_lists_longer_than_their_rows_are_flagged():
     c = Case([700, 90], 8, 2, 128, seed=15)
     pages, lens, out = c.out(4)
