@@ -154,6 +154,10 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
+try:
+    from . import _marshal
+except ImportError as _e:
+    raise ImportError("_marshal.so is missing or does not load (%s): build it with `python -m paper_2501_08090_b200.build`" % _e) from _e
 
 
 def last_error() -> str:
@@ -193,22 +197,10 @@ def kv_index_bytes(cfg: Config) -> int:
     return int(lib.kv_index_bytes(ctypes.byref(cfg)))
 
 
-def _on(device: int, t: torch.Tensor, dtype: torch.dtype, what: str, *shape: int) -> int:
-    """The address of a contiguous tensor of this type and shape on this device."""
-    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s %s on %s%s"
-                     % (what, dtype, shape, device, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided"))
-
-
-def _rows_on(device: int, t: torch.Tensor, what: str, *shape: int):
-    """(address, stride between tokens) of bf16 rows [tokens][heads][d] whose tokens may lie apart."""
-    if t.dtype is torch.bfloat16 and t.shape == shape and t.get_device() == device:
-        token, head, element = t.stride()
-        if element == 1 and (head == shape[2] or shape[1] == 1):
-            return t.data_ptr(), token
-    raise ValueError("%s must be bfloat16 rows of shape %s on cuda:%d, contiguous within a token, got %s %s (strides %s) on %s"
-                     % (what, shape, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+# _on(device, tensor, dtype, what, *shape): the address of a contiguous tensor of this type and shape there;
+# _rows_on(device, tensor, what, tokens, heads, d): (address, stride between tokens) of bf16 rows whose tokens may lie
+# apart.  Anything else is a ValueError that says what was expected and what came.
+_on, _rows_on = _marshal.on, _marshal.rows_on
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -339,7 +331,7 @@ class KvPool:
         k_ptr, k_stride = _rows_on(dev, k_new, "k_new", tokens, c.num_kv_heads, c.head_dim)
         v_ptr, v_stride = _rows_on(dev, v_new, "v_new", tokens, c.num_kv_heads, c.head_dim)
         half = int(inv_freq.shape[0])
-        _check(lib.kv_append_rope(self._h, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
+        _check(_marshal.kv_append_rope(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
                                   None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
                                   _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half, 1 if interleaved else 0, scale,
                                   q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride, _stream_ptr(stream)))
@@ -354,13 +346,13 @@ class KvPool:
     def kv_index_update(self, layer: int, block_tables, seq_lens, index, *, last_tokens: int = 0, stream=None) -> None:
         """Recompute the key bounds of the pages that hold each request's last `last_tokens` tokens (0: all)."""
         batch = self._tables_of(block_tables, seq_lens)
-        _check(lib.kv_index_update(self._h, layer, batch, block_tables.data_ptr(), seq_lens.data_ptr(), int(last_tokens),
+        _check(_marshal.kv_index_update(self._h.value, layer, batch, block_tables.data_ptr(), seq_lens.data_ptr(), int(last_tokens),
                                    self._index_on(index), self._index_bytes, _stream_ptr(stream)))
 
     def kv_index_values(self, layer: int, index, out, stream=None) -> None:
         """The key bounds of a layer as numbers: out bf16 [pages][Hkv][2][d]."""
         c = self.cfg
-        _check(lib.kv_index_values(self._h, layer, self._index_on(index), self._index_bytes,
+        _check(_marshal.kv_index_values(self._h.value, layer, self._index_on(index), self._index_bytes,
                                    _on(self._index, out, torch.bfloat16, "out", c.num_pages, c.num_kv_heads, 2, c.head_dim),
                                    _stream_ptr(stream)))
 
@@ -376,13 +368,13 @@ class KvPool:
                             stream=None) -> None:
         """Choose pages.shape[2] pages per (request, kv head) for the new queries; writes pages and lens."""
         batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
-        _check(lib.decode_select_pages(self._h, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream)))
+        _check(_marshal.decode_select_pages(self._h.value, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream)))
 
     def decode_attention_pages(self, layer: int, pages, lens, q, out, stream=None) -> None:
         """decode_attention over a list of pages per (request, kv head): pages [batch][Hkv][budget], lens [batch]."""
         c, dev = self.cfg, self._index
         batch, budget = int(lens.shape[0]), int(pages.shape[-1])
-        _check(lib.decode_attention_pages(self._h, layer, batch, budget,
+        _check(_marshal.decode_attention_pages(self._h.value, layer, batch, budget,
                                           _on(dev, pages, torch.int32, "pages", batch, c.num_kv_heads, budget),
                                           _on(dev, lens, torch.int32, "lens", batch),
                                           _on(dev, q, torch.bfloat16, "q", batch, c.num_q_heads, c.head_dim),
@@ -394,7 +386,7 @@ class KvPool:
         """decode_select_pages, then decode_attention_pages over what it chose."""
         c = self.cfg
         batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
-        _check(lib.decode_attention_sparse(self._h, layer, batch, *ins, budget, sink, recent, *outs,
+        _check(_marshal.decode_attention_sparse(self._h.value, layer, batch, *ins, budget, sink, recent, *outs,
                                            _on(self._index, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
                                            _stream_ptr(stream)))
 
@@ -577,7 +569,7 @@ def draft_verify(draft_tokens, target_probs, draft_probs, u_accept, u_sample, to
 
     p_ptr, p_stride = rows(target_probs, "target_probs", n + 1)
     q_ptr, q_stride = rows(draft_probs, "draft_probs", n) if draft_probs is not None else (None, 0)
-    _check(lib.draft_verify(batch, n, vocab, PROBS_F32 if dtype == torch.float32 else PROBS_BF16,
+    _check(_marshal.draft_verify(batch, n, vocab, PROBS_F32 if dtype == torch.float32 else PROBS_BF16,
                             _on(dev, draft_tokens, torch.int32, "draft_tokens", batch, n),
                             None if draft_lens is None else _on(dev, draft_lens, torch.int32, "draft_lens", batch),
                             p_ptr, p_stride, q_ptr, q_stride, _on(dev, u_accept, torch.float32, "u_accept", batch, n),

@@ -13,6 +13,7 @@ HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "
                                           "ckv_sparse.cuh", "ckv_verify.cuh")] + \
           [os.path.join(_ROOT, "include", n) for n in ("chiron_kv.h", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
+MARSHAL_SOURCE, MARSHAL = os.path.join(CSRC, "ckv_marshal.cpp"), os.path.join(_HERE, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -36,8 +37,29 @@ def is_stale() -> bool:
     return any(os.path.getmtime(p) > built for p in SOURCES + HEADERS)
 
 
+def build_marshal(force: bool = False) -> str:
+    """Build _marshal.so, the argument marshalling of the hot calls (g++, Python's and torch's headers)."""
+    sources = [MARSHAL_SOURCE, os.path.join(_ROOT, "include", "chiron_kv.h")]
+    if force or not os.path.exists(MARSHAL) or any(os.path.getmtime(p) > os.path.getmtime(MARSHAL) for p in sources):
+        import sysconfig
+
+        import torch
+        home = os.path.dirname(torch.__file__)
+        tmp = MARSHAL + ".tmp.%d" % os.getpid()
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+               "-I", os.path.join(_ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+               "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               "-o", tmp, MARSHAL_SOURCE, "-L", _HERE, "-l:libchiron_kv.so", "-Wl,-rpath,$ORIGIN",
+               "-L", os.path.join(home, "lib"), "-ltorch_python", "-ltorch", "-lc10", "-Wl,-rpath," + os.path.join(home, "lib")]
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("g++ failed:\n%s\n%s" % (res.stdout, res.stderr))
+        os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libchiron_kv.so if missing or older than its sources; return its path."""
+    """Build libchiron_kv.so (and _marshal.so) if missing or older than their sources; return its path."""
     if force or is_stale():
         tmp = LIBRARY + ".tmp.%d" % os.getpid()
         cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
@@ -47,6 +69,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose:
             print(res.stderr)
         os.replace(tmp, LIBRARY)
+    build_marshal(force)
     return LIBRARY
 
 

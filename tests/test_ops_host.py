@@ -82,3 +82,27 @@ def test_plain_verification_by_hand():
     assert ref_ops.verify([0], p, None, [0.5], 0.3) == (0, [1])           # 0.5 >= 0.5; p without token 0
     assert ref_ops.verify([], p[:1], None, [], 0.5) == (0, [1])
     assert ref_ops.verify([2], p, q, [0.0], 0.2) == (0, [1])              # p = 0: refused even at u = 0
+
+
+def test_marshalling_refuses_what_the_library_cannot_see(b):
+    """Checks of the tensors and numbers of a call, none of which reaches CUDA."""
+    import torch
+    m = b._marshal
+    x = torch.zeros(2, 3, 4, dtype=torch.bfloat16)
+    for bad in (x, None, 3, torch.zeros(2, 3)):
+        with pytest.raises(ValueError) as e:
+            m.on(0, bad, torch.bfloat16, "thing", 2, 3, 4)
+        assert "thing" in str(e.value)
+        with pytest.raises(ValueError) as e:
+            m.rows_on(0, bad, "rows", 2, 3, 4)
+        assert "rows" in str(e.value)
+    with pytest.raises(TypeError):
+        m.on(0, x)
+    with pytest.raises(TypeError):
+        m.draft_verify(1, 2, 3)
+    ok = [2, 3, 100, 0, 16, None, 4096, 100, 8192, 100, 64, 96, 128, 256, None]
+    assert m.draft_verify(*[-1 if i == 1 else v for i, v in enumerate(ok)]) == b.CKV_EINVAL and "max_draft" in b.last_error()
+    for at, wrong, kind in ((0, 2 ** 31, OverflowError), (0, "two", TypeError), (4, "address", TypeError), (6, 1.5, TypeError)):
+        with pytest.raises(kind):
+            m.draft_verify(*[wrong if i == at else v for i, v in enumerate(ok)])
+    assert m.kv_index_update(None, 0, 1, None, None, 0, None, 0, None) == b.CKV_EINVAL
