@@ -203,9 +203,11 @@ def kv_index_bytes(cfg: Config) -> int:
 _on, _rows_on = _marshal.on, _marshal.rows_on
 
 
-def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream_ptr(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
     # the raw handle: building the current stream's Python object takes 3 us, as long as a launch
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 class KvPool:
@@ -334,7 +336,7 @@ class KvPool:
         _check(_marshal.kv_append_rope(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
                                   None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
                                   _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half, 1 if interleaved else 0, scale,
-                                  q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride, _stream_ptr(stream)))
+                                  q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride, _stream_ptr(stream, self._index)))
 
     def make_index(self) -> torch.Tensor:
         """An empty index of the pool's keys (uint8, kv_index_bytes), for kv_index_update and the sparse calls."""
@@ -347,14 +349,14 @@ class KvPool:
         """Recompute the key bounds of the pages that hold each request's last `last_tokens` tokens (0: all)."""
         batch = self._tables_of(block_tables, seq_lens)
         _check(_marshal.kv_index_update(self._h.value, layer, batch, block_tables.data_ptr(), seq_lens.data_ptr(), int(last_tokens),
-                                   self._index_on(index), self._index_bytes, _stream_ptr(stream)))
+                                   self._index_on(index), self._index_bytes, _stream_ptr(stream, self._index)))
 
     def kv_index_values(self, layer: int, index, out, stream=None) -> None:
         """The key bounds of a layer as numbers: out bf16 [pages][Hkv][2][d]."""
         c = self.cfg
         _check(_marshal.kv_index_values(self._h.value, layer, self._index_on(index), self._index_bytes,
                                    _on(self._index, out, torch.bfloat16, "out", c.num_pages, c.num_kv_heads, 2, c.head_dim),
-                                   _stream_ptr(stream)))
+                                   _stream_ptr(stream, self._index)))
 
     def _select_args(self, block_tables, seq_lens, q, index, pages, lens):
         c, dev = self.cfg, self._index
@@ -368,7 +370,7 @@ class KvPool:
                             stream=None) -> None:
         """Choose pages.shape[2] pages per (request, kv head) for the new queries; writes pages and lens."""
         batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
-        _check(_marshal.decode_select_pages(self._h.value, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream)))
+        _check(_marshal.decode_select_pages(self._h.value, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream, self._index)))
 
     def decode_attention_pages(self, layer: int, pages, lens, q, out, stream=None) -> None:
         """decode_attention over a list of pages per (request, kv head): pages [batch][Hkv][budget], lens [batch]."""
@@ -379,7 +381,7 @@ class KvPool:
                                           _on(dev, lens, torch.int32, "lens", batch),
                                           _on(dev, q, torch.bfloat16, "q", batch, c.num_q_heads, c.head_dim),
                                           _on(dev, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
-                                          _stream_ptr(stream)))
+                                          _stream_ptr(stream, self._index)))
 
     def decode_attention_sparse(self, layer: int, block_tables, seq_lens, q, index, pages, lens, out, *, sink: int = 1,
                                 recent: int = 2, stream=None) -> None:
@@ -388,7 +390,7 @@ class KvPool:
         batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
         _check(_marshal.decode_attention_sparse(self._h.value, layer, batch, *ins, budget, sink, recent, *outs,
                                            _on(self._index, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
-                                           _stream_ptr(stream)))
+                                           _stream_ptr(stream, self._index)))
 
     def swap_image_bytes(self, n_pages: int) -> int:
         c = self.cfg
@@ -556,26 +558,19 @@ def draft_verify(draft_tokens, target_probs, draft_probs, u_accept, u_sample, to
     [batch]; writes tokens int32 [batch][n + 1] and accepted int32 [batch]."""
     dev = torch.cuda.current_device()
     batch, n = draft_tokens.shape
-    vocab, dtype = int(target_probs.shape[2]), target_probs.dtype
+    vocab, dtype = target_probs.shape[-1], target_probs.dtype
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("probabilities must be float32 or bfloat16, got %s" % dtype)
 
-    def rows(t, what, count):
-        if t.dtype != dtype or t.get_device() != dev or tuple(t.shape) != (batch, count, vocab) or \
-                (t.stride(2) != 1 and vocab > 1) or (batch > 1 and count > 0 and t.stride(0) != count * t.stride(1)):
-            raise ValueError("%s must be %s rows [%d][%d][%d], evenly spaced, on cuda:%d, got %s %s (strides %s) on %s"
-                             % (what, dtype, batch, count, vocab, dev, t.dtype, tuple(t.shape), t.stride(), t.device))
-        return t.data_ptr(), t.stride(1)
-
-    p_ptr, p_stride = rows(target_probs, "target_probs", n + 1)
-    q_ptr, q_stride = rows(draft_probs, "draft_probs", n) if draft_probs is not None else (None, 0)
+    p_ptr, p_stride = _marshal.probs_on(dev, target_probs, dtype, "target_probs", batch, n + 1, vocab)
+    q_ptr, q_stride = _marshal.probs_on(dev, draft_probs, dtype, "draft_probs", batch, n, vocab) if draft_probs is not None else (None, 0)
     _check(_marshal.draft_verify(batch, n, vocab, PROBS_F32 if dtype == torch.float32 else PROBS_BF16,
                             _on(dev, draft_tokens, torch.int32, "draft_tokens", batch, n),
                             None if draft_lens is None else _on(dev, draft_lens, torch.int32, "draft_lens", batch),
                             p_ptr, p_stride, q_ptr, q_stride, _on(dev, u_accept, torch.float32, "u_accept", batch, n),
                             _on(dev, u_sample, torch.float32, "u_sample", batch),
                             _on(dev, tokens, torch.int32, "tokens", batch, n + 1),
-                            _on(dev, accepted, torch.int32, "accepted", batch), _stream_ptr(stream)))
+                            _on(dev, accepted, torch.int32, "accepted", batch), _stream_ptr(stream, dev)))
 
 
 class LocalAutoscaler:

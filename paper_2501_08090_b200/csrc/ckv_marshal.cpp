@@ -104,6 +104,29 @@ PyObject *rows_on(PyObject *, PyObject *const *args, Py_ssize_t n)
     return nullptr;
 }
 
+// probs_on(device, tensor, dtype, what, batch, count, vocab): (address, stride between rows) of evenly spaced rows of
+// probabilities.
+PyObject *probs_on(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "probs_on(device, tensor, dtype, what, batch, count, vocab)");
+        return nullptr;
+    }
+    const long device = PyLong_AsLong(args[0]);
+    if (THPVariable_Check(args[1]) && THPDtype_Check(args[2])) {
+        const at::Tensor &v = THPVariable_Unpack(args[1]);
+        if (v.scalar_type() == reinterpret_cast<THPDtype *>(args[2])->scalar_type && fits(v, device, args + 4, 3) &&
+            (v.stride(2) == 1 || v.size(2) == 1) && (v.size(0) == 1 || v.size(1) == 0 || v.stride(0) == v.size(1) * v.stride(1)))
+            return Py_BuildValue("(NL)", PyLong_FromVoidPtr(v.data_ptr()), (long long)v.stride(1));
+    }
+    if (PyErr_Occurred()) return nullptr;
+    PyObject *wanted = PyUnicode_FromFormat("evenly spaced %S rows", args[2]);
+    if (!wanted) return nullptr;
+    refuse(args[1], args[3], wanted, device, args + 4, 3);
+    Py_DECREF(wanted);
+    return nullptr;
+}
+
 // A Python number as an argument of the C ABI: an address (None: NULL), an int32, an int64, a size or a float.
 template <typename T>
 T argument(PyObject *x)
@@ -151,6 +174,7 @@ CKV_WRAP(draft_verify)
 PyMethodDef methods[] = {
     {"on", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(on)), METH_FASTCALL, "Address of a tensor after its checks."},
     {"rows_on", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rows_on)), METH_FASTCALL, "Address and token stride of rows."},
+    {"probs_on", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(probs_on)), METH_FASTCALL, "Address and row stride of probabilities."},
     CKV_METHOD(kv_append_rope), CKV_METHOD(kv_index_update), CKV_METHOD(kv_index_values), CKV_METHOD(decode_select_pages),
     CKV_METHOD(decode_attention_pages), CKV_METHOD(decode_attention_sparse), CKV_METHOD(draft_verify),
     {nullptr, nullptr, 0, nullptr}};
