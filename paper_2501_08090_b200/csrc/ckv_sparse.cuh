@@ -415,10 +415,16 @@ struct QueryFragments {
     uint32_t neg[kPieces][4], pos[kPieces][4];
     float step0, step1;
 
+    // fetch: the loads; convert: what they brought in whole numbers (raw stays live in between)
     __device__ __forceinline__ void load(const uint16_t *q, int group, int lane)
     {
-        const int g = lane >> 2, t = lane & 3;
         uint32_t raw[kPieces][8];
+        fetch(raw, q, group, lane);
+        convert(raw, group, lane);
+    }
+    static __device__ __forceinline__ void fetch(uint32_t (&raw)[kPieces][8], const uint16_t *q, int group, int lane)
+    {
+        const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
@@ -430,6 +436,10 @@ struct QueryFragments {
             raw[i][0] = a.x; raw[i][1] = a.y; raw[i][2] = a.z; raw[i][3] = a.w;
             raw[i][4] = b.x; raw[i][5] = b.y; raw[i][6] = b.z; raw[i][7] = b.w;
         }
+    }
+    __device__ __forceinline__ void convert(uint32_t (&raw)[kPieces][8], int group, int lane)
+    {
+        const int g = lane >> 2, t = lane & 3;
         // the largest magnitude, two at a time; a NaN would win, as an infinity does
         __nv_bfloat162 most = __nv_bfloat162(__ushort_as_bfloat16(0), __ushort_as_bfloat16(0));
 #pragma unroll
@@ -581,47 +591,56 @@ score_pages_kernel(const SelectParams p)
     ic.tile = (st.begin - st.before) % ic.tiles;
     TileCursor cc = ic;
 
-    // ---- issue side: lane (g, t) copies its quarter of the records of rows g and g + 8; the table entries
-    // of the next two tiles are on their way already
-    int ids[2][2], ids_h[2];
-    int fetched = 0;
-    auto fetch_ids = [&](int (&id)[2], int &h) {
-        if (fetched >= n_tiles) return;
-        if (fetched++ > 0) ic.next(p);
-        const int32_t *table = p.block_tables + (size_t)ic.r * p.max_pages_per_req + p.sink;
-        const int c = ic.tile * 16 + g;
-        id[0] = c < ic.cand ? __ldg(table + c) : 0;
-        id[1] = c + 8 < ic.cand ? __ldg(table + c + 8) : 0;
-        h = ic.h;
+    // ---- the first pair's queries are on their way while the first copies are prepared
+    uint32_t q_raw[QueryFragments<D>::kPieces][8];
+    QueryFragments<D>::fetch(q_raw, p.q + (size_t)(ic.r * p.num_kv_heads + ic.h) * p.group * D, p.group, lane);
+
+    // ---- issue side: lane (g, t) copies its quarter of the records of rows g and g + 8.  Table entries travel
+    // in registers, 32 (two tiles) at a time, fetched one such chunk ahead.
+    TileCursor pc = ic;                          // the chunk that is fetched next holds this tile
+    auto fetch_chunk = [&]() -> int {
+        if (pc.tiles == 0) return 0;             // behind the last request
+        const int32_t *table = p.block_tables + (size_t)pc.r * p.max_pages_per_req + p.sink;
+        const int c = (pc.tile & ~1) * 16 + lane;
+        const int id = c < pc.cand ? __ldg(table + c) : 0;
+        pc.tile |= 1;                            // on to the next chunk
+        if (pc.tile >= pc.tiles) pc.tile = pc.tiles - 1;
+        pc.next(p);
+        return id;
     };
+    int cur_ids = fetch_chunk(), next_ids = fetch_chunk();
     int issued = 0;
     auto issue = [&]() {
         if (issued < n_tiles) {
             const uint32_t stage = ring + (issued % kScoreStages) * Lay::kStageBytes;
-            ++issued;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                int page = ids[0][x];
+                int page = __shfl_sync(0xffffffffu, cur_ids, (ic.tile & 1) * 16 + x * 8 + g);
                 if (page < 0 || page >= p.num_pages) { atomicOr(p.status, kStatusBadPage); page = 0; }
-                const size_t at = (size_t)page * p.num_kv_heads + ids_h[0];
+                const size_t at = (size_t)page * p.num_kv_heads + ic.h;
                 const uint8_t *src = p.records + at * 2 * D + t * 16;
 #pragma unroll
                 for (int i = 0; i < P; ++i) cp_async_16(stage + (x * P + i) * 512 + lane * 16, src + i * 64);
                 if (t == x) cp_async_4(stage + Lay::kStepsOff + (x * 8 + g) * 4, p.steps + at);
             }
-            ids[0][0] = ids[1][0]; ids[0][1] = ids[1][1]; ids_h[0] = ids_h[1];
-            fetch_ids(ids[1], ids_h[1]);
+            if (++issued < n_tiles) {
+                const bool last_of_chunk = (ic.tile & 1) || ic.tile + 1 == ic.tiles;
+                ic.next(p);
+                if (last_of_chunk) {
+                    cur_ids = next_ids;
+                    next_ids = fetch_chunk();
+                }
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    fetch_ids(ids[0], ids_h[0]);
-    fetch_ids(ids[1], ids_h[1]);
 #pragma unroll
     for (int s = 0; s < kScoreStages; ++s) issue();
 
     // ---- compute side
     QueryFragments<D> q;
-    int q_pair = -1;
+    q.convert(q_raw, p.group, lane);
+    int q_pair = cc.r * p.num_kv_heads + cc.h;
     for (int done = 0; done < n_tiles; ++done) {
         const int pair = cc.r * p.num_kv_heads + cc.h;
         if (pair != q_pair) {
