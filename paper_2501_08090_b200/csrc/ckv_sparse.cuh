@@ -18,7 +18,6 @@ namespace ckv {
 // step: it is nearly always selected, and attention then shows what a full pass would have shown.
 // Records come first, all layers, then all steps.
 // ------------------------------------------------------------------------------------------
-constexpr int kIndexMinExp = -100;
 constexpr float kIndexStepOfInvalid = 2.658455991569832e36f;      // 2^121
 
 // Step exponent for a largest magnitude m; 2^-exponent comes back in `inv`.
