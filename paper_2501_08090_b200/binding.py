@@ -309,7 +309,7 @@ class KvPool:
     # -- around a long decode step
     def _tables_of(self, block_tables, seq_lens) -> int:
         """The batch of these lengths; both on the pool's device, the table as wide as the configuration says."""
-        batch = int(seq_lens.shape[0])
+        batch = seq_lens.numel()
         _on(self._index, seq_lens, torch.int32, "seq_lens", batch)
         _on(self._index, block_tables, torch.int32, "block_tables", batch, self.cfg.max_pages_per_req)
         return batch
@@ -318,11 +318,11 @@ class KvPool:
                        interleaved: bool = False, scale: float = 1.0, stream=None) -> None:
         """Rotate the new tokens' queries (into q_out) and keys by their positions, append keys and values.
 
-        q, q_out [tokens][Hq][d] (both may be None; q_out may be q), k_new, v_new [tokens][Hkv][d]: bf16, tokens may lie apart (slices of one
-        projection's output).  new_start int32 [batch + 1]: each request's first token; without it
-        every request has the same number.  inv_freq fp32 [rotary_dim / 2]."""
+        q, q_out [tokens][Hq][d] (both may be None; q_out may be q), k_new, v_new [tokens][Hkv][d]: bf16, tokens may
+        lie apart (slices of one projection's output).  new_start int32 [batch + 1]: each request's first token;
+        without it every request has the same number.  inv_freq fp32 [rotary_dim / 2]."""
         c, dev = self.cfg, self._index
-        batch, tokens = self._tables_of(block_tables, seq_lens), int(k_new.shape[0])
+        batch, tokens = self._tables_of(block_tables, seq_lens), k_new.size(0)
         q_ptr = out_ptr = None
         q_stride = out_stride = 0
         if (q is None) != (q_out is None):
@@ -332,7 +332,7 @@ class KvPool:
             out_ptr, out_stride = _rows_on(dev, q_out, "q_out", tokens, c.num_q_heads, c.head_dim)
         k_ptr, k_stride = _rows_on(dev, k_new, "k_new", tokens, c.num_kv_heads, c.head_dim)
         v_ptr, v_stride = _rows_on(dev, v_new, "v_new", tokens, c.num_kv_heads, c.head_dim)
-        half = int(inv_freq.shape[0])
+        half = inv_freq.numel()
         _check(_marshal.kv_append_rope(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
                                   None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
                                   _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half, 1 if interleaved else 0, scale,

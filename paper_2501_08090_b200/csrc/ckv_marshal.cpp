@@ -42,6 +42,7 @@ PyObject *refuse(PyObject *t, PyObject *what, PyObject *wanted, long device, PyO
     }
     PyObject *dtype = attr_text(t, "dtype"), *got = attr_text(t, "shape"), *where = attr_text(t, "device");
     PyObject *strides = PyObject_CallMethod(t, "stride", nullptr);
+    if (!strides) PyErr_Clear();
     PyErr_Format(PyExc_ValueError, "%S must be %S of shape %S on cuda:%ld, got %S %S (strides %S) on %S", what, wanted, want,
                  device, dtype, got, strides ? strides : Py_None, where);
     Py_XDECREF(strides);
@@ -50,6 +51,18 @@ PyObject *refuse(PyObject *t, PyObject *what, PyObject *wanted, long device, PyO
     Py_DECREF(got);
     Py_DECREF(where);
     return nullptr;
+}
+
+// Whether `test` holds of the tensor.  A sparse, nested or functional tensor throws when it is asked for strides or an
+// address: it does not fit.
+template <typename Test>
+bool holds(const at::Tensor &v, Test test) noexcept
+{
+    try {
+        return test(v);
+    } catch (...) {
+        return false;
+    }
 }
 
 bool fits(const at::Tensor &v, long device, PyObject *const *shape, Py_ssize_t dims)
@@ -69,9 +82,14 @@ PyObject *on(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     const long device = PyLong_AsLong(args[0]);
     if (THPVariable_Check(args[1]) && THPDtype_Check(args[2])) {
-        const at::Tensor &v = THPVariable_Unpack(args[1]);
-        if (v.scalar_type() == reinterpret_cast<THPDtype *>(args[2])->scalar_type && fits(v, device, args + 4, n - 4) && v.is_contiguous())
-            return PyLong_FromVoidPtr(v.data_ptr());
+        const at::ScalarType type = reinterpret_cast<THPDtype *>(args[2])->scalar_type;
+        void *at = nullptr;
+        if (holds(THPVariable_Unpack(args[1]), [&](const at::Tensor &v) {
+                if (v.scalar_type() != type || !fits(v, device, args + 4, n - 4) || !v.is_contiguous()) return false;
+                at = v.data_ptr();
+                return true;
+            }))
+            return PyLong_FromVoidPtr(at);
     }
     if (PyErr_Occurred()) return nullptr;
     PyObject *wanted = PyUnicode_FromFormat("a contiguous %S tensor", args[2]);
@@ -91,10 +109,17 @@ PyObject *rows_on(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     const long device = PyLong_AsLong(args[0]);
     if (THPVariable_Check(args[1])) {
-        const at::Tensor &v = THPVariable_Unpack(args[1]);
-        if (v.scalar_type() == at::kBFloat16 && fits(v, device, args + 3, 3) && v.stride(2) == 1 &&
-            (v.stride(1) == v.size(2) || v.size(1) == 1))
-            return Py_BuildValue("(NL)", PyLong_FromVoidPtr(v.data_ptr()), (long long)v.stride(0));
+        void *at = nullptr;
+        long long stride = 0;
+        if (holds(THPVariable_Unpack(args[1]), [&](const at::Tensor &v) {
+                if (v.scalar_type() != at::kBFloat16 || !fits(v, device, args + 3, 3) || v.stride(2) != 1 ||
+                    (v.stride(1) != v.size(2) && v.size(1) != 1))
+                    return false;
+                at = v.data_ptr();
+                stride = v.stride(0);
+                return true;
+            }))
+            return Py_BuildValue("(NL)", PyLong_FromVoidPtr(at), stride);
     }
     if (PyErr_Occurred()) return nullptr;
     PyObject *wanted = PyUnicode_FromString("bfloat16 rows, contiguous within a token,");
@@ -114,10 +139,18 @@ PyObject *probs_on(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     const long device = PyLong_AsLong(args[0]);
     if (THPVariable_Check(args[1]) && THPDtype_Check(args[2])) {
-        const at::Tensor &v = THPVariable_Unpack(args[1]);
-        if (v.scalar_type() == reinterpret_cast<THPDtype *>(args[2])->scalar_type && fits(v, device, args + 4, 3) &&
-            (v.stride(2) == 1 || v.size(2) == 1) && (v.size(0) == 1 || v.size(1) == 0 || v.stride(0) == v.size(1) * v.stride(1)))
-            return Py_BuildValue("(NL)", PyLong_FromVoidPtr(v.data_ptr()), (long long)v.stride(1));
+        const at::ScalarType type = reinterpret_cast<THPDtype *>(args[2])->scalar_type;
+        void *at = nullptr;
+        long long stride = 0;
+        if (holds(THPVariable_Unpack(args[1]), [&](const at::Tensor &v) {
+                if (v.scalar_type() != type || !fits(v, device, args + 4, 3) || (v.stride(2) != 1 && v.size(2) != 1) ||
+                    (v.size(0) != 1 && v.size(1) != 0 && v.stride(0) != v.size(1) * v.stride(1)))
+                    return false;
+                at = v.data_ptr();
+                stride = v.stride(1);
+                return true;
+            }))
+            return Py_BuildValue("(NL)", PyLong_FromVoidPtr(at), stride);
     }
     if (PyErr_Occurred()) return nullptr;
     PyObject *wanted = PyUnicode_FromFormat("evenly spaced %S rows", args[2]);

@@ -265,6 +265,12 @@ def test_refusals():
         kp.kv_append_rope(0, btd, sld, odd.as_strided((2, 4, 64), (260, 64, 1)), k, v, out, freq)
     with pytest.raises(b.CkvError):                                      # in place with another stride
         kp.kv_append_rope(0, btd, sld, odd[:512].view(2, 4, 64), k, v, odd.as_strided((2, 4, 64), (264, 64, 1)), freq)
+    for odd_kind in (lambda t: t.to_sparse(), lambda t: torch.nested.nested_tensor([t[0], t[1]])):
+        with pytest.raises(ValueError) as e:
+            kp.kv_append_rope(0, btd, sld, odd_kind(q), k, v, out, freq)
+        assert "q must be" in str(e.value)
+        with pytest.raises(ValueError):
+            kp.kv_append_rope(0, btd, sld, q, k, v, out, odd_kind(torch.ones(2, 16, device="cuda")))
     for wrong in (q.float(), q[:, :3], q.transpose(1, 2).contiguous().transpose(1, 2), q.cpu()):
         with pytest.raises(ValueError):
             kp.kv_append_rope(0, btd, sld, wrong, k, v, out, freq)
