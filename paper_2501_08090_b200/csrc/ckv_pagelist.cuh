@@ -222,7 +222,9 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
             mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, x));
         }
         const float mn0 = fmaxf(m0, mx0 * p.scale_log2), mn1 = fmaxf(m1, mx1 * p.scale_log2);
-        const float al0 = fast_exp2(m0 - mn0), al1 = fast_exp2(m1 - mn1);
+        // so far only scores of -inf (infinite keys): exponentials are taken against 0 and come out 0
+        const float ref0 = mn0 == -INFINITY ? 0.f : mn0, ref1 = mn1 == -INFINITY ? 0.f : mn1;
+        const float al0 = fast_exp2(m0 - ref0), al1 = fast_exp2(m1 - ref1);
         m0 = mn0; m1 = mn1;
         l0 *= al0; l1 *= al1;
 #pragma unroll
@@ -230,8 +232,8 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
         uint32_t pb[kPagesPerTile][2];
 #pragma unroll
         for (int mt = 0; mt < kPagesPerTile; ++mt) {
-            const float p0 = fast_exp2(fmaf(s[mt][0], p.scale_log2, -mn0)), p1 = fast_exp2(fmaf(s[mt][1], p.scale_log2, -mn1));
-            const float p2 = fast_exp2(fmaf(s[mt][2], p.scale_log2, -mn0)), p3 = fast_exp2(fmaf(s[mt][3], p.scale_log2, -mn1));
+            const float p0 = fast_exp2(fmaf(s[mt][0], p.scale_log2, -ref0)), p1 = fast_exp2(fmaf(s[mt][1], p.scale_log2, -ref1));
+            const float p2 = fast_exp2(fmaf(s[mt][2], p.scale_log2, -ref0)), p3 = fast_exp2(fmaf(s[mt][3], p.scale_log2, -ref1));
             l0 += p0 + p2;
             l1 += p1 + p3;
             pb[mt][0] = movmatrix_trans(pack_bf16x2(p0, p1));
@@ -292,7 +294,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < W; ++w) M = fmaxf(M, parts[w * kPartStride + kMaxGroup * Lay::kPitch + g]);
-        const float ref = M == -INFINITY ? 0.f : M;              // no warp of this CTA had a tile
+        const float ref = M == -INFINITY ? 0.f : M;              // no warp of this CTA had a tile, or only scores of -inf
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             const float *src = parts + w * kPartStride;
@@ -318,7 +320,7 @@ page_list_attn_kernel(const __grid_constant__ CUtensorMap tmap, const ListParams
         float M = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int c = 0; c < ctas; ++c) M = fmaxf(M, ld_cluster_f32(cluster_map(ml, c)));
-        const float ref = M == -INFINITY ? 0.f : M;              // only after a wait gave up everywhere
+        const float ref = M == -INFINITY ? 0.f : M;              // only scores of -inf (0 / 0 below), or a wait gave up everywhere
         for (int c = 0; c < ctas; ++c) {
             const float f = fast_exp2(ld_cluster_f32(cluster_map(ml, c)) - ref);
             l += f * ld_cluster_f32(cluster_map(ml + 4 * kMaxGroup, c));
