@@ -482,7 +482,7 @@ __device__ __forceinline__ int fold_finish(const FoldJob j, const FoldCtx c)
             const uint32_t ml = (t0 + i == j.alt_t) ? j.alt_base + j.alt_ml_off : j.base + i * j.stride + j.ml_off;
             Mr = fmaxf(Mr, ld_shared_f32(ml + 4 * g));
         }
-        // a column that no partial so far has seen a token for keeps -inf (multi-token steps):
+        // a column that no partial so far has seen a finite score for keeps -inf:
         // exponentials are then taken against 0 and come out 0
         const float Mn = fmaxf(M, Mr);
         const float ref = Mn == -INFINITY ? 0.f : Mn;
@@ -947,7 +947,8 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
             mx1 *= p.scale_log2;
             // The reference a column's exponentials are taken against only has to be near its maximum:
             // it moves (with the reduction across lanes and the rescale that this costs) only when
-            // some score of the tile exceeds it by more than 2^8.
+            // some score of the tile exceeds it by more than 2^8.  A column with nothing above -inf so far
+            // (no visible token, or keys that hold infinities) takes them against 0: they come out 0.
             float mn0 = m0, mn1 = m1;
             if (__any_sync(0xffffffffu, mx0 > m0 + 8.f || mx1 > m1 + 8.f)) {
 #pragma unroll
@@ -958,10 +959,8 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                 const float mo0 = m0, mo1 = m1;
                 mn0 = fmaxf(mo0, mx0); mn1 = fmaxf(mo1, mx1);
                 m0 = mn0; m1 = mn1;
-                if (kMulti) {
-                    mn0 = (mn0 == -INFINITY) ? 0.f : mn0;
-                    mn1 = (mn1 == -INFINITY) ? 0.f : mn1;
-                }
+                mn0 = (mn0 == -INFINITY) ? 0.f : mn0;
+                mn1 = (mn1 == -INFINITY) ? 0.f : mn1;
                 const float al0 = fast_exp2(mo0 - mn0), al1 = fast_exp2(mo1 - mn1);
                 l0 *= al0; l1 *= al1;
 #pragma unroll
@@ -969,7 +968,7 @@ paged_decode_attn_kernel(const __grid_constant__ CUtensorMap tmap, const AttnPar
                     o[dt][0] *= al0; o[dt][2] *= al0;
                     o[dt][1] *= al1; o[dt][3] *= al1;
                 }
-            } else if (kMulti) {
+            } else {
                 mn0 = (mn0 == -INFINITY) ? 0.f : mn0;
                 mn1 = (mn1 == -INFINITY) ? 0.f : mn1;
             }

@@ -89,3 +89,53 @@ def test_selected_by_their_bounds(kind, lens):
     chosen = pages.cpu().numpy()
     c.check("sparse", lambda r, h: [int(x) for x in chosen[r, h] if x >= 0])
     c.kp.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 128), (4, 1, 64), (14, 2, 128)])
+def test_over_whole_contexts(kind, Hq, Hkv, d):
+    """decode_attention with the context whole in one warp, in a CTA, and cut over many."""
+    c = Batch(kind, Hq, Hkv, d, seed=33)
+    default = c.kp.get_partition()
+    for spans in (default, 1, 3, 100):
+        c.kp.set_partition(spans)
+        c.out.fill_(float("nan"))
+        c.kp.decode_attention(0, c.btd, c.sld, c.qd, c.out)
+        c.check("%d spans" % spans)
+    c.kp.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_of_a_fused_step(kind):
+    """decode_step, whose new key is the last token's."""
+    c = Batch(kind, 8, 2, 128, seed=34)
+    pool = c.kp.pool_view()[0]
+    last = [(int(c.bt[r][(L - 1) // 16]), (int(L) - 1) % 16) for r, L in enumerate(c.lens)]
+    k, v = (torch.stack([pool[p, :, kv, s] for p, s in last]).contiguous() for kv in (0, 1))
+    for p, s in last:
+        pool[p, :, :, s] = float("nan")                                  # the step stores it
+    torch.cuda.synchronize()
+    c.kp.decode_step(0, c.btd, c.sld, c.qd, k, v, c.out)
+    c.check("decode_step")
+    c.kp.close()
+
+
+@pytest.mark.parametrize("q_len", [2, 5])
+@pytest.mark.parametrize("kind", ["first tile", "every other tile", "none"])
+def test_of_several_new_tokens(kind, q_len):
+    """decode_attention_multi: each new token's own context."""
+    lens = (65, 100, 1000, 4001)
+    c = Batch(kind, 8, 2, 128, seed=35, lens=lens)
+    q = wl.normal_bf16((len(lens), q_len, 8, 128), 35, 3)
+    q[..., CHANNEL] = c.q[:, None, :, CHANNEL]
+    out = torch.full((len(lens), q_len, 8, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    c.kp.decode_attention_multi(0, q_len, c.btd, c.sld, bits_to_dev(q), out)
+    assert c.kp.check_status() == 0
+    pool, q = widen(c.pool), widen(q)
+    for r, L in enumerate(lens):
+        pages = [int(x) for x in c.bt[r][:-(-L // 16)]]
+        for i in range(q_len):
+            for h in range(2):
+                ref = ref_ops.attend(pool, pages, L - q_len + 1 + i, q[r, i, h * 4:h * 4 + 4], h)
+                assert_close(dev_to_bits(out[r, i, h * 4:h * 4 + 4]), ref, "request %d token %d kv head %d" % (r, i, h))
+    c.kp.close()
