@@ -130,7 +130,8 @@ PyObject *rows_on(PyObject *, PyObject *const *args, Py_ssize_t n)
 }
 
 // probs_on(device, tensor, dtype, what, batch, count, vocab): (address, stride between rows) of evenly spaced rows of
-// probabilities.
+// probabilities.  The stride of a dimension of size 1 means nothing: one row a request lies as far from the next as
+// the requests do.
 PyObject *probs_on(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != 7) {
@@ -143,11 +144,10 @@ PyObject *probs_on(PyObject *, PyObject *const *args, Py_ssize_t n)
         void *at = nullptr;
         long long stride = 0;
         if (holds(THPVariable_Unpack(args[1]), [&](const at::Tensor &v) {
-                if (v.scalar_type() != type || !fits(v, device, args + 4, 3) || (v.stride(2) != 1 && v.size(2) != 1) ||
-                    (v.size(0) != 1 && v.size(1) != 0 && v.stride(0) != v.size(1) * v.stride(1)))
-                    return false;
+                if (v.scalar_type() != type || !fits(v, device, args + 4, 3) || (v.stride(2) != 1 && v.size(2) != 1)) return false;
+                stride = v.size(1) != 1 ? v.stride(1) : v.size(0) != 1 ? v.stride(0) : v.size(2);
+                if (v.size(0) != 1 && v.size(1) > 1 && v.stride(0) != v.size(1) * stride) return false;
                 at = v.data_ptr();
-                stride = v.stride(1);
                 return true;
             }))
             return Py_BuildValue("(NL)", PyLong_FromVoidPtr(at), stride);
