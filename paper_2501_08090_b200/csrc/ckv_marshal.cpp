@@ -174,13 +174,18 @@ T argument(PyObject *x)
     }
 }
 
-// One wrapper per function: its arguments in order, the status returned.
+// One wrapper per function: its arguments in order, the status returned.  Other Python threads run meanwhile: with
+// the launch queue full, a launch blocks until the GPU has caught up.
 template <typename... P, size_t... I>
 PyObject *call(int32_t (*fn)(P...), PyObject *const *args, std::index_sequence<I...>)
 {
     const std::tuple<P...> values{argument<P>(args[I])...};
     if (PyErr_Occurred()) return nullptr;
-    return PyLong_FromLong(std::apply(fn, values));
+    int32_t status;
+    Py_BEGIN_ALLOW_THREADS
+    status = std::apply(fn, values);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
 }
 
 template <typename... P>
