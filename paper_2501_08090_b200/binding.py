@@ -1,17 +1,21 @@
-"""ctypes binding of libchiron_kv.so (see include/chiron_kv.h): argument marshalling only.
+"""Binding of libchiron_kv.so (see include/chiron_kv.h): argument marshalling only, through ctypes and an extension module.
 
 Every computation runs in the library's CUDA kernels.  There is no fallback: if the shared
-library has not been built, importing this module raises.  torch is used for device memory and
+library has not been built, importing this module raises, and where the extension module that passes
+some calls' arguments is missing, those calls raise.  torch is used for device memory and
 streams, nothing else.
 """
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import Optional, Sequence
 
 import numpy as np
 import torch
+
+from .build import marshal_path
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
@@ -154,10 +158,33 @@ def _load() -> ctypes.CDLL:
 
 
 lib = _load()
-try:
-    from . import _marshal
-except ImportError as _e:
-    raise ImportError("_marshal.so is missing or does not load (%s): build it with `python -m paper_2501_08090_b200.build`" % _e) from _e
+
+
+class _Unavailable:
+    """Stands in for the extension module where none fits this Python and torch: each of its calls says so."""
+
+    def __init__(self, why: str):
+        self._why = why
+
+    def __getattr__(self, name):
+        def refuse(*args):
+            raise ImportError("the extension module that passes this call's arguments is missing or does not load (%s): build it "
+                              "with `python -m paper_2501_08090_b200.build`" % self._why)
+        return refuse
+
+
+def _load_marshal():
+    path = marshal_path()
+    spec = importlib.util.spec_from_file_location(__package__ + "._marshal", path)
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        return module
+    except ImportError as e:
+        return _Unavailable(str(e))
+
+
+_marshal = _load_marshal()
 
 
 def last_error() -> str:

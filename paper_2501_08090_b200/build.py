@@ -13,7 +13,7 @@ HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "
                                           "ckv_sparse.cuh", "ckv_verify.cuh")] + \
           [os.path.join(_ROOT, "include", n) for n in ("chiron_kv.h", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
-MARSHAL_SOURCE, MARSHAL = os.path.join(CSRC, "ckv_marshal.cpp"), os.path.join(_HERE, "_marshal.so")
+MARSHAL_SOURCE = os.path.join(CSRC, "ckv_marshal.cpp")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -37,15 +37,25 @@ def is_stale() -> bool:
     return any(os.path.getmtime(p) > built for p in SOURCES + HEADERS)
 
 
+def marshal_path() -> str:
+    """Where the extension module lies.  It uses Python's and torch's own structures, so its name holds both versions:
+    a module built for others is neither loaded nor taken for up to date."""
+    import sysconfig
+
+    import torch
+    return os.path.join(_HERE, "_marshal.torch-%s%s" % (torch.__version__, sysconfig.get_config_var("EXT_SUFFIX")))
+
+
 def build_marshal(force: bool = False) -> str:
-    """Build _marshal.so, the argument marshalling of the hot calls (g++, Python's and torch's headers)."""
+    """Build the extension module, the argument marshalling of the hot calls (g++, Python's and torch's headers)."""
     sources = [MARSHAL_SOURCE, os.path.join(_ROOT, "include", "chiron_kv.h")]
-    if force or not os.path.exists(MARSHAL) or any(os.path.getmtime(p) > os.path.getmtime(MARSHAL) for p in sources):
+    path = marshal_path()
+    if force or not os.path.exists(path) or any(os.path.getmtime(p) > os.path.getmtime(path) for p in sources):
         import sysconfig
 
         import torch
         home = os.path.dirname(torch.__file__)
-        tmp = MARSHAL + ".tmp.%d" % os.getpid()
+        tmp = path + ".tmp.%d" % os.getpid()
         cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
                "-I", os.path.join(_ROOT, "include"), "-I", sysconfig.get_paths()["include"],
                "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
@@ -54,12 +64,12 @@ def build_marshal(force: bool = False) -> str:
         res = subprocess.run(cmd, capture_output=True, text=True)
         if res.returncode != 0:
             raise RuntimeError("g++ failed:\n%s\n%s" % (res.stdout, res.stderr))
-        os.replace(tmp, MARSHAL)
-    return MARSHAL
+        os.replace(tmp, path)
+    return path
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libchiron_kv.so (and _marshal.so) if missing or older than their sources; return its path."""
+    """Build libchiron_kv.so (and the extension module) if missing or older than their sources; return its path."""
     if force or is_stale():
         tmp = LIBRARY + ".tmp.%d" % os.getpid()
         cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + SOURCES
