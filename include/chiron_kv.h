@@ -234,12 +234,18 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *                     thread blocks owns a (request, KV head): ckv_set_partition and the span timeline
  *                     do not apply, and results are bit-identical from run to run.
  *   decode_attention_sparse  both.
+ *   ckv_set_select_scratch   the memory for a selection's scores, batch * Hkv * max_pages_per_req (rounded up to
+ *                     4) * 4 bytes, 16-byte aligned; kv_select_bytes() is enough for every batch of the
+ *                     configuration (0 if it is invalid).  It stays the caller's, needs no clearing, and is
+ *                     kept until another is set (NULL: none); selections in flight must be done by then.
+ *                     decode_attention_sparse needs none for few short tables (128 (request, KV head) pairs,
+ *                     256 pages beyond the first and last ones), nor does a budget that holds every page.
  * 1 <= recent, 0 <= sink, sink + recent <= budget.  For selection max_pages_per_req <= 49152 and
- * batch * Hkv * max_pages_per_req (rounded up to 4) <= 2^26.  Scores live in the handle's workspace: as
+ * batch * Hkv * max_pages_per_req (rounded up to 4) <= 2^26.  The scratch belongs to the handle: as
  * with every attention call, two calls on one handle must not overlap on the GPU.  All inputs may
  * come from the kernel that directly precedes the call.  The other appends and kv_swap_in do not
  * touch an index: update it after them.
- * Errors: CKV_EINVAL, CKV_ENOMEM (index too small, too many scores), CKV_ECUDA.
+ * Errors: CKV_EINVAL, CKV_ENOMEM (index or scratch too small, too many scores), CKV_ECUDA.
  */
 size_t kv_index_bytes(const ckv_config *cfg);
 int32_t kv_index_update(ckv_pool *pool, int32_t layer, int32_t batch, const int32_t *d_block_tables,
@@ -247,6 +253,8 @@ int32_t kv_index_update(ckv_pool *pool, int32_t layer, int32_t batch, const int3
                         size_t index_bytes, void *stream);
 int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size_t index_bytes,
                         void *d_out, void *stream);
+size_t kv_select_bytes(const ckv_config *cfg);
+int32_t ckv_set_select_scratch(ckv_pool *pool, void *d_scratch, size_t scratch_bytes);
 int32_t decode_select_pages(ckv_pool *pool, int32_t layer, int32_t batch,
                             const int32_t *d_block_tables, const int32_t *d_seq_lens, const void *d_q,
                             const void *d_index, size_t index_bytes, int32_t budget, int32_t sink,

@@ -33,7 +33,7 @@ EXPORTS = (
     "ckv_launch_count", "ckv_last_error", "ckv_read_span_trace", "ckv_set_overlap",
     "decode_attention_noalloc", "decode_step", "kv_swap_out", "kv_swap_in",
     "kv_append_multi", "decode_attention_multi", "kv_read_probe", "ckv_wait_limit_selftest", "ckv_set_host_route",
-    "kv_append_rope", "kv_index_bytes", "kv_index_update", "kv_index_values", "decode_select_pages",
+    "kv_append_rope", "kv_index_bytes", "kv_index_update", "kv_index_values", "kv_select_bytes", "ckv_set_select_scratch", "decode_select_pages",
     "decode_attention_pages", "decode_attention_sparse", "draft_verify",
     "local_autoscaler_instance_slo", "local_autoscaler_create", "local_autoscaler_destroy",
     "local_autoscaler_update", "local_autoscaler_get", "local_autoscaler_simulate",
@@ -110,6 +110,8 @@ def _load() -> ctypes.CDLL:
     lib.kv_index_bytes.restype = sz; lib.kv_index_bytes.argtypes = [cfgp]
     lib.kv_index_update.restype = i32; lib.kv_index_update.argtypes = [vp, i32, i32, vp, vp, i32, vp, sz, vp]
     lib.kv_index_values.restype = i32; lib.kv_index_values.argtypes = [vp, i32, vp, sz, vp, vp]
+    lib.kv_select_bytes.restype = sz; lib.kv_select_bytes.argtypes = [cfgp]
+    lib.ckv_set_select_scratch.restype = i32; lib.ckv_set_select_scratch.argtypes = [vp, vp, sz]
     lib.decode_select_pages.restype = i32
     lib.decode_select_pages.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, i32, i32, vp, vp, vp]
     lib.decode_attention_pages.restype = i32; lib.decode_attention_pages.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
@@ -224,6 +226,10 @@ def kv_index_bytes(cfg: Config) -> int:
     return int(lib.kv_index_bytes(ctypes.byref(cfg)))
 
 
+def kv_select_bytes(cfg: Config) -> int:
+    return int(lib.kv_select_bytes(ctypes.byref(cfg)))
+
+
 # _on(device, tensor, dtype, what, *shape): the address of a contiguous tensor of this type and shape there;
 # _rows_on(device, tensor, what, tokens, heads, d): (address, stride between tokens) of bf16 rows whose tokens may lie
 # apart.  Anything else is a ValueError that says what was expected and what came.
@@ -241,7 +247,9 @@ class KvPool:
     """A paged bf16 KV cache in caller-owned device memory plus the library's scratch.
 
     `pool` (bf16, kv_pool_bytes) and `workspace` (uint8, kv_workspace_bytes) may be passed in;
-    otherwise they are allocated with torch on `device`.  The tensors are kept alive here.
+    otherwise they are allocated with torch on `device`.  The tensors are kept alive here.  The
+    memory for a page selection's scores (kv_select_bytes) is allocated by make_index, or by the
+    first selection.
     """
 
     def __init__(self, cfg: Config, device="cuda:0", pool: Optional[torch.Tensor] = None,
@@ -259,6 +267,7 @@ class KvPool:
         self._h = ctypes.c_void_p()
         index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._index, self._index_bytes = index, kv_index_bytes(cfg)
+        self._scores: Optional[torch.Tensor] = None
         _check(lib.kv_pool_create(ctypes.byref(cfg), _dev_ptr(pool), pool.numel() * pool.element_size(),
                                   _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
                                   index, ctypes.byref(self._h)))
@@ -367,7 +376,15 @@ class KvPool:
 
     def make_index(self) -> torch.Tensor:
         """An empty index of the pool's keys (uint8, kv_index_bytes), for kv_index_update and the sparse calls."""
+        self._hold_scores()
         return torch.zeros(kv_index_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+
+    def _hold_scores(self, stream: Optional[torch.cuda.Stream] = None) -> None:
+        if self._scores is None:
+            with torch.cuda.stream(stream):      # memory that work queued elsewhere still uses must not be handed out
+                scores = torch.empty(kv_select_bytes(self.cfg), dtype=torch.uint8, device=self.device)
+            _check(lib.ckv_set_select_scratch(self._h, scores.data_ptr(), scores.numel()))
+            self._scores = scores
 
     def _index_on(self, index) -> int:
         return _on(self._index, index, torch.uint8, "index", self._index_bytes)
@@ -385,8 +402,10 @@ class KvPool:
                                    _on(self._index, out, torch.bfloat16, "out", c.num_pages, c.num_kv_heads, 2, c.head_dim),
                                    _stream_ptr(stream, self._index)))
 
-    def _select_args(self, block_tables, seq_lens, q, index, pages, lens):
+    def _select_args(self, block_tables, seq_lens, q, index, pages, lens, stream):
         c, dev = self.cfg, self._index
+        if self._scores is None:
+            self._hold_scores(stream)
         batch, budget = self._tables_of(block_tables, seq_lens), int(pages.shape[-1])
         return batch, budget, (block_tables.data_ptr(), seq_lens.data_ptr(),
                                _on(dev, q, torch.bfloat16, "q", batch, c.num_q_heads, c.head_dim),
@@ -396,7 +415,7 @@ class KvPool:
     def decode_select_pages(self, layer: int, block_tables, seq_lens, q, index, pages, lens, *, sink: int = 1, recent: int = 2,
                             stream=None) -> None:
         """Choose pages.shape[2] pages per (request, kv head) for the new queries; writes pages and lens."""
-        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
+        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens, stream)
         _check(_marshal.decode_select_pages(self._h.value, layer, batch, *ins, budget, sink, recent, *outs, _stream_ptr(stream, self._index)))
 
     def decode_attention_pages(self, layer: int, pages, lens, q, out, stream=None) -> None:
@@ -414,7 +433,7 @@ class KvPool:
                                 recent: int = 2, stream=None) -> None:
         """decode_select_pages, then decode_attention_pages over what it chose."""
         c = self.cfg
-        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens)
+        batch, budget, ins, outs = self._select_args(block_tables, seq_lens, q, index, pages, lens, stream)
         _check(_marshal.decode_attention_sparse(self._h.value, layer, batch, *ins, budget, sink, recent, *outs,
                                            _on(self._index, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
                                            _stream_ptr(stream, self._index)))

@@ -83,7 +83,6 @@ WorkspaceLayout carve(const ckv_config &c)
     w.st_k = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_v = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_out = take((size_t)c.max_batch * c.num_q_heads * d2);
-    w.sel_keys = take(sizeof(uint32_t) * (size_t)std::min((long long)c.max_batch * c.num_kv_heads * ckv::key_stride(c), ckv::kMaxSelectKeys));
     w.total = at;
     return w;
 }
@@ -318,6 +317,8 @@ int32_t kv_pool_create(const ckv_config *cfg, void *d_pool, size_t pool_bytes, v
     p->pool_written = false;
     p->inputs_from_predecessor = false;
     p->host_route = CKV_HOST_ROUTE_AUTO;
+    p->d_scores = nullptr;
+    p->score_room = 0;
     p->ev_used = 0;
 
     if (int32_t rc = encode_pool_map(cfg, d_pool, &p->tmap, "kv_pool_create")) {

@@ -31,7 +31,7 @@ inline int32_t fail(int32_t code, const char *fmt, ...)
                         __FILE__, __LINE__);                                                  \
     } while (0)
 
-// Scores that one selection may hold in the workspace: every page of every table, up to this many.
+// Scores that one selection may hold: every page of every table, up to this many.
 constexpr long long kMaxSelectKeys = 64ll << 20;
 
 // Scores of a (request, kv head), the number rounded up for 16-byte loads.
@@ -40,7 +40,6 @@ inline int32_t key_stride(const ckv_config &c) { return (c.max_pages_per_req + 3
 struct WorkspaceLayout {
     size_t status, header, span_start, part, arrivals, trace;
     size_t st_tables, st_lens, st_q, st_k, st_v, st_out;
-    size_t sel_keys;
     size_t total;
 };
 
@@ -61,6 +60,8 @@ struct ckv_pool {
     bool pool_written;               // a kernel other than the fused step wrote the pool since the last attention launch
     bool inputs_from_predecessor;    // the next attention launch reads tables and lengths its predecessor in the stream writes
     int host_route;                  // decode_step_host: CKV_HOST_ROUTE_*
+    uint32_t *d_scores;              // ckv_set_select_scratch: room for `score_room` scores of a page selection
+    long long score_room;
     std::vector<cudaEvent_t> ev;     // pairs (start, stop)
     int ev_used;
 

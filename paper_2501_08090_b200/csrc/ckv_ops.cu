@@ -194,13 +194,16 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
     sp.key_stride = ckv::key_stride(c);
     const long long keys = (long long)batch * c.num_kv_heads * sp.key_stride;
     if (keys > ckv::kMaxSelectKeys)
-        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need room for %lld scores, the workspace holds %lld", fn, batch,
+        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need %lld scores, a selection holds %lld", fn, batch,
                     c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
-    sp.keys = pool->wsp<uint32_t>(pool->ws.sel_keys);
     const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
     // 5 requests of up to 187 pages: 7.8 us in one launch, 8.1 in two, and a launch is 2.4 us of the caller's time
     *selected = !(attend && cand <= kListSelectPages && (long long)batch * c.num_kv_heads <= kListSelectPairs && budget <= kMaxListInKernel);
     if (!*selected) return CKV_OK;
+    if (cand > 0 && keys > pool->score_room)
+        return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need room for %lld scores, the scratch (ckv_set_select_scratch) holds %lld",
+                    fn, batch, c.max_pages_per_req, keys, pool->score_room);
+    sp.keys = pool->d_scores;
     return c.head_dim == 128 ? launch_select<128>(pool, sp, cand, stream) : launch_select<64>(pool, sp, cand, stream);
 }
 
@@ -337,6 +340,22 @@ int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size
     CKV_CUDA(c.head_dim == 128 ? enqueue(ckv::kv_index_values_kernel<128>, vp, blocks, 256, 0, pool->overlap, 0, stream)
                                : enqueue(ckv::kv_index_values_kernel<64>, vp, blocks, 256, 0, pool->overlap, 0, stream));
     pool->launches += 1;
+    return CKV_OK;
+}
+
+size_t kv_select_bytes(const ckv_config *cfg)
+{
+    if (kv_pool_bytes(cfg) == 0) return 0;       // says why the configuration is invalid
+    return sizeof(uint32_t) * (size_t)std::min((long long)cfg->max_batch * cfg->num_kv_heads * ckv::key_stride(*cfg), ckv::kMaxSelectKeys);
+}
+
+int32_t ckv_set_select_scratch(ckv_pool *pool, void *d_scratch, size_t scratch_bytes)
+{
+    const char *fn = "ckv_set_select_scratch";
+    if (int32_t rc = check_device(pool, fn)) return rc;
+    if (!aligned16(d_scratch)) return fail(CKV_EINVAL, "%s: scratch not 16-byte aligned", fn);
+    pool->d_scores = static_cast<uint32_t *>(d_scratch);
+    pool->score_room = d_scratch ? (long long)(scratch_bytes / sizeof(uint32_t)) : 0;
     return CKV_OK;
 }
 
