@@ -228,6 +228,7 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *                     and NaN in q count as 0 here.  Requests of at most `budget` pages keep all.
  *                       d_pages  int32 [batch][Hkv][budget]: page ids in context order, then -1s
  *                       d_lens   int32 [batch]: tokens in the chosen pages (0 for an unusable length)
+ *                     Neither may overlap d_block_tables or d_seq_lens, nor the other.
  *   decode_attention_pages   attention as decode_attention's over such lists: d_pages and d_lens take the
  *                     places of block tables and lengths, with a row of `budget` pages per (request,
  *                     KV head).  It may directly follow the kernel that writes them.  A cluster of
@@ -289,6 +290,7 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch,
  *   d_u_accept       fp32 [batch][max_draft];  d_u_sample fp32 [batch]
  *   d_tokens         int32 [batch][max_draft + 1]: the accepted drafts, the drawn token, then -1s
  *   d_accepted       int32 [batch]: number of accepted drafts
+ * d_tokens and d_accepted overlap neither the inputs nor one another.
  * Rows are read where they decide something, in aligned pieces of 16 bytes: up to 15 bytes beside a row
  * may be read with it, and are not used.
  * Errors: CKV_EINVAL, CKV_ECUDA.

@@ -106,6 +106,13 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
                       int32_t budget, int32_t sink, int32_t recent, int32_t *d_pages, int32_t *d_lens, bool attend,
                       SelectParams *out_params, bool *selected, void *stream);
 
+// Whether two arrays of 32-bit entries share memory (NULL: no).
+inline bool overlap(const void *a, long long na, const void *b, long long nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x && y && x < y + (uintptr_t)nb * 4 && y < x + (uintptr_t)na * 4;
+}
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace ckv

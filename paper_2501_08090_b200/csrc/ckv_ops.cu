@@ -14,6 +14,7 @@ using ckv::aligned16;
 using ckv::check_call;
 using ckv::check_device;
 using ckv::fail;
+using ckv::overlap;
 
 namespace {
 
@@ -173,6 +174,11 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
     if (c.max_pages_per_req > kMaxSelectPages)
         return fail(CKV_EINVAL, "%s: selection holds at most %d pages of a request, the tables have %d", fn, kMaxSelectPages, c.max_pages_per_req);
     if (int32_t rc = check_index(pool, fn, d_index, index_bytes)) return rc;
+    // blocks of one request write its results while others still read its length and pages
+    const long long tables_n = (long long)batch * c.max_pages_per_req, pages_n = (long long)batch * c.num_kv_heads * budget;
+    if (overlap(d_pages, pages_n, d_block_tables, tables_n) || overlap(d_pages, pages_n, d_seq_lens, batch) ||
+        overlap(d_lens, batch, d_block_tables, tables_n) || overlap(d_lens, batch, d_seq_lens, batch) || overlap(d_pages, pages_n, d_lens, batch))
+        return fail(CKV_EINVAL, "%s: pages and lens must not overlap the tables, the lengths or one another", fn);
     SelectParams &sp = *out_params;
     sp = SelectParams{};
     sp.records = layer_records(pool, d_index, layer);
@@ -384,6 +390,13 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
     const uintptr_t size = dtype == CKV_PROBS_F32 ? 4 : 2;
     const uintptr_t at = reinterpret_cast<uintptr_t>(d_target_probs) | reinterpret_cast<uintptr_t>(d_draft_probs);
     if (at % size != 0) return fail(CKV_EINVAL, "%s: probabilities not aligned to their type", fn);
+    // blocks of one request write its results while others still read its drafts
+    const long long drafts_n = (long long)batch * max_draft, tokens_n = drafts_n + batch;
+    if (overlap(d_tokens, tokens_n, d_draft_tokens, drafts_n) || overlap(d_tokens, tokens_n, d_draft_lens, batch) ||
+        overlap(d_accepted, batch, d_draft_tokens, drafts_n) || overlap(d_accepted, batch, d_draft_lens, batch) ||
+        overlap(d_tokens, tokens_n, d_u_sample, batch) || overlap(d_accepted, batch, d_u_sample, batch) ||
+        overlap(d_tokens, tokens_n, d_u_accept, drafts_n) || overlap(d_accepted, batch, d_u_accept, drafts_n) || overlap(d_tokens, tokens_n, d_accepted, batch))
+        return fail(CKV_EINVAL, "%s: tokens and accepted must not overlap the drafts, their lengths, the random numbers or one another", fn);
     ckv::VerifyParams vp{};
     vp.draft_tokens = d_draft_tokens;
     vp.draft_lens = d_draft_lens;
