@@ -278,7 +278,8 @@ int32_t decode_attention_sparse(ckv_pool *pool, int32_t layer, int32_t batch,
  *   at the first refusal j the next token is drawn from the weights max(p_j - q_j, 0) (from p_j where
  *   they are all 0); after n acceptances it is drawn from p_n;
  *   drawn: the first token whose running sum of weights exceeds u_sample * (sum of the weights).
- * Products are formed in fp64, differences and sums to 48 bits or more.  A NaN weight counts as 0; a
+ * Products are formed in fp64, differences to 48 bits, sums to 38 bits or more (vocabularies
+ * of up to 2^18 tokens; draws are fp32, 24 bits).  A NaN weight counts as 0; a
  * row without any weight, or with an infinite one, gives token -1.  A drafted token outside the
  * vocabulary is refused.  Runs on the current device and needs no pool.
  *   dtype            CKV_PROBS_F32 or CKV_PROBS_BF16, of both probability arrays

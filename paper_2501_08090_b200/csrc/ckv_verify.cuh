@@ -13,9 +13,11 @@ namespace ckv {
 // whose running sum of weights exceeds u * (sum of all weights).  Without draft rows q_j is a point
 // mass at x_j.  If the differences leave nothing (p_j <= q_j everywhere), the weights are p_j.
 //
-// Products are formed in 64 bits, differences and sums to 48 bits or more (fp32 pairs whose rounding
-// errors are kept, added up in fp64): over 10^5 tokens a sum in 32 bits moves the borders between
-// tokens by more than many tokens' probability.
+// Products are formed in 64 bits; weights are summed in pairs of fp32 whose rounding errors are kept, the
+// pairs in fp64, their errors and the lower parts of differences in fp32: over 10^5 tokens a sum in 32 bits moves
+// the borders between tokens by more than many tokens' probability.  Each error is at most 2^-24 of its
+// pair, so a chain's sum of them is at most 2^-23 of its weights and each of its additions is off by 2^-24 of that.
+// With one CTA a row a chain has V / 512 additions: 2^-38 of the sum at V = 2^18, 2^-41 in clusters of 8.
 //
 // Bound by reading the one or two rows that decide (4 V bytes each in fp32).  A cluster works on a
 // request; every warp owns a contiguous segment of the vocabulary and adds up its weights, the
@@ -84,7 +86,7 @@ struct ProbVec {
     }
 };
 
-// A sum of weights: fp64, and the rounding errors of the fp32 sums that went into it.
+// A sum of weights: fp64, and in fp32 the rounding errors of the fp32 sums that went into it.
 struct WeightSum {
     double hi = 0.0;
     float lo = 0.f;
