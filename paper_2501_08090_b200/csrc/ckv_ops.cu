@@ -104,27 +104,34 @@ int32_t launch_index_update(ckv_pool *pool, const ckv::IndexParams &ip, unsigned
     return CKV_OK;
 }
 
-template <typename T>
-int32_t launch_verify(const ckv::VerifyParams &vp, unsigned cluster, void *stream)
-{
-    static thread_local int configured_device = -1;
-    auto kernel = ckv::draft_verify_kernel<T>;
-    int device = -1;
-    CKV_CUDA(cudaGetDevice(&device));
-    if (configured_device != device) {
-        CKV_CUDA(allow(kernel, true, 0));
-        configured_device = device;
-    }
-    CKV_CUDA(enqueue(kernel, vp, (unsigned)vp.batch * cluster, ckv::kVerifyThreads, 0, true, cluster, stream));
-    return CKV_OK;
-}
-
 // The smallest power of two that is at least x, within [1, 16].
 unsigned cluster_of(long long x)
 {
     unsigned c = 1;
     while (c < 16 && c < x) c *= 2;
     return c;
+}
+
+// CTAs of a request: enough to fill the GPU (four CTAs an SM), of 2048 tokens or, the number being rounded up to
+// a power of two, at least half as many.  256 requests of 128256 tokens: 2 CTAs 42 us, 4 CTAs 36, 8 CTAs 42;
+// clusters of 16 start slowly (64 requests of 50257 tokens: 20 us against 10 with 8) and pay only for a few
+// requests (one of 128256: 6.2 us against 8.0).
+template <typename T>
+int32_t launch_verify(const ckv::VerifyParams &vp, void *stream)
+{
+    static thread_local int configured_device = -1, num_sms = 0;
+    auto kernel = ckv::draft_verify_kernel<T>;
+    int device = -1;
+    CKV_CUDA(cudaGetDevice(&device));
+    if (configured_device != device) {
+        CKV_CUDA(allow(kernel, true, 0));
+        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
+        configured_device = device;
+    }
+    const long long fill = (4ll * num_sms + vp.batch - 1) / vp.batch;
+    const unsigned cluster = cluster_of(std::min<long long>(std::min<long long>(fill, vp.vocab / 2048), vp.batch <= 8 ? 16 : 8));
+    CKV_CUDA(enqueue(kernel, vp, (unsigned)vp.batch * cluster, ckv::kVerifyThreads, 0, true, cluster, stream));
+    return CKV_OK;
 }
 
 int32_t check_index(const ckv_pool *pool, const char *fn, const void *d_index, size_t index_bytes)
@@ -411,13 +418,7 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
     vp.batch = batch;
     vp.max_draft = max_draft;
     vp.vocab = vocab;
-    // CTAs of a request: enough to fill the GPU (four CTAs an SM), each with at least 2048 tokens.  256
-    // requests of 128256 tokens: 2 CTAs 42 us, 4 CTAs 36, 8 CTAs 42; clusters of 16 start slowly (64 requests
-    // of 50257 tokens: 20 us against 10 with 8) and pay only for a few requests (one of 128256: 6.2 us
-    // against 8.0).
-    const long long fill = (4ll * 148 + batch - 1) / batch;
-    const unsigned cluster = cluster_of(std::min<long long>(std::min<long long>(fill, vocab / 2048), batch <= 8 ? 16 : 8));
-    return dtype == CKV_PROBS_F32 ? launch_verify<float>(vp, cluster, stream) : launch_verify<__nv_bfloat16>(vp, cluster, stream);
+    return dtype == CKV_PROBS_F32 ? launch_verify<float>(vp, stream) : launch_verify<__nv_bfloat16>(vp, stream);
 }
 
 }  // extern "C"
