@@ -26,7 +26,8 @@
  *  - seq_lens[r] is the context length AFTER this iteration's append: attention of request r
  *    covers tokens 0 .. seq_lens[r]-1 and the appended token has position seq_lens[r]-1.
  *  - Query head h uses KV head h / (num_q_heads / num_kv_heads).  Softmax scale is
- *    1/sqrt(head_dim).
+ *    1/sqrt(head_dim).  A score of minus infinity (a key with an infinity) weighs 0; a row whose
+ *    scores are all minus infinity, or hold a NaN or plus infinity, is NaN.
  *  - Invalid device-side data (a length < 1 or beyond the table, a page id outside the pool) is
  *    never followed: the access is skipped or redirected to page 0, a bit is set in a device
  *    status word, and kv_check_status() reports it.  Output rows of a request with an invalid
@@ -200,7 +201,7 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  * Page-sparse decode attention: for long contexts, each (request, KV head) attends to the `budget`
  * pages whose keys can matter most to its new token, instead of to all of them; the iteration's time then stops
  * growing with the context (the "self-attention computation" of Section 2.3).  It reads an index of the
- * cache that is 1/30 of its size, and `budget` pages.
+ * cache that is 1/31 of its size, and `budget` pages.
  *
  * The index (caller-owned, kv_index_bytes(), 16-byte aligned) holds for every (layer, page, KV head)
  * lower and upper bounds of the page's keys, channel by channel, as 8-bit whole numbers of steps of a
@@ -215,8 +216,9 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
  *                     appended count, or at least before a page leaves the `recent` ones: those
  *                     are attended to without being looked up.  A page that requests share must be full
  *                     in all of them.  Unusable lengths and page ids: status bit, skipped.
- *   kv_index_values   the bounds of a layer as numbers (lo * step, hi * step, exact): bf16
- *                     [num_pages][Hkv][2][head_dim], 16-byte aligned.
+ *   kv_index_values   the bounds of a layer as numbers (lo * step, hi * step, exact; 2^128, which keys beside
+ *                     bf16's largest round up to, comes as an infinity): bf16 [num_pages][Hkv][2][head_dim],
+ *                     16-byte aligned.
  *   decode_select_pages   chooses pages for the batch's new queries (d_q bf16 [batch][Hq][head_dim],
  *                     16-byte aligned).  A request of n > budget pages keeps its first `sink` and last
  *                     `recent` pages and, of the others, the budget - sink - recent with the highest scores,
@@ -358,8 +360,8 @@ int32_t ckv_get_partition(const ckv_pool *pool);
  *     step must have grown by at most one token since (the same lengths replayed, as a benchmark
  *     does, are fine too); an engine that rewrites older positions in place calls kv_append or
  *     turns overlap off.
- * The library's other writers are taken care of: after kv_append, kv_append_multi or kv_swap_in
- * on this handle the next decode_step keeps all its loads behind the wait.
+ * The library's other writers are taken care of: after kv_append, kv_append_multi, kv_append_rope or
+ * kv_swap_in on this handle the next decode_step keeps all its loads behind the wait.
  * Turning overlap off restores plain stream order.  Errors: CKV_EINVAL. */
 int32_t ckv_set_overlap(ckv_pool *pool, int32_t enable);
 

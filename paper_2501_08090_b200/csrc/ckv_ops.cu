@@ -210,7 +210,7 @@ int32_t select_launch(ckv_pool *pool, const char *fn, int32_t layer, int32_t bat
         return fail(CKV_ENOMEM, "%s: %d requests of up to %d pages need %lld scores, a selection holds %lld", fn, batch,
                     c.max_pages_per_req, keys, ckv::kMaxSelectKeys);
     const int cand = c.max_pages_per_req > budget && budget > sink + recent ? c.max_pages_per_req - sink - recent : 0;
-    // 5 requests of up to 187 pages: 7.8 us in one launch, 8.1 in two, and a launch is 2.4 us of the caller's time
+    // one launch where tables are short and pairs few (measured at page_list_attn_kernel)
     *selected = !(attend && cand <= kListSelectPages && (long long)batch * c.num_kv_heads <= kListSelectPairs && budget <= kMaxListInKernel);
     if (!*selected) return CKV_OK;
     if (cand > 0 && keys > pool->score_room)

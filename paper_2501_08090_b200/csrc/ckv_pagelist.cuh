@@ -18,6 +18,11 @@ namespace ckv {
 //
 //   M = max m_i,  out = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i   over warps, then over CTAs.
 //
+// Weights are rounded to bf16 for P V, as in paged_decode_attn_kernel (the matrix instruction takes one type, and V is
+// bf16), and summed unrounded in fp32: 2^-8 of each weight at most, which averages out over the tokens.  Against 64 bits
+// the outputs are off by 1.9e-3 of their size (root of squares) where fp32 weights leave 1.7e-3, the output's own
+// rounding.
+//
 // Bound by HBM where the pairs fill the GPU (512 pairs of 128 pages 80.8 us against 87 in even spans; 768
 // of 33 pages 37.8 against 44), by latency where they do not (5 pairs of 24 pages 3.8 us against 8.8).
 // Six warps and two CTAs an SM: 296 CTAs at a time.  Of the same 12 warps an SM, 4 x 3 leave 512 pairs a second
@@ -71,8 +76,11 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
 
 // kSelect: the lists are not there yet.  Every CTA of a cluster scores and selects its pair's pages for
 // itself (few short tables: kListSelectPages), and the first one writes the list out: one launch in
-// place of three.  (Selecting here behind score_pages_kernel, for any table, was slower than
-// select_pages_kernel: 768 pairs 73 us in all against 70, since two CTAs an SM select while nothing is loaded.)
+// place of three.  One launch against three, device time: 8 pairs of 64 pages, 24 kept, 8.1 us against 10.7; 8 of 256
+// pages 9.9 against 10.9; 128 of 64 pages 11.9 against 16.8; 128 of 256 pages 14.1 against 17.4, with 128 kept 30.8
+// against 33.6 (head_dim 128); 5 of 256 pages 8.4 against 9.6 (64).  A launch is 2.4 us of the caller's time besides.
+// (Selecting here behind score_pages_kernel, for any table, was slower than select_pages_kernel: 768 pairs 73 us in
+// all against 70, since two CTAs an SM select while nothing is loaded.)
 constexpr int kListSelectKeys = 4;               // a thread
 constexpr int kListSelectPages = 256, kListSelectPairs = 128;
 template <int D, bool kSelect>
