@@ -12,7 +12,6 @@
 
 using ckv::aligned16;
 using ckv::check_call;
-using ckv::check_device;
 using ckv::fail;
 using ckv::overlap;
 
@@ -365,7 +364,7 @@ size_t kv_select_bytes(const ckv_config *cfg)
 int32_t ckv_set_select_scratch(ckv_pool *pool, void *d_scratch, size_t scratch_bytes)
 {
     const char *fn = "ckv_set_select_scratch";
-    if (int32_t rc = check_device(pool, fn)) return rc;
+    if (!pool) return fail(CKV_EINVAL, "%s: pool is NULL", fn);
     if (!aligned16(d_scratch)) return fail(CKV_EINVAL, "%s: scratch not 16-byte aligned", fn);
     pool->d_scores = static_cast<uint32_t *>(d_scratch);
     pool->score_room = d_scratch ? (long long)(scratch_bytes / sizeof(uint32_t)) : 0;
