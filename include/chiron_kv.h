@@ -307,6 +307,130 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
                      int32_t *d_tokens, int32_t *d_accepted, void *stream);
 
 /*
+ * A cache in 8 bits: half the bytes of the bf16 cache, so that an instance holds twice the tokens and reads
+ * half as much per token (what bounds its batch size and its inter-token latency, Section 2.3).
+ *
+ * The cache is  int8 records[layers][pages][Hkv][2 (K, V)][16][head_dim], then  float steps[layers][pages][Hkv][2],
+ * kv8_pool_bytes() in all.  A block -- one page's keys, or values, of one KV head -- shares a step, a power of two,
+ * and an element is record * step, exact in bf16.  Rows x that a call appends to a page, beginning at slot a:
+ *   m = max |x| of the block's new rows;  need = 2^(floor(log2 max(m, 2^-100)) - 6)
+ *   a = 0: step = need;  a > 0: step = max(the block's step, need), and where it grew the records of slots 0 .. a-1 are
+ *   multiplied by old / new step and rounded;  record = x / step, rounded, cut to -127 .. 127
+ * (nearest, ties to even).  So |record * step - x| <= step / 2 and m / 128 < step <= m / 64, and a block's bits depend on
+ * its rows and on which calls appended them, not on the launch.  An infinity or a NaN among the rows makes the
+ * block's step NaN, and with it every value of the block, until slot 0 of its page is written again.
+ *
+ *   kv8_pool_create   a handle like kv_pool_create's, over d_cache (256-byte aligned, kv8_pool_bytes()) and a workspace of
+ *                     kv_workspace_bytes().  It is destroyed, checked (kv_check_status), and set (ckv_set_overlap) as any
+ *                     handle; the calls below, and kv_pages_*, take it.  Calls on a bf16 cache refuse it, and
+ *                     kv8_* calls refuse a bf16 handle: CKV_EINVAL.
+ *   kv8_append        kv_append_rope into the 8-bit cache: the same arguments and rules; keys are rounded to bf16 after the
+ *                     rotation, then quantised.  d_inv_freq NULL: nothing is rotated, d_q and d_q_out are NULL too.
+ *   kv8_gather        the values of each request's last tokens, row by row as kv8_append takes them:
+ *                     d_start int32 [batch + 1], request r's rows start[r] .. start[r+1] - 1 (NULL: n_tokens / batch
+ *                     each) receive its tokens at positions seq_lens[r] - n_r .. seq_lens[r] - 1.  d_k, d_v: bf16 rows
+ *                     [n_tokens][Hkv][head_dim], 16-byte aligned, each with its own stride.  Rows of a request of
+ *                     unusable length (status bit), or of a page id outside the pool (status bit), are zero-filled; other
+ *                     rows are left as they were.
+ *   kv8_attention     decode_attention_multi over the 8-bit cache; window and sink as below, window 0: the whole context.
+ *                     Scores and weights see the values exactly; queries are rounded to 11 bits below their
+ *                     largest element's 2^-22, weights to 11 bits for the product with V.
+ * Errors: CKV_EINVAL, CKV_ENOMEM, CKV_ECUDA.
+ */
+size_t kv8_pool_bytes(const ckv_config *cfg);
+int32_t kv8_pool_create(const ckv_config *cfg, void *d_cache, size_t cache_bytes, void *d_workspace,
+                        size_t workspace_bytes, int32_t device, ckv_pool **out_pool);
+int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens, const int32_t *d_block_tables,
+                   const int32_t *d_seq_lens, const int32_t *d_new_start, const float *d_inv_freq, int32_t rotary_dim,
+                   int32_t interleaved, float scale, const void *d_q, int64_t q_stride, const void *d_k_new,
+                   int64_t k_stride, const void *d_v_new, int64_t v_stride, void *d_q_out, int64_t q_out_stride,
+                   void *stream);
+int32_t kv8_gather(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens, const int32_t *d_block_tables,
+                   const int32_t *d_seq_lens, const int32_t *d_start, void *d_k, int64_t k_stride, void *d_v,
+                   int64_t v_stride, void *stream);
+int32_t kv8_attention(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables,
+                      const int32_t *d_seq_lens, const void *d_q, void *d_out, int32_t window, int32_t sink,
+                      void *stream);
+
+/*
+ * Attention with a sliding window and a few first tokens that stay visible: of models trained so, and of long
+ * generations that keep their cost per token constant.  As decode_attention_multi, but new token i of request r,
+ * at position p = seq_lens[r] - q_len + i, sees token t <= p only if t > p - window or t < sink.  Pages in which
+ * no new token of a launch sees anything are not read, and their table entries neither.
+ *   d_q, d_out   bf16 [batch][q_len][num_q_heads][head_dim], 16-byte aligned; 1 <= q_len <= 8; window >= 1, sink >= 0
+ * What a token does not see does not reach it, infinities and NaN among it.  Several launches where
+ * q_len * (num_q_heads / num_kv_heads) > 8, as there.  All inputs may come from the kernel that directly
+ * precedes the call.  ckv_set_partition, ckv_profile_* and the span timeline do not apply.  The workspace belongs to
+ * the handle: as with every attention call, two calls on one handle must not overlap on the GPU.
+ * Results are bit-identical from run to run.  Errors: CKV_EINVAL, CKV_ECUDA.
+ */
+int32_t decode_attention_window(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables,
+                                const int32_t *d_seq_lens, const void *d_q, void *d_out, int32_t window, int32_t sink,
+                                void *stream);
+
+/*
+ * Block tables, lengths and slots from request lengths, on the GPU (Section 2.1 "PagedAttention": pages are allocated
+ * on demand), so that a decode loop needs no host between its steps and can be captured into a graph.  Free pages
+ * are a stack: d_free_pages int32 [num_pages], of which the first *d_free_count are free.
+ *
+ *   kv_pages_assign   request r grows by new_tokens[r] >= 0 tokens from seq_lens[r] >= 0 and takes
+ *                     ceil((L + n) / 16) - ceil(L / 16) pages.  It is served if it needs none, or if the needs of the
+ *                     requests up to and including it fit the free pages.  The k-th page taken, in the order of requests
+ *                     and of their contexts, is free_pages[count - 1 - k]; it is written to the request's row of d_block_tables.
+ *                       d_lens_out    int32 [batch]: L + n, or L where the request was not served
+ *                       d_count_out   int32 [1]: pages that stay free
+ *                       d_step_lens   int32 [batch]: L + n, or 0: the lengths for this step's calls, in which a request that was not
+ *                                     served counts as of unusable length: nothing appended, its rows zero-filled.  NULL: not wanted
+ *                       d_new_start   int32 [batch + 1]: sums of new_tokens, the list of kv_append_rope and kv8_append.  NULL: not wanted
+ *                       d_slots       int64 [n_slots]: for every new token page * 16 + slot, -1 where it was not served;
+ *                                     tokens from n_slots on are left out, entries behind the last token left as they were.  NULL (n_slots 0): not wanted
+ *   kv_pages_release  request r, of seq_lens[r] tokens, keeps its first keep_lens[r] (0: it has finished) and gives back
+ *                     ceil(L / 16) - ceil(keep / 16) pages; the k-th of all N goes to free_pages[count + N - 1 - k].  An
+ *                     assignment that is released again leaves the list as it was.  Table entries stay as they are.
+ *                     Pages that requests share must not be given back while another holds them.
+ * d_lens_out may be d_seq_lens (or the amounts), d_count_out may be d_free_count; otherwise arrays that are written overlap no other.
+ * Lengths and amounts that are negative or beyond the table: status bit, nothing moves for that request.  A count
+ * outside 0 .. num_pages is cut to it, a page id outside the pool becomes -1, and pages beyond num_pages are
+ * dropped: status bit.  On either kind of handle; a decode step on the same handle may follow directly.
+ * Errors: CKV_EINVAL, CKV_ECUDA.
+ */
+int32_t kv_pages_assign(ckv_pool *pool, int32_t batch, int32_t *d_block_tables, const int32_t *d_seq_lens,
+                        const int32_t *d_new_tokens, const int32_t *d_free_pages, const int32_t *d_free_count,
+                        int32_t *d_lens_out, int32_t *d_count_out, int32_t *d_step_lens, int32_t *d_new_start,
+                        int64_t *d_slots, int32_t n_slots, void *stream);
+int32_t kv_pages_release(ckv_pool *pool, int32_t batch, const int32_t *d_block_tables, const int32_t *d_seq_lens,
+                         const int32_t *d_keep_lens, int32_t *d_free_pages, const int32_t *d_free_count,
+                         int32_t *d_lens_out, int32_t *d_count_out, void *stream);
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on logits, and the probabilities that draft_verify
+ * reads.  Row j of a request stands after its first j drafted tokens.  With n_v the number of times that token v was
+ * generated (history[prompt_len .. history_len), and drafts 0 .. j-1), in fp32 and in this order:
+ *   v generated, or in the prompt (history[0 .. prompt_len)):  x = x > 0 ? x / repetition : x * repetition
+ *   x -= frequency * n_v;   n_v > 0: x -= presence;   x += bias[v];   the mask's bit v is 0: excluded
+ *   probs != 0:  p_v = exp((x_v - max x) / temperature) / sum;  temperature <= 0: 1 at the largest, the first of equals, else 0;
+ *                a row in which nothing is allowed, or minus infinity only, is 0 (draft_verify then gives token -1);
+ *                a NaN or plus infinity among what is allowed makes the row NaN
+ *   probs == 0:  x_v, minus infinity where excluded; the temperature is left to whoever forms probabilities
+ *   d_logits, d_out   [batch][rows] rows of `vocab` (1 .. 262128), their strides (>= vocab) apart, CKV_PROBS_F32 or CKV_PROBS_BF16 each;
+ *                     d_out may be d_logits (same type and stride), otherwise they do not overlap
+ *   d_params          fp32 [batch][4]: repetition, presence, frequency, temperature; NULL: 1, 0, 0, 1
+ *   d_history         int32 [batch] rows, history_stride apart, of history_lens[r] tokens (0 .. history_stride), the first
+ *                     prompt_lens[r] of them the prompt.  NULL: none.  Tokens outside the vocabulary (-1) count for nothing
+ *   d_drafts          int32 [batch][rows - 1]; NULL: none
+ *   d_bias_ids, d_bias   int32, fp32 [batch][n_bias]; ids outside the vocabulary (-1) are skipped, the last of equal ids counts
+ *   d_mask            bits, 32 to a word, lowest first, 1: allowed; [batch][rows] rows, mask_stride words apart; NULL: all allowed
+ * Logits are read in aligned pieces of 16 bytes: up to 15 bytes beside a row may be read with it, and are not used.
+ * Runs on the current device and needs no pool; results are bit-identical from run to run.
+ * Errors: CKV_EINVAL, CKV_ECUDA.
+ */
+int32_t logits_process(int32_t batch, int32_t rows, int32_t vocab, int32_t in_dtype, int32_t out_dtype, int32_t probs,
+                       const void *d_logits, int64_t logits_stride, const float *d_params, const int32_t *d_history,
+                       int64_t history_stride, const int32_t *d_prompt_lens, const int32_t *d_history_lens,
+                       const int32_t *d_drafts, const int32_t *d_bias_ids, const float *d_bias, int32_t n_bias,
+                       const uint32_t *d_mask, int64_t mask_stride, void *d_out, int64_t out_stride, void *stream);
+
+/*
  * The split-KV partition decode_attention uses for these lengths, copied to the host for
  * inspection (runs a small kernel and synchronises `stream`; decode_attention itself derives the
  * same partition inside its attention kernel and launches no plan kernel).  A "tile" is 32

@@ -35,6 +35,8 @@ EXPORTS = (
     "kv_append_multi", "decode_attention_multi", "kv_read_probe", "ckv_wait_limit_selftest", "ckv_set_host_route",
     "kv_append_rope", "kv_index_bytes", "kv_index_update", "kv_index_values", "kv_select_bytes", "ckv_set_select_scratch", "decode_select_pages",
     "decode_attention_pages", "decode_attention_sparse", "draft_verify",
+    "kv8_pool_bytes", "kv8_pool_create", "kv8_append", "kv8_gather", "kv8_attention", "decode_attention_window",
+    "kv_pages_assign", "kv_pages_release", "logits_process",
     "local_autoscaler_instance_slo", "local_autoscaler_create", "local_autoscaler_destroy",
     "local_autoscaler_update", "local_autoscaler_get", "local_autoscaler_simulate",
     "global_request_groups", "global_waiting_time", "global_batch_backpressure", "global_batch_autoscale",
@@ -119,6 +121,17 @@ def _load() -> ctypes.CDLL:
     lib.decode_attention_sparse.argtypes = [vp, i32, i32, vp, vp, vp, vp, sz, i32, i32, i32, vp, vp, vp, vp]
     lib.draft_verify.restype = i32
     lib.draft_verify.argtypes = [i32, i32, i32, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+    lib.kv8_pool_bytes.restype = sz; lib.kv8_pool_bytes.argtypes = [cfgp]
+    lib.kv8_pool_create.restype = i32
+    lib.kv8_pool_create.argtypes = [cfgp, vp, sz, vp, sz, i32, ctypes.POINTER(vp)]
+    lib.kv8_append.restype = i32; lib.kv8_append.argtypes = lib.kv_append_rope.argtypes
+    lib.kv8_gather.restype = i32; lib.kv8_gather.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
+    for fn in (lib.kv8_attention, lib.decode_attention_window):
+        fn.restype = i32; fn.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, i32, i32, vp]
+    lib.kv_pages_assign.restype = i32; lib.kv_pages_assign.argtypes = [vp, i32] + [vp] * 10 + [i32, vp]
+    lib.kv_pages_release.restype = i32; lib.kv_pages_release.argtypes = [vp, i32] + [vp] * 8
+    lib.logits_process.restype = i32
+    lib.logits_process.argtypes = [i32] * 6 + [vp, i64, vp, vp, i64, vp, vp, vp, vp, vp, i32, vp, i64, vp, i64, vp]
     lib.decode_plan.restype = i32; lib.decode_plan.argtypes = [vp, i32, vp, vp, vp, vp]
     lib.ckv_set_partition.restype = i32; lib.ckv_set_partition.argtypes = [vp, i32]
     lib.ckv_set_overlap.restype = i32; lib.ckv_set_overlap.argtypes = [vp, i32]
@@ -208,6 +221,10 @@ def kv_pool_bytes(cfg: Config) -> int:
     return int(lib.kv_pool_bytes(ctypes.byref(cfg)))
 
 
+def kv8_pool_bytes(cfg: Config) -> int:
+    return int(lib.kv8_pool_bytes(ctypes.byref(cfg)))
+
+
 def kv_workspace_bytes(cfg: Config) -> int:
     return int(lib.kv_workspace_bytes(ctypes.byref(cfg)))
 
@@ -252,15 +269,17 @@ class KvPool:
     first selection.
     """
 
+    _create, _cache_bytes, _cache_type = lib.kv_pool_create, staticmethod(kv_pool_bytes), torch.bfloat16
+
     def __init__(self, cfg: Config, device="cuda:0", pool: Optional[torch.Tensor] = None,
                  workspace: Optional[torch.Tensor] = None):
         self.cfg = cfg
         self.device = torch.device(device)
-        need_pool, need_ws = kv_pool_bytes(cfg), kv_workspace_bytes(cfg)
+        need_pool, need_ws = self._cache_bytes(cfg), kv_workspace_bytes(cfg)
         if need_pool == 0 or need_ws == 0:
             raise CkvError(CKV_EINVAL, last_error())
         if pool is None:
-            pool = torch.empty(need_pool // 2, dtype=torch.bfloat16, device=self.device)
+            pool = torch.empty(need_pool // self._cache_type.itemsize, dtype=self._cache_type, device=self.device)
         if workspace is None:
             workspace = torch.empty(need_ws, dtype=torch.uint8, device=self.device)
         self.pool, self.workspace = pool, workspace
@@ -268,9 +287,9 @@ class KvPool:
         index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._index, self._index_bytes = index, kv_index_bytes(cfg)
         self._scores: Optional[torch.Tensor] = None
-        _check(lib.kv_pool_create(ctypes.byref(cfg), _dev_ptr(pool), pool.numel() * pool.element_size(),
-                                  _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
-                                  index, ctypes.byref(self._h)))
+        _check(self._create(ctypes.byref(cfg), _dev_ptr(pool), pool.numel() * pool.element_size(),
+                            _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
+                            index, ctypes.byref(self._h)))
 
     # -- lifetime
     def close(self) -> None:
@@ -438,6 +457,44 @@ class KvPool:
                                            _on(self._index, out, torch.bfloat16, "out", batch, c.num_q_heads, c.head_dim),
                                            _stream_ptr(stream, self._index)))
 
+    # -- windows, and pages handed out on the GPU
+    def _attend(self, call, layer, block_tables, seq_lens, q, out, window, sink, stream) -> None:
+        c, dev = self.cfg, self._index
+        batch = self._tables_of(block_tables, seq_lens)
+        shape = (batch, c.num_q_heads, c.head_dim) if q.dim() == 3 else (batch, q.size(1) if q.dim() > 1 else 1, c.num_q_heads, c.head_dim)
+        _check(call(self._h.value, layer, batch, 1 if q.dim() == 3 else shape[1], block_tables.data_ptr(), seq_lens.data_ptr(),
+                    _on(dev, q, torch.bfloat16, "q", *shape), _on(dev, out, torch.bfloat16, "out", *shape), window, sink, _stream_ptr(stream, dev)))
+
+    def decode_attention_window(self, layer: int, block_tables, seq_lens, q, out, *, window: int, sink: int = 0, stream=None) -> None:
+        """Attention of new tokens to the last `window` tokens (their own included) and the first `sink`.
+
+        q, out [batch][Hq][d], or [batch][q_len][Hq][d] with up to 8 new tokens a request."""
+        self._attend(_marshal.decode_attention_window, layer, block_tables, seq_lens, q, out, window, sink, stream)
+
+    def pages_assign(self, block_tables, seq_lens, new_tokens, free_pages, free_count, *, lens_out, count_out, step_lens=None, new_start=None,
+                     slots=None, stream=None) -> None:
+        """Give every request the pages that `new_tokens` more tokens need, from the list of free ones.
+
+        free_pages int32 [num_pages], free_count int32 [1]; writes block_tables' new entries, lens_out (may be seq_lens), count_out
+        (may be free_count) and, if wanted, step_lens [batch], new_start [batch + 1] and slots int64 (one a new token)."""
+        dev, batch = self._index, self._tables_of(block_tables, seq_lens)
+        n_slots = 0 if slots is None else slots.numel()
+        _check(_marshal.kv_pages_assign(
+            self._h.value, batch, block_tables.data_ptr(), seq_lens.data_ptr(), _on(dev, new_tokens, torch.int32, "new_tokens", batch),
+            _on(dev, free_pages, torch.int32, "free_pages", self.cfg.num_pages), _on(dev, free_count, torch.int32, "free_count", 1),
+            _on(dev, lens_out, torch.int32, "lens_out", batch), _on(dev, count_out, torch.int32, "count_out", 1),
+            None if step_lens is None else _on(dev, step_lens, torch.int32, "step_lens", batch),
+            None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
+            _on(dev, slots, torch.int64, "slots", n_slots) if n_slots else None, n_slots, _stream_ptr(stream, dev)))
+
+    def pages_release(self, block_tables, seq_lens, keep_lens, free_pages, free_count, *, lens_out, count_out, stream=None) -> None:
+        """Return the pages behind each request's first keep_lens tokens (0: all) to the list of free ones."""
+        dev, batch = self._index, self._tables_of(block_tables, seq_lens)
+        _check(_marshal.kv_pages_release(
+            self._h.value, batch, block_tables.data_ptr(), seq_lens.data_ptr(), _on(dev, keep_lens, torch.int32, "keep_lens", batch),
+            _on(dev, free_pages, torch.int32, "free_pages", self.cfg.num_pages), _on(dev, free_count, torch.int32, "free_count", 1),
+            _on(dev, lens_out, torch.int32, "lens_out", batch), _on(dev, count_out, torch.int32, "count_out", 1), _stream_ptr(stream, dev)))
+
     def swap_image_bytes(self, n_pages: int) -> int:
         c = self.cfg
         return c.num_layers * int(n_pages) * c.num_kv_heads * 2 * c.page_size * c.head_dim * 2
@@ -572,6 +629,62 @@ class KvPool:
         return int(lib.ckv_launch_count(self._h))
 
 
+class Kv8Pool(KvPool):
+    """A paged KV cache in 8 bits, in steps of a power of two per page, KV head and side (kv8_pool_bytes).
+
+    `pool` (uint8, kv8_pool_bytes) and `workspace` may be passed in.  It is read and written by the kv8_ methods; those of
+    KvPool for a bf16 cache raise CkvError here."""
+
+    _create, _cache_bytes, _cache_type = lib.kv8_pool_create, staticmethod(kv8_pool_bytes), torch.uint8
+
+    def pool_view(self):
+        """([layers][pages][Hkv][2][P][d] int8 records, [layers][pages][Hkv][2] fp32 steps): views of the pool tensor."""
+        c = self.cfg
+        blocks = (c.num_layers, c.num_pages, c.num_kv_heads, 2)
+        cut, end = kv8_pool_bytes(c) - 4 * c.num_layers * c.num_pages * c.num_kv_heads * 2, kv8_pool_bytes(c)
+        flat = self.pool.view(-1)
+        return flat[:cut].view(torch.int8).view(*blocks, c.page_size, c.head_dim), flat[cut:end].view(torch.float32).view(*blocks)
+
+    def kv8_append(self, layer: int, block_tables, seq_lens, k_new, v_new, *, q=None, q_out=None, inv_freq=None, new_start=None,
+                   interleaved: bool = False, scale: float = 1.0, stream=None) -> None:
+        """Quantise new keys and values into their pages; with inv_freq (fp32 [rotary_dim / 2]) turn keys, and queries into
+        q_out, by their positions first.  Arguments as kv_append_rope's."""
+        c, dev = self.cfg, self._index
+        batch, tokens = self._tables_of(block_tables, seq_lens), k_new.size(0)
+        q_ptr = out_ptr = None
+        q_stride = out_stride = 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q is not None:
+            q_ptr, q_stride = _rows_on(dev, q, "q", tokens, c.num_q_heads, c.head_dim)
+            out_ptr, out_stride = _rows_on(dev, q_out, "q_out", tokens, c.num_q_heads, c.head_dim)
+        k_ptr, k_stride = _rows_on(dev, k_new, "k_new", tokens, c.num_kv_heads, c.head_dim)
+        v_ptr, v_stride = _rows_on(dev, v_new, "v_new", tokens, c.num_kv_heads, c.head_dim)
+        half = 0 if inv_freq is None else inv_freq.numel()
+        _check(_marshal.kv8_append(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
+                                   None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
+                                   None if inv_freq is None else _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half,
+                                   1 if interleaved else 0, scale, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride,
+                                   _stream_ptr(stream, dev)))
+
+    def kv8_gather(self, layer: int, block_tables, seq_lens, k, v, *, start=None, stream=None) -> None:
+        """The values of each request's last tokens: k, v bf16 [tokens][Hkv][d], tokens may lie apart.  start int32 [batch + 1]: each
+        request's first row; without it every request has the same number."""
+        c, dev = self.cfg, self._index
+        batch, tokens = self._tables_of(block_tables, seq_lens), k.size(0)
+        k_ptr, k_stride = _rows_on(dev, k, "k", tokens, c.num_kv_heads, c.head_dim)
+        v_ptr, v_stride = _rows_on(dev, v, "v", tokens, c.num_kv_heads, c.head_dim)
+        _check(_marshal.kv8_gather(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
+                                   None if start is None else _on(dev, start, torch.int32, "start", batch + 1), k_ptr, k_stride, v_ptr, v_stride,
+                                   _stream_ptr(stream, dev)))
+
+    def kv8_attention(self, layer: int, block_tables, seq_lens, q, out, *, window: int = 0, sink: int = 0, stream=None) -> None:
+        """Attention of new tokens over the 8-bit cache: the whole context, or the last `window` tokens and the first `sink`.
+
+        q, out [batch][Hq][d], or [batch][q_len][Hq][d] with up to 8 new tokens a request."""
+        self._attend(_marshal.kv8_attention, layer, block_tables, seq_lens, q, out, window, sink, stream)
+
+
 def decode_attention_noalloc(cfg: Config, pool: torch.Tensor, layer: int, block_tables, seq_lens, q, out,
                              num_spans: int = 0, stream=None, sync: bool = True) -> int:
     """decode_attention for callers that cannot allocate a workspace: partial results go into a fixed
@@ -617,6 +730,45 @@ def draft_verify(draft_tokens, target_probs, draft_probs, u_accept, u_sample, to
                             _on(dev, u_sample, torch.float32, "u_sample", batch),
                             _on(dev, tokens, torch.int32, "tokens", batch, n + 1),
                             _on(dev, accepted, torch.int32, "accepted", batch), _stream_ptr(stream, dev)))
+
+
+_PROBS = {torch.float32: PROBS_F32, torch.bfloat16: PROBS_BF16}
+
+
+def logits_process(logits, out, *, probs: bool = True, params=None, history=None, prompt_lens=None, history_lens=None, drafts=None,
+                   bias_ids=None, bias=None, mask=None, stream=None) -> None:
+    """Penalties, biases and masks on logits, then probabilities (or, probs=False, the logits), on the current device.
+
+    logits, out [batch][rows][vocab], fp32 or bf16 each, rows evenly spaced; out may be logits.  params fp32 [batch][4]: repetition,
+    presence, frequency, temperature.  history int32 [batch][n] with prompt_lens and history_lens [batch]; drafts int32 [batch][rows - 1];
+    bias_ids int32 and bias fp32 [batch][m]; mask int32 [batch][rows][ceil(vocab / 32)], bit 1: allowed."""
+    dev = torch.cuda.current_device()
+    if logits.dim() != 3 or logits.dtype not in _PROBS or out.dtype not in _PROBS:
+        raise ValueError("logits and out must be [batch][rows][vocab] of float32 or bfloat16, got %s of %s and %s"
+                         % (tuple(logits.shape), logits.dtype, out.dtype))
+    batch, rows, vocab = logits.shape
+    x_ptr, x_stride = _marshal.probs_on(dev, logits, logits.dtype, "logits", batch, rows, vocab)
+    out_ptr, out_stride = _marshal.probs_on(dev, out, out.dtype, "out", batch, rows, vocab)
+    n = n_bias = 0
+    h_ptr = p_ptr = l_ptr = d_ptr = i_ptr = b_ptr = None
+    if (history is None) != (prompt_lens is None) or (history is None) != (history_lens is None):
+        raise ValueError("history, prompt_lens and history_lens go together")
+    if history is not None:
+        n = history.size(-1)
+        h_ptr = _on(dev, history, torch.int32, "history", batch, n)
+        p_ptr, l_ptr = _on(dev, prompt_lens, torch.int32, "prompt_lens", batch), _on(dev, history_lens, torch.int32, "history_lens", batch)
+    if drafts is not None:
+        d_ptr = _on(dev, drafts, torch.int32, "drafts", batch, rows - 1)
+    if (bias_ids is None) != (bias is None):
+        raise ValueError("bias_ids and bias go together")
+    if bias is not None:
+        n_bias = bias.size(-1)
+        i_ptr, b_ptr = _on(dev, bias_ids, torch.int32, "bias_ids", batch, n_bias), _on(dev, bias, torch.float32, "bias", batch, n_bias)
+    words = (vocab + 31) // 32
+    _check(_marshal.logits_process(batch, rows, vocab, _PROBS[logits.dtype], _PROBS[out.dtype], 1 if probs else 0, x_ptr, x_stride,
+                                   None if params is None else _on(dev, params, torch.float32, "params", batch, 4), h_ptr, n, p_ptr, l_ptr, d_ptr,
+                                   i_ptr, b_ptr, n_bias, None if mask is None else _on(dev, mask, torch.int32, "mask", batch, rows, words), words,
+                                   out_ptr, out_stride, _stream_ptr(stream, dev)))
 
 
 class LocalAutoscaler:

@@ -8,9 +8,10 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
-SOURCES = [os.path.join(CSRC, n) for n in ("ckv_api.cu", "ckv_ops.cu", "ckv_autoscaler.cc", "ckv_global_sim.cc")]
-HEADERS = [os.path.join(CSRC, n) for n in ("ckv_common.cuh", "ckv_device.cuh", "ckv_host.cuh", "ckv_pagelist.cuh", "ckv_rope.cuh",
-                                          "ckv_sparse.cuh", "ckv_verify.cuh")] + \
+SOURCES = [os.path.join(CSRC, n) for n in ("ckv_api.cu", "ckv_ops.cu", "ckv_step.cu", "ckv_autoscaler.cc", "ckv_global_sim.cc")]
+HEADERS = [os.path.join(CSRC, n) for n in ("ckv_cache8.cuh", "ckv_cache_attn.cuh", "ckv_common.cuh", "ckv_device.cuh", "ckv_host.cuh",
+                                          "ckv_logits.cuh", "ckv_pagelist.cuh", "ckv_rope.cuh", "ckv_sparse.cuh", "ckv_tables.cuh",
+                                          "ckv_verify.cuh")] + \
           [os.path.join(_ROOT, "include", n) for n in ("chiron_kv.h", "chiron_autoscaler.h")]
 LIBRARY = os.path.join(_HERE, "libchiron_kv.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "ckv_marshal.cpp")

@@ -83,6 +83,7 @@ WorkspaceLayout carve(const ckv_config &c)
     w.st_k = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_v = take((size_t)c.max_batch * c.num_kv_heads * d2);
     w.st_out = take((size_t)c.max_batch * c.num_q_heads * d2);
+    w.cuts = take(sizeof(int4) * ckv::kMaxSpans);
     w.total = at;
     return w;
 }
@@ -110,18 +111,21 @@ EncodeTiledFn encode_tiled_fn(const char **why)
 
 // Tensor map over a whole pool seen as rows of head_dim bf16; one box = 32 rows (the 16 key rows
 // and 16 value rows of one (page, kv head)) x 64 columns, stored with the 128-byte swizzle.
-int32_t encode_pool_map(const ckv_config *cfg, const void *d_pool, CUtensorMap *out, const char *fn_name)
+// An 8-bit cache's: rows of head_dim bytes, one box = a (page, kv head) at whole width, swizzled over its row's bytes.
+int32_t encode_pool_map(const ckv_config *cfg, int bits, const void *d_pool, CUtensorMap *out, const char *fn_name)
 {
     const char *why = "";
     const EncodeTiledFn encode = encode_tiled_fn(&why);
     if (!encode) return fail(CKV_ECUDA, "%s: cuTensorMapEncodeTiled not available (%s)", fn_name, why);
     const cuuint64_t rows = (cuuint64_t)cfg->num_layers * cfg->num_pages * cfg->num_kv_heads * 32;
     const cuuint64_t dims[2] = {(cuuint64_t)cfg->head_dim, rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)cfg->head_dim * 2};
-    const cuuint32_t box[2] = {64, 32};
+    const cuuint64_t strides[1] = {(cuuint64_t)cfg->head_dim * bits / 8};
+    const cuuint32_t box[2] = {bits == 8 ? (cuuint32_t)cfg->head_dim : 64, 32};
     const cuuint32_t estr[2] = {1, 1};
-    const CUresult cr = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(d_pool), dims, strides, box, estr,
-                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const CUtensorMapDataType type = bits == 8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const CUtensorMapSwizzle swizzle = bits == 8 && cfg->head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    const CUresult cr = encode(out, type, 2, const_cast<void *>(d_pool), dims, strides, box, estr,
+                               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (cr != CUDA_SUCCESS) return fail(CKV_ECUDA, "%s: cuTensorMapEncodeTiled returned %d", fn_name, (int)cr);
     return CKV_OK;
@@ -263,6 +267,66 @@ int32_t launch_read_probe(ckv_pool *pool, const ckv::ProbeParams &pp, cudaStream
 
 }  // namespace
 
+namespace ckv {
+
+int32_t create_pool(const char *fn, const ckv_config *cfg, int bits, void *d_pool, size_t pool_bytes, void *d_workspace,
+                    size_t workspace_bytes, int32_t device, ckv_pool **out_pool)
+{
+    const char *why;
+    if (!out_pool) return fail(CKV_EINVAL, "%s: out_pool is NULL", fn);
+    *out_pool = nullptr;
+    if (!config_ok(cfg, &why)) return fail(CKV_EINVAL, "%s: %s", fn, why);
+    if (!d_pool || !d_workspace) return fail(CKV_EINVAL, "%s: NULL device buffer", fn);
+    if (reinterpret_cast<uintptr_t>(d_pool) & 255u) return fail(CKV_EINVAL, "%s: the cache is not 256-byte aligned", fn);
+    if (reinterpret_cast<uintptr_t>(d_workspace) & 255u) return fail(CKV_EINVAL, "%s: d_workspace not 256-byte aligned", fn);
+    const size_t need = bits == 8 ? kv8_pool_bytes(cfg) : kv_pool_bytes(cfg);
+    if (pool_bytes < need) return fail(CKV_ENOMEM, "%s: the cache's buffer holds %zu bytes, %zu needed", fn, pool_bytes, need);
+    const WorkspaceLayout ws = carve(*cfg);
+    if (workspace_bytes < ws.total) return fail(CKV_ENOMEM, "%s: workspace holds %zu bytes, %zu needed", fn, workspace_bytes, ws.total);
+    if (device < 0) return fail(CKV_EINVAL, "%s: device < 0", fn);
+
+    CKV_CUDA(cudaSetDevice(device));
+    int cc_major = 0, sms = 0;
+    CKV_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, device));
+    CKV_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    if (cc_major != 10) return fail(CKV_ECUDA, "%s: device %d is sm_%dx; this library is built for sm_100a only", fn, device, cc_major);
+
+    ckv_pool *p = new (std::nothrow) ckv_pool();
+    if (!p) return fail(CKV_ENOMEM, "%s: host allocation failed", fn);
+    p->cfg = *cfg;
+    p->bits = bits;
+    p->device = device;
+    p->num_sms = sms;
+    p->num_spans = std::min(sms * (cfg->head_dim == 128 ? kWarps128 : kWarps64), ckv::kMaxSpans);
+    p->d_pool = static_cast<uint8_t *>(d_pool);
+    p->d_ws = static_cast<uint8_t *>(d_workspace);
+    p->ws = ws;
+    p->launches = 0;
+    p->profile = false;
+    p->overlap = true;
+    p->pool_written = false;
+    p->inputs_from_predecessor = false;
+    p->host_route = CKV_HOST_ROUTE_AUTO;
+    p->d_scores = nullptr;
+    p->score_room = 0;
+    p->ev_used = 0;
+
+    if (int32_t rc = encode_pool_map(cfg, bits, d_pool, &p->tmap, fn)) {
+        delete p;
+        return rc;
+    }
+    cudaError_t me = cudaMemset(d_workspace, 0, ws.total);
+    if (me == cudaSuccess) me = cudaDeviceSynchronize();
+    if (me != cudaSuccess) {
+        delete p;
+        return fail(CKV_ECUDA, "%s: clearing the workspace failed: %s", fn, cudaGetErrorString(me));
+    }
+    *out_pool = p;
+    return CKV_OK;
+}
+
+}  // namespace ckv
+
 extern "C" {
 
 const char *ckv_last_error(void) { return ckv::g_error; }
@@ -284,55 +348,20 @@ size_t kv_workspace_bytes(const ckv_config *cfg)
 int32_t kv_pool_create(const ckv_config *cfg, void *d_pool, size_t pool_bytes, void *d_workspace,
                        size_t workspace_bytes, int32_t device, ckv_pool **out_pool)
 {
+    return ckv::create_pool("kv_pool_create", cfg, 16, d_pool, pool_bytes, d_workspace, workspace_bytes, device, out_pool);
+}
+
+size_t kv8_pool_bytes(const ckv_config *cfg)
+{
     const char *why;
-    if (!out_pool) return fail(CKV_EINVAL, "kv_pool_create: out_pool is NULL");
-    *out_pool = nullptr;
-    if (!config_ok(cfg, &why)) return fail(CKV_EINVAL, "kv_pool_create: %s", why);
-    if (!d_pool || !d_workspace) return fail(CKV_EINVAL, "kv_pool_create: NULL device buffer");
-    if (reinterpret_cast<uintptr_t>(d_pool) & 255u) return fail(CKV_EINVAL, "kv_pool_create: d_pool not 256-byte aligned");
-    if (reinterpret_cast<uintptr_t>(d_workspace) & 255u) return fail(CKV_EINVAL, "kv_pool_create: d_workspace not 256-byte aligned");
-    if (pool_bytes < kv_pool_bytes(cfg)) return fail(CKV_ENOMEM, "kv_pool_create: pool buffer holds %zu bytes, %zu needed", pool_bytes, kv_pool_bytes(cfg));
-    const WorkspaceLayout ws = carve(*cfg);
-    if (workspace_bytes < ws.total) return fail(CKV_ENOMEM, "kv_pool_create: workspace holds %zu bytes, %zu needed", workspace_bytes, ws.total);
-    if (device < 0) return fail(CKV_EINVAL, "kv_pool_create: device < 0");
+    if (!config_ok(cfg, &why)) { fail(CKV_EINVAL, "kv8_pool_bytes: %s", why); return 0; }
+    return (size_t)cfg->num_layers * cfg->num_pages * cfg->num_kv_heads * 2 * (cfg->page_size * (size_t)cfg->head_dim + sizeof(float));
+}
 
-    CKV_CUDA(cudaSetDevice(device));
-    int cc_major = 0, sms = 0;
-    CKV_CUDA(cudaDeviceGetAttribute(&cc_major, cudaDevAttrComputeCapabilityMajor, device));
-    CKV_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    if (cc_major != 10) return fail(CKV_ECUDA, "kv_pool_create: device %d is sm_%dx; this library is built for sm_100a only", device, cc_major);
-
-    ckv_pool *p = new (std::nothrow) ckv_pool();
-    if (!p) return fail(CKV_ENOMEM, "kv_pool_create: host allocation failed");
-    p->cfg = *cfg;
-    p->device = device;
-    p->num_sms = sms;
-    p->num_spans = std::min(sms * (cfg->head_dim == 128 ? kWarps128 : kWarps64), ckv::kMaxSpans);
-    p->d_pool = static_cast<uint8_t *>(d_pool);
-    p->d_ws = static_cast<uint8_t *>(d_workspace);
-    p->ws = ws;
-    p->launches = 0;
-    p->profile = false;
-    p->overlap = true;
-    p->pool_written = false;
-    p->inputs_from_predecessor = false;
-    p->host_route = CKV_HOST_ROUTE_AUTO;
-    p->d_scores = nullptr;
-    p->score_room = 0;
-    p->ev_used = 0;
-
-    if (int32_t rc = encode_pool_map(cfg, d_pool, &p->tmap, "kv_pool_create")) {
-        delete p;
-        return rc;
-    }
-    cudaError_t me = cudaMemset(d_workspace, 0, ws.total);
-    if (me == cudaSuccess) me = cudaDeviceSynchronize();
-    if (me != cudaSuccess) {
-        delete p;
-        return fail(CKV_ECUDA, "kv_pool_create: clearing the workspace failed: %s", cudaGetErrorString(me));
-    }
-    *out_pool = p;
-    return CKV_OK;
+int32_t kv8_pool_create(const ckv_config *cfg, void *d_cache, size_t cache_bytes, void *d_workspace,
+                        size_t workspace_bytes, int32_t device, ckv_pool **out_pool)
+{
+    return ckv::create_pool("kv8_pool_create", cfg, 8, d_cache, cache_bytes, d_workspace, workspace_bytes, device, out_pool);
 }
 
 int32_t kv_pool_destroy(ckv_pool *pool)
@@ -750,6 +779,7 @@ int32_t step_latency_sweep(ckv_pool *pool, int32_t n_sizes, const int32_t *batch
                            double *out_median_us, double *out_min_us)
 {
     if (int32_t rc = check_device(pool, "step_latency_sweep")) return rc;
+    if (int32_t rc = ckv::check_bits(pool, 16, "step_latency_sweep")) return rc;
     if (n_sizes < 1 || !batch_sizes || !out_median_us || !out_min_us) return fail(CKV_EINVAL, "step_latency_sweep: bad size list or outputs");
     if (warmup < 0 || iters < 1 || iters > 100000) return fail(CKV_EINVAL, "step_latency_sweep: bad warmup/iters");
     if (batch_stride < 1 || batch_stride > pool->cfg.max_batch) return fail(CKV_EINVAL, "step_latency_sweep: bad batch_stride");
@@ -827,6 +857,7 @@ int32_t ckv_read_span_trace(ckv_pool *pool, void *stream, uint64_t *h_trace, int
 {
     if (!pool || !h_trace) return fail(CKV_EINVAL, "ckv_read_span_trace: NULL argument");
     if (int32_t rc = check_device(pool, "ckv_read_span_trace")) return rc;
+    if (int32_t rc = ckv::check_bits(pool, 16, "ckv_read_span_trace")) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     CKV_CUDA(cudaMemcpyAsync(h_trace, pool->d_ws + pool->ws.trace, sizeof(uint64_t) * 8 * pool->num_spans,
                              cudaMemcpyDeviceToHost, s));
@@ -907,7 +938,7 @@ int32_t decode_attention_noalloc(const ckv_config *cfg, const void *d_pool, int3
 
     // Tensor map over the caller's pool, built on the stack (a host-side encode, no allocation).
     CUtensorMap tmap;
-    if (int32_t rc = encode_pool_map(cfg, d_pool, &tmap, "decode_attention_noalloc")) return rc;
+    if (int32_t rc = encode_pool_map(cfg, 16, d_pool, &tmap, "decode_attention_noalloc")) return rc;
 
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     // The scratch keeps whatever the previous call left: the status word and the arrival counters
@@ -956,6 +987,7 @@ static int32_t swap_launch(ckv_pool *pool, const char *fn, bool to_host, int32_t
                            void *h_image, size_t image_bytes, void *stream)
 {
     if (int32_t rc = check_device(pool, fn)) return rc;
+    if (int32_t rc = ckv::check_bits(pool, 16, fn)) return rc;
     if (n_pages < 1 || !d_page_ids || !h_image) return fail(CKV_EINVAL, "%s: bad page list or image", fn);
     const ckv_config &c = pool->cfg;
     const size_t page_bytes = (size_t)c.num_kv_heads * 2 * c.page_size * c.head_dim * 2;

@@ -40,6 +40,7 @@ inline int32_t key_stride(const ckv_config &c) { return (c.max_pages_per_req + 3
 struct WorkspaceLayout {
     size_t status, header, span_start, part, arrivals, trace;
     size_t st_tables, st_lens, st_q, st_k, st_v, st_out;
+    size_t cuts;
     size_t total;
 };
 
@@ -47,6 +48,7 @@ struct WorkspaceLayout {
 
 struct ckv_pool {
     ckv_config cfg;
+    int bits;                        // a cached element's: 16, or 8 (kv8_pool_create)
     int device;
     int num_sms;
     int num_spans;                   // partition width: one span per warp of the attention kernel
@@ -79,9 +81,17 @@ inline int32_t check_device(const ckv_pool *pool, const char *fn)
     return CKV_OK;
 }
 
-inline int32_t check_call(ckv_pool *pool, int32_t layer, int32_t batch, const char *fn)
+// The handle's cache must be of the type that the call reads or writes.
+inline int32_t check_bits(const ckv_pool *pool, int bits, const char *fn)
+{
+    if (pool->bits != bits) return fail(CKV_EINVAL, "%s: the handle holds a cache of %d bits an element, the call is for %d", fn, pool->bits, bits);
+    return CKV_OK;
+}
+
+inline int32_t check_call(ckv_pool *pool, int32_t layer, int32_t batch, const char *fn, int bits = 16)
 {
     if (int32_t rc = check_device(pool, fn)) return rc;
+    if (int32_t rc = check_bits(pool, bits, fn)) return rc;
     if (layer < 0 || layer >= pool->cfg.num_layers)
         return fail(CKV_EINVAL, "%s: layer %d outside [0, %d)", fn, layer, pool->cfg.num_layers);
     if (batch < 1 || batch > pool->cfg.max_batch)
@@ -114,5 +124,41 @@ inline bool overlap(const void *a, long long na, const void *b, long long nb)
 }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Enqueue a kernel; `overlap`: its prologue may run under its predecessor's tail; `cluster`: CTAs of a cluster.
+template <typename... P, typename... A>
+cudaError_t enqueue(void (*kernel)(P...), unsigned blocks, unsigned threads, size_t smem, bool overlap, unsigned cluster, void *stream,
+                    const A &...args)
+{
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(blocks);
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = overlap ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
+// More than 8 CTAs in a cluster and more than 48 KB of shared memory have to be allowed once per
+// kernel and device.
+template <typename Kernel>
+cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
+{
+    cudaError_t e = cudaSuccess;
+    if (wide_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e;
+}
+
+// The handle of kv_pool_create and kv8_pool_create (ckv_api.cu).
+int32_t create_pool(const char *fn, const ckv_config *cfg, int bits, void *d_pool, size_t pool_bytes, void *d_workspace,
+                    size_t workspace_bytes, int32_t device, ckv_pool **out_pool);
 
 }  // namespace ckv

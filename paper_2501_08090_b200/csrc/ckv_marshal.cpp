@@ -207,6 +207,13 @@ CKV_WRAP(decode_select_pages)
 CKV_WRAP(decode_attention_pages)
 CKV_WRAP(decode_attention_sparse)
 CKV_WRAP(draft_verify)
+CKV_WRAP(kv8_append)
+CKV_WRAP(kv8_gather)
+CKV_WRAP(kv8_attention)
+CKV_WRAP(decode_attention_window)
+CKV_WRAP(kv_pages_assign)
+CKV_WRAP(kv_pages_release)
+CKV_WRAP(logits_process)
 
 #define CKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
@@ -215,6 +222,8 @@ PyMethodDef methods[] = {
     {"probs_on", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(probs_on)), METH_FASTCALL, "Address and row stride of probabilities."},
     CKV_METHOD(kv_append_rope), CKV_METHOD(kv_index_update), CKV_METHOD(kv_index_values), CKV_METHOD(decode_select_pages),
     CKV_METHOD(decode_attention_pages), CKV_METHOD(decode_attention_sparse), CKV_METHOD(draft_verify),
+    CKV_METHOD(kv8_append), CKV_METHOD(kv8_gather), CKV_METHOD(kv8_attention), CKV_METHOD(decode_attention_window),
+    CKV_METHOD(kv_pages_assign), CKV_METHOD(kv_pages_release), CKV_METHOD(logits_process),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of libchiron_kv.so.", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -11,45 +11,15 @@
 #include "ckv_verify.cuh"
 
 using ckv::aligned16;
+using ckv::allow;
 using ckv::check_call;
+using ckv::enqueue;
 using ckv::fail;
 using ckv::overlap;
 
 namespace {
 
 size_t index_records(const ckv_config &c) { return (size_t)c.num_layers * c.num_pages * c.num_kv_heads; }
-
-// Enqueue a kernel; `overlap`: its prologue may run under its predecessor's tail; `cluster`: CTAs of a cluster.
-template <typename Kernel, typename Params>
-cudaError_t enqueue(Kernel kernel, const Params &params, unsigned blocks, unsigned threads, size_t smem, bool overlap,
-                    unsigned cluster, void *stream)
-{
-    cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3(blocks);
-    lc.blockDim = dim3(threads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = overlap ? 1 : 0;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    lc.attrs = attr;
-    lc.numAttrs = cluster > 0 ? 2 : 1;
-    return cudaLaunchKernelEx(&lc, kernel, params);
-}
-
-// More than 8 CTAs in a cluster and more than 48 KB of shared memory have to be allowed once per
-// kernel and device.
-template <typename Kernel>
-cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
-{
-    cudaError_t e = cudaSuccess;
-    if (wide_cluster) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess && smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return e;
-}
 
 // Pages that one request may hold where pages are selected: their scores fit an SM's shared memory.
 constexpr int kMaxSelectPages = 49152;
@@ -72,13 +42,13 @@ int32_t launch_select(ckv_pool *pool, ckv::SelectParams &sp, int cand, void *str
     if (cand > 0) {
         const long long warps = pairs * ((cand + 15) / 16);      // no more than there can be tiles
         const unsigned blocks = (unsigned)std::min<long long>((warps + ckv::kScoreWarps - 1) / ckv::kScoreWarps, (long long)ckv::kScoreCtas * pool->num_sms);
-        CKV_CUDA(enqueue(score, sp, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream));
+        CKV_CUDA(enqueue(score, blocks, ckv::kScoreWarps * 32, score_smem, pool->overlap, 0, stream, sp));
         pool->launches += 1;
         sp.after_scores = 1;
     }
     const auto select = [&](auto kernel, int keys) {             // `keys` a thread
         const int threads = std::min(ckv::kMaxSelectThreads, std::max(64, (cand + keys * 32 - 1) / (keys * 32) * 32));
-        return enqueue(kernel, sp, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream);
+        return enqueue(kernel, (unsigned)pairs, threads, (size_t)cand * 4, pool->overlap, 0, stream, sp);
     };
     CKV_CUDA(cand <= 4 * ckv::kMaxSelectThreads    ? select(ckv::select_pages_kernel<4>, 4)
              : cand <= 8 * ckv::kMaxSelectThreads  ? select(ckv::select_pages_kernel<8>, 8)
@@ -98,7 +68,7 @@ int32_t launch_index_update(ckv_pool *pool, const ckv::IndexParams &ip, unsigned
         CKV_CUDA(allow(kernel, false, smem));
         configured_device = pool->device;
     }
-    CKV_CUDA(enqueue(kernel, ip, blocks, ckv::kIndexWarps * 32, smem, pool->overlap, 0, stream));
+    CKV_CUDA(enqueue(kernel, blocks, ckv::kIndexWarps * 32, smem, pool->overlap, 0, stream, ip));
     pool->launches += 1;
     return CKV_OK;
 }
@@ -129,7 +99,7 @@ int32_t launch_verify(const ckv::VerifyParams &vp, void *stream)
     }
     const long long fill = (4ll * num_sms + vp.batch - 1) / vp.batch;
     const unsigned cluster = cluster_of(std::min<long long>(std::min<long long>(fill, vp.vocab / 2048), vp.batch <= 8 ? 16 : 8));
-    CKV_CUDA(enqueue(kernel, vp, (unsigned)vp.batch * cluster, ckv::kVerifyThreads, 0, true, cluster, stream));
+    CKV_CUDA(enqueue(kernel, (unsigned)vp.batch * cluster, ckv::kVerifyThreads, 0, true, cluster, stream, vp));
     return CKV_OK;
 }
 
@@ -283,8 +253,8 @@ int32_t kv_append_rope(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_t
     const int several = (long long)pool->num_sms * 8 * 4 <= n_tokens ? 4 : 1;
     const unsigned threads = (unsigned)std::max(32 * several, (rows_per_turn * units + 31) / 32 * 32), blocks = (unsigned)((n_tokens + several - 1) / several);
     const auto launch = [&](auto one, auto four) {
-        return several == 1 ? enqueue(one, rp, blocks, threads, 0, pool->overlap, 0, stream)
-                            : enqueue(four, rp, blocks, threads, 0, pool->overlap, 0, stream);
+        return several == 1 ? enqueue(one, blocks, threads, 0, pool->overlap, 0, stream, rp)
+                            : enqueue(four, blocks, threads, 0, pool->overlap, 0, stream, rp);
     };
     cudaError_t e;
     if (c.head_dim == 128)
@@ -349,8 +319,8 @@ int32_t kv_index_values(ckv_pool *pool, int32_t layer, const void *d_index, size
     vp.records_n = (long long)c.num_pages * c.num_kv_heads;
     const long long pieces = vp.records_n * (2 * c.head_dim / 8);
     const unsigned blocks = (unsigned)((pieces + 1023) / 1024);
-    CKV_CUDA(c.head_dim == 128 ? enqueue(ckv::kv_index_values_kernel<128>, vp, blocks, 256, 0, pool->overlap, 0, stream)
-                               : enqueue(ckv::kv_index_values_kernel<64>, vp, blocks, 256, 0, pool->overlap, 0, stream));
+    CKV_CUDA(c.head_dim == 128 ? enqueue(ckv::kv_index_values_kernel<128>, blocks, 256, 0, pool->overlap, 0, stream, vp)
+                               : enqueue(ckv::kv_index_values_kernel<64>, blocks, 256, 0, pool->overlap, 0, stream, vp));
     pool->launches += 1;
     return CKV_OK;
 }

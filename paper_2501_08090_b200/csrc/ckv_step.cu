@@ -1,0 +1,374 @@
+// Host runtime and C ABI of a decode step whose state stays on the GPU (include/chiron_kv.h): the 8-bit cache,
+// windowed attention, page tables, logits.
+#include "chiron_kv.h"
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "ckv_cache8.cuh"
+#include "ckv_cache_attn.cuh"
+#include "ckv_host.cuh"
+#include "ckv_logits.cuh"
+#include "ckv_tables.cuh"
+
+using ckv::aligned16;
+using ckv::allow;
+using ckv::check_call;
+using ckv::enqueue;
+using ckv::fail;
+using ckv::overlap;
+
+namespace {
+
+size_t blocks_of(const ckv_config &c) { return (size_t)c.num_pages * c.num_kv_heads * 2; }      // of a layer: a (page, kv head)'s keys or values
+
+uint8_t *layer_records(const ckv_pool *pool, int32_t layer)
+{
+    return pool->d_pool + (size_t)layer * blocks_of(pool->cfg) * pool->cfg.page_size * pool->cfg.head_dim;
+}
+
+float *all_steps(const ckv_pool *pool)
+{
+    const ckv_config &c = pool->cfg;
+    return reinterpret_cast<float *>(pool->d_pool + (size_t)c.num_layers * blocks_of(c) * c.page_size * c.head_dim);
+}
+
+// Rows of tokens, each with its own stride: aligned, and apart by at least a token's elements.
+struct Rows {
+    const char *name;
+    const void *ptr;
+    int64_t stride, row;
+};
+
+int32_t check_rows(const char *fn, int32_t n_tokens, std::initializer_list<Rows> rows)
+{
+    for (const Rows &x : rows) {
+        if (!x.ptr) continue;
+        if (!aligned16(x.ptr)) return fail(CKV_EINVAL, "%s: %s not 16-byte aligned", fn, x.name);
+        if (n_tokens > 1 && (x.stride < x.row || x.stride % 8 != 0))
+            return fail(CKV_EINVAL, "%s: %s's stride between tokens, %lld, is below a token's %lld elements or no multiple of 8", fn, x.name,
+                        (long long)x.stride, (long long)x.row);
+    }
+    return CKV_OK;
+}
+
+// CTAs of a launch that has one for every page that a request's last tokens can touch (page_of_tokens).
+unsigned page_ctas(int32_t n_tokens, int32_t batch) { return (unsigned)(n_tokens / ckv::kPageSize + 2 * (long long)batch); }
+
+template <int D, bool k8>
+int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *stream)
+{
+    using Lay = ckv::CacheAttnLayout<D, k8>;
+    static thread_local int configured_device = -1;
+    auto kernel = ckv::cache_attn_kernel<D, k8>;
+    if (configured_device != pool->device) {
+        CKV_CUDA(allow(kernel, false, Lay::kSmemBytes));
+        configured_device = pool->device;
+    }
+    const unsigned ctas = std::min(pool->num_sms, ckv::kMaxSpans / Lay::kWarps);
+    ap.num_spans = (int32_t)ctas * Lay::kWarps;
+    CKV_CUDA(enqueue(kernel, ctas, Lay::kWarps * 32, Lay::kSmemBytes, pool->overlap, 0, stream, pool->tmap, ap));
+    const float bias = k8 ? std::ldexp(1.f, -ckv::kCacheSumBias) : 1.f;
+    CKV_CUDA(enqueue(ckv::cache_attn_fold_kernel<D>, 4 * ckv::kFoldBlocks, ckv::kFoldWarps * 32, 0, pool->overlap, 0, stream, ap, bias));
+    pool->launches += 2;
+    return CKV_OK;
+}
+
+int32_t cache_attention(ckv_pool *pool, const char *fn, int bits, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables,
+                        const int32_t *d_seq_lens, const void *d_q, void *d_out, int32_t window, int32_t sink, void *stream)
+{
+    if (int32_t rc = check_call(pool, layer, batch, fn, bits)) return rc;
+    if (q_len < 1 || q_len > ckv::kMaxGroup) return fail(CKV_EINVAL, "%s: q_len %d outside [1, %d]", fn, q_len, ckv::kMaxGroup);
+    if (window < (bits == 8 ? 0 : 1) || sink < 0) return fail(CKV_EINVAL, "%s: window %d or sink %d out of range", fn, window, sink);
+    if (!d_block_tables || !d_seq_lens || !d_q || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (!aligned16(d_q) || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: q/out not 16-byte aligned", fn);
+    const ckv_config &c = pool->cfg;
+    ckv::CacheAttnParams ap{};
+    ap.block_tables = d_block_tables;
+    ap.seq_lens = d_seq_lens;
+    ap.q = static_cast<const uint16_t *>(d_q);
+    ap.out = static_cast<uint16_t *>(d_out);
+    ap.steps = bits == 8 ? reinterpret_cast<const float2 *>(all_steps(pool)) : nullptr;
+    ap.part = pool->wsp<float>(pool->ws.part);
+    ap.cuts = pool->wsp<int4>(pool->ws.cuts);
+    ap.status = pool->wsp<uint32_t>(pool->ws.status);
+    ap.batch = batch;
+    ap.max_pages_per_req = c.max_pages_per_req;
+    ap.num_pages = c.num_pages;
+    ap.num_kv_heads = c.num_kv_heads;
+    ap.group = c.num_q_heads / c.num_kv_heads;
+    ap.layer_page_base = layer * c.num_pages;
+    ap.q_len = q_len;
+    ap.window = window;
+    ap.sink = window > 0 ? sink : 0;
+    ap.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c.head_dim));
+    // a launch holds 8 (new token, head) columns
+    const int per_pass = ckv::kMaxGroup / ap.group;
+    for (int base = 0; base < q_len; base += per_pass) {
+        ap.q_base = base;
+        ap.q_pass = std::min(per_pass, q_len - base);
+        const int32_t rc = c.head_dim == 128 ? (bits == 8 ? launch_cache_attention<128, true>(pool, ap, stream) : launch_cache_attention<128, false>(pool, ap, stream))
+                                             : (bits == 8 ? launch_cache_attention<64, true>(pool, ap, stream) : launch_cache_attention<64, false>(pool, ap, stream));
+        if (rc) return rc;
+    }
+    return CKV_OK;
+}
+
+// What both page calls check, and their launch.
+template <bool kAssign>
+int32_t launch_pages(ckv_pool *pool, const char *fn, const ckv::TablesParams &args, int32_t batch, void *stream)
+{
+    if (int32_t rc = ckv::check_device(pool, fn)) return rc;
+    if (batch < 1 || batch > pool->cfg.max_batch) return fail(CKV_EINVAL, "%s: batch %d outside [1, %d]", fn, batch, pool->cfg.max_batch);
+    ckv::TablesParams tp = args;
+    if (!tp.block_tables || !tp.seq_lens || !tp.amounts || !tp.free_pages || !tp.free_count || !tp.lens_out || !tp.count_out)
+        return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (tp.n_slots < 0 || (tp.n_slots > 0 && !tp.slots)) return fail(CKV_EINVAL, "%s: %d slots, or no array for them", fn, tp.n_slots);
+    if (reinterpret_cast<uintptr_t>(tp.slots) % 8 != 0) return fail(CKV_EINVAL, "%s: slots not 8-byte aligned", fn);
+    tp.batch = batch;
+    tp.max_pages_per_req = pool->cfg.max_pages_per_req;
+    tp.num_pages = pool->cfg.num_pages;
+    tp.status = pool->wsp<uint32_t>(pool->ws.status);
+    // lengths and count may be written in place; everything else that is written lies apart from what is read
+    const long long tables_n = (long long)batch * tp.max_pages_per_req;
+    const struct { const void *ptr; long long n; } a[] = {
+        {tp.lens_out, batch}, {tp.count_out, 1}, {tp.step_lens, batch}, {tp.new_start, batch + 1ll}, {tp.slots, 2ll * tp.n_slots},
+        {tp.block_tables, tables_n}, {tp.free_pages, tp.num_pages},
+        {tp.lens_out == tp.seq_lens ? nullptr : tp.seq_lens, batch}, {tp.lens_out == tp.amounts ? nullptr : tp.amounts, batch},
+        {tp.count_out == tp.free_count ? nullptr : tp.free_count, 1}};
+    for (int i = 0; i < 7; ++i)
+        for (int k = i + 1; k < 10; ++k)
+            if (overlap(a[i].ptr, a[i].n, a[k].ptr, a[k].n)) return fail(CKV_EINVAL, "%s: two of the arrays overlap", fn);
+    // the sums of 8192 requests, three words each, fit an SM's shared memory; one CTA writes about 8 slots a thread in
+    // the time that a cluster's start costs
+    static thread_local int configured_device = -1;
+    auto kernel = ckv::pages_kernel<kAssign>;
+    if (configured_device != pool->device) {
+        CKV_CUDA(allow(kernel, false, sizeof(int) * ckv::kTablesWords * ckv::kMaxBatch));
+        configured_device = pool->device;
+    }
+    const long long most = std::max<long long>(batch, tp.n_slots);
+    CKV_CUDA(enqueue(kernel, most > 8192 ? 8 : 1, most > 256 ? 1024 : 256, sizeof(int) * ckv::kTablesWords * batch, pool->overlap, most > 8192 ? 8 : 1,
+                     stream, tp));
+    pool->launches += 1;
+    pool->inputs_from_predecessor = true;        // a decode step that follows directly must not read its tables ahead
+    return CKV_OK;
+}
+
+template <typename Tin, typename Tout>
+int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
+{
+    static thread_local int configured_device = -1, num_sms = 0;
+    auto kernel = ckv::logits_process_kernel<Tin, Tout>;
+    int device = -1;
+    CKV_CUDA(cudaGetDevice(&device));
+    if (configured_device != device) {
+        CKV_CUDA(allow(kernel, true, ckv::kLogitsSlice * 4));
+        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
+        configured_device = device;
+    }
+    // CTAs of a row: as few as hold it, more while there are few rows and a slice is more than 2048 tokens
+    constexpr int E = 16 / sizeof(Tin);
+    const int pieces = (lp.vocab + 2 * E - 2) / E;               // wherever in its first piece the row begins
+    const long long rows = (long long)batch * lp.rows;
+    unsigned cluster = 1;
+    while (cluster < 16 && ((pieces + cluster - 1) / cluster * E > ckv::kLogitsSlice || (2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster)))
+        cluster *= 2;
+    lp.pieces = (int)((pieces + cluster - 1) / cluster);
+    const bool counts = lp.history || lp.drafts || lp.bias_ids;
+    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), ckv::kLogitsThreads, counts ? (size_t)lp.pieces * E * 4 : 0, true, cluster, stream, lp));
+    return CKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens, const int32_t *d_block_tables,
+                   const int32_t *d_seq_lens, const int32_t *d_new_start, const float *d_inv_freq, int32_t rotary_dim,
+                   int32_t interleaved, float scale, const void *d_q, int64_t q_stride, const void *d_k_new,
+                   int64_t k_stride, const void *d_v_new, int64_t v_stride, void *d_q_out, int64_t q_out_stride,
+                   void *stream)
+{
+    const char *fn = "kv8_append";
+    if (int32_t rc = check_call(pool, layer, batch, fn, 8)) return rc;
+    const ckv_config &c = pool->cfg;
+    if (n_tokens < 0) return fail(CKV_EINVAL, "%s: n_tokens < 0", fn);
+    if (!d_block_tables || !d_seq_lens) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (d_inv_freq && (rotary_dim < 16 || rotary_dim > c.head_dim || rotary_dim % 16 != 0))
+        return fail(CKV_EINVAL, "%s: rotary_dim %d is not a multiple of 16 in [16, %d]", fn, rotary_dim, c.head_dim);
+    if (!d_new_start && n_tokens % batch != 0)
+        return fail(CKV_EINVAL, "%s: %d tokens do not split evenly over %d requests", fn, n_tokens, batch);
+    if (n_tokens == 0) return CKV_OK;
+    if (!d_k_new || !d_v_new) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if ((d_q == nullptr) != (d_q_out == nullptr)) return fail(CKV_EINVAL, "%s: q and q_out go together", fn);
+    if (d_q && !d_inv_freq) return fail(CKV_EINVAL, "%s: queries are only turned, and there is no inv_freq", fn);
+    const int64_t q_row = (int64_t)c.num_q_heads * c.head_dim, kv_row = (int64_t)c.num_kv_heads * c.head_dim;
+    if (int32_t rc = check_rows(fn, n_tokens, {{"q", d_q, q_stride, q_row}, {"k_new", d_k_new, k_stride, kv_row}, {"v_new", d_v_new, v_stride, kv_row},
+                                               {"q_out", d_q_out, q_out_stride, q_row}}))
+        return rc;
+    if (d_q && d_q_out == d_q && n_tokens > 1 && q_out_stride != q_stride)
+        return fail(CKV_EINVAL, "%s: q_out in place of q must have its stride", fn);
+    ckv::Append8Params ap{};
+    ckv::RopeParams &rp = ap.rope;
+    rp.q = static_cast<const uint16_t *>(d_q);
+    rp.k = static_cast<const uint16_t *>(d_k_new);
+    rp.v = static_cast<const uint16_t *>(d_v_new);
+    rp.q_out = static_cast<uint16_t *>(d_q_out);
+    rp.q_stride = q_stride; rp.k_stride = k_stride; rp.v_stride = v_stride; rp.q_out_stride = q_out_stride;
+    rp.inv_freq = d_inv_freq;
+    rp.new_start = d_new_start;
+    rp.block_tables = d_block_tables;
+    rp.seq_lens = d_seq_lens;
+    rp.status = pool->wsp<uint32_t>(pool->ws.status);
+    rp.batch = batch;
+    rp.q_len = n_tokens / batch;
+    rp.max_pages_per_req = c.max_pages_per_req;
+    rp.num_pages = c.num_pages;
+    rp.num_q_heads = c.num_q_heads;
+    rp.num_kv_heads = c.num_kv_heads;
+    rp.rotary = rotary_dim;
+    rp.n_tokens = n_tokens;
+    rp.scale = scale;
+    ap.records = layer_records(pool, layer);
+    ap.steps = all_steps(pool) + layer * blocks_of(c);
+    const auto kernel = c.head_dim == 128 ? (interleaved ? ckv::kv8_append_kernel<128, true> : ckv::kv8_append_kernel<128, false>)
+                                          : (interleaved ? ckv::kv8_append_kernel<64, true> : ckv::kv8_append_kernel<64, false>);
+    CKV_CUDA(enqueue(kernel, page_ctas(n_tokens, batch), ckv::kAppend8Warps * 32, 0, pool->overlap, 0, stream, ap));
+    pool->launches += 1;
+    return CKV_OK;
+}
+
+int32_t kv8_gather(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_tokens, const int32_t *d_block_tables,
+                   const int32_t *d_seq_lens, const int32_t *d_start, void *d_k, int64_t k_stride, void *d_v,
+                   int64_t v_stride, void *stream)
+{
+    const char *fn = "kv8_gather";
+    if (int32_t rc = check_call(pool, layer, batch, fn, 8)) return rc;
+    const ckv_config &c = pool->cfg;
+    if (n_tokens < 0) return fail(CKV_EINVAL, "%s: n_tokens < 0", fn);
+    if (!d_block_tables || !d_seq_lens) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (!d_start && n_tokens % batch != 0)
+        return fail(CKV_EINVAL, "%s: %d tokens do not split evenly over %d requests", fn, n_tokens, batch);
+    if (n_tokens == 0) return CKV_OK;
+    if (!d_k || !d_v) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    const int64_t row = (int64_t)c.num_kv_heads * c.head_dim;
+    if (int32_t rc = check_rows(fn, n_tokens, {{"k", d_k, k_stride, row}, {"v", d_v, v_stride, row}})) return rc;
+    ckv::Gather8Params gp{};
+    gp.records = layer_records(pool, layer);
+    gp.steps = all_steps(pool) + layer * blocks_of(c);
+    gp.start = d_start;
+    gp.block_tables = d_block_tables;
+    gp.seq_lens = d_seq_lens;
+    gp.k = static_cast<uint16_t *>(d_k);
+    gp.v = static_cast<uint16_t *>(d_v);
+    gp.k_stride = k_stride;
+    gp.v_stride = v_stride;
+    gp.status = pool->wsp<uint32_t>(pool->ws.status);
+    gp.batch = batch;
+    gp.each = n_tokens / batch;
+    gp.n_tokens = n_tokens;
+    gp.max_pages_per_req = c.max_pages_per_req;
+    gp.num_pages = c.num_pages;
+    gp.num_kv_heads = c.num_kv_heads;
+    CKV_CUDA(enqueue(c.head_dim == 128 ? ckv::kv8_gather_kernel<128> : ckv::kv8_gather_kernel<64>, page_ctas(n_tokens, batch), 256, 0, pool->overlap, 0,
+                     stream, gp));
+    pool->launches += 1;
+    return CKV_OK;
+}
+
+int32_t kv8_attention(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables, const int32_t *d_seq_lens,
+                      const void *d_q, void *d_out, int32_t window, int32_t sink, void *stream)
+{
+    return cache_attention(pool, "kv8_attention", 8, layer, batch, q_len, d_block_tables, d_seq_lens, d_q, d_out, window, sink, stream);
+}
+
+int32_t decode_attention_window(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables,
+                                const int32_t *d_seq_lens, const void *d_q, void *d_out, int32_t window, int32_t sink, void *stream)
+{
+    return cache_attention(pool, "decode_attention_window", 16, layer, batch, q_len, d_block_tables, d_seq_lens, d_q, d_out, window, sink, stream);
+}
+
+int32_t kv_pages_assign(ckv_pool *pool, int32_t batch, int32_t *d_block_tables, const int32_t *d_seq_lens, const int32_t *d_new_tokens,
+                        const int32_t *d_free_pages, const int32_t *d_free_count, int32_t *d_lens_out, int32_t *d_count_out,
+                        int32_t *d_step_lens, int32_t *d_new_start, int64_t *d_slots, int32_t n_slots, void *stream)
+{
+    ckv::TablesParams tp{};
+    tp.block_tables = d_block_tables;
+    tp.seq_lens = d_seq_lens;
+    tp.amounts = d_new_tokens;
+    tp.free_pages = const_cast<int32_t *>(d_free_pages);
+    tp.free_count = d_free_count;
+    tp.lens_out = d_lens_out;
+    tp.count_out = d_count_out;
+    tp.step_lens = d_step_lens;
+    tp.new_start = d_new_start;
+    tp.slots = reinterpret_cast<long long *>(d_slots);
+    tp.n_slots = n_slots;
+    return launch_pages<true>(pool, "kv_pages_assign", tp, batch, stream);
+}
+
+int32_t kv_pages_release(ckv_pool *pool, int32_t batch, const int32_t *d_block_tables, const int32_t *d_seq_lens, const int32_t *d_keep_lens,
+                         int32_t *d_free_pages, const int32_t *d_free_count, int32_t *d_lens_out, int32_t *d_count_out, void *stream)
+{
+    ckv::TablesParams tp{};
+    tp.block_tables = const_cast<int32_t *>(d_block_tables);
+    tp.seq_lens = d_seq_lens;
+    tp.amounts = d_keep_lens;
+    tp.free_pages = d_free_pages;
+    tp.free_count = d_free_count;
+    tp.lens_out = d_lens_out;
+    tp.count_out = d_count_out;
+    return launch_pages<false>(pool, "kv_pages_release", tp, batch, stream);
+}
+
+int32_t logits_process(int32_t batch, int32_t rows, int32_t vocab, int32_t in_dtype, int32_t out_dtype, int32_t probs, const void *d_logits,
+                       int64_t logits_stride, const float *d_params, const int32_t *d_history, int64_t history_stride, const int32_t *d_prompt_lens,
+                       const int32_t *d_history_lens, const int32_t *d_drafts, const int32_t *d_bias_ids, const float *d_bias, int32_t n_bias,
+                       const uint32_t *d_mask, int64_t mask_stride, void *d_out, int64_t out_stride, void *stream)
+{
+    const char *fn = "logits_process";
+    if (batch < 1 || rows < 1 || (long long)batch * rows * 16 >= (1ll << 31)) return fail(CKV_EINVAL, "%s: batch %d or rows %d out of range", fn, batch, rows);
+    if (vocab < 1 || vocab > ckv::kLogitsMaxVocab) return fail(CKV_EINVAL, "%s: vocab %d outside [1, %d]", fn, vocab, ckv::kLogitsMaxVocab);
+    for (int32_t d : {in_dtype, out_dtype})
+        if (d != CKV_PROBS_F32 && d != CKV_PROBS_BF16) return fail(CKV_EINVAL, "%s: unknown dtype %d", fn, d);
+    if (!d_logits || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
+    if (d_history && (!d_prompt_lens || !d_history_lens || history_stride < 0))
+        return fail(CKV_EINVAL, "%s: the history needs its lengths and a stride of at least 0", fn);
+    if ((d_history || d_drafts) && !d_params) return fail(CKV_EINVAL, "%s: the history and the drafts are counted for penalties, and there are no params", fn);
+    if (n_bias < 0 || (n_bias > 0 && (!d_bias_ids || !d_bias))) return fail(CKV_EINVAL, "%s: n_bias %d, or no biases", fn, n_bias);
+    if (logits_stride < vocab || out_stride < vocab) return fail(CKV_EINVAL, "%s: a row's stride is below the vocabulary", fn);
+    if (d_mask && mask_stride < (vocab + 31) / 32) return fail(CKV_EINVAL, "%s: the mask's stride is below the vocabulary's words", fn);
+    const uintptr_t in_size = in_dtype == CKV_PROBS_F32 ? 4 : 2, out_size = out_dtype == CKV_PROBS_F32 ? 4 : 2;
+    const uintptr_t in_at = reinterpret_cast<uintptr_t>(d_logits), out_at = reinterpret_cast<uintptr_t>(d_out);
+    if (in_at % in_size != 0 || out_at % out_size != 0) return fail(CKV_EINVAL, "%s: logits or out not aligned to their type", fn);
+    const long long n = (long long)batch * rows;
+    const uintptr_t in_end = in_at + ((n - 1) * logits_stride + vocab) * in_size, out_end = out_at + ((n - 1) * out_stride + vocab) * out_size;
+    if (in_at < out_end && out_at < in_end && !(in_at == out_at && in_dtype == out_dtype && (n == 1 || logits_stride == out_stride)))
+        return fail(CKV_EINVAL, "%s: out overlaps the logits without being them", fn);
+    ckv::LogitsParams lp{};
+    lp.logits = d_logits;
+    lp.out = d_out;
+    lp.stride = logits_stride;
+    lp.out_stride = out_stride;
+    lp.params = d_params;
+    lp.history = history_stride > 0 ? d_history : nullptr;
+    lp.prompt_lens = d_prompt_lens;
+    lp.history_lens = d_history_lens;
+    lp.drafts = rows > 1 ? d_drafts : nullptr;
+    lp.bias_ids = n_bias > 0 ? d_bias_ids : nullptr;
+    lp.bias = d_bias;
+    lp.mask = d_mask;
+    lp.history_stride = history_stride;
+    lp.mask_stride = mask_stride;
+    lp.rows = rows;
+    lp.vocab = vocab;
+    lp.n_bias = n_bias;
+    lp.probs = probs;
+    if (in_dtype == CKV_PROBS_F32)
+        return out_dtype == CKV_PROBS_F32 ? launch_logits<float, float>(lp, batch, stream) : launch_logits<float, __nv_bfloat16>(lp, batch, stream);
+    return out_dtype == CKV_PROBS_F32 ? launch_logits<__nv_bfloat16, float>(lp, batch, stream) : launch_logits<__nv_bfloat16, __nv_bfloat16>(lp, batch, stream);
+}
+
+}  // extern "C"
