@@ -333,8 +333,8 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  *                     unusable length (status bit), or of a page id outside the pool (status bit), are zero-filled; other
  *                     rows are left as they were.
  *   kv8_attention     decode_attention_multi over the 8-bit cache; window and sink as below, window 0: the whole context.
- *                     Scores and weights see the values exactly; queries are rounded to 11 bits below their
- *                     largest element's 2^-22, weights to 11 bits for the product with V.
+ *                     Products see the cache's values exactly; a query's elements are rounded to 2^-21 of its
+ *                     largest, weights to fp16 for the product with V.  A query with an infinity or a NaN gives NaN.
  * Errors: CKV_EINVAL, CKV_ENOMEM, CKV_ECUDA.
  */
 size_t kv8_pool_bytes(const ckv_config *cfg);

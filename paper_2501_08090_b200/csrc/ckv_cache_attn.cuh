@@ -15,21 +15,27 @@ namespace ckv {
 // from the front, then a gap of `skip` pages, `count` pages in all.  Within them every token is either
 // visible or masked by its position; a tile of 32 tokens (2 pages) that all columns see entirely takes no mask.
 //
-// How the work is split.  Contexts (and windows longer than many contexts) differ a thousandfold, so the tiles
-// of all (request, kv head) pairs lie on one axis, kCacheCost units ahead of each pair for what a piece costs
-// besides its tiles, and every warp takes an even span of it, as it reads them: one kernel, no plan on the
-// host.  A warp is independent: a ring of kStages tiles of its own, filled by TMA some tiles ahead, mma.sync on
-// them, the softmax in the log2 domain with a running maximum.  A pair that lies within one span is finished
-// there; of one that spans cut, each span leaves a partial (m, l, O) and cache_attn_fold_kernel joins them.
+// How the work is split.  A warp is independent: a ring of tiles of its own, filled by TMA some tiles ahead,
+// mma.sync on them, the softmax in the log2 domain with a running maximum; what it has of a pair at the end is a
+// partial (m, l, O):   M = max m_i,  out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
+//   cache_attn_pair_kernel   (windows, short tables: pairs of one length, nearly)  a cluster of CTAs owns a (request, kv
+//       head), its warps take the tiles in turn; partials are folded in (distributed) shared memory.
+//   cache_attn_span_kernel   (contexts that differ a thousandfold)  the tiles of all pairs lie on one axis, kCacheCost
+//       units ahead of each pair for what a piece costs besides its tiles, and every warp takes an even span of
+//       it: no plan on the host.  A pair within one span is finished there, one within a CTA by the CTA at its end;
+//       of a pair that CTAs cut, each CTA leaves one partial, and cache_attn_fold_kernel joins them.
 //
 //   S^T[tok 16 x col 8] = K[tok 16 x d] . Q^T[d x col 8],   O^T[d 16 x col 8] += V^T[d 16 x tok 16] . P^T[tok 16 x col 8]
 //
 // 8-bit records.  value = n * step, n a whole number of magnitude <= 127, a step per (page, head, K | V): a
 // block's 16 tokens are one m16 block of the matrix instruction, so a step is one factor for a block's scores, and one
-// for its weights.  n is exact in fp16, as 1152 + n - 1152: its byte with the sign bit flipped, under the
+// for its weights.
+// K is multiplied as it lies, by the 8-bit matrix instruction: a query is scaled by a power of two, so that its largest
+// element has magnitude 2^20 to 2^21, rounded to a whole number and cut into three signed bytes (exact down to 2^-13 of
+// the largest element, below that to within 2^-21 of it); the three products' sums are exact.
+// V meets weights in fp16: n is exact there, as 1152 + n - 1152: its byte with the sign bit flipped, under the
 // byte 0x64, is the fp16 number 1152 + n (two logic operations a pair of numbers, then a subtraction that is
-// exact).  Queries are scaled by a power of two per column so that their largest has magnitude 2^7 to 2^8, and
-// rounded to fp16: exact down to 2^-22 of the largest, below that to within 2^-33 of it.
+// exact).
 // V's steps: the contribution of token t to O is 2^(s_t - m) step_t n_t, so with e_t = log2(step_t) the weights
 // P_t = 2^(s_t + e_t - M), M the running maximum of s + e, are at most 2^8 whatever the steps are, and
 // l = sum_t P_t 2^-e_t.  They are rounded to fp16 (2^-11) for P V and summed unrounded in fp32.
@@ -45,8 +51,8 @@ struct CacheAttnParams {
     const uint16_t *q;              // [batch][q_len][Hq][d]
     uint16_t *out;
     const float2 *steps;            // 8-bit cache: [layers][pages][Hkv] (K's, V's)
-    float *part;                    // [2 * spans] partials: m[8], l[8], rows [8][D]
-    int4 *cuts;                     // [spans] the pair that a span begins and does not end: request, kv head, last span; request -1: none
+    float *part;                    // partials (PartLayout): two a CTA, then one a span
+    int4 *cuts;                     // [CTAs] the pair that a CTA begins and does not end: request, kv head, last CTA; request -1: none
     uint32_t *status;
     int32_t batch, max_pages_per_req, num_pages, num_kv_heads, group;
     int32_t layer_page_base;        // layer * num_pages
@@ -138,24 +144,34 @@ __device__ __forceinline__ TilePlace span_begin(const CacheAttnParams &p, long l
     return at;
 }
 
-template <int D, bool k8>
+// A partial: m[8], l[8], then eight rows of D floats at a pitch that spreads the banks.
+template <int D>
+struct PartLayout {
+    static constexpr int kHead = 2 * kMaxGroup, kPitch = D + 4, kFloats = kHead + kMaxGroup * kPitch;
+};
+
+// W warps a CTA, each with a ring of S tiles.
+template <int D, bool k8, int W, int S>
 struct CacheAttnLayout {
-    static constexpr int kWarps = k8 ? 12 : 6;
-    static constexpr int kStages = D == 128 ? 2 : 4;
     static constexpr int kPageBytes = 32 * D * (k8 ? 1 : 2);
     static constexpr int kHalfBytes = 32 * 128;                  // bf16: a box of 64 columns
     static constexpr int kBoxes = k8 ? 1 : D / 64;               // TMA boxes of a page
     static constexpr int kTileBytes = kPagesPerTile * kPageBytes;
-    static constexpr int kRingBytes = kStages * kTileBytes;
-    static constexpr int kStepsOff = kWarps * kRingBytes;        // float2 a page of a stage
-    static constexpr int kBarOff = kStepsOff + (k8 ? kWarps * kStages * kPagesPerTile * 8 : 0);
-    static constexpr int kSmemBytes = kBarOff + kWarps * kStages * 8 + 1024;     // 1024: alignment of the swizzle's pattern
+    static constexpr int kRingBytes = S * kTileBytes;
+    static constexpr int kStepsOff = W * kRingBytes;             // float2 a page of a stage
+    static constexpr int kBarOff = kStepsOff + (k8 ? W * S * kPagesPerTile * 8 : 0);
+    static constexpr int kSmemBytes = kBarOff + W * S * 8 + 1024;                // 1024: alignment of the swizzle's pattern
+    static_assert(PartLayout<D>::kFloats * 4 <= kRingBytes, "a warp's partial takes its ring's place");
 };
-
-constexpr int kPartHead = 2 * kMaxGroup;         // m[8], l[8] in front of a partial's rows
 
 // l is kept 2^-5 smaller than it is: with steps of 2^-106 to 2^121 it stays a normal number for 2^16 tokens and more.
 constexpr int kCacheSumBias = 5;
+
+template <bool k8>
+__device__ __forceinline__ float sum_bias()
+{
+    return k8 ? __uint_as_float((uint32_t)(127 - kCacheSumBias) << 23) : 1.f;
+}
 
 __device__ __forceinline__ uint32_t sub_1152(uint32_t x)
 {
@@ -170,12 +186,26 @@ __device__ __forceinline__ void records_to_half(uint32_t x, uint32_t &even, uint
     odd = sub_1152(((x >> 8) & 0x00ff00ffu) ^ 0x64806480u);
 }
 
-__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+// D(16x8, fp32) += A(16x16, row) * B(16x8, col), fp16 or bf16.  Not volatile, so that independent products overlap.
+template <bool kHalf>
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    if constexpr (!kHalf)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// D(16x8, int32) += A(16x32, int8, row) * B(32x8, int8, col)
+__device__ __forceinline__ void mma_s8_16832(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
@@ -185,50 +215,484 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return d;
 }
 
+// Byte offset of the 16 bytes c of a row within a page's box, as TMA's swizzle lays them.
 template <int D, bool k8>
-__global__ void __launch_bounds__(CacheAttnLayout<D, k8>::kWarps * 32, 1)
-cache_attn_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParams p)
+__device__ __forceinline__ int piece_at(int row, int c)
 {
-    using Lay = CacheAttnLayout<D, k8>;
-    constexpr int W = Lay::kWarps, NS = Lay::kStages, kSteps16 = D / 16;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int span = blockIdx.x * W + warp;
-    const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
-    const uint32_t ring = smem_u32(smem) + warp * Lay::kRingBytes;
-    const uint32_t step_ring = smem_u32(smem + Lay::kStepsOff) + warp * NS * kPagesPerTile * 8;
-    const uint32_t bars = smem_u32(smem + Lay::kBarOff) + warp * NS * 8;
-    if (lane == 0) {
-        prefetch_tensormap(&tmap);
-        // a stage is full when its boxes have landed and, 8-bit, the copies of its steps by lanes 0 and 1
-        for (int s = 0; s < NS; ++s) mbar_init(bars + s * 8, k8 ? 1 + kPagesPerTile : 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        fence_proxy_async();
-    }
-    __syncwarp();
-    grid_dependency_wait();                       // every input may come from the preceding kernel
-    grid_launch_dependents();
+    if constexpr (k8 && D == 64) return row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+    else return row * 128 + ((c ^ (row & 7)) << 4);
+}
 
-    if (span == 0) {                              // requests of unusable length: rows cleared, status
-        const int row_elems = p.q_pass * heads * D;
-        for (int base = 0; base < p.batch; base += 32) {
-            const int r = base + lane;
-            unsigned todo = __ballot_sync(0xffffffffu, r < p.batch && visited_pages(__ldg(p.seq_lens + r), p).tiles == 0);
-            if (todo && lane == 0) atomicOr(p.status, kStatusBadLength);
-            for (; todo; todo &= todo - 1) {
-                uint4 *row = (uint4 *)(p.out + ((size_t)(base + __ffs(todo) - 1) * p.q_len + p.q_base) * heads * D);
-                for (int i = lane; i < row_elems / 8; i += 32) row[i] = make_uint4(0u, 0u, 0u, 0u);
+// One warp's part of a pair: its queries, what it sees, and what it has summed.  Columns of the matrix products are
+// (new token c / G, head c % G), ncols of the eight live; a lane accumulates columns g0 and g0 + 1.
+template <int D, bool k8>
+struct PairPart {
+    static constexpr int kSteps16 = D / 16, kQueryRegs = k8 ? 3 * D / 32 : D / 16;
+    uint32_t qf[kQueryRegs][2];     // B fragments; 8-bit: D / 32 of the queries' high bytes, then of the middle and the low ones
+    float qs0, qs1;                 // what a score is multiplied by: scale and, 8-bit, the query's power of two
+    int earliest, pos0, pos1;       // position of the launch's first new token, and of the lane's columns' tokens
+    int i0, i1;                     // those tokens
+    float m0, m1, l0, l1;
+    float o[kSteps16][4];
+
+    __device__ __forceinline__ void begin(const CacheAttnParams &p, int r, int h, int L, int lane)
+    {
+        const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
+        const int g0 = (lane & 3) * 2, c = lane >> 2, j = lane & 3;
+        i0 = min(g0 / G, p.q_pass - 1);
+        i1 = min((g0 + 1) / G, p.q_pass - 1);
+        earliest = L - p.q_len + p.q_base;
+        pos0 = earliest + i0;
+        pos1 = earliest + i1;
+        qs0 = qs1 = p.scale_log2;
+        const uint16_t *row = p.q + (((size_t)r * p.q_len + p.q_base + c / G) * heads + h * G + c % G) * D;
+        if constexpr (k8) {
+            // four elements of every 16 of column lane / 4
+            uint2 raw[kSteps16];
+            uint32_t most = 0;
+#pragma unroll
+            for (int ks = 0; ks < kSteps16; ++ks) {
+                raw[ks] = c < ncols ? __ldg((const uint2 *)(row + ks * 16 + j * 4)) : make_uint2(0u, 0u);
+                most = __vmaxu2(most, __vmaxu2(raw[ks].x & 0x7fff7fffu, raw[ks].y & 0x7fff7fffu));
+            }
+            most = max(most & 0xffffu, most >> 16);
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int e = max((int)(most >> 7), 21);             // biased exponent of the largest
+            const float up = __uint_as_float((uint32_t)(254 + 20 - min(e, 254)) << 23);
+            // with an infinity or a NaN in the query every score is infinite or NaN, and so is the row NaN
+            const float back = most >= 0x7f80u ? NAN : __uint_as_float((uint32_t)(e - 20) << 23) * p.scale_log2;
+#pragma unroll
+            for (int ks = 0; ks < kSteps16; ++ks) {
+                // x up + 1.5 2^23 + 0x8080, rounded to a whole number: its lowest bytes are the digits, plus 128, 128 and 64
+                constexpr float kMagic = 12582912.f + 32896.f;
+                const uint32_t f0 = __float_as_uint(fmaf(__uint_as_float(raw[ks].x << 16), up, kMagic));
+                const uint32_t f1 = __float_as_uint(fmaf(__uint_as_float(raw[ks].x & 0xffff0000u), up, kMagic));
+                const uint32_t f2 = __float_as_uint(fmaf(__uint_as_float(raw[ks].y << 16), up, kMagic));
+                const uint32_t f3 = __float_as_uint(fmaf(__uint_as_float(raw[ks].y & 0xffff0000u), up, kMagic));
+                const uint32_t a = __byte_perm(f0, f1, 0x5140), b = __byte_perm(f2, f3, 0x5140);
+                qf[ks / 2][ks % 2] = (__byte_perm(__byte_perm(f0, f1, 0x0062), __byte_perm(f2, f3, 0x0062), 0x5410) + 0x40404040u) ^ 0x80808080u;
+                qf[D / 32 + ks / 2][ks % 2] = __byte_perm(a, b, 0x7632) ^ 0x80808080u;
+                qf[2 * (D / 32) + ks / 2][ks % 2] = __byte_perm(a, b, 0x5410) ^ 0x80808080u;
+            }
+            qs0 = __shfl_sync(0xffffffffu, back, g0 * 4);
+            qs1 = __shfl_sync(0xffffffffu, back, g0 * 4 + 4);
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < kSteps16; ++ks) {
+                qf[ks][0] = c < ncols ? __ldg((const uint32_t *)row + ks * 8 + j) : 0u;
+                qf[ks][1] = c < ncols ? __ldg((const uint32_t *)row + ks * 8 + 4 + j) : 0u;
+            }
+        }
+        m0 = m1 = -INFINITY;
+        l0 = l1 = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < kSteps16; ++ks) o[ks][0] = o[ks][1] = o[ks][2] = o[ks][3] = 0.f;
+    }
+
+    __device__ __forceinline__ static bool sees(int pos, int t, const CacheAttnParams &p)
+    {
+        return t <= pos && (p.window <= 0 || t > pos - p.window || t < p.sink);
+    }
+
+    // A tile in shared memory at sb, its steps at steps.
+    __device__ __forceinline__ void tile(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
+    {
+        constexpr int kPageBytes = 32 * D * (k8 ? 1 : 2), kHalfBytes = 32 * 128;
+        const int row16 = (lane & 7) + ((lane >> 3) & 1) * 8;    // ldmatrix: this lane's row of a page's keys
+        const int np = min(kPagesPerTile, vis.count - ti * kPagesPerTile);
+        const int latest = earliest + p.q_pass - 1;
+        int base[kPagesPerTile];                 // first token of each page
+        bool all_seen = np == kPagesPerTile;
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+            const int v = ti * kPagesPerTile + mt;
+            base[mt] = (v < vis.head ? v : v + vis.skip) * kPageSize;
+            all_seen = all_seen && base[mt] + kPageSize - 1 <= earliest &&
+                       (p.window <= 0 || base[mt] > latest - p.window || base[mt] + kPageSize <= p.sink);
+        }
+        // ---- S^T = K Q^T
+        float s[kPagesPerTile][4];
+        if constexpr (k8) {
+            int d[kPagesPerTile][3][4];
+#pragma unroll
+            for (int i = 0; i < kPagesPerTile * 12; ++i) (&d[0][0][0])[i] = 0;
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+#pragma unroll
+                for (int mt = 0; mt < kPagesPerTile; ++mt) {
+                    if (mt >= np) continue;
+                    uint32_t a[4];
+                    ldmatrix_x4(a, sb + mt * kPageBytes + piece_at<D, k8>(row16, 2 * ks + (lane >> 4)));
+#pragma unroll
+                    for (int digit = 0; digit < 3; ++digit) mma_s8_16832(d[mt][digit], a, qf[digit * (D / 32) + ks][0], qf[digit * (D / 32) + ks][1]);
+                }
+            }
+#pragma unroll
+            for (int mt = 0; mt < kPagesPerTile; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[mt][i] = fmaf((float)d[mt][0][i], 65536.f, (float)(d[mt][1][i] * 256 + d[mt][2][i]));
+        } else {
+#pragma unroll
+            for (int mt = 0; mt < kPagesPerTile; ++mt) s[mt][0] = s[mt][1] = s[mt][2] = s[mt][3] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < kSteps16; ++ks) {
+#pragma unroll
+                for (int mt = 0; mt < kPagesPerTile; ++mt) {
+                    if (mt >= np) continue;
+                    uint32_t a[4];
+                    ldmatrix_x4(a, sb + mt * kPageBytes + (ks / 4) * kHalfBytes + piece_at<D, k8>(row16, ks % 4 * 2 + (lane >> 4)));
+                    mma_16816<k8>(s[mt], a[0], a[1], a[2], a[3], qf[ks][0], qf[ks][1]);
+                }
+            }
+        }
+        // ---- scores in the log2 domain, V's step among them
+        float wl[kPagesPerTile];                 // what a weight counts for in l
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+            float a0 = qs0, a1 = qs1, add = 0.f;
+            wl[mt] = 1.f;
+            if constexpr (k8) {
+                float ks, vs;
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(steps + mt * 8));
+                const int e = (int)(__float_as_uint(vs) >> 23 & 255u);
+                a0 *= ks;
+                a1 *= ks;
+                add = (float)(e - 127) + (vs - vs);              // NaN where the block is
+                wl[mt] = __uint_as_float((uint32_t)max(254 - kCacheSumBias - e, 0) << 23);
+            }
+            s[mt][0] = fmaf(s[mt][0], a0, add);
+            s[mt][1] = fmaf(s[mt][1], a1, add);
+            s[mt][2] = fmaf(s[mt][2], a0, add);
+            s[mt][3] = fmaf(s[mt][3], a1, add);
+            if (!all_seen) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = base[mt] + (lane >> 2) + (i >= 2 ? 8 : 0);
+                    if (mt >= np || !sees(i & 1 ? pos1 : pos0, token, p)) s[mt][i] = -INFINITY;      // selected, never multiplied
+                }
+            }
+            mx0 = fmaxf(mx0, fmaxf(s[mt][0], s[mt][2]));
+            mx1 = fmaxf(mx1, fmaxf(s[mt][1], s[mt][3]));
+        }
+        // The reference that a column's exponentials are taken against moves only when a score exceeds it by
+        // more than 2^8; a column with nothing above -inf so far takes them against 0: they come out 0.
+        if (__any_sync(0xffffffffu, mx0 > m0 + 8.f || mx1 > m1 + 8.f)) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) {
+                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, x));
+                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, x));
+            }
+            const float old0 = m0, old1 = m1;
+            m0 = fmaxf(m0, mx0);
+            m1 = fmaxf(m1, mx1);
+            const float al0 = fast_exp2(old0 - (m0 == -INFINITY ? 0.f : m0)), al1 = fast_exp2(old1 - (m1 == -INFINITY ? 0.f : m1));
+            l0 *= al0;
+            l1 *= al1;
+#pragma unroll
+            for (int c = 0; c < kSteps16; ++c) { o[c][0] *= al0; o[c][2] *= al0; o[c][1] *= al1; o[c][3] *= al1; }
+        }
+        const float ref0 = m0 == -INFINITY ? 0.f : m0, ref1 = m1 == -INFINITY ? 0.f : m1;
+        uint32_t pb[kPagesPerTile][2];
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+            const float p0 = fast_exp2(s[mt][0] - ref0), p1 = fast_exp2(s[mt][1] - ref1);
+            const float p2 = fast_exp2(s[mt][2] - ref0), p3 = fast_exp2(s[mt][3] - ref1);
+            l0 = fmaf(p0 + p2, wl[mt], l0);
+            l1 = fmaf(p1 + p3, wl[mt], l1);
+            pb[mt][0] = movmatrix_trans(k8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1));          // tokens 0..7 of the page
+            pb[mt][1] = movmatrix_trans(k8 ? pack_f16x2(p2, p3) : pack_bf16x2(p2, p3));          // tokens 8..15
+        }
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+            if (mt >= np) continue;
+            const uint32_t vb = sb + mt * kPageBytes;
+            if constexpr (k8) {
+#pragma unroll
+                for (int c = 0; c < kSteps16; c += 2) {
+                    uint32_t x[4], lo0, hi0, lo1, hi1;
+                    ldmatrix_x4_trans(x, vb + piece_at<D, k8>(16 + row16, c + (lane >> 4)));
+                    records_to_half(x[0], lo0, hi0);
+                    records_to_half(x[1], lo1, hi1);
+                    mma_16816<k8>(o[c], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
+                    records_to_half(x[2], lo0, hi0);
+                    records_to_half(x[3], lo1, hi1);
+                    mma_16816<k8>(o[c + 1], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
+                }
+            } else {
+                const int vrow = 16 + (lane & 7) + (lane >> 4) * 8, vsel = (lane >> 3) & 1;
+                if (all_seen) {
+#pragma unroll
+                    for (int c = 0; c < kSteps16; ++c) {
+                        uint32_t a[4];
+                        ldmatrix_x4_trans(a, vb + (c / 4) * kHalfBytes + piece_at<D, k8>(vrow, c % 4 * 2 + vsel));
+                        mma_16816<k8>(o[c], a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < p.q_pass; ++i) {         // one new token's columns, the rows it sees
+                        uint32_t keep[2];
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const int t = base[mt] + half * 8 + (lane & 3) * 2;
+                            keep[half] = (sees(earliest + i, t, p) ? 0xffffu : 0u) | (sees(earliest + i, t + 1, p) ? 0xffff0000u : 0u);
+                        }
+#pragma unroll
+                        for (int c = 0; c < kSteps16; ++c) {
+                            uint32_t a[4];
+                            ldmatrix_x4_trans(a, vb + (c / 4) * kHalfBytes + piece_at<D, k8>(vrow, c % 4 * 2 + vsel));
+                            a[0] &= keep[0]; a[1] &= keep[0]; a[2] &= keep[1]; a[3] &= keep[1];
+                            float x[4] = {0.f, 0.f, 0.f, 0.f};   // other tokens' columns may hold anything
+                            mma_16816<k8>(x, a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                            if (i0 == i) { o[c][0] += x[0]; o[c][2] += x[2]; }
+                            if (i1 == i) { o[c][1] += x[1]; o[c][3] += x[3]; }
+                        }
+                    }
+                }
             }
         }
     }
+
+    // Sum l over the lanes that share a column.
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, x);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+        }
+    }
+
+    // Calls put(column, element, x, y) with pairs of neighbouring elements.  8-bit: a lane holds elements d, d + 1
+    // (d = 16 c + 2 (lane / 4)) of its two columns; bf16: elements d and d + 8 (d = 16 c + lane / 4), and neighbouring
+    // lanes trade, so that each has pairs of one column.
+    template <typename Put>
+    __device__ __forceinline__ void elements(int lane, float f0, float f1, Put put) const
+    {
+        const int g0 = (lane & 3) * 2;
+        const bool odd = (lane >> 2) & 1;
+#pragma unroll
+        for (int c = 0; c < kSteps16; ++c) {
+            const float x0 = o[c][0] * f0, x1 = o[c][1] * f1, y0 = o[c][2] * f0, y1 = o[c][3] * f1;
+            if constexpr (k8) {
+                put(g0, c * 16 + (lane >> 2) * 2, x0, y0);
+                put(g0 + 1, c * 16 + (lane >> 2) * 2, x1, y1);
+            } else {
+                const float tx = __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 4), ty = __shfl_xor_sync(0xffffffffu, odd ? y0 : y1, 4);
+                const int d = c * 16 + (lane >> 3) * 2;
+                put(g0 + odd, d, odd ? tx : x0, odd ? x1 : tx);
+                put(g0 + odd, d + 8, odd ? ty : y0, odd ? y1 : ty);
+            }
+        }
+    }
+
+    // To a partial in shared or global memory.  A warp that gave up leaves NaN.
+    __device__ __forceinline__ void store_partial(float *part, int lane, bool alive) const
+    {
+        using Part = PartLayout<D>;
+        const int g0 = (lane & 3) * 2;
+        if (lane < 4) {
+            *(float2 *)(part + g0) = make_float2(m0, m1);
+            *(float2 *)(part + kMaxGroup + g0) = alive ? make_float2(l0, l1) : make_float2(NAN, NAN);
+        }
+        elements(lane, 1.f, 1.f, [&](int g, int d, float x, float y) { *(float2 *)(part + Part::kHead + g * Part::kPitch + d) = make_float2(x, y); });
+    }
+
+    // To the output.
+    __device__ __forceinline__ void store_out(const CacheAttnParams &p, int r, int h, int lane, bool alive) const
+    {
+        const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
+        uint16_t *rows = p.out + ((size_t)r * p.q_len + p.q_base) * heads * D + (size_t)h * G * D;
+        const float bias = sum_bias<k8>();
+        // (O bias) / l: with the largest steps O / l alone would overflow
+        elements(lane, bias, bias, [&](int g, int d, float x, float y) {
+            const float inv = 1.f / ((g & 1) ? l1 : l0);
+            if (alive && g < ncols) *(uint32_t *)(rows + ((size_t)(g / G) * heads + g % G) * D + d) = pack_bf16x2(x * inv, y * inv);
+        });
+    }
+};
+
+// A column of partials folded by one warp, in their order: the lane's elements are 4 lane .. 4 lane + 3.
+struct FoldSum {
+    float m, l;
+    float4 acc;
+};
+
+// Partial i is at(i), in shared or global memory, for i in the list: list(i) is the one behind i (>= n: none), and
+// candidates of the maximum are spread over the lanes.
+template <int D, typename At, typename Next>
+__device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at, Next next)
+{
+    using Part = PartLayout<D>;
+    FoldSum f = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int i = lane; i < n; i += 32)
+        if (next(i - 1) == i) f.m = fmaxf(f.m, at(i)[col]);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) f.m = fmaxf(f.m, __shfl_xor_sync(0xffffffffu, f.m, x));
+    const float ref = f.m == -INFINITY ? 0.f : f.m;
+#pragma unroll 4
+    for (int i = next(-1); i < n; i = next(i)) {
+        const float *part = at(i);
+        const float w = fast_exp2(part[col] - ref);
+        f.l += w * part[kMaxGroup + col];
+        if (lane * 4 < D) {
+            const float4 a = *(const float4 *)(part + Part::kHead + col * Part::kPitch + lane * 4);
+            f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;
+        }
+    }
+    return f;
+}
+
+template <int D, typename At>
+__device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at)
+{
+    return fold_column<D>(n, col, lane, at, [](int i) { return i + 1; });
+}
+
+template <int D>
+__device__ __forceinline__ void store_fold(const CacheAttnParams &p, int r, int h, int col, const FoldSum &f, float bias, int lane)
+{
+    const int G = p.group, heads = p.num_kv_heads * G;
+    const float inv = 1.f / f.l;
+    uint16_t *row = p.out + ((size_t)r * p.q_len + p.q_base + col / G) * heads * D + (size_t)(h * G + col % G) * D;
+    if (lane * 4 < D)
+        *(uint2 *)(row + lane * 4) = make_uint2(pack_bf16x2(f.acc.x * bias * inv, f.acc.y * bias * inv), pack_bf16x2(f.acc.z * bias * inv, f.acc.w * bias * inv));
+}
+
+template <int D>
+__device__ __forceinline__ void store_fold_partial(float *part, int col, const FoldSum &f, int lane)
+{
+    using Part = PartLayout<D>;
+    if (lane == 0) { part[col] = f.m; part[kMaxGroup + col] = f.l; }
+    if (lane * 4 < D) *(float4 *)(part + Part::kHead + col * Part::kPitch + lane * 4) = f.acc;
+}
+
+// Requests of unusable length: rows cleared, status.  By one warp of the grid.
+template <int D>
+__device__ __forceinline__ void clear_unusable(const CacheAttnParams &p, int lane)
+{
+    const int heads = p.num_kv_heads * p.group, row_elems = p.q_pass * heads * D;
+    for (int base = 0; base < p.batch; base += 32) {
+        const int r = base + lane;
+        unsigned todo = __ballot_sync(0xffffffffu, r < p.batch && visited_pages(__ldg(p.seq_lens + r), p).tiles == 0);
+        if (todo && lane == 0) atomicOr(p.status, kStatusBadLength);
+        for (; todo; todo &= todo - 1) {
+            uint4 *row = (uint4 *)(p.out + ((size_t)(base + __ffs(todo) - 1) * p.q_len + p.q_base) * heads * D);
+            for (int i = lane; i < row_elems / 8; i += 32) row[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
+// A warp's ring of S tiles: barriers, fills, waits.
+template <int D, bool k8, int W, int S>
+struct TileRing {
+    using Lay = CacheAttnLayout<D, k8, W, S>;
+    uint32_t ring, steps, bars;
+    int issued, done;
+    bool alive;
+
+    __device__ __forceinline__ void init(uint8_t *smem, int warp, int lane, const CUtensorMap *tmap)
+    {
+        ring = smem_u32(smem) + warp * Lay::kRingBytes;
+        steps = smem_u32(smem + Lay::kStepsOff) + warp * S * kPagesPerTile * 8;
+        bars = smem_u32(smem + Lay::kBarOff) + warp * S * 8;
+        issued = done = 0;
+        alive = true;
+        if (lane == 0) {
+            prefetch_tensormap(tmap);
+            // a stage is full when its boxes have landed and, 8-bit, the copies of its steps by lanes 0 and 1
+            for (int s = 0; s < S; ++s) mbar_init(bars + s * 8, k8 ? 1 + kPagesPerTile : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            fence_proxy_async();
+        }
+        __syncwarp();
+    }
+
+    // Fill the next stage with a tile of np pages of kv head h; lane i holds the id of its page i / kBoxes.
+    __device__ __forceinline__ void issue(const CUtensorMap *tmap, const CacheAttnParams &p, int h, int np, int page, uint64_t policy, int lane)
+    {
+        const int stage = issued % S, pg = lane / Lay::kBoxes, box = lane % Lay::kBoxes;
+        const uint32_t bar = bars + stage * 8;
+        if (lane == 0) mbar_arrive_expect_tx(bar, np * Lay::kPageBytes);
+        __syncwarp();
+        if (pg < np) {
+            if (page < 0 || page >= p.num_pages) {
+                atomicOr(p.status, kStatusBadPage);
+                page = 0;
+            }
+            const int block = (p.layer_page_base + page) * p.num_kv_heads + h;
+            tma_load_2d(ring + stage * Lay::kTileBytes + pg * Lay::kPageBytes + box * Lay::kHalfBytes, tmap, box * 64, block * 32, bar, policy);
+            if constexpr (k8)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8;"
+                             ::"r"(steps + (stage * kPagesPerTile + pg) * 8), "l"(p.steps + block) : "memory");
+        }
+        if constexpr (k8) {
+            if (lane < kPagesPerTile) asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+        }
+        ++issued;
+    }
+
+    // Wait for the oldest stage; false once a wait has given up.
+    __device__ __forceinline__ bool wait(uint32_t *status)
+    {
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait_bounded(bars + done % S * 8, (done / S) & 1, status));
+        return alive;
+    }
+    __device__ __forceinline__ uint32_t tile() const { return ring + done % S * Lay::kTileBytes; }
+    __device__ __forceinline__ uint32_t tile_steps() const { return steps + done % S * kPagesPerTile * 8; }
+    __device__ __forceinline__ void drain(uint32_t *status) const
+    {
+        // do not go on while copies may be in flight (only after a wait gave up)
+        if (!alive)
+            for (int i = max(0, issued - S); i < issued; ++i) mbar_wait_bounded(bars + (i % S) * 8, (i / S) & 1, status);
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Even spans of all pairs' tiles.
+// ------------------------------------------------------------------------------------------
+template <int D, bool k8>
+struct SpanShape {
+    static constexpr int kWarps = k8 ? 12 : 6, kStages = D == 128 ? 2 : 4;
+    using Layout = CacheAttnLayout<D, k8, kWarps, kStages>;
+};
+
+// What a warp leaves of a pair that its span cuts: [2 w] of its first piece, if others follow it (the partial is
+// in global memory, since the ring is still in use), [2 w + 1] of its last piece (in its ring).
+struct Contribution {
+    int r, h;                       // r = -1: none
+    int first, last;                // the CTAs that hold the pair's first and last tiles
+};
+
+template <int D, bool k8>
+__global__ void __launch_bounds__(SpanShape<D, k8>::kWarps * 32, 1)
+cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParams p)
+{
+    using Shape = SpanShape<D, k8>;
+    using Part = PartLayout<D>;
+    constexpr int W = Shape::kWarps, S = Shape::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Contribution s_left[2 * W];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int span = blockIdx.x * W + warp;
+    TileRing<D, k8, W, S> ring;
+    ring.init(smem, warp, lane, &tmap);
+    if (lane < 2) s_left[2 * warp + lane].r = -1;
+    __syncwarp();
+    grid_dependency_wait();                       // every input may come from the preceding kernel
+    grid_launch_dependents();
+    if (threadIdx.x == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
+
+    if (span == 0) clear_unusable<D>(p, lane);
     const long long q_units = span_units(p, lane), begin = span * q_units, end = begin + q_units;
-    TilePlace ic = span_begin(p, begin, end, lane);
-    int4 cut = make_int4(-1, -1, -1, -1);
+    TilePlace ic = span_begin(p, begin, end, lane);              // the next tile to fetch
+    TilePlace cc = ic;                                           // the next to compute
 
     const uint64_t policy = l2_evict_first_policy();
-    // ---- issue side: the next tile to fetch, and its pages: lane i holds page 32 * chunk + i of the pair's visited ones
-    TilePlace cc = ic;                            // compute side
+    // lane i holds page 32 * chunk + i of the pair's visited ones
     constexpr int kTilesPerChunk = 32 / kPagesPerTile;
     auto load_chunk = [&](int r, const Visited &vis, int chunk) {
         const int v = chunk * 32 + lane;
@@ -239,7 +703,6 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParam
         chunk_now = load_chunk(ic.r, ic.vis, ic.tile / kTilesPerChunk);
         chunk_next = load_chunk(ic.r, ic.vis, ic.tile / kTilesPerChunk + 1);
     }
-    int issued = 0;
     // Moves to the next tile of the axis; false at the span's end.
     auto advance = [&](TilePlace &at) {
         ++at.v;
@@ -258,28 +721,9 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParam
     };
     bool more = ic.r >= 0;
     auto issue_next = [&]() {
-        const int stage = issued % NS;
         const int np = min(kPagesPerTile, ic.vis.count - ic.tile * kPagesPerTile);
-        const int pg = lane / Lay::kBoxes, box = lane % Lay::kBoxes;
-        int page = __shfl_sync(0xffffffffu, chunk_now, (ic.tile % kTilesPerChunk * kPagesPerTile + pg) & 31);
-        const uint32_t bar = bars + stage * 8;
-        if (lane == 0) mbar_arrive_expect_tx(bar, np * Lay::kPageBytes);
-        __syncwarp();
-        if (pg < np) {
-            if (page < 0 || page >= p.num_pages) {
-                atomicOr(p.status, kStatusBadPage);
-                page = 0;
-            }
-            const int block = (p.layer_page_base + page) * p.num_kv_heads + ic.h;
-            tma_load_2d(ring + stage * Lay::kTileBytes + pg * Lay::kPageBytes + box * Lay::kHalfBytes, &tmap, box * 64, block * 32, bar, policy);
-            if constexpr (k8)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8;"
-                             ::"r"(step_ring + (stage * kPagesPerTile + pg) * 8), "l"(p.steps + block) : "memory");
-        }
-        if constexpr (k8) {
-            if (lane < kPagesPerTile) asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-        }
-        ++issued;
+        const int page = __shfl_sync(0xffffffffu, chunk_now, (ic.tile % kTilesPerChunk * kPagesPerTile + lane / Shape::Layout::kBoxes) & 31);
+        ring.issue(&tmap, p, ic.h, np, page, policy, lane);
         const int r = ic.r, h = ic.h;
         more = advance(ic);
         if (!more) return;
@@ -291,379 +735,220 @@ cache_attn_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParam
             chunk_next = load_chunk(ic.r, ic.vis, ic.tile / kTilesPerChunk + 1);
         }
     };
-    while (issued < NS && more) issue_next();
+    while (ring.issued < S && more) issue_next();
 
-    // ---- compute side
-    const int g0 = (lane & 3) * 2;               // first of the two columns this lane accumulates
-    const int i0 = min(g0 / G, p.q_pass - 1), i1 = min((g0 + 1) / G, p.q_pass - 1);              // their new tokens
-    const int row16 = (lane & 7) + ((lane >> 3) & 1) * 8;        // ldmatrix: this lane's row of a page's keys
-    auto piece_at = [&](int row, int c) {        // byte offset of the 16 bytes c of a row in a page's box
-        if constexpr (!k8) return row * 128 + ((c ^ (row & 7)) << 4);
-        else if constexpr (D == 128) return row * 128 + ((c ^ (row & 7)) << 4);
-        else return row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
-    };
-    bool alive = true;
-    int done = 0;
+    float *parked = p.part + (size_t)(2 * gridDim.x + span) * Part::kFloats;
+    float *mine = (float *)(smem + warp * Shape::Layout::kRingBytes);
+    PairPart<D, k8> part;
     bool go = cc.r >= 0;
     while (go) {
-        const int r = cc.r, h = cc.h, L = cc.L, tile0 = cc.tile;
+        const int r = cc.r, h = cc.h, tile0 = cc.tile;
         const Visited vis = cc.vis;
         const int n = (int)min((long long)(vis.tiles - tile0), end - cc.v);
         const long long v0 = cc.v;
-        // ---- queries: column c = (new token c / G, head c % G), this lane holds four elements of every 16 of column lane / 4
-        uint32_t qf[kSteps16][2];
-        float qs0 = p.scale_log2, qs1 = p.scale_log2;
-        {
-            const int c = lane >> 2, j = lane & 3;
-            const uint16_t *row = p.q + (((size_t)r * p.q_len + p.q_base + c / G) * heads + h * G + c % G) * D;
-            if constexpr (k8) {
-                uint2 raw[kSteps16];
-                uint32_t most = 0;
-#pragma unroll
-                for (int ks = 0; ks < kSteps16; ++ks) {
-                    raw[ks] = c < ncols ? __ldg((const uint2 *)(row + ks * 16 + j * 4)) : make_uint2(0u, 0u);
-                    most = max(max(most, raw[ks].x & 0x7fffu), max(raw[ks].x >> 16 & 0x7fffu, max(raw[ks].y & 0x7fffu, raw[ks].y >> 16 & 0x7fffu)));
-                }
-                most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-                most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                // the largest comes to lie in [2^7, 2^8); infinities stay, and what is left beside them does not matter
-                const int e = min(max((int)(most >> 7), 8), 254);                // biased exponent
-                const float up = __uint_as_float((uint32_t)(254 + 7 - e) << 23);
-                float back = __uint_as_float((uint32_t)max(e - 7, 1) << 23) * p.scale_log2;
-#pragma unroll
-                for (int ks = 0; ks < kSteps16; ++ks) {
-                    const float x0 = __uint_as_float(raw[ks].x << 16), x1 = __uint_as_float(raw[ks].x & 0xffff0000u);
-                    const float x2 = __uint_as_float(raw[ks].y << 16), x3 = __uint_as_float(raw[ks].y & 0xffff0000u);
-                    qf[ks][0] = pack_f16x2(x0 * up, x2 * up);
-                    qf[ks][1] = pack_f16x2(x1 * up, x3 * up);
-                }
-                qs0 = __shfl_sync(0xffffffffu, back, g0 * 4);
-                qs1 = __shfl_sync(0xffffffffu, back, g0 * 4 + 4);
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < kSteps16; ++ks) {
-                    qf[ks][0] = c < ncols ? __ldg((const uint32_t *)row + ks * 8 + j) : 0u;
-                    qf[ks][1] = c < ncols ? __ldg((const uint32_t *)row + ks * 8 + 4 + j) : 0u;
-                }
-            }
-        }
-        const int earliest = L - p.q_len + p.q_base;
-        const int pos0 = earliest + i0, pos1 = earliest + i1, latest = earliest + p.q_pass - 1;
-        // the first token of each window
-        const int from0 = p.window > 0 ? pos0 - p.window + 1 : 0, from1 = p.window > 0 ? pos1 - p.window + 1 : 0;
-        const int from_latest = p.window > 0 ? latest - p.window + 1 : 0;
-        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-        float o[kSteps16][4];
-#pragma unroll
-        for (int c = 0; c < kSteps16; ++c) o[c][0] = o[c][1] = o[c][2] = o[c][3] = 0.f;
-
+        part.begin(p, r, h, cc.L, lane);
 #pragma unroll 1
-        for (int ti = tile0; ti < tile0 + n; ++ti, ++done) {
-            const int stage = done % NS;
-            if (alive) alive = __all_sync(0xffffffffu, mbar_wait_bounded(bars + stage * 8, (done / NS) & 1, p.status));
-            if (!alive) continue;
-            const uint32_t sb = ring + stage * Lay::kTileBytes;
-            const int np = min(kPagesPerTile, vis.count - ti * kPagesPerTile);
-            int base[kPagesPerTile];             // first token of each page
-            bool all_seen = np == kPagesPerTile;
-#pragma unroll
-            for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                const int v = ti * kPagesPerTile + mt;
-                base[mt] = (v < vis.head ? v : v + vis.skip) * kPageSize;
-                all_seen = all_seen && base[mt] + kPageSize - 1 <= earliest && (base[mt] >= from_latest || base[mt] + kPageSize <= p.sink);
-            }
-            // ---- S^T = K Q^T
-            float s[kPagesPerTile][4];
-#pragma unroll
-            for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                s[mt][0] = s[mt][1] = s[mt][2] = s[mt][3] = 0.f;
-                if (mt < np) {
-                    const uint32_t kb = sb + mt * Lay::kPageBytes;
-                    if constexpr (k8) {
-#pragma unroll
-                        for (int c = 0; c < kSteps16; c += 2) {
-                            uint32_t x[4], lo0, hi0, lo1, hi1;
-                            ldmatrix_x4(x, kb + piece_at(row16, c + (lane >> 4)));
-                            records_to_half(x[0], lo0, hi0);
-                            records_to_half(x[1], lo1, hi1);
-                            mma_f16_16816(s[mt], lo0, lo1, hi0, hi1, qf[c][0], qf[c][1]);
-                            records_to_half(x[2], lo0, hi0);
-                            records_to_half(x[3], lo1, hi1);
-                            mma_f16_16816(s[mt], lo0, lo1, hi0, hi1, qf[c + 1][0], qf[c + 1][1]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int ks = 0; ks < kSteps16; ++ks) {
-                            uint32_t a[4];
-                            ldmatrix_x4(a, kb + (ks / 4) * Lay::kHalfBytes + piece_at(row16, ks % 4 * 2 + (lane >> 4)));
-                            mma_bf16_16816(s[mt], a, qf[ks][0], qf[ks][1]);
-                        }
-                    }
-                }
-            }
-            // ---- scores in the log2 domain, V's step among them
-            float wl[kPagesPerTile];             // what a weight counts for in l
-            float mx0 = -INFINITY, mx1 = -INFINITY;
-#pragma unroll
-            for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                float a0 = qs0, a1 = qs1, add = 0.f;
-                wl[mt] = 1.f;
-                if constexpr (k8) {
-                    float ks, vs;
-                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(step_ring + (stage * kPagesPerTile + mt) * 8));
-                    const int e = (int)(__float_as_uint(vs) >> 23 & 255u);
-                    a0 *= ks;
-                    a1 *= ks;
-                    add = (float)(e - 127) + (vs - vs);                          // NaN where the block is
-                    wl[mt] = __uint_as_float((uint32_t)max(254 - kCacheSumBias - e, 0) << 23);
-                }
-                s[mt][0] = fmaf(s[mt][0], a0, add);
-                s[mt][1] = fmaf(s[mt][1], a1, add);
-                s[mt][2] = fmaf(s[mt][2], a0, add);
-                s[mt][3] = fmaf(s[mt][3], a1, add);
-                if (!all_seen) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = base[mt] + (lane >> 2) + (i >= 2 ? 8 : 0);
-                        const int pos = i & 1 ? pos1 : pos0, from = i & 1 ? from1 : from0;
-                        if (mt >= np || t > pos || (t < from && t >= p.sink)) s[mt][i] = -INFINITY;            // selected, never multiplied
-                    }
-                }
-                mx0 = fmaxf(mx0, fmaxf(s[mt][0], s[mt][2]));
-                mx1 = fmaxf(mx1, fmaxf(s[mt][1], s[mt][3]));
-            }
-            // The reference that a column's exponentials are taken against moves only when a score exceeds it by
-            // more than 2^8; a column with nothing above -inf so far takes them against 0: they come out 0.
-            if (__any_sync(0xffffffffu, mx0 > m0 + 8.f || mx1 > m1 + 8.f)) {
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) {
-                    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, x));
-                    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, x));
-                }
-                const float old0 = m0, old1 = m1;
-                m0 = fmaxf(m0, mx0);
-                m1 = fmaxf(m1, mx1);
-                const float al0 = fast_exp2(old0 - (m0 == -INFINITY ? 0.f : m0)), al1 = fast_exp2(old1 - (m1 == -INFINITY ? 0.f : m1));
-                l0 *= al0;
-                l1 *= al1;
-#pragma unroll
-                for (int c = 0; c < kSteps16; ++c) { o[c][0] *= al0; o[c][2] *= al0; o[c][1] *= al1; o[c][3] *= al1; }
-            }
-            const float ref0 = m0 == -INFINITY ? 0.f : m0, ref1 = m1 == -INFINITY ? 0.f : m1;
-            uint32_t pb[kPagesPerTile][2];
-#pragma unroll
-            for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                const float p0 = fast_exp2(s[mt][0] - ref0), p1 = fast_exp2(s[mt][1] - ref1);
-                const float p2 = fast_exp2(s[mt][2] - ref0), p3 = fast_exp2(s[mt][3] - ref1);
-                l0 = fmaf(p0 + p2, wl[mt], l0);
-                l1 = fmaf(p1 + p3, wl[mt], l1);
-                pb[mt][0] = movmatrix_trans(k8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1));      // tokens 0..7 of the page
-                pb[mt][1] = movmatrix_trans(k8 ? pack_f16x2(p2, p3) : pack_bf16x2(p2, p3));      // tokens 8..15
-            }
-            // ---- O^T += V^T P^T
-#pragma unroll
-            for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                if (mt >= np) continue;
-                const uint32_t vb = sb + mt * Lay::kPageBytes;
-                if constexpr (k8) {
-#pragma unroll
-                    for (int c = 0; c < kSteps16; c += 2) {
-                        uint32_t x[4], lo0, hi0, lo1, hi1;
-                        ldmatrix_x4_trans(x, vb + piece_at(16 + row16, c + (lane >> 4)));
-                        records_to_half(x[0], lo0, hi0);
-                        records_to_half(x[1], lo1, hi1);
-                        mma_f16_16816(o[c], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
-                        records_to_half(x[2], lo0, hi0);
-                        records_to_half(x[3], lo1, hi1);
-                        mma_f16_16816(o[c + 1], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
-                    }
-                } else {
-                    const int vrow = 16 + (lane & 7) + (lane >> 4) * 8, vsel = (lane >> 3) & 1;
-                    if (all_seen) {
-#pragma unroll
-                        for (int c = 0; c < kSteps16; ++c) {
-                            uint32_t a[4];
-                            ldmatrix_x4_trans(a, vb + (c / 4) * Lay::kHalfBytes + piece_at(vrow, c % 4 * 2 + vsel));
-                            mma_bf16_16816(o[c], a, pb[mt][0], pb[mt][1]);
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int i = 0; i < p.q_pass; ++i) {                     // one new token's columns, the rows it sees
-                            const int pos = earliest + i, from = p.window > 0 ? pos - p.window + 1 : 0;
-                            uint32_t keep[2];
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const int t = base[mt] + half * 8 + (lane & 3) * 2;
-                                const bool s0 = t <= pos && (t >= from || t < p.sink), s1 = t + 1 <= pos && (t + 1 >= from || t + 1 < p.sink);
-                                keep[half] = (s0 ? 0xffffu : 0u) | (s1 ? 0xffff0000u : 0u);
-                            }
-#pragma unroll
-                            for (int c = 0; c < kSteps16; ++c) {
-                                uint32_t a[4];
-                                ldmatrix_x4_trans(a, vb + (c / 4) * Lay::kHalfBytes + piece_at(vrow, c % 4 * 2 + vsel));
-                                a[0] &= keep[0]; a[1] &= keep[0]; a[2] &= keep[1]; a[3] &= keep[1];
-                                float x[4] = {0.f, 0.f, 0.f, 0.f};               // other tokens' columns may hold anything
-                                mma_bf16_16816(x, a, pb[mt][0], pb[mt][1]);
-                                if (i0 == i) { o[c][0] += x[0]; o[c][2] += x[2]; }
-                                if (i1 == i) { o[c][1] += x[1]; o[c][3] += x[3]; }
-                            }
-                        }
-                    }
-                }
-            }
+        for (int ti = tile0; ti < tile0 + n; ++ti, ++ring.done) {
+            if (!ring.wait(p.status)) continue;
+            part.tile(p, vis, ti, ring.tile(), ring.tile_steps(), lane);
             __syncwarp();                         // the stage has been read
-            if (more) issue_next();               // refill it with the tile NS ahead
+            if (more) issue_next();               // refill it with the tile S ahead
         }
-
-        // ---- the piece's end
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) {
-            l0 += __shfl_xor_sync(0xffffffffu, l0, x);
-            l1 += __shfl_xor_sync(0xffffffffu, l1, x);
-        }
+        part.finish();
         const bool whole = n == vis.tiles;
-        // 8-bit: a lane holds elements d, d + 1 (d = 16 c + 2 (lane / 4)) of its two columns; bf16: elements d and d + 8
-        // (d = 16 c + lane / 4), and neighbouring lanes trade, so that each has a pair of one column
-        const bool odd = (lane >> 2) & 1;
-        if (whole) {
-            const float bias = k8 ? __uint_as_float((uint32_t)(127 - kCacheSumBias) << 23) : 1.f;
-            const float inv0 = 1.f / l0, inv1 = 1.f / l1;
-            uint16_t *rows = p.out + ((size_t)r * p.q_len + p.q_base) * heads * D + (size_t)h * G * D;
-            auto row_of = [&](int c) { return rows + ((size_t)(c / G) * heads + c % G) * D; };
-#pragma unroll
-            for (int c = 0; c < kSteps16; ++c) {
-                const float x0 = o[c][0] * bias * inv0, x1 = o[c][1] * bias * inv1, y0 = o[c][2] * bias * inv0, y1 = o[c][3] * bias * inv1;
-                if constexpr (k8) {
-                    const int d = c * 16 + (lane >> 2) * 2;
-                    if (alive && g0 < ncols) *(uint32_t *)(row_of(g0) + d) = pack_bf16x2(x0, y0);
-                    if (alive && g0 + 1 < ncols) *(uint32_t *)(row_of(g0 + 1) + d) = pack_bf16x2(x1, y1);
-                } else {
-                    const float tx = __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 4), ty = __shfl_xor_sync(0xffffffffu, odd ? y0 : y1, 4);
-                    const int d = c * 16 + (lane >> 3) * 2, col = g0 + odd;
-                    if (alive && col < ncols) {
-                        *(uint32_t *)(row_of(col) + d) = odd ? pack_bf16x2(tx, x1) : pack_bf16x2(x0, tx);
-                        *(uint32_t *)(row_of(col) + d + 8) = odd ? pack_bf16x2(ty, y1) : pack_bf16x2(y0, ty);
-                    }
-                }
-            }
-        } else {
-            // a pair's first piece in slot 2 span + 1, any other in slot 2 span: a span has at most one of each
-            const int slot = 2 * span + (tile0 == 0 ? 1 : 0);
-            float *part = p.part + (size_t)slot * (kPartHead + kMaxGroup * D), *rows = part + kPartHead;
-            if (tile0 == 0) cut = make_int4(r, h, (int)((v0 + vis.tiles - 1) / q_units), 0);
-            if (lane < 4) {
-                // a warp that gave up leaves NaN, not what it had
-                *(float2 *)(part + g0) = make_float2(m0, m1);
-                *(float2 *)(part + kMaxGroup + g0) = alive ? make_float2(l0, l1) : make_float2(NAN, NAN);
-            }
-#pragma unroll
-            for (int c = 0; c < kSteps16; ++c) {
-                if constexpr (k8) {
-                    const int d = c * 16 + (lane >> 2) * 2;
-                    *(float2 *)(rows + g0 * D + d) = make_float2(o[c][0], o[c][2]);
-                    *(float2 *)(rows + (g0 + 1) * D + d) = make_float2(o[c][1], o[c][3]);
-                } else {
-                    const float tx = __shfl_xor_sync(0xffffffffu, odd ? o[c][0] : o[c][1], 4), ty = __shfl_xor_sync(0xffffffffu, odd ? o[c][2] : o[c][3], 4);
-                    const int d = c * 16 + (lane >> 3) * 2, col = g0 + odd;
-                    *(float2 *)(rows + col * D + d) = odd ? make_float2(tx, o[c][1]) : make_float2(o[c][0], tx);
-                    *(float2 *)(rows + col * D + d + 8) = odd ? make_float2(ty, o[c][3]) : make_float2(o[c][2], ty);
-                }
-            }
-        }
-        // on to the next piece
         cc.tile = tile0 + n - 1;
         cc.v = v0 + n - 1;
         go = advance(cc);
-    }
-    // do not leave while copies may be in flight (only after a wait gave up)
-    if (!alive)
-        for (int i = max(0, issued - NS); i < issued; ++i) mbar_wait_bounded(bars + (i % NS) * 8, (i / NS) & 1, p.status);
-    if (lane == 0) p.cuts[span] = cut;
-}
-
-// ------------------------------------------------------------------------------------------
-// The partials of the pairs that spans cut:  M = max m_i,  out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i, in the
-// spans' order, so results are bit-identical from run to run.  A block looks after the cuts of some spans and
-// two of the eight columns; a warp folds a column of few partials, the whole block one of many.
-// ------------------------------------------------------------------------------------------
-constexpr int kFoldWarps = 8, kFoldFew = 16, kFoldBlocks = 148;
-
-template <int D>
-struct FoldSum {
-    float m, l;
-    float4 acc;                     // elements 4 lane .. 4 lane + 3
-};
-
-// Partials first, first + step, ... below n of a pair whose first piece's span is s.
-template <int D>
-__device__ __forceinline__ FoldSum<D> fold_partials(const float *part, int s, int first, int step, int n, int col, int lane)
-{
-    constexpr size_t kSlot = kPartHead + kMaxGroup * D;
-    FoldSum<D> f = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    auto slot = [&](int i) { return part + (size_t)(i == 0 ? 2 * s + 1 : 2 * (s + i)) * kSlot; };
-    for (int i = first + lane * step; i < n; i += 32 * step) f.m = fmaxf(f.m, slot(i)[col]);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) f.m = fmaxf(f.m, __shfl_xor_sync(0xffffffffu, f.m, x));
-    const float ref = f.m == -INFINITY ? 0.f : f.m;
-#pragma unroll 4
-    for (int i = first; i < n; i += step) {
-        const float *at = slot(i);
-        const float w = fast_exp2(at[col] - ref);
-        f.l += w * at[kMaxGroup + col];
-        if (lane * 4 < D) {
-            const float4 a = *(const float4 *)(at + kPartHead + col * D + lane * 4);
-            f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;
+        if (whole) {
+            part.store_out(p, r, h, lane, ring.alive);
+        } else {
+            if (!go) ring.drain(p.status);
+            part.store_partial(go ? parked : mine, lane, ring.alive);
+            const long long pair0 = v0 - tile0;   // the pair's first tile's unit
+            if (lane == 0) s_left[2 * warp + (go ? 0 : 1)] = {r, h, (int)(pair0 / q_units / W), (int)((pair0 + vis.tiles - 1) / q_units / W)};
         }
     }
-    return f;
+    ring.drain(p.status);
+    __syncthreads();
+    // ---- the CTA's fold: consecutive contributions to one pair, a column a warp
+    const Contribution left = s_left[min(lane, 2 * W - 1)];
+    const unsigned there = __ballot_sync(0xffffffffu, lane < 2 * W && left.r >= 0);
+    const unsigned before = there & ((1u << lane) - 1u);
+    const int other = before ? 31 - __clz(before) : lane;
+    const bool leads = (there >> lane & 1u) &&
+                       (before == 0u || s_left[min(other, 2 * W - 1)].r != left.r || s_left[min(other, 2 * W - 1)].h != left.h);
+    const int ncols = p.q_pass * p.group;
+    int turn = 0;
+    for (unsigned leaders = __ballot_sync(0xffffffffu, leads); leaders != 0u; leaders &= leaders - 1u) {
+        const int a = __ffs(leaders) - 1;
+        const unsigned behind = leaders & (leaders - 1u);        // from the next pair on
+        const unsigned mine_too = there & ~((1u << a) - 1u) & (behind ? (behind & -behind) - 1u : 0xffffffffu);
+        const Contribution c = s_left[a];
+        const bool here = c.first == c.last;     // the whole pair is this CTA's
+        float *slot = p.part + (size_t)(2 * blockIdx.x + (c.first == blockIdx.x ? 1 : 0)) * Part::kFloats;
+        for (int col = 0; col < ncols; ++col) {
+            if (turn++ % W != warp) continue;
+            const FoldSum f = fold_column<D>(
+                2 * W, col, lane,
+                [&](int i) -> const float * {
+                    return i & 1 ? (const float *)(smem + i / 2 * Shape::Layout::kRingBytes) : p.part + (size_t)(2 * gridDim.x + blockIdx.x * W + i / 2) * Part::kFloats;
+                },
+                [&](int i) { const unsigned rest = mine_too >> (i + 1); return rest ? i + __ffs(rest) : 2 * W; });
+            if (here) store_fold<D>(p, c.r, c.h, col, f, sum_bias<k8>(), lane);
+            else store_fold_partial<D>(slot, col, f, lane);
+        }
+        if (!here && c.first == blockIdx.x && threadIdx.x == 0) p.cuts[blockIdx.x] = make_int4(c.r, c.h, c.last, 0);
+    }
 }
 
+// ------------------------------------------------------------------------------------------
+// The pairs that CTAs cut: the first CTA's partial lies in its second slot, the others' in their first.  A block
+// looks after one CTA's cut; its warps take the eight columns, kFoldGroups warps a column.  (The last CTA to arrive folding
+// them in the span kernel saves the launch, and was 1 to 5 us slower in a row of calls: fences and counters at every
+// CTA's end, where this kernel starts under the others' tails.)
+// ------------------------------------------------------------------------------------------
+constexpr int kFoldGroups = 4;
+
 template <int D>
-__global__ void __launch_bounds__(kFoldWarps * 32)
+__global__ void __launch_bounds__(kMaxGroup * kFoldGroups * 32)
 cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
 {
-    __shared__ float s_ml[kFoldWarps][2];
-    __shared__ float4 s_acc[kFoldWarps][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
+    using Part = PartLayout<D>;
+    __shared__ __align__(16) float s_part[kFoldGroups][Part::kFloats];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = warp % kMaxGroup, group = warp / kMaxGroup;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int part_of = blockIdx.x / kFoldBlocks;                // columns part_of and part_of + 4
-    auto store = [&](const int4 &cut, int col, const FoldSum<D> &f) {
-        const float inv = 1.f / f.l;
-        uint16_t *row = p.out + ((size_t)cut.x * p.q_len + p.q_base + col / G) * heads * D + (size_t)(cut.y * G + col % G) * D;
-        if (lane * 4 < D)
-            *(uint2 *)(row + lane * 4) = make_uint2(pack_bf16x2(f.acc.x * bias * inv, f.acc.y * bias * inv), pack_bf16x2(f.acc.z * bias * inv, f.acc.w * bias * inv));
+    const int first = blockIdx.x;
+    const int4 cut = p.cuts[first];
+    if (cut.x < 0) return;
+    const int n = cut.z - first + 1;
+    if (col < p.q_pass * p.group) {
+        const FoldSum f = fold_column<D>((n - group + kFoldGroups - 1) / kFoldGroups, col, lane, [&](int i) -> const float * {
+            const int cta = first + group + i * kFoldGroups;
+            return p.part + (size_t)(2 * cta + (cta == first ? 1 : 0)) * Part::kFloats;
+        });
+        store_fold_partial<D>(s_part[group], col, f, lane);
+    }
+    __syncthreads();
+    if (group == 0 && col < p.q_pass * p.group)
+        store_fold<D>(p, cut.x, cut.y, col, fold_column<D>(kFoldGroups, col, lane, [&](int i) -> const float * { return s_part[i]; }), bias, lane);
+}
+
+// ------------------------------------------------------------------------------------------
+// A cluster of CTAs per pair and block of new tokens; q_pass: new tokens of a block.
+// ------------------------------------------------------------------------------------------
+template <int D, bool k8>
+struct PairShape {
+    static constexpr int kWarps = 6, kStages = (k8 ? 2 : 1) * (D == 128 ? 1 : 2), kCtas = 2;     // CTAs resident on an SM
+    using Layout = CacheAttnLayout<D, k8, kWarps, kStages>;
+    static constexpr int kCtaPartOff = Layout::kRingBytes / 2;   // the CTA's partial lies in the second half of warp 0's ring
+    static_assert(PartLayout<D>::kFloats * 4 <= Layout::kRingBytes / 2, "two partials must fit a ring");
+};
+
+__device__ __forceinline__ float4 ld_dsmem_f32x4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+
+__device__ __forceinline__ float ld_dsmem_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
+    return v;
+}
+
+template <int D, bool k8>
+__global__ void __launch_bounds__(PairShape<D, k8>::kWarps * 32, PairShape<D, k8>::kCtas)
+cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttnParams params)
+{
+    using Shape = PairShape<D, k8>;
+    using Part = PartLayout<D>;
+    constexpr int W = Shape::kWarps, S = Shape::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
+    // blocks of new tokens that the columns hold at a time: neighbours, so that they meet in L2
+    const int per_pass = params.q_pass, passes = (params.q_len + per_pass - 1) / per_pass;
+    CacheAttnParams p = params;
+    p.q_base = blockIdx.x / ctas % passes * per_pass;
+    p.q_pass = min(per_pass, p.q_len - p.q_base);
+    const int pair = blockIdx.x / ctas / passes, r = pair / p.num_kv_heads, h = pair % p.num_kv_heads;
+    const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
+    TileRing<D, k8, W, S> ring;
+    ring.init(smem, warp, lane, &tmap);
+    grid_dependency_wait();                       // every input may come from the preceding kernel
+    grid_launch_dependents();
+    const int L = __ldg(p.seq_lens + r);
+    const Visited vis = visited_pages(L, p);
+    if (vis.tiles == 0) {                         // unusable: the same for the whole cluster
+        if (rank == 0) {
+            for (int i = threadIdx.x; i < ncols * D / 8; i += W * 32) {
+                const int c = i / (D / 8);
+                uint16_t *row = p.out + ((size_t)r * p.q_len + p.q_base + c / G) * heads * D + (size_t)(h * G + c % G) * D;
+                ((uint4 *)row)[i % (D / 8)] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            if (threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
+        }
+        return;
+    }
+    const uint64_t policy = l2_evict_first_policy();
+    const int step = ctas * W;
+    int next = rank * W + warp;                   // the next tile to fetch
+    auto page_of = [&](int tile) {
+        const int v = tile * kPagesPerTile + lane / Shape::Layout::kBoxes;
+        return lane / Shape::Layout::kBoxes < kPagesPerTile && v < vis.count
+                   ? __ldg(p.block_tables + (size_t)r * p.max_pages_per_req + (v < vis.head ? v : v + vis.skip)) : 0;
     };
-    int turn = 0;
-    for (int s = blockIdx.x % kFoldBlocks; s < p.num_spans; s += kFoldBlocks) {
-        const int4 cut = p.cuts[s];
-        if (cut.x < 0) continue;
-        const int n = cut.z - s + 1;
-        for (int col = part_of; col < ncols; col += 4) {
-            if (n <= kFoldFew) {
-                if (turn++ % kFoldWarps == warp) store(cut, col, fold_partials<D>(p.part, s, 0, 1, n, col, lane));
-            } else {
-                const FoldSum<D> f = fold_partials<D>(p.part, s, warp, kFoldWarps, n, col, lane);
-                __syncthreads();                  // the last one has been read
-                if (lane == 0) { s_ml[warp][0] = f.m; s_ml[warp][1] = f.l; }
-                s_acc[warp][lane] = f.acc;
-                __syncthreads();
-                if (warp == 0) {
-                    FoldSum<D> t = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-                    for (int w = 0; w < kFoldWarps; ++w) t.m = fmaxf(t.m, s_ml[w][0]);
-                    const float ref = t.m == -INFINITY ? 0.f : t.m;
-                    for (int w = 0; w < kFoldWarps; ++w) {
-                        const float x = fast_exp2(s_ml[w][0] - ref);
-                        const float4 a = s_acc[w][lane];
-                        t.l += x * s_ml[w][1];
-                        t.acc.x += x * a.x; t.acc.y += x * a.y; t.acc.z += x * a.z; t.acc.w += x * a.w;
-                    }
-                    store(cut, col, t);
-                }
+    int page = page_of(next);
+    auto issue_next = [&]() {
+        const int now = page;
+        page = page_of(next + step);
+        ring.issue(&tmap, p, h, min(kPagesPerTile, vis.count - next * kPagesPerTile), now, policy, lane);
+        next += step;
+    };
+    while (ring.issued < S && next < vis.tiles) issue_next();
+    PairPart<D, k8> part;
+    part.begin(p, r, h, L, lane);
+#pragma unroll 1
+    for (int ti = rank * W + warp; ti < vis.tiles; ti += step, ++ring.done) {
+        if (!ring.wait(p.status)) break;
+        part.tile(p, vis, ti, ring.tile(), ring.tile_steps(), lane);
+        __syncwarp();
+        if (next < vis.tiles) issue_next();
+    }
+    ring.drain(p.status);
+    part.finish();
+    part.store_partial((float *)(smem + warp * Shape::Layout::kRingBytes), lane, ring.alive);
+    __syncthreads();
+    // ---- the CTA's fold, a column a warp
+    float *mine = (float *)(smem + Shape::kCtaPartOff);
+    for (int col = warp; col < ncols; col += W) {
+        const FoldSum f = fold_column<D>(W, col, lane, [&](int i) -> const float * { return (const float *)(smem + i * Shape::Layout::kRingBytes); });
+        if (ctas == 1) store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
+        else store_fold_partial<D>(mine, col, f, lane);
+    }
+    if (ctas == 1) return;
+    cluster_barrier();
+    // ---- the cluster's fold: CTA c takes columns c, c + ctas, ...
+    for (int col = rank + warp * ctas; col < ncols; col += W * ctas) {
+        const uint32_t head = smem_u32(mine) + col * 4, row = smem_u32(mine) + (Part::kHead + col * Part::kPitch + lane * 4) * 4;
+        FoldSum f = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        for (int c = 0; c < ctas; ++c) f.m = fmaxf(f.m, ld_dsmem_f32(cluster_map(head, c)));
+        const float ref = f.m == -INFINITY ? 0.f : f.m;
+        for (int c = 0; c < ctas; ++c) {
+            const float w = fast_exp2(ld_dsmem_f32(cluster_map(head, c)) - ref);
+            f.l += w * ld_dsmem_f32(cluster_map(head + 4 * kMaxGroup, c));
+            if (lane * 4 < D) {
+                const float4 a = ld_dsmem_f32x4(cluster_map(row, c));
+                f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;
             }
         }
+        store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
     }
+    cluster_barrier();                            // nobody leaves while others read its partial
 }
 
 }  // namespace ckv

@@ -64,6 +64,8 @@ def attend(q, k, v, length, window, sink, steps=None):
         out[i], size[i] = w @ v[t], w @ np.abs(v[t])
         mass[i] = (np.abs(q[i]) @ np.abs(k[t]).T / math.sqrt(d)).max(1)
         if steps is not None:
+            # queries are rounded to 2^-21 of their largest element: a quarter of 2^-19 on top of what scores are summed with
+            mass[i] += (np.abs(q[i]).max(1, keepdims=True) * np.abs(k[t]).sum(1)).max(1) / math.sqrt(d) / 4
             # a weight is held as a fraction of a reference no larger than the largest weight * step, in fp16: fractions below
             # 2^-14 are off by 2^-25 at most, times a record of at most 127
             floor[i] = 2.0 ** -25 * 127 * len(t) * (w * steps[t]).max(1)
