@@ -158,45 +158,59 @@ int32_t launch_pages(ckv_pool *pool, const char *fn, const ckv::TablesParams &ar
     for (int i = 0; i < 7; ++i)
         for (int k = i + 1; k < 10; ++k)
             if (overlap(a[i].ptr, a[i].n, a[k].ptr, a[k].n)) return fail(CKV_EINVAL, "%s: two of the arrays overlap", fn);
-    // the sums of 8192 requests, three words each, fit an SM's shared memory; one CTA writes about 8 slots a thread in
-    // the time that a cluster's start costs
+    // the sums of 8192 requests, three words each, fit an SM's shared memory
     static thread_local int configured_device = -1;
     auto kernel = ckv::pages_kernel<kAssign>;
     if (configured_device != pool->device) {
-        CKV_CUDA(allow(kernel, false, sizeof(int) * ckv::kTablesWords * ckv::kMaxBatch));
+        CKV_CUDA(allow(kernel, true, sizeof(int) * ckv::kTablesWords * ckv::kMaxBatch));
         configured_device = pool->device;
     }
-    const long long most = std::max<long long>(batch, tp.n_slots);
-    CKV_CUDA(enqueue(kernel, most > 8192 ? 8 : 1, most > 256 ? 1024 : 256, sizeof(int) * ckv::kTablesWords * batch, pool->overlap, most > 8192 ? 8 : 1,
-                     stream, tp));
+    // A thread for each page or slot that may have to move, in CTAs of few threads, since what a move costs is instructions:
+    // 50000 slots by 256 CTAs of 256 threads 3.7 us, by 64 6.0, by 16 16.0.  In place there are no more than a
+    // cluster's 16, of 1024 threads where that is too few (9.9 us); so many too where a CTA's own sums are long.
+    tp.in_place = tp.lens_out == tp.seq_lens || tp.lens_out == tp.amounts || tp.count_out == tp.free_count;
+    const long long moves = kAssign ? std::max<long long>(tp.n_slots, batch) : tables_n;
+    const unsigned threads = batch > 1024 || (tp.in_place && moves > 4096) ? 1024 : 256;
+    unsigned ctas = 1;
+    while (ctas < (tp.in_place ? 16 : 256) && moves > (long long)threads * ctas) ctas *= 2;
+    CKV_CUDA(enqueue(kernel, ctas, threads, sizeof(int) * ckv::kTablesWords * batch, pool->overlap, tp.in_place ? ctas : 0, stream, tp));
     pool->launches += 1;
     pool->inputs_from_predecessor = true;        // a decode step that follows directly must not read its tables ahead
+    return CKV_OK;
+}
+
+template <typename Tin, typename Tout, int T>
+int32_t launch_logits(ckv::LogitsParams &lp, long long rows, int pieces, void *stream)
+{
+    static thread_local int configured_device = -1, num_sms = 0;
+    auto kernel = ckv::logits_process_kernel<Tin, Tout, T>;
+    constexpr int E = 16 / sizeof(Tin), kMost = T * ckv::kLogitsElements / E;    // pieces of a CTA
+    int device = -1;
+    CKV_CUDA(cudaGetDevice(&device));
+    if (configured_device != device) {
+        CKV_CUDA(allow(kernel, true, 2 * sizeof(uint32_t) * kMost * E));
+        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
+        configured_device = device;
+    }
+    // CTAs of a row: as few as hold it, up to 16 while there are few rows and a slice is more than 2048 tokens
+    unsigned cluster = (unsigned)((pieces + kMost - 1) / kMost);
+    while (cluster < 16 && 2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster) cluster = std::min(16u, 2 * cluster);
+    lp.pieces = (int)((pieces + cluster - 1) / cluster);
+    const int arrays = (lp.history || lp.drafts ? 1 : 0) + (lp.bias_ids ? 1 : 0);
+    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), T, sizeof(uint32_t) * arrays * lp.pieces * E, true, cluster, stream, lp));
     return CKV_OK;
 }
 
 template <typename Tin, typename Tout>
 int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
 {
-    static thread_local int configured_device = -1, num_sms = 0;
-    auto kernel = ckv::logits_process_kernel<Tin, Tout>;
-    int device = -1;
-    CKV_CUDA(cudaGetDevice(&device));
-    if (configured_device != device) {
-        CKV_CUDA(allow(kernel, true, ckv::kLogitsSlice * 4));
-        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
-        configured_device = device;
-    }
-    // CTAs of a row: as few as hold it, more while there are few rows and a slice is more than 2048 tokens
     constexpr int E = 16 / sizeof(Tin);
-    const int pieces = (lp.vocab + 2 * E - 2) / E;               // wherever in its first piece the row begins
     const long long rows = (long long)batch * lp.rows;
-    unsigned cluster = 1;
-    while (cluster < 16 && ((pieces + cluster - 1) / cluster * E > ckv::kLogitsSlice || (2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster)))
-        cluster *= 2;
-    lp.pieces = (int)((pieces + cluster - 1) / cluster);
-    const bool counts = lp.history || lp.drafts || lp.bias_ids;
-    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), ckv::kLogitsThreads, counts ? (size_t)lp.pieces * E * 4 : 0, true, cluster, stream, lp));
-    return CKV_OK;
+    // pieces of a row, wherever in its first one it may begin
+    const bool aligned = aligned16(lp.logits) && (lp.stride % E == 0 || rows == 1);
+    const int pieces = (lp.vocab + (aligned ? E - 1 : 2 * E - 2)) / E;
+    return pieces <= 16 * ckv::kLogitsThreads * ckv::kLogitsElements / E ? launch_logits<Tin, Tout, ckv::kLogitsThreads>(lp, rows, pieces, stream)
+                                                                         : launch_logits<Tin, Tout, 512>(lp, rows, pieces, stream);
 }
 
 }  // namespace

@@ -14,9 +14,9 @@ namespace ckv {
 // requests before.  A request is served if it needs no page, or if the needs of all requests up to and including
 // it fit F: whoever is refused takes nothing, and nobody after it jumps the queue with a need of its own.
 //
-// Latency-bound: a few KB move, after lengths, count and pages have been fetched one after another.  One CTA where
-// that is all; a cluster of CTAs, each of which sums for itself, where many slots are written.  Everything that may
-// be written in place is read before the cluster's barrier.
+// Latency-bound: a few KB move, after lengths, count and pages have been fetched one after another.  Every CTA sums for
+// itself, and CTAs share what is to be moved.  Where lengths or count are written in place the grid is one
+// cluster, and all of them are read before its barrier.
 struct TablesParams {
     int32_t *block_tables;
     const int32_t *seq_lens;
@@ -28,6 +28,7 @@ struct TablesParams {
     long long *slots;               // assign; may be NULL
     uint32_t *status;
     int32_t batch, max_pages_per_req, num_pages, n_slots;
+    int32_t in_place;               // lengths or count are written where they are read: the grid is one cluster
 };
 
 __host__ __device__ __forceinline__ int pages_of(int tokens) { return tokens / kPageSize + (tokens % kPageSize != 0); }
@@ -51,8 +52,9 @@ __device__ __forceinline__ void block_sums(long long &a, long long &b, long long
     __syncthreads();
     long long before_a = 0, before_b = 0;
     total_a = total_b = 0;
+#pragma unroll 4
     for (int w = 0; w < warps; ++w) {
-        if (w < warp) { before_a += s_a[w]; before_b += s_b[w]; }
+        if (w == warp) { before_a = total_a; before_b = total_b; }
         total_a += s_a[w];
         total_b += s_b[w];
     }
@@ -60,16 +62,14 @@ __device__ __forceinline__ void block_sums(long long &a, long long &b, long long
     b = before_b + ib - b;
 }
 
-// The first request whose sum exceeds k; `n` if none does.
+// How many of the `n` sums, which do not decrease, are at most k: the first request whose sum exceeds it.
 __device__ __forceinline__ int first_above(const int *sums, int n, int k)
 {
-    int lo = 0;
-    while (n > 0) {
-        const int half = n / 2;
-        if (sums[lo + half] > k) n = half;
-        else { lo += half + 1; n -= half + 1; }
-    }
-    return lo;
+    int r = 0;
+#pragma unroll 1
+    for (int half = 1 << (31 - __clz(n)); half > 0; half >>= 1)
+        if (r + half <= n && sums[r + half - 1] <= k) r += half;
+    return r;
 }
 
 __device__ __forceinline__ int clamp_int(long long x) { return (int)min(x, 0x7fffffffll); }
@@ -87,10 +87,11 @@ __global__ void __launch_bounds__(1024)
 pages_kernel(const TablesParams p)
 {
     extern __shared__ int s_words[];
-    int *s_upto = s_words, *s_tokens = s_upto + p.batch, *s_len = s_tokens + p.batch;     // s_len: assign the length, release the pages kept
+    // s_len: assign the length, -1 where the request is not served; release the pages kept, -1 where its length is unusable
+    int *s_upto = s_words, *s_tokens = s_upto + p.batch, *s_len = s_tokens + p.batch;
     __shared__ int s_taken;
-    const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
-    const int each = (p.batch + blockDim.x - 1) / blockDim.x, r0 = min((int)threadIdx.x * each, p.batch), r1 = min(r0 + each, p.batch);
+    const int rank = (int)blockIdx.x, ctas = (int)gridDim.x;
+    const int chunk = (p.batch + blockDim.x - 1) / blockDim.x, r0 = min((int)threadIdx.x * chunk, p.batch), r1 = min(r0 + chunk, p.batch);
     const long long room = min((long long)p.max_pages_per_req * kPageSize, 0x7fffffffll);          // tokens that a table can hold
     if (threadIdx.x == 0) s_taken = 0;
     grid_dependency_wait();                       // every input may come from the preceding kernel
@@ -113,25 +114,24 @@ pages_kernel(const TablesParams p)
     block_sums(pages, tokens, total_pages, total_tokens);
     int taken = 0;
     for (int r = r0; r < r1; ++r) {
-        pages += s_upto[r];
-        const int n = s_tokens[r];
+        const int moved = s_upto[r], n = s_tokens[r];
+        pages += moved;
+        if (pages <= F) taken = clamp_int(pages);
+        else if (kAssign && moved > 0) s_len[r] = -1;
         s_upto[r] = clamp_int(pages);
         s_tokens[r] = clamp_int(tokens);
         tokens += n;
-        if (pages <= F) taken = clamp_int(pages);
     }
     if (kAssign && taken > 0) atomicMax(&s_taken, taken);
     __syncthreads();
-    if (ctas > 1) cluster_barrier();              // every CTA has read the inputs
+    if (p.in_place) cluster_barrier();            // every CTA has read the inputs
     taken = kAssign ? s_taken : clamp_int(total_pages);          // pages that move
     auto upto_before = [&](int r) { return r > 0 ? s_upto[r - 1] : 0; };
-    auto served = [&](int r) { return s_len[r] >= 0 && (s_upto[r] == upto_before(r) || s_upto[r] <= F); };
     const int at = rank * blockDim.x + threadIdx.x, stride = ctas * blockDim.x;
-
     if (rank == 0) {
         for (int r = r0; r < r1; ++r) {
             const int L = p.seq_lens[r], x = p.amounts[r];       // this thread alone writes their places
-            const bool ok = kAssign ? served(r) : s_len[r] >= 0;
+            const bool ok = s_len[r] >= 0;
             p.lens_out[r] = !ok ? L : kAssign ? L + x : x;
             if (kAssign && p.step_lens != nullptr) p.step_lens[r] = ok ? L + x : 0;
             if (kAssign && p.new_start != nullptr) p.new_start[r] = s_tokens[r];
@@ -142,35 +142,37 @@ pages_kernel(const TablesParams p)
             *p.count_out = kAssign ? F - taken : (int)min((long long)F + total_pages, (long long)p.num_pages);
         }
     }
+    // (Loops of one step each: the code runs once, cold, and four steps at a time cost 3 us more in fetching it than they saved.)
     if constexpr (kAssign) {
         // the k-th page that is taken; -1 where the list holds none
         auto page_taken = [&](int k) {
             const int id = p.free_pages[F - 1 - k];
             return id >= 0 && id < p.num_pages ? id : -1;
         };
-        for (int k = at; k < taken; k += stride) {
-            const int r = first_above(s_upto, p.batch, k), id = page_taken(k);
+#pragma unroll 1
+        for (long long k = at; k < taken; k += stride) {
+            const int r = first_above(s_upto, p.batch, (int)k), id = page_taken((int)k);
             if (id < 0) atomicOr(p.status, kStatusBadPage);
-            p.block_tables[(size_t)r * p.max_pages_per_req + pages_of(s_len[r]) + k - upto_before(r)] = id;
+            p.block_tables[(size_t)r * p.max_pages_per_req + pages_of(s_len[r]) + (int)k - upto_before(r)] = id;
         }
-        if (p.slots != nullptr) {
-            const int n = (int)min(total_tokens, (long long)p.n_slots);
-            for (int t = at; t < n; t += stride) {
-                const int r = first_above(s_tokens, p.batch, t) - 1;
-                long long slot = -1;
-                if (served(r)) {
-                    const int pos = s_len[r] + t - s_tokens[r], column = pos / kPageSize, held = pages_of(s_len[r]);
-                    const int id = column < held ? p.block_tables[(size_t)r * p.max_pages_per_req + column] : page_taken(upto_before(r) + column - held);
-                    if (id >= 0 && id < p.num_pages) slot = (long long)id * kPageSize + pos % kPageSize;
-                    else atomicOr(p.status, kStatusBadPage);
-                }
-                p.slots[t] = slot;
+        const int n = p.slots != nullptr ? (int)min(total_tokens, (long long)p.n_slots) : 0;
+#pragma unroll 1
+        for (long long t = at; t < n; t += stride) {
+            const int r = first_above(s_tokens, p.batch, (int)t) - 1, L = s_len[r];
+            long long slot = -1;
+            if (L >= 0) {
+                const int pos = L + (int)t - s_tokens[r], column = pos / kPageSize, held = pages_of(L);
+                const int id = column < held ? p.block_tables[(size_t)r * p.max_pages_per_req + column] : page_taken(upto_before(r) + column - held);
+                if (id >= 0 && id < p.num_pages) slot = (long long)id * kPageSize + pos % kPageSize;
+                else atomicOr(p.status, kStatusBadPage);
             }
+            p.slots[t] = slot;
         }
     } else {
-        for (int k = at; k < taken; k += stride) {
-            const int r = first_above(s_upto, p.batch, k);
-            int id = p.block_tables[(size_t)r * p.max_pages_per_req + s_len[r] + k - upto_before(r)];
+#pragma unroll 1
+        for (long long k = at; k < taken; k += stride) {
+            const int r = first_above(s_upto, p.batch, (int)k);
+            int id = p.block_tables[(size_t)r * p.max_pages_per_req + s_len[r] + (int)k - upto_before(r)];
             if (id < 0 || id >= p.num_pages) {
                 atomicOr(p.status, kStatusBadPage);
                 id = -1;

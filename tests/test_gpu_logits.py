@@ -206,6 +206,17 @@ def test_masks_that_leave_nothing_or_one():
     c.check(c.run(probs=False), probs=False)
 
 
+@pytest.mark.parametrize("level", [-5000.0, -150.0, 150.0, 5000.0])
+def test_slices_without_anything_allowed_beside_logits_far_from_zero(level):
+    """Whole slices of a row are masked; what is allowed lies far above or below 0."""
+    c = Case(3, 1, 60000, 13).with_mask(0.0)
+    c.mask[0, 0, 100:120] = c.mask[1, 0, 59990:] = c.mask[2, 0, 20000:40000] = True
+    c.x += level
+    c.check(c.run())
+    c.x[:, :, ::7] = float("-inf")
+    c.check(c.run())
+
+
 def test_what_is_not_finite():
     """NaN and infinities in masked places count for nothing; allowed, they make the row NaN; minus infinity is no weight."""
     c = Case(7, 1, 5000, 6).with_mask(0.5)
