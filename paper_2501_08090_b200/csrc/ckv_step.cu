@@ -54,7 +54,10 @@ int32_t check_rows(const char *fn, int32_t n_tokens, std::initializer_list<Rows>
 }
 
 // CTAs of a launch that has one for every page that a request's last tokens can touch (page_of_tokens).
-unsigned page_ctas(int32_t n_tokens, int32_t batch) { return (unsigned)(n_tokens / ckv::kPageSize + 2 * (long long)batch); }
+unsigned page_ctas(const int32_t *d_start, int32_t n_tokens, int32_t batch)
+{
+    return d_start ? (unsigned)(n_tokens / ckv::kPageSize + 2 * (long long)batch) : (unsigned)(batch * (long long)ckv::pages_touched(n_tokens / batch));
+}
 
 template <int D, bool k8>
 int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *stream)
@@ -265,9 +268,15 @@ int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
     rp.scale = scale;
     ap.records = layer_records(pool, layer);
     ap.steps = all_steps(pool) + layer * blocks_of(c);
+    ap.q_heads_inv = c.num_q_heads > 1 ? ckv::inverse_of(c.num_q_heads) : 0;
     const auto kernel = c.head_dim == 128 ? (interleaved ? ckv::kv8_append_kernel<128, true> : ckv::kv8_append_kernel<128, false>)
                                           : (interleaved ? ckv::kv8_append_kernel<64, true> : ckv::kv8_append_kernel<64, false>);
-    CKV_CUDA(enqueue(kernel, page_ctas(n_tokens, batch), ckv::kAppend8Warps * 32, 0, pool->overlap, 0, stream, ap));
+    // where pages are few, several CTAs a page, as far as they fit the GPU at a time: their blocks and query rows are chains of
+    // look-ups and loads (one token 4.1 us in one CTA, 3.3 in several)
+    const unsigned pages = page_ctas(d_new_start, n_tokens, batch);
+    ap.parts = 1;
+    while (ap.parts < 4 && pages * 2u * ap.parts <= 3u * pool->num_sms) ap.parts *= 2;
+    CKV_CUDA(enqueue(kernel, pages * ap.parts, ckv::kAppend8Warps * 32, 0, pool->overlap, 0, stream, ap));
     pool->launches += 1;
     return CKV_OK;
 }
@@ -304,7 +313,8 @@ int32_t kv8_gather(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
     gp.max_pages_per_req = c.max_pages_per_req;
     gp.num_pages = c.num_pages;
     gp.num_kv_heads = c.num_kv_heads;
-    CKV_CUDA(enqueue(c.head_dim == 128 ? ckv::kv8_gather_kernel<128> : ckv::kv8_gather_kernel<64>, page_ctas(n_tokens, batch), 256, 0, pool->overlap, 0,
+    gp.per_token_inv = ckv::inverse_of(2 * c.num_kv_heads);
+    CKV_CUDA(enqueue(c.head_dim == 128 ? ckv::kv8_gather_kernel<128> : ckv::kv8_gather_kernel<64>, page_ctas(d_start, n_tokens, batch), 256, 0, pool->overlap, 0,
                      stream, gp));
     pool->launches += 1;
     return CKV_OK;
