@@ -13,11 +13,13 @@ namespace ckv {
 //   excluded where the mask's bit is 0;  p_v = 2^((x_v - max x) log2(e) / temperature) / their sum
 //   temperature <= 0: 1 at the first largest, else 0;  nothing allowed, or only minus infinities: all 0
 //
-// Bound by HBM: a logit is read once and a result written once.  A cluster of CTAs owns a row, a CTA a slice of
-// at most 8192 tokens that its threads hold in registers, 32 each, as pieces of 16 aligned bytes.  While they are
-// on their way the CTA counts the history's tokens of its slice, and looks up the biases' last entries, in arrays in
-// shared memory (whole numbers, and the largest of entries: the order of atomics does not show).  Tokens that change
-// are few: a bit tells their thread, which takes them out of its registers and handles them one by one.
+// Bound by HBM: a logit is read once and a result written once.  A cluster of CTAs owns a row, a CTA a slice of it.  The
+// slice is brought into L2 by one bulk prefetch as the CTA starts, and read there twice, as pieces of 16 aligned
+// bytes: for the maximum and the sum, and for the results.  (Held in registers between, 32 tokens a thread, it cost 64
+// registers and two to four CTAs an SM: LOGITS_OLD us for 512 rows of 50257 tokens with everything, against LOGITS_NEW; alone LOGITS_OLD0 against LOGITS_NEW0.)
+// Tokens that change are few.  Meanwhile the CTA marks them, a bit each; the marks before a token give it a place in short
+// arrays in shared memory, where its occurrences are counted and its bias's last entry is found (whole numbers, and
+// the largest of entries: the order of atomics does not show), and where the CTA's threads handle them in turn.
 // The CTAs exchange (max, sum, place of the max) once through distributed shared memory.
 struct LogitsParams {
     const void *logits;
@@ -33,13 +35,12 @@ struct LogitsParams {
     long long history_stride, mask_stride;
     int32_t rows, vocab, n_bias, probs;
     int32_t pieces;                 // pieces of 16 bytes that a CTA owns
+    int32_t marked;                 // tokens of a CTA that can change
 };
 
-// Threads of a CTA: 256, in four CTAs an SM, so that some load while others meet (a row of 50257 tokens in 8 CTAs of 256
-// 59 us for 512 rows, in 4 of 512 63); 512 where sixteen CTAs of 256 do not hold the row.
-constexpr int kLogitsThreads = 256, kLogitsElements = 32;
-// Sixteen slices of 512 threads, less what a row loses to its place within its first and last piece.
-constexpr int kLogitsMaxVocab = 16 * 512 * kLogitsElements - 16;
+constexpr int kLogitsThreads = 256, kLogitsCtas = 6;             // CTAs an SM
+// Words of marks that a CTA has, so that sixteen CTAs hold a row.
+constexpr int kLogitsWords = 2 * kLogitsThreads, kLogitsMaxVocab = 16 * 32 * kLogitsWords - 16;
 
 // The elements of a piece of 16 bytes.
 __device__ __forceinline__ void piece_elements(const uint4 &raw, float (&x)[4])
@@ -84,137 +85,208 @@ __device__ __forceinline__ void store_elements(T *dst, const float *x, bool whol
     }
 }
 
-template <typename Tin, typename Tout, int T>
-__global__ void __launch_bounds__(T, 1024 / T)
+// The allowed ones of a piece's E tokens, from token v on of the row: those in the row whose mask bit is 1.
+template <int E>
+__device__ __forceinline__ uint32_t allowed_bits(const uint32_t *__restrict__ words, int v, int V)
+{
+    const int from = max(0, -v), to = min(E, V - v);
+    uint32_t bits = to > from ? (1u << to) - (1u << from) : 0u;
+    if (words != nullptr) {
+        const int w = v >> 5, last = (V - 1) >> 5;               // a piece before the row's first token begins in word -1
+        const uint32_t lo = w >= 0 && w <= last ? __ldg(words + w) : 0u, hi = (v & 31) > 32 - E && w < last ? __ldg(words + w + 1) : 0u;
+        bits &= __funnelshift_r(lo, hi, v & 31);
+    }
+    return bits;
+}
+
+template <typename Tin, typename Tout>
+__global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
 logits_process_kernel(const LogitsParams p)
 {
-    constexpr int E = 16 / sizeof(Tin), K = kLogitsElements / E;                 // elements of a piece, pieces of a thread
-    constexpr int kWarps = T / 32;
-    extern __shared__ uint32_t s_token[];         // [slice]: times generated, bit 31: in the prompt; then, with biases, [slice]: the entry plus 1
-    __shared__ uint32_t s_changes[T];             // a bit per element of a thread: counted or biased
+    constexpr int T = kLogitsThreads, kWarps = T / 32;
+    constexpr int E = 16 / sizeof(Tin), U = 16 / E;              // elements of a piece, pieces of a thread at a time
+    extern __shared__ uint32_t s_marked[];        // [marked]: the tokens' places in the slice; counts, bit 31: in the prompt, then values; entries plus 1
+    __shared__ uint32_t s_marks[kLogitsWords];    // a bit per token of the slice
+    __shared__ int s_base[kLogitsWords];          // marks before a word's
+    __shared__ int s_total[kWarps];
     __shared__ float s_max[kWarps], s_sum[kWarps];
-    __shared__ int s_at[kWarps];
+    __shared__ unsigned s_at[kWarps];
     __shared__ uint4 s_share[16];                 // every CTA's maximum, sum and place of the maximum, written by them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
     const int row = blockIdx.x / ctas, b = row / p.rows, j = row % p.rows, V = p.vocab;
     const Tin *in = static_cast<const Tin *>(p.logits) + row * p.stride;
     Tout *out = static_cast<Tout *>(p.out) + row * p.out_stride;
+    const uint32_t *words = p.mask != nullptr ? p.mask + row * p.mask_stride : nullptr;
     const int off = (int)(reinterpret_cast<uintptr_t>(in) / sizeof(Tin) % E);    // elements before the row in its first piece
     const int first = rank * p.pieces * E - off, last = min(first + p.pieces * E, V);            // the slice; `first` may lie below 0
-    const unsigned used = (unsigned)max(0, last - first);
-    const bool counted = p.history != nullptr || p.drafts != nullptr, biased = p.bias_ids != nullptr;
-    uint32_t *s_count = s_token, *s_entry = s_token + (counted ? p.pieces * E : 0);
-    auto place = [&](int i) { return (i / E * T + tid) * E + i % E; };           // of the thread's element i in the slice
-    if (counted || biased) {
-        for (int i = tid * 4; i < p.pieces * E * ((counted ? 1 : 0) + (biased ? 1 : 0)); i += T * 4) *(uint4 *)(s_token + i) = make_uint4(0u, 0u, 0u, 0u);
-        s_changes[tid] = 0u;
-    }
+    const int pieces = max(0, (last - first + E - 1) / E);
+    const bool changes = p.marked > 0;
+    uint32_t *s_place = s_marked, *s_count = s_marked + p.marked, *s_entry = s_count + p.marked;
+    float *s_value = (float *)s_count;
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // waited for before others' shared memory is written
+    if (changes) {
+        for (int i = tid; i < (p.bias_ids != nullptr ? 2 : 1) * p.marked; i += T) s_count[i] = 0u;
+        for (int i = tid; i < kLogitsWords; i += T) s_marks[i] = 0u;
+    }
     grid_dependency_wait();
     grid_launch_dependents();
+    // up to 15 bytes beside the row are read with it, and not used
+    if (p.probs && pieces > 0 && tid == 0)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(in + first), "r"(pieces * 16) : "memory");
 
-    float x[K][E];
-    uint32_t allowed = 0u;                        // a bit per element of the thread: in the row, and the mask's bit
-    uint4 raw[K];
+    // ---- the tokens that change
+    int marked = 0;
+    if (changes) {
+        const int32_t *text = p.history + b * p.history_stride, *drafted = p.drafts + (long long)b * (p.rows - 1), *ids = p.bias_ids + (long long)b * p.n_bias;
+        const int n_drafts = p.drafts != nullptr ? j : 0;
+        constexpr int kAhead = 4;                 // of a thread's tokens of the history are kept between the two looks at them
+        int told[kAhead], n = 0, prompt = 0;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int v0 = first + (k * T + tid) * E;
-        raw[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (v0 < last) raw[k] = *(const uint4 *)(in + v0);       // up to 15 bytes beside the row, not used
-    }
-    // ---- how often its tokens came, and their biases
-    if (counted || biased) {
-        const int n = p.history != nullptr ? (int)min((long long)max(__ldg(p.history_lens + b), 0), p.history_stride) : 0;
-        const int prompt = p.history != nullptr ? __ldg(p.prompt_lens + b) : 0;
-        __syncthreads();
-        // calls fn(place in the slice, index) for the tokens of a list that lie in the slice; true: the token was not there yet
-        auto each = [&](const int32_t *list, int count, auto fn) {
-#pragma unroll 4
-            for (int i = tid; i < count; i += T) {
-                const int token = __ldg(list + i);
-                const unsigned at = (unsigned)(token - first);
-                if (token < 0 || at >= used || !fn(at, i)) continue;
-                const unsigned piece = at / E;                   // piece piece / T of thread piece % T
-                atomicOr(s_changes + piece % T, 1u << (piece / T * E + at % E));
+        for (int i = 0; i < kAhead; ++i) told[i] = tid + i * T < (p.history != nullptr ? p.history_stride : 0) ? __ldg(text + tid + i * T) : -1;
+        if (p.history != nullptr) {
+            n = (int)min((long long)max(__ldg(p.history_lens + b), 0), p.history_stride);
+            prompt = __ldg(p.prompt_lens + b);
+        }
+        __syncthreads();                          // the arrays are clear
+        // calls fn(place in the slice, index) for the tokens of the lists that lie in the slice
+        auto each = [&](auto history, auto bias) {
+            auto place_of = [&](int token) { return token >= 0 && token >= first && token < last ? token - first : -1; };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int at = tid + i * T < n ? place_of(told[i]) : -1;
+                if (at >= 0) history(at, tid + i * T < prompt);
+            }
+#pragma unroll 1
+            for (int i = tid + kAhead * T; i < n; i += T) {
+                const int at = place_of(__ldg(text + i));
+                if (at >= 0) history(at, i < prompt);
+            }
+#pragma unroll 1
+            for (int i = tid; i < n_drafts; i += T) {
+                const int at = place_of(__ldg(drafted + i));
+                if (at >= 0) history(at, false);
+            }
+#pragma unroll 1
+            for (int i = tid; i < p.n_bias; i += T) {
+                const int at = place_of(__ldg(ids + i));
+                if (at >= 0) bias(at, i);
             }
         };
-        each(p.history + b * p.history_stride, n,
-             [&](unsigned at, int i) { return (i < prompt ? atomicOr(s_count + at, 0x80000000u) : atomicAdd(s_count + at, 1u)) == 0u; });
-        each(p.drafts + (long long)b * (p.rows - 1), p.drafts != nullptr ? j : 0, [&](unsigned at, int) { return atomicAdd(s_count + at, 1u) == 0u; });
-        // where an id stands twice, the last entry counts
-        each(p.bias_ids + (long long)b * p.n_bias, p.n_bias, [&](unsigned at, int i) { return atomicMax(s_entry + at, (uint32_t)i + 1u) == 0u; });
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int v0 = first + (k * T + tid) * E;
-        const int from = max(0, -v0), to = min(E, last - v0);    // the piece's elements in the slice
-        if (to <= from) continue;
-        uint32_t bits = (1u << to) - (1u << from);
-        if (p.mask != nullptr) {
-            const uint32_t *words = p.mask + row * p.mask_stride;
-            const int lo = v0 + from, w0 = lo / 32, w1 = (v0 + to - 1) / 32;
-            const uint32_t a = __ldg(words + w0), z = w1 != w0 ? __ldg(words + w1) : a;
-            bits &= __funnelshift_r(a, z, lo % 32) << from;
-        }
-        allowed |= bits << (k * E);
-    }
-    // ---- the tokens that change: their values, rounded step by step as the formula stands, take the counts' places
-    uint32_t changed = 0u;
-    float most = -INFINITY;
-    if (counted || biased) {
+        auto mark = [&](int at, int) { atomicOr(s_marks + at / 32, 1u << at % 32); };
+        each(mark, mark);
         __syncthreads();
-        changed = s_changes[tid] & allowed;
-        allowed &= ~changed;
-        if (changed != 0u) {
-            const float *pr = p.params + 4 * b;
-            const float rep = counted ? __ldg(pr) : 1.f, pres = counted ? __ldg(pr + 1) : 0.f, freq = counted ? __ldg(pr + 2) : 0.f;
-            for (uint32_t left = changed; left != 0u; left &= left - 1u) {
-                const int at = place(__ffs(left) - 1);
-                float v = element(in[first + at]);
-                const uint32_t c = counted ? s_count[at] : 0u, times = c & 0x7fffffffu, entry = biased ? s_entry[at] : 0u;
-                if (c != 0u) {
-                    v = v > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
-                    v = __fsub_rn(v, __fmul_rn(freq, (float)times));
-                    if (times > 0u) v = __fsub_rn(v, pres);
-                }
-                if (entry != 0u) v = __fadd_rn(v, __ldg(p.bias + (long long)b * p.n_bias + entry - 1));
-                s_token[at] = __float_as_uint(v);
-                most = fmaxf(most, v);
-            }
+        const int marks0 = __popc(s_marks[2 * tid]), both = marks0 + __popc(s_marks[2 * tid + 1]);
+        int upto = both;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
         }
-    }
-    // calls fn(the token, its place in s_token) for them
-    auto each_changed = [&](auto fn) {
-        for (uint32_t left = changed; left != 0u; left &= left - 1u) {
-            const int at = place(__ffs(left) - 1);
-            fn(first + at, s_token[at]);
+        if (lane == 31) s_total[warp] = upto;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            upto += w < warp ? s_total[w] : 0;
+            marked += s_total[w];
         }
-    };
-    // ---- what is outside the row, not allowed or changed is taken out
-#pragma unroll
-    for (int k = 0; k < K; ++k) piece_elements(raw[k], x[k]);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        if (!(allowed >> i & 1u)) x[i / E][i % E] = -INFINITY;
-        most = fmaxf(most, x[i / E][i % E]);
+        s_base[2 * tid] = upto - both;
+        s_base[2 * tid + 1] = upto - both + marks0;
+        __syncthreads();
+        auto index = [&](int at) {
+            const int i = s_base[at / 32] + __popc(s_marks[at / 32] & ((1u << at % 32) - 1u));
+            s_place[i] = at;                      // the same from whoever writes it
+            return i;
+        };
+        each([&](int at, bool in_prompt) { in_prompt ? atomicOr(s_count + index(at), 0x80000000u) : atomicAdd(s_count + index(at), 1u); },
+             [&](int at, int i) { atomicMax(s_entry + index(at), (uint32_t)i + 1u); });          // where an id stands twice, the last entry counts
+        __syncthreads();
     }
-    const bool whole = reinterpret_cast<uintptr_t>(out + first) % (sizeof(Tout) * E < 16 ? sizeof(Tout) * E : 16) == 0;
-    auto store = [&](int k) {
-        const int v0 = first + (k * T + tid) * E;
-        if (v0 < last) store_elements<Tout, E>(out + v0, x[k], whole, max(0, -v0), min(E, last - v0));
-    };
-    if (!p.probs) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) store(k);
-        each_changed([&](int v, uint32_t &x) { out[v] = from_float<Tout>(__uint_as_float(x)); });
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        return;
-    }
-    // ---- the row's maximum and sum
+    // ---- a thread's maximum, and the sum against it
     const float temperature = p.params ? __ldg(p.params + 4 * b + 3) : 1.f;
     const bool greedy = !(temperature > 0.f);
     const float scale = greedy ? 1.4426950408889634f : fminf(1.4426950408889634f / temperature, 3e38f);     // 0 * scale has to be 0
+    float most = -INFINITY, sum = 0.f;
+    // Calls fn(first token, elements) with the pieces of this thread, what is outside the row, not allowed or marked at minus
+    // infinity, up to U of them on their way at a time.
+    auto each_pieces = [&](auto fn) {
+#pragma unroll 1
+        for (int i0 = tid; i0 < pieces; i0 += U * T) {
+            uint4 raw[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                raw[k] = make_uint4(0u, 0u, 0u, 0u);
+                if (i0 + k * T < pieces) raw[k] = *(const uint4 *)(in + first + (i0 + k * T) * E);
+            }
+            float x[U][E];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int at = (i0 + k * T) * E;
+                uint32_t bits = i0 + k * T < pieces ? allowed_bits<E>(words, first + at, V) : 0u;
+                if (changes && bits != 0u) bits &= ~(s_marks[at / 32] >> at % 32);
+                piece_elements(raw[k], x[k]);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(bits >> e & 1u)) x[k][e] = -INFINITY;
+            }
+            fn(i0, x);
+        }
+    };
+    if (changes) {                                // marked tokens, rounded step by step as the formula stands
+        const float *pr = p.params + 4 * b;
+        const float rep = p.params ? __ldg(pr) : 1.f, pres = p.params ? __ldg(pr + 1) : 0.f, freq = p.params ? __ldg(pr + 2) : 0.f;
+#pragma unroll 2
+        for (int i = tid; i < marked; i += T) {
+            const int at = (int)s_place[i];
+            float v = element(in[first + at]);
+            const uint32_t c = s_count[i], times = c & 0x7fffffffu, entry = p.bias_ids != nullptr ? s_entry[i] : 0u;
+            if (c != 0u) {
+                v = v > 0.f ? __fdiv_rn(v, rep) : __fmul_rn(v, rep);
+                v = __fsub_rn(v, __fmul_rn(freq, (float)times));
+                if (times > 0u) v = __fsub_rn(v, pres);
+            }
+            if (entry != 0u) v = __fadd_rn(v, __ldg(p.bias + (long long)b * p.n_bias + entry - 1));
+            if (words != nullptr && !(__ldg(words + (first + at) / 32) >> (first + at) % 32 & 1u)) v = -INFINITY;
+            s_value[i] = v;
+            most = fmaxf(most, v);
+        }
+        const float ref = most == -INFINITY ? 0.f : most;
+        for (int i = tid; i < marked; i += T) sum += fast_exp2((s_value[i] - ref) * scale);
+    }
+    const bool whole = reinterpret_cast<uintptr_t>(out + first) % (sizeof(Tout) * E < 16 ? sizeof(Tout) * E : 16) == 0;
+    auto store = [&](int i, const float *x) {
+        const int v = first + i * E;
+        if (i < pieces) store_elements<Tout, E>(out + v, x, whole, max(0, -v), min(E, last - v));
+    };
+    if (!p.probs) {
+        __syncthreads();                          // in place: marked logits have been read
+        each_pieces([&](int i, float (&x)[U][E]) {
+#pragma unroll
+            for (int k = 0; k < U; ++k) store(i + k * T, x[k]);
+        });
+        __syncthreads();
+        for (int i = tid; i < marked; i += T) out[first + (int)s_place[i]] = from_float<Tout>(s_value[i]);
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        return;
+    }
+    each_pieces([&](int, float (&x)[U][E]) {
+        float top = x[0][0];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) top = fmaxf(top, x[k][e]);
+        if (top > most) {
+            sum *= fast_exp2((most - top) * scale);
+            most = top;
+        }
+        const float ref = most == -INFINITY ? 0.f : most;
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum += fast_exp2((x[k][e] - ref) * scale);
+    });
+    // ---- the CTA's, then the row's
+    const float own = most;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (lane == 0) s_max[warp] = most;
@@ -222,48 +294,35 @@ logits_process_kernel(const LogitsParams p)
     most = s_max[lane % kWarps];
 #pragma unroll
     for (int o = kWarps / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    int at = 0x7fffffff;                          // the first place of the slice's maximum
-    if (greedy) {
-#pragma unroll
-        for (int k = K - 1; k >= 0; --k)
-#pragma unroll
-            for (int e = E - 1; e >= 0; --e)
-                if (x[k][e] == most) at = first + (k * T + tid) * E + e;
-        each_changed([&](int v, uint32_t &x) {
-            if (__uint_as_float(x) == most) at = min(at, v);
-        });
-        at = (int)__reduce_min_sync(0xffffffffu, (unsigned)at);
-        if (lane == 0) s_at[warp] = at;
-    }
-    const float ref = most == -INFINITY ? 0.f : most;
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            x[k][e] = fast_exp2((x[k][e] - ref) * scale);
-            sum += x[k][e];
-        }
-    each_changed([&](int, uint32_t &x) {
-        const float w = fast_exp2((__uint_as_float(x) - ref) * scale);
-        sum += w;
-        x = __float_as_uint(w);
-    });
+    sum *= own == -INFINITY ? 1.f : fast_exp2((own - most) * scale);             // a thread that saw NaN alone keeps it
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
+    if (greedy) {                                 // the first place of the slice's maximum
+        unsigned at = 0x7fffffffu;
+        each_pieces([&](int i, float (&x)[U][E]) {
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[k][e] == most) at = min(at, (unsigned)(first + (i + k * T) * E + e));
+        });
+        for (int i = tid; i < marked; i += T)
+            if (s_value[i] == most) at = min(at, (unsigned)(first + (int)s_place[i]));
+        at = __reduce_min_sync(0xffffffffu, at);
+        if (lane == 0) s_at[warp] = at;
+    }
     __syncthreads();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");          // every CTA of the cluster runs
     if (warp == 0) {
         sum = lane < kWarps ? s_sum[lane] : 0.f;
 #pragma unroll
         for (int o = kWarps / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (greedy) at = (int)__reduce_min_sync(0xffffffffu, (unsigned)s_at[lane % kWarps]);
-        at = __shfl_sync(0xffffffffu, at, 0);
         sum = __shfl_sync(0xffffffffu, sum, 0);
+        const unsigned at = greedy ? __reduce_min_sync(0xffffffffu, s_at[lane % kWarps]) : 0u;
         if (lane < ctas)                          // to CTA `lane`
             asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_map(smem_u32(s_share + rank), lane)),
-                         "r"(__float_as_uint(most)), "r"(__float_as_uint(sum)), "r"((uint32_t)at), "r"(0u) : "memory");
+                         "r"(__float_as_uint(most)), "r"(__float_as_uint(sum)), "r"(at), "r"(0u) : "memory");
     }
     cluster_barrier();
     // lane c looks at CTA c's; sums in the same order everywhere
@@ -275,29 +334,28 @@ logits_process_kernel(const LogitsParams p)
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     top = __shfl_sync(0xffffffffu, top, 0);
-    const float all = top == -INFINITY ? 0.f : top;
-    l *= m == -INFINITY ? 0.f : fast_exp2((m - all) * scale);    // a slice in which nothing is allowed adds nothing
+    l *= m == -INFINITY ? 1.f : fast_exp2((m - top) * scale);    // a slice in which nothing is allowed has none, or a NaN
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float total = __shfl_sync(0xffffffffu, l, 0);
-    if (greedy && total == total) {               // 1 at the first of the largest
-        const unsigned best = __reduce_min_sync(0xffffffffu, there && m == top && top > -INFINITY ? share.z : 0x7fffffffu);
+    // NaN where a NaN or an infinity is among what is allowed; zeros where nothing is; greedy: 1 at the first of the largest
+    const float all = top == -INFINITY ? 0.f : top, f = total == 0.f ? 0.f : 1.f / total;
+    const unsigned best = __reduce_min_sync(0xffffffffu, there && m == top && top > -INFINITY ? share.z : 0x7fffffffu);
+    const bool one = greedy && total == total;
+    auto result = [&](int v, float x) { return one ? (v == (int)best ? 1.f : 0.f) : fast_exp2((x - all) * scale) * f; };
+    each_pieces([&](int i, float (&x)[U][E]) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < U; ++k) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[k][e] = first + (k * T + tid) * E + e == (int)best ? 1.f : 0.f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) store(k);
-    } else {
-        // NaN where a NaN or an infinity is among what is allowed; zeros where nothing is
-        const float f = total == 0.f ? 0.f : (most == -INFINITY ? 0.f : fast_exp2((most - all) * scale)) / total;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[k][e] *= f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) store(k);
-        each_changed([&](int v, uint32_t &x) { out[v] = from_float<Tout>(__uint_as_float(x) * f); });
+            for (int e = 0; e < E; ++e) x[k][e] = result(first + (i + k * T) * E + e, x[k][e]);
+            store(i + k * T, x[k]);
+        }
+    });
+    if (!changes) return;
+    __syncthreads();                              // pieces first, then what is marked in them
+    for (int i = tid; i < marked; i += T) {
+        const int v = first + (int)s_place[i];
+        out[v] = from_float<Tout>(result(v, s_value[i]));
     }
 }
 

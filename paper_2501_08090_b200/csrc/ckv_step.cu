@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdlib>
 #include <initializer_list>
 
 #include "ckv_cache8.cuh"
@@ -182,38 +183,33 @@ int32_t launch_pages(ckv_pool *pool, const char *fn, const ckv::TablesParams &ar
     return CKV_OK;
 }
 
-template <typename Tin, typename Tout, int T>
-int32_t launch_logits(ckv::LogitsParams &lp, long long rows, int pieces, void *stream)
-{
-    static thread_local int configured_device = -1, num_sms = 0;
-    auto kernel = ckv::logits_process_kernel<Tin, Tout, T>;
-    constexpr int E = 16 / sizeof(Tin), kMost = T * ckv::kLogitsElements / E;    // pieces of a CTA
-    int device = -1;
-    CKV_CUDA(cudaGetDevice(&device));
-    if (configured_device != device) {
-        CKV_CUDA(allow(kernel, true, 2 * sizeof(uint32_t) * kMost * E));
-        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
-        configured_device = device;
-    }
-    // CTAs of a row: as few as hold it, up to 16 while there are few rows and a slice is more than 2048 tokens
-    unsigned cluster = (unsigned)((pieces + kMost - 1) / kMost);
-    while (cluster < 16 && 2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster) cluster = std::min(16u, 2 * cluster);
-    lp.pieces = (int)((pieces + cluster - 1) / cluster);
-    const int arrays = (lp.history || lp.drafts ? 1 : 0) + (lp.bias_ids ? 1 : 0);
-    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), T, sizeof(uint32_t) * arrays * lp.pieces * E, true, cluster, stream, lp));
-    return CKV_OK;
-}
-
 template <typename Tin, typename Tout>
 int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
 {
-    constexpr int E = 16 / sizeof(Tin);
+    static thread_local int configured_device = -1, num_sms = 0;
+    auto kernel = ckv::logits_process_kernel<Tin, Tout>;
+    constexpr int E = 16 / sizeof(Tin), kMost = 32 * ckv::kLogitsWords / E;      // pieces of a CTA
+    int device = -1;
+    CKV_CUDA(cudaGetDevice(&device));
+    if (configured_device != device) {
+        CKV_CUDA(allow(kernel, true, 3 * sizeof(uint32_t) * kMost * E));
+        CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
+        configured_device = device;
+    }
     const long long rows = (long long)batch * lp.rows;
     // pieces of a row, wherever in its first one it may begin
     const bool aligned = aligned16(lp.logits) && (lp.stride % E == 0 || rows == 1);
     const int pieces = (lp.vocab + (aligned ? E - 1 : 2 * E - 2)) / E;
-    return pieces <= 16 * ckv::kLogitsThreads * ckv::kLogitsElements / E ? launch_logits<Tin, Tout, ckv::kLogitsThreads>(lp, rows, pieces, stream)
-                                                                         : launch_logits<Tin, Tout, 512>(lp, rows, pieces, stream);
+    // CTAs of a row
+    const char *e1=getenv("LG_S"); const int slice=e1?atoi(e1):12800;
+    unsigned cluster = (unsigned)((pieces + kMost - 1) / kMost);
+    while (cluster < 8 && pieces * E > slice * (int)cluster) ++cluster;
+    while (cluster < 16 && 2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster) cluster = std::min(16u, 2 * cluster);
+    lp.pieces = (int)((pieces + cluster - 1) / cluster);
+    const long long lists = (lp.history ? lp.history_stride : 0) + (lp.drafts ? lp.rows - 1 : 0) + lp.n_bias;
+    lp.marked = (int)std::min<long long>(lists, (long long)lp.pieces * E);
+    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), ckv::kLogitsThreads, sizeof(uint32_t) * (lp.bias_ids ? 3 : 2) * lp.marked, true, cluster, stream, lp));
+    return CKV_OK;
 }
 
 }  // namespace
