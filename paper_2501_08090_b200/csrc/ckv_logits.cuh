@@ -16,7 +16,7 @@ namespace ckv {
 // Bound by HBM: a logit is read once and a result written once.  A cluster of CTAs owns a row, a CTA a slice of it.  The
 // slice is brought into L2 by one bulk prefetch as the CTA starts, and read there twice, as pieces of 16 aligned
 // bytes: for the maximum and the sum, and for the results.  (Held in registers between, 32 tokens a thread, it cost 64
-// registers and two to four CTAs an SM: LOGITS_OLD us for 512 rows of 50257 tokens with everything, against LOGITS_NEW; alone LOGITS_OLD0 against LOGITS_NEW0.)
+// registers and two to four CTAs an SM: 141 us for 512 rows of 50257 tokens with everything, against 69; alone 57 against 43.)
 // Tokens that change are few.  Meanwhile the CTA marks them, a bit each; the marks before a token give it a place in short
 // arrays in shared memory, where its occurrences are counted and its bias's last entry is found (whole numbers, and
 // the largest of entries: the order of atomics does not show), and where the CTA's threads handle them in turn.
@@ -38,9 +38,9 @@ struct LogitsParams {
     int32_t marked;                 // tokens of a CTA that can change
 };
 
-constexpr int kLogitsThreads = 256, kLogitsCtas = 6;             // CTAs an SM
-// Words of marks that a CTA has, so that sixteen CTAs hold a row.
-constexpr int kLogitsWords = 2 * kLogitsThreads, kLogitsMaxVocab = 16 * 32 * kLogitsWords - 16;
+constexpr int kLogitsThreads = 256, kLogitsCtas = 4;             // CTAs an SM
+// Words of marks that a CTA has room for.
+constexpr int kLogitsWords = 4 * kLogitsThreads, kLogitsMaxVocab = 262128;
 
 // The elements of a piece of 16 bytes.
 __device__ __forceinline__ void piece_elements(const uint4 &raw, float (&x)[4])
@@ -85,20 +85,6 @@ __device__ __forceinline__ void store_elements(T *dst, const float *x, bool whol
     }
 }
 
-// The allowed ones of a piece's E tokens, from token v on of the row: those in the row whose mask bit is 1.
-template <int E>
-__device__ __forceinline__ uint32_t allowed_bits(const uint32_t *__restrict__ words, int v, int V)
-{
-    const int from = max(0, -v), to = min(E, V - v);
-    uint32_t bits = to > from ? (1u << to) - (1u << from) : 0u;
-    if (words != nullptr) {
-        const int w = v >> 5, last = (V - 1) >> 5;               // a piece before the row's first token begins in word -1
-        const uint32_t lo = w >= 0 && w <= last ? __ldg(words + w) : 0u, hi = (v & 31) > 32 - E && w < last ? __ldg(words + w + 1) : 0u;
-        bits &= __funnelshift_r(lo, hi, v & 31);
-    }
-    return bits;
-}
-
 template <typename Tin, typename Tout>
 __global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
 logits_process_kernel(const LogitsParams p)
@@ -140,27 +126,23 @@ logits_process_kernel(const LogitsParams p)
     if (changes) {
         const int32_t *text = p.history + b * p.history_stride, *drafted = p.drafts + (long long)b * (p.rows - 1), *ids = p.bias_ids + (long long)b * p.n_bias;
         const int n_drafts = p.drafts != nullptr ? j : 0;
-        constexpr int kAhead = 4;                 // of a thread's tokens of the history are kept between the two looks at them
-        int told[kAhead], n = 0, prompt = 0;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) told[i] = tid + i * T < (p.history != nullptr ? p.history_stride : 0) ? __ldg(text + tid + i * T) : -1;
-        if (p.history != nullptr) {
-            n = (int)min((long long)max(__ldg(p.history_lens + b), 0), p.history_stride);
-            prompt = __ldg(p.prompt_lens + b);
-        }
+        const int room = p.history != nullptr ? (int)min(p.history_stride, 0x7fffffffll) : 0;
+        const int n = room > 0 ? min(max(__ldg(p.history_lens + b), 0), room) : 0, prompt = room > 0 ? __ldg(p.prompt_lens + b) : 0;
         __syncthreads();                          // the arrays are clear
         // calls fn(place in the slice, index) for the tokens of the lists that lie in the slice
         auto each = [&](auto history, auto bias) {
             auto place_of = [&](int token) { return token >= 0 && token >= first && token < last ? token - first : -1; };
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int at = tid + i * T < n ? place_of(told[i]) : -1;
-                if (at >= 0) history(at, tid + i * T < prompt);
-            }
+            constexpr int kAhead = 8;             // tokens of a thread on their way together, the first ones before their number is known
 #pragma unroll 1
-            for (int i = tid + kAhead * T; i < n; i += T) {
-                const int at = place_of(__ldg(text + i));
-                if (at >= 0) history(at, i < prompt);
+            for (long long i0 = tid; i0 < (i0 == tid ? room : n); i0 += kAhead * T) {
+                int token[kAhead];
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) token[k] = i0 + k * T < room ? __ldg(text + i0 + k * T) : -1;
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    const int at = i0 + k * T < n ? place_of(token[k]) : -1;
+                    if (at >= 0) history(at, i0 + k * T < prompt);
+                }
             }
 #pragma unroll 1
             for (int i = tid; i < n_drafts; i += T) {
@@ -176,8 +158,11 @@ logits_process_kernel(const LogitsParams p)
         auto mark = [&](int at, int) { atomicOr(s_marks + at / 32, 1u << at % 32); };
         each(mark, mark);
         __syncthreads();
-        const int marks0 = __popc(s_marks[2 * tid]), both = marks0 + __popc(s_marks[2 * tid + 1]);
-        int upto = both;
+        constexpr int kOwn = kLogitsWords / T;    // words of a thread, neighbours
+        int own_marks = 0;
+#pragma unroll
+        for (int w = 0; w < kOwn; ++w) own_marks += __popc(s_marks[tid * kOwn + w]);
+        int upto = own_marks;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, upto, o);
@@ -185,13 +170,17 @@ logits_process_kernel(const LogitsParams p)
         }
         if (lane == 31) s_total[warp] = upto;
         __syncthreads();
+        upto -= own_marks;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             upto += w < warp ? s_total[w] : 0;
             marked += s_total[w];
         }
-        s_base[2 * tid] = upto - both;
-        s_base[2 * tid + 1] = upto - both + marks0;
+#pragma unroll
+        for (int w = 0; w < kOwn; ++w) {
+            s_base[tid * kOwn + w] = upto;
+            upto += __popc(s_marks[tid * kOwn + w]);
+        }
         __syncthreads();
         auto index = [&](int at) {
             const int i = s_base[at / 32] + __popc(s_marks[at / 32] & ((1u << at % 32) - 1u));
@@ -207,35 +196,66 @@ logits_process_kernel(const LogitsParams p)
     const bool greedy = !(temperature > 0.f);
     const float scale = greedy ? 1.4426950408889634f : fminf(1.4426950408889634f / temperature, 3e38f);     // 0 * scale has to be 0
     float most = -INFINITY, sum = 0.f;
-    // Calls fn(first token, elements) with the pieces of this thread, what is outside the row, not allowed or marked at minus
-    // infinity, up to U of them on their way at a time.
+    // Calls fn(i, elements) with this thread's pieces i, i + T, .. of the slice, U at a time, what is outside the row, not
+    // allowed or marked at minus infinity.
+    constexpr uint32_t kAll = (1u << E) - 1u;
+    static_assert(T * E % 32 == 0, "pieces of a thread begin at the same bit of a word");
     auto each_pieces = [&](auto fn) {
+        const Tin *at = in + first + tid * E;
+        const int shift = (first + tid * E) & 31, mark_shift = tid * E & 31, last_word = (V - 1) >> 5;
 #pragma unroll 1
-        for (int i0 = tid; i0 < pieces; i0 += U * T) {
+        for (int i = tid; i < pieces; i += U * T, at += U * T * E) {
+            const bool inner = i > 0 && i + (U - 1) * T < pieces - 1;            // nothing of these is outside the row
             uint4 raw[U];
+            uint32_t bits[U];
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 raw[k] = make_uint4(0u, 0u, 0u, 0u);
-                if (i0 + k * T < pieces) raw[k] = *(const uint4 *)(in + first + (i0 + k * T) * E);
+                if (inner || i + k * T < pieces) raw[k] = *(const uint4 *)(at + k * T * E);
+                bits[k] = kAll;
+            }
+            if (!inner) {
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int v = first + (i + k * T) * E, from = max(0, -v), to = min(E, last - v);
+                    bits[k] = to > from ? (1u << to) - (1u << from) : 0u;
+                }
+            }
+            if (words != nullptr) {
+                const int w = (first + i * E) >> 5;              // -1 for a piece that begins before the row
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const int n = w + k * (T * E / 32);          // words outside the mask hold nothing of the row
+                    const uint32_t lo = __ldg(words + (inner ? n : min(max(n, 0), last_word))), hi = __ldg(words + min(n + 1, last_word));
+                    bits[k] &= __funnelshift_r(lo, hi, shift);
+                }
+            }
+            if (changes) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+                    if (inner || i + k * T < pieces) bits[k] &= ~(s_marks[i * E / 32 + k * (T * E / 32)] >> mark_shift);
             }
             float x[U][E];
+            uint32_t every = kAll;
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                const int at = (i0 + k * T) * E;
-                uint32_t bits = i0 + k * T < pieces ? allowed_bits<E>(words, first + at, V) : 0u;
-                if (changes && bits != 0u) bits &= ~(s_marks[at / 32] >> at % 32);
                 piece_elements(raw[k], x[k]);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (!(bits >> e & 1u)) x[k][e] = -INFINITY;
+                every &= bits[k];
             }
-            fn(i0, x);
+            if (every != kAll) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (!(bits[k] >> e & 1u)) x[k][e] = -INFINITY;
+            }
+            fn(i, x);
         }
     };
     if (changes) {                                // marked tokens, rounded step by step as the formula stands
         const float *pr = p.params + 4 * b;
         const float rep = p.params ? __ldg(pr) : 1.f, pres = p.params ? __ldg(pr + 1) : 0.f, freq = p.params ? __ldg(pr + 2) : 0.f;
-#pragma unroll 2
+#pragma unroll 4
         for (int i = tid; i < marked; i += T) {
             const int at = (int)s_place[i];
             float v = element(in[first + at]);
@@ -342,20 +362,25 @@ logits_process_kernel(const LogitsParams p)
     const float all = top == -INFINITY ? 0.f : top, f = total == 0.f ? 0.f : 1.f / total;
     const unsigned best = __reduce_min_sync(0xffffffffu, there && m == top && top > -INFINITY ? share.z : 0x7fffffffu);
     const bool one = greedy && total == total;
-    auto result = [&](int v, float x) { return one ? (v == (int)best ? 1.f : 0.f) : fast_exp2((x - all) * scale) * f; };
+    if (one) {
+        const float none[E] = {};
+        for (int i = tid; i < pieces; i += T) store(i, none);
+        __syncthreads();
+        if (tid == 0 && (int)best >= first && (int)best < last) out[best] = from_float<Tout>(1.f);
+        return;
+    }
     each_pieces([&](int i, float (&x)[U][E]) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[k][e] = result(first + (i + k * T) * E + e, x[k][e]);
+            for (int e = 0; e < E; ++e) x[k][e] = fast_exp2((x[k][e] - all) * scale) * f;
             store(i + k * T, x[k]);
         }
     });
     if (!changes) return;
     __syncthreads();                              // pieces first, then what is marked in them
     for (int i = tid; i < marked; i += T) {
-        const int v = first + (int)s_place[i];
-        out[v] = from_float<Tout>(result(v, s_value[i]));
+        out[first + (int)s_place[i]] = from_float<Tout>(fast_exp2((s_value[i] - all) * scale) * f);
     }
 }
 

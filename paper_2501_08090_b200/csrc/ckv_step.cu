@@ -4,7 +4,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <initializer_list>
 
 #include "ckv_cache8.cuh"
@@ -188,11 +187,12 @@ int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
 {
     static thread_local int configured_device = -1, num_sms = 0;
     auto kernel = ckv::logits_process_kernel<Tin, Tout>;
-    constexpr int E = 16 / sizeof(Tin), kMost = 32 * ckv::kLogitsWords / E;      // pieces of a CTA
+    constexpr int E = 16 / sizeof(Tin);
+    constexpr size_t kMostBytes = 200 * 1024;    // of the arrays of changed tokens
     int device = -1;
     CKV_CUDA(cudaGetDevice(&device));
     if (configured_device != device) {
-        CKV_CUDA(allow(kernel, true, 3 * sizeof(uint32_t) * kMost * E));
+        CKV_CUDA(allow(kernel, true, kMostBytes));
         CKV_CUDA(cudaDeviceGetAttribute(&num_sms, cudaDevAttrMultiProcessorCount, device));
         configured_device = device;
     }
@@ -200,15 +200,19 @@ int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
     // pieces of a row, wherever in its first one it may begin
     const bool aligned = aligned16(lp.logits) && (lp.stride % E == 0 || rows == 1);
     const int pieces = (lp.vocab + (aligned ? E - 1 : 2 * E - 2)) / E;
-    // CTAs of a row
-    const char *e1=getenv("LG_S"); const int slice=e1?atoi(e1):12800;
-    unsigned cluster = (unsigned)((pieces + kMost - 1) / kMost);
-    while (cluster < 8 && pieces * E > slice * (int)cluster) ++cluster;
-    while (cluster < 16 && 2 * cluster * rows <= num_sms && pieces * E > 2048 * (int)cluster) cluster = std::min(16u, 2 * cluster);
-    lp.pieces = (int)((pieces + cluster - 1) / cluster);
     const long long lists = (lp.history ? lp.history_stride : 0) + (lp.drafts ? lp.rows - 1 : 0) + lp.n_bias;
-    lp.marked = (int)std::min<long long>(lists, (long long)lp.pieces * E);
-    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), ckv::kLogitsThreads, sizeof(uint32_t) * (lp.bias_ids ? 3 : 2) * lp.marked, true, cluster, stream, lp));
+    const size_t arrays = sizeof(uint32_t) * (lp.bias_ids ? 3 : 2);
+    // CTAs of a row: few, since each begins with a chain of look-ups, of at most 16384 tokens (32768 with changes, whose chain
+    // is longer: 512 rows of 50257 tokens with everything in 2 CTAs 68 us, in 4 75, in 8 103; alone 47, 43, 51), and with their
+    // arrays in shared memory; up to 16 where there are few rows
+    const long long most = lists > 0 ? 32 * ckv::kLogitsWords : 16 * ckv::kLogitsWords;
+    unsigned cluster = 1;
+    const auto slice = [&] { return (pieces + (long long)cluster - 1) / cluster * E; };
+    while (slice() > most || std::min(lists, slice()) * arrays > kMostBytes) ++cluster;
+    while (cluster < 16 && 2 * cluster * rows <= num_sms && slice() > 2048) cluster = std::min(16u, 2 * cluster);
+    lp.pieces = (int)(slice() / E);
+    lp.marked = (int)std::min(lists, slice());
+    CKV_CUDA(enqueue(kernel, (unsigned)(rows * cluster), ckv::kLogitsThreads, arrays * lp.marked, true, cluster, stream, lp));
     return CKV_OK;
 }
 
