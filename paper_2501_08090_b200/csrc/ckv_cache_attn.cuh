@@ -208,6 +208,14 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], const uint32_t (&a)[4]
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The same with nothing to add to.
+__device__ __forceinline__ void mma_s8_16832_first(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0));
+}
+
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
 {
     uint32_t d;
@@ -215,7 +223,38 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     return d;
 }
 
-// Byte offset of the 16 bytes c of a row within a page's box, as TMA's swizzle lays them.
+// ldmatrix at addr + kOffset.  Volatile: ordered behind the waits for the tile.
+template <int kOffset>
+__device__ __forceinline__ void ldmatrix_x4_at(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4+%5];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr), "n"(kOffset));
+}
+
+template <int kOffset>
+__device__ __forceinline__ void ldmatrix_x4_trans_at(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4+%5];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr), "n"(kOffset));
+}
+
+template <int N>
+struct Const {
+    static constexpr int value = N;
+};
+
+// f(Const<0>) .. f(Const<N - 1>), so that an index may be part of a type.
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f)
+{
+    if constexpr (N > 0) {
+        unrolled<N - 1>(f);
+        f(Const<N - 1>());
+    }
+}
+
+// Byte offset of the 16 bytes c of a row within a page's box, as TMA's swizzle lays them.  In a box that begins at a multiple
+// of the swizzle's pattern, the offset of pieces 2 k + c (c = 0, 1) is that of piece c with bits 5 and up changed by k << 5.
 template <int D, bool k8>
 __device__ __forceinline__ int piece_at(int row, int c)
 {
@@ -232,10 +271,12 @@ struct PairPart {
     float qs0, qs1;                 // what a score is multiplied by: scale and, 8-bit, the query's power of two
     int earliest, pos0, pos1;       // position of the launch's first new token, and of the lane's columns' tokens
     int i0, i1;                     // those tokens
+    int seen_head, seen_from, seen_to;           // tiles that every column sees entirely: [0, seen_head) and [seen_from, seen_to)
+    uint32_t k_off, v_off;          // ldmatrix: this lane's rows of a page's keys and values, piece 0 or 1
     float m0, m1, l0, l1;
     float o[kSteps16][4];
 
-    __device__ __forceinline__ void begin(const CacheAttnParams &p, int r, int h, int L, int lane)
+    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Visited &vis, int r, int h, int L, int lane)
     {
         const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
         const int g0 = (lane & 3) * 2, c = lane >> 2, j = lane & 3;
@@ -244,6 +285,17 @@ struct PairPart {
         earliest = L - p.q_len + p.q_base;
         pos0 = earliest + i0;
         pos1 = earliest + i1;
+        {
+            // whole pages up to the first new token's, from the one on that begins behind the last one's window's start
+            const int whole = (earliest + 1) / kPageSize, start = earliest + p.q_pass - 1 - p.window;
+            const int from = p.window > 0 && start >= 0 ? start / kPageSize + 1 : 0;
+            seen_head = min(min(vis.head, p.sink / kPageSize), whole) / kPagesPerTile;
+            seen_from = (from - vis.skip + kPagesPerTile - 1) / kPagesPerTile;
+            seen_to = (whole - vis.skip) / kPagesPerTile;
+            const int row = (lane & 7) + ((lane >> 3) & 1) * 8, row_v = k8 ? 16 + row : 16 + (lane & 7) + (lane >> 4) * 8;
+            k_off = piece_at<D, k8>(row, lane >> 4);
+            v_off = piece_at<D, k8>(row_v, k8 ? lane >> 4 : (lane >> 3) & 1);
+        }
         qs0 = qs1 = p.scale_log2;
         const uint16_t *row = p.q + (((size_t)r * p.q_len + p.q_base + c / G) * heads + h * G + c % G) * D;
         if constexpr (k8) {
@@ -298,36 +350,40 @@ struct PairPart {
     // A tile in shared memory at sb, its steps at steps.
     __device__ __forceinline__ void tile(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
     {
+        if (ti < seen_head || (ti >= seen_from && ti < seen_to)) tile_as<true>(p, vis, ti, sb, steps, lane);
+        else tile_as<false>(p, vis, ti, sb, steps, lane);
+    }
+
+    // all_seen: two whole pages, which every column sees entirely.
+    template <bool all_seen>
+    __device__ __forceinline__ void tile_as(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
+    {
         constexpr int kPageBytes = 32 * D * (k8 ? 1 : 2), kHalfBytes = 32 * 128;
-        const int row16 = (lane & 7) + ((lane >> 3) & 1) * 8;    // ldmatrix: this lane's row of a page's keys
-        const int np = min(kPagesPerTile, vis.count - ti * kPagesPerTile);
-        const int latest = earliest + p.q_pass - 1;
-        int base[kPagesPerTile];                 // first token of each page
-        bool all_seen = np == kPagesPerTile;
-#pragma unroll
-        for (int mt = 0; mt < kPagesPerTile; ++mt) {
+        const int np = all_seen ? kPagesPerTile : min(kPagesPerTile, vis.count - ti * kPagesPerTile);
+        auto first_token = [&](int mt) {
             const int v = ti * kPagesPerTile + mt;
-            base[mt] = (v < vis.head ? v : v + vis.skip) * kPageSize;
-            all_seen = all_seen && base[mt] + kPageSize - 1 <= earliest &&
-                       (p.window <= 0 || base[mt] > latest - p.window || base[mt] + kPageSize <= p.sink);
-        }
+            return (v < vis.head ? v : v + vis.skip) * kPageSize;
+        };
         // ---- S^T = K Q^T
         float s[kPagesPerTile][4];
+        const uint32_t k_at = sb + k_off, v_at = sb + v_off;
         if constexpr (k8) {
             int d[kPagesPerTile][3][4];
-#pragma unroll
-            for (int i = 0; i < kPagesPerTile * 12; ++i) (&d[0][0][0])[i] = 0;
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) {
-#pragma unroll
-                for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                    if (mt >= np) continue;
+            unrolled<D / 32>([&](auto step) {
+                constexpr int ks = decltype(step)::value;
+                unrolled<kPagesPerTile>([&](auto page) {
+                    constexpr int mt = decltype(page)::value;
+                    if (!all_seen && mt >= np && ks > 0) return;                 // what a page that is not there gives is not looked at
                     uint32_t a[4];
-                    ldmatrix_x4(a, sb + mt * kPageBytes + piece_at<D, k8>(row16, 2 * ks + (lane >> 4)));
+                    ldmatrix_x4_at<mt * kPageBytes>(a, k_at ^ (ks << 5));
 #pragma unroll
-                    for (int digit = 0; digit < 3; ++digit) mma_s8_16832(d[mt][digit], a, qf[digit * (D / 32) + ks][0], qf[digit * (D / 32) + ks][1]);
-                }
-            }
+                    for (int digit = 0; digit < 3; ++digit) {
+                        const uint32_t b0 = qf[digit * (D / 32) + ks][0], b1 = qf[digit * (D / 32) + ks][1];
+                        if constexpr (ks == 0) mma_s8_16832_first(d[mt][digit], a, b0, b1);
+                        else mma_s8_16832(d[mt][digit], a, b0, b1);
+                    }
+                });
+            });
 #pragma unroll
             for (int mt = 0; mt < kPagesPerTile; ++mt)
 #pragma unroll
@@ -335,16 +391,16 @@ struct PairPart {
         } else {
 #pragma unroll
             for (int mt = 0; mt < kPagesPerTile; ++mt) s[mt][0] = s[mt][1] = s[mt][2] = s[mt][3] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < kSteps16; ++ks) {
-#pragma unroll
-                for (int mt = 0; mt < kPagesPerTile; ++mt) {
-                    if (mt >= np) continue;
+            unrolled<kSteps16>([&](auto step) {
+                constexpr int ks = decltype(step)::value;
+                unrolled<kPagesPerTile>([&](auto page) {
+                    constexpr int mt = decltype(page)::value;
+                    if (!all_seen && mt >= np) return;
                     uint32_t a[4];
-                    ldmatrix_x4(a, sb + mt * kPageBytes + (ks / 4) * kHalfBytes + piece_at<D, k8>(row16, ks % 4 * 2 + (lane >> 4)));
+                    ldmatrix_x4_at<mt * kPageBytes + (ks / 4) * kHalfBytes>(a, k_at ^ (ks % 4 << 5));
                     mma_16816<k8>(s[mt], a[0], a[1], a[2], a[3], qf[ks][0], qf[ks][1]);
-                }
-            }
+                });
+            });
         }
         // ---- scores in the log2 domain, V's step among them
         float wl[kPagesPerTile];                 // what a weight counts for in l
@@ -369,7 +425,7 @@ struct PairPart {
             if (!all_seen) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int token = base[mt] + (lane >> 2) + (i >= 2 ? 8 : 0);
+                    const int token = first_token(mt) + (lane >> 2) + (i >= 2 ? 8 : 0);
                     if (mt >= np || !sees(i & 1 ? pos1 : pos0, token, p)) s[mt][i] = -INFINITY;      // selected, never multiplied
                 }
             }
@@ -405,54 +461,50 @@ struct PairPart {
             pb[mt][1] = movmatrix_trans(k8 ? pack_f16x2(p2, p3) : pack_bf16x2(p2, p3));          // tokens 8..15
         }
         // ---- O^T += V^T P^T
-#pragma unroll
-        for (int mt = 0; mt < kPagesPerTile; ++mt) {
-            if (mt >= np) continue;
-            const uint32_t vb = sb + mt * kPageBytes;
+        unrolled<kPagesPerTile>([&](auto page) {
+            constexpr int mt = decltype(page)::value;
+            if (!all_seen && mt >= np) return;
             if constexpr (k8) {
-#pragma unroll
-                for (int c = 0; c < kSteps16; c += 2) {
+                unrolled<D / 32>([&](auto step) {
+                    constexpr int c = 2 * decltype(step)::value;
                     uint32_t x[4], lo0, hi0, lo1, hi1;
-                    ldmatrix_x4_trans(x, vb + piece_at<D, k8>(16 + row16, c + (lane >> 4)));
+                    ldmatrix_x4_trans_at<mt * kPageBytes>(x, v_at ^ (c << 4));
                     records_to_half(x[0], lo0, hi0);
                     records_to_half(x[1], lo1, hi1);
                     mma_16816<k8>(o[c], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
                     records_to_half(x[2], lo0, hi0);
                     records_to_half(x[3], lo1, hi1);
                     mma_16816<k8>(o[c + 1], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
-                }
+                });
+            } else if constexpr (all_seen) {
+                unrolled<kSteps16>([&](auto step) {
+                    constexpr int c = decltype(step)::value;
+                    uint32_t a[4];
+                    ldmatrix_x4_trans_at<mt * kPageBytes + (c / 4) * kHalfBytes>(a, v_at ^ (c % 4 << 5));
+                    mma_16816<k8>(o[c], a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                });
             } else {
-                const int vrow = 16 + (lane & 7) + (lane >> 4) * 8, vsel = (lane >> 3) & 1;
-                if (all_seen) {
-#pragma unroll
-                    for (int c = 0; c < kSteps16; ++c) {
-                        uint32_t a[4];
-                        ldmatrix_x4_trans(a, vb + (c / 4) * kHalfBytes + piece_at<D, k8>(vrow, c % 4 * 2 + vsel));
-                        mma_16816<k8>(o[c], a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
-                    }
-                } else {
 #pragma unroll 1
-                    for (int i = 0; i < p.q_pass; ++i) {         // one new token's columns, the rows it sees
-                        uint32_t keep[2];
+                for (int i = 0; i < p.q_pass; ++i) {             // one new token's columns, the rows it sees
+                    uint32_t keep[2];
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const int t = base[mt] + half * 8 + (lane & 3) * 2;
-                            keep[half] = (sees(earliest + i, t, p) ? 0xffffu : 0u) | (sees(earliest + i, t + 1, p) ? 0xffff0000u : 0u);
-                        }
-#pragma unroll
-                        for (int c = 0; c < kSteps16; ++c) {
-                            uint32_t a[4];
-                            ldmatrix_x4_trans(a, vb + (c / 4) * kHalfBytes + piece_at<D, k8>(vrow, c % 4 * 2 + vsel));
-                            a[0] &= keep[0]; a[1] &= keep[0]; a[2] &= keep[1]; a[3] &= keep[1];
-                            float x[4] = {0.f, 0.f, 0.f, 0.f};   // other tokens' columns may hold anything
-                            mma_16816<k8>(x, a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
-                            if (i0 == i) { o[c][0] += x[0]; o[c][2] += x[2]; }
-                            if (i1 == i) { o[c][1] += x[1]; o[c][3] += x[3]; }
-                        }
+                    for (int half = 0; half < 2; ++half) {
+                        const int t = first_token(mt) + half * 8 + (lane & 3) * 2;
+                        keep[half] = (sees(earliest + i, t, p) ? 0xffffu : 0u) | (sees(earliest + i, t + 1, p) ? 0xffff0000u : 0u);
                     }
+                    unrolled<kSteps16>([&](auto step) {
+                        constexpr int c = decltype(step)::value;
+                        uint32_t a[4];
+                        ldmatrix_x4_trans_at<mt * kPageBytes + (c / 4) * kHalfBytes>(a, v_at ^ (c % 4 << 5));
+                        a[0] &= keep[0]; a[1] &= keep[0]; a[2] &= keep[1]; a[3] &= keep[1];
+                        float x[4] = {0.f, 0.f, 0.f, 0.f};       // other tokens' columns may hold anything
+                        mma_16816<k8>(x, a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                        if (i0 == i) { o[c][0] += x[0]; o[c][2] += x[2]; }
+                        if (i1 == i) { o[c][1] += x[1]; o[c][3] += x[3]; }
+                    });
                 }
             }
-        }
+        });
     }
 
     // Sum l over the lanes that share a column.
@@ -746,7 +798,7 @@ cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
         const Visited vis = cc.vis;
         const int n = (int)min((long long)(vis.tiles - tile0), end - cc.v);
         const long long v0 = cc.v;
-        part.begin(p, r, h, cc.L, lane);
+        part.begin(p, vis, r, h, cc.L, lane);
 #pragma unroll 1
         for (int ti = tile0; ti < tile0 + n; ++ti, ++ring.done) {
             if (!ring.wait(p.status)) continue;
@@ -911,7 +963,7 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
     };
     while (ring.issued < S && next < vis.tiles) issue_next();
     PairPart<D, k8> part;
-    part.begin(p, r, h, L, lane);
+    part.begin(p, vis, r, h, L, lane);
 #pragma unroll 1
     for (int ti = rank * W + warp; ti < vis.tiles; ti += step, ++ring.done) {
         if (!ring.wait(p.status)) break;
