@@ -704,10 +704,15 @@ struct TileRing {
 
 // ------------------------------------------------------------------------------------------
 // Even spans of all pairs' tiles.
+//
+// Warps: what their rings hold is in flight, 128 KB an SM with eight warps of the 8-bit kernel.  More streams at once cost
+// bandwidth: 64 contexts of 8700 tokens (1.14 GB) take 177 us with eight warps of two stages (99 % of a copy's rate), 180
+// with eight of three, 189 with ten of two, 193 with twelve of two, 220 with six of two.  In long runs the GPU's power limit
+// holds them at 184 to 199 us.
 // ------------------------------------------------------------------------------------------
 template <int D, bool k8>
 struct SpanShape {
-    static constexpr int kWarps = k8 ? 12 : 6, kStages = D == 128 ? 2 : 4;
+    static constexpr int kWarps = k8 ? 8 : 6, kStages = D == 128 ? 2 : 4;
     using Layout = CacheAttnLayout<D, k8, kWarps, kStages>;
 };
 

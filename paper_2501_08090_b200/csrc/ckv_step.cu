@@ -83,10 +83,11 @@ int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *s
     unsigned cluster = 1;
     while (cluster < 16 && (long long)cluster * Pair::kWarps < tiles && 2 * cluster * blocks <= (long long)Pair::kCtas * pool->num_sms) cluster *= 2;
     // Pairs that a window cuts are of one length, nearly: a cluster owns each, if the clusters fill the GPU.  Otherwise that
-    // pays while a warp has few tiles: the even spans cost 10 us before they win.  Measured, us, pairs against spans: windows of
-    // 2048 of 64 requests, bf16 80.5 and 93.9, 8-bit 49.9 and 54.4; one request, 8-bit, of 8192 tokens 10.9 and 17.6, of 32000
-    // 25.9 and 23.8; 64 requests of 1 to 512 tokens 15.4 and 20.7, of 1 to 2048 38.0 and 34.7.
-    if (tiles <= 5ll * cluster * Pair::kWarps || (windowed && blocks * cluster > pool->num_sms)) {
+    // pays while a warp has few tiles: the even spans cost 4 us before they win.  Measured, us, pairs against spans: windows of
+    // 2048 of 64 requests, bf16 78.9 and 88.3, 8-bit 46.4 and 51.5; one request, 8-bit, of 16384 tokens (5 tiles a warp) 15.4
+    // and 16.6, of 32000 (10) 23.1 and 20.9; 64 requests of 1 to 1024 tokens (at most 5) 21.5 and 24.2, of 1 to 4096 (21)
+    // 60.6 and 51.7.
+    if (tiles <= 8ll * cluster * Pair::kWarps || (windowed && blocks * cluster > pool->num_sms)) {
         ap.q_pass = per_pass;
         CKV_CUDA(enqueue(pair, (unsigned)(blocks * cluster), Pair::kWarps * 32, Pair::Layout::kSmemBytes, pool->overlap, cluster, stream, pool->tmap, ap));
         pool->launches += 1;
