@@ -408,15 +408,15 @@ int32_t kv_pages_release(ckv_pool *pool, int32_t batch, const int32_t *d_block_t
  * generated (history[prompt_len .. history_len), and drafts 0 .. j-1), in fp32 and in this order:
  *   v generated, or in the prompt (history[0 .. prompt_len)):  x = x > 0 ? x / repetition : x * repetition
  *   x -= frequency * n_v;   n_v > 0: x -= presence;   x += bias[v];   the mask's bit v is 0: excluded
- *   probs != 0:  p_v = exp((x_v - max x) / temperature) / sum;  temperature <= 0: 1 at the largest, the first of equals, else 0;
+ *   probs != 0:  p_v = exp((x_v - max x) / temperature) / sum;  temperature <= 0 or NaN: 1 at the largest, the first of equals, else 0;
  *                a row in which nothing is allowed, or minus infinity only, is 0 (draft_verify then gives token -1);
  *                a NaN or plus infinity among what is allowed makes the row NaN
  *   probs == 0:  x_v, minus infinity where excluded; the temperature is left to whoever forms probabilities
  *   d_logits, d_out   [batch][rows] rows of `vocab` (1 .. 262128), their strides (>= vocab) apart, CKV_PROBS_F32 or CKV_PROBS_BF16 each;
  *                     d_out may be d_logits (same type and stride), otherwise they do not overlap
  *   d_params          fp32 [batch][4]: repetition, presence, frequency, temperature; NULL: 1, 0, 0, 1
- *   d_history         int32 [batch] rows, history_stride apart, of history_lens[r] tokens (0 .. history_stride), the first
- *                     prompt_lens[r] of them the prompt.  NULL: none.  Tokens outside the vocabulary (-1) count for nothing
+ *   d_history         int32 [batch][history_stride], all of it readable; row r holds history_lens[r] tokens (0 .. history_stride), the
+ *                     first prompt_lens[r] of them the prompt.  NULL: none.  Tokens outside the vocabulary (-1) count for nothing
  *   d_drafts          int32 [batch][rows - 1]; NULL: none
  *   d_bias_ids, d_bias   int32, fp32 [batch][n_bias]; ids outside the vocabulary (-1) are skipped, the last of equal ids counts
  *   d_mask            bits, 32 to a word, lowest first, 1: allowed; [batch][rows] rows, mask_stride words apart; NULL: all allowed

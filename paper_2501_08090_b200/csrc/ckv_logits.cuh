@@ -194,7 +194,8 @@ logits_process_kernel(const LogitsParams p)
     // ---- a thread's maximum, and the sum against it
     const float temperature = p.params ? __ldg(p.params + 4 * b + 3) : 1.f;
     const bool greedy = !(temperature > 0.f);
-    const float scale = greedy ? 1.4426950408889634f : fminf(1.4426950408889634f / temperature, 3e38f);     // 0 * scale has to be 0
+    // neither infinite nor 0: 0 * scale has to be 0, and minus infinity times it minus infinity
+    const float scale = greedy ? 1.4426950408889634f : fminf(fmaxf(1.4426950408889634f / temperature, 1e-44f), 3e38f);
     float most = -INFINITY, sum = 0.f;
     // Calls fn(i, elements) with this thread's pieces i, i + T, .. of the slice, U at a time, what is outside the row, not
     // allowed or marked at minus infinity.

@@ -247,6 +247,19 @@ def test_extreme_temperatures():
         assert abs(out[b].sum() - 1) < 1e-5 and out[b].max() / out[b].min() < 1.01
 
 
+def test_an_infinite_temperature():
+    """What is allowed gets the same weight, what is not gets none: sums of ones are exact, so only 1 / n is rounded."""
+    c = Case(3, 2, 40000, 9).with_mask(0.5).penalise(20)
+    c.params[:, 3] = [float("inf"), 3e38, float("inf")]
+    c.mask[2, 1] = False
+    out = c.run().double().cpu().numpy()
+    for b in range(3):
+        for j in range(2):
+            n = int(c.mask[b, j].sum())
+            want = np.where(c.mask[b, j], 1 / max(n, 1), 0)
+            assert np.all(np.abs(out[b, j] - want) <= want * 2.0 ** -23), (b, j)
+
+
 @pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
 @pytest.mark.parametrize("V", [7, 64, 1001])
 def test_rows_of_every_alignment(V, dtype, out_dtype):
