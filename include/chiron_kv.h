@@ -321,7 +321,7 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  * block's step NaN, and with it every value of the block, until slot 0 of its page is written again.
  *
  *   kv8_pool_create   a handle like kv_pool_create's, over d_cache (256-byte aligned, kv8_pool_bytes()) and a workspace of
- *                     kv_workspace_bytes().  It is destroyed, checked (kv_check_status), and set (ckv_set_overlap) as any
+ *                     kv_workspace_bytes(), of up to 2047 query heads.  It is destroyed, checked (kv_check_status), and set (ckv_set_overlap) as any
  *                     handle; the calls below, and kv_pages_*, take it.  Calls on a bf16 cache refuse it, and
  *                     kv8_* calls refuse a bf16 handle: CKV_EINVAL.
  *   kv8_append        kv_append_rope into the 8-bit cache: the same arguments and rules; keys are rounded to bf16 after the

@@ -276,6 +276,7 @@ int32_t create_pool(const char *fn, const ckv_config *cfg, int bits, void *d_poo
     if (!out_pool) return fail(CKV_EINVAL, "%s: out_pool is NULL", fn);
     *out_pool = nullptr;
     if (!config_ok(cfg, &why)) return fail(CKV_EINVAL, "%s: %s", fn, why);
+    if (bits == 8 && cfg->num_q_heads > ckv::kCache8MaxHeads) return fail(CKV_EINVAL, "%s: num_q_heads above %d", fn, ckv::kCache8MaxHeads);
     if (!d_pool || !d_workspace) return fail(CKV_EINVAL, "%s: NULL device buffer", fn);
     if (reinterpret_cast<uintptr_t>(d_pool) & 255u) return fail(CKV_EINVAL, "%s: the cache is not 256-byte aligned", fn);
     if (reinterpret_cast<uintptr_t>(d_workspace) & 255u) return fail(CKV_EINVAL, "%s: d_workspace not 256-byte aligned", fn);

@@ -31,7 +31,8 @@ struct Append8Params {
     uint32_t q_heads_inv;           // inverse_of(query heads)
 };
 
-// Quotients of small numbers by a divisor >= 2 that is known at the launch: exact for x < 2^16 and d < 2^16.
+// Quotients of small numbers by a divisor >= 2 that is known at the launch: exact for x < 2^16 and d < 2^16, which
+// the rows of a page's tokens are with kCache8MaxHeads query heads.
 inline uint32_t inverse_of(uint32_t d) { return (uint32_t)((0x100000000ull + d - 1) / d); }
 __device__ __forceinline__ int quotient(int x, uint32_t inverse) { return (int)__umulhi((uint32_t)x, inverse); }
 

@@ -17,6 +17,7 @@ constexpr int kTileTokens = kPageSize * kPagesPerTile;
 constexpr int kMaxGroup = 8;         // query heads per KV head handled by one MMA column block
 constexpr int kMaxSpans = 2048;      // upper bound on the partition width (one span per warp)
 constexpr int kMaxBatch = 8192;
+constexpr int kCache8MaxHeads = 2047; // query heads of an 8-bit cache: rows of a page are counted in 16 bits
 constexpr int kTreeFrom = 24;        // pairs cut into more partials than this are merged in two levels
 
 constexpr uint32_t kStatusBadLength = 1u;

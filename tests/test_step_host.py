@@ -46,6 +46,14 @@ def test_create_refuses_buffers_before_any_cuda_call(b):
         assert needle in b.last_error() and "kv8_pool_create" in b.last_error()
 
 
+def test_create_refuses_more_heads_than_a_pages_rows_are_counted_for(b):
+    h = ctypes.c_void_p()
+    for heads, needle in ((2048, "num_q_heads"), (2047, "NULL")):
+        cfg = b.make_config(1, heads, heads, 64, 16, 4, 4)
+        assert b.lib.kv8_pool_create(ctypes.byref(cfg), None, 1 << 40, None, 1 << 40, 0, ctypes.byref(h)) == b.CKV_EINVAL and not h.value
+        assert needle in b.last_error()
+
+
 @pytest.mark.parametrize("change,needle", [
     (dict(batch=0), "batch"), (dict(rows=0), "rows"), (dict(batch=1 << 20, rows=1 << 10), "rows"), (dict(vocab=0), "vocab"),
     (dict(vocab=262129), "vocab"), (dict(in_dtype=2), "dtype"), (dict(out_dtype=-1), "dtype"), (dict(logits=None), "NULL"), (dict(out=None), "NULL"),
