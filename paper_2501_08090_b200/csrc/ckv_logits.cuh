@@ -38,9 +38,8 @@ struct LogitsParams {
     int32_t marked;                 // tokens of a CTA that can change
 };
 
-constexpr int kLogitsThreads = 256, kLogitsCtas = 4;             // CTAs an SM
 // Words of marks that a CTA has room for.
-constexpr int kLogitsWords = 4 * kLogitsThreads, kLogitsMaxVocab = 262128;
+constexpr int kLogitsWords = 1024, kLogitsMaxVocab = 262128;
 
 // The elements of a piece of 16 bytes.
 __device__ __forceinline__ void piece_elements(const uint4 &raw, float (&x)[4])
@@ -85,11 +84,11 @@ __device__ __forceinline__ void store_elements(T *dst, const float *x, bool whol
     }
 }
 
-template <typename Tin, typename Tout>
-__global__ void __launch_bounds__(kLogitsThreads, kLogitsCtas)
+template <typename Tin, typename Tout, int T>
+__global__ void __launch_bounds__(T, 1024 / T)
 logits_process_kernel(const LogitsParams p)
 {
-    constexpr int T = kLogitsThreads, kWarps = T / 32;
+    constexpr int kWarps = T / 32;
     constexpr int E = 16 / sizeof(Tin), U = 16 / E;              // elements of a piece, pieces of a thread at a time
     extern __shared__ uint32_t s_marked[];        // [marked]: the tokens' places in the slice; counts, bit 31: in the prompt, then values; entries plus 1
     __shared__ uint32_t s_marks[kLogitsWords];    // a bit per token of the slice

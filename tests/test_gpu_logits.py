@@ -136,6 +136,21 @@ def test_the_largest_vocabularies(V):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("B,R,V,length,dtype", [(60, 1, 50257, 700, F32), (1, 5, 128256, 4096, BF16), (1, 2, 99991, 9000, F32), (140, 1, 16384, 0, BF16)])
+def test_few_long_slices(B, R, V, length, dtype):
+    """What wide CTAs take: probabilities, the best tokens, logits, and in place."""
+    c = Case(B, R, V, V + B, dtype)
+    c.with_mask(0.6)
+    if length:
+        c.penalise(length).with_bias(40)
+    c.check(c.run())
+    x = c.x.cuda()
+    c.check(c.run(probs=False, x=x, out=x), probs=False)
+    if length:
+        c.params[:, 3] = 0.0
+        c.check(c.run())
+
+
 @pytest.mark.parametrize("part", ["nothing", "params", "history", "drafts", "bias", "mask"])
 @pytest.mark.parametrize("B,R", [(1, 1), (1, 7), (5, 4), (150, 2)])
 def test_each_part_alone(B, R, part):
