@@ -286,6 +286,8 @@ class KvPool:
         self._h = ctypes.c_void_p()
         index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._index, self._index_bytes = index, kv_index_bytes(cfg)
+        self._sizes = Config.from_buffer_copy(cfg)              # as the library's, whatever becomes of cfg
+        self._place = ctypes.addressof(self._sizes), index
         self._scores: Optional[torch.Tensor] = None
         _check(self._create(ctypes.byref(cfg), _dev_ptr(pool), pool.numel() * pool.element_size(),
                             _dev_ptr(workspace), workspace.numel() * workspace.element_size(),
@@ -458,18 +460,12 @@ class KvPool:
                                            _stream_ptr(stream, self._index)))
 
     # -- windows, and pages handed out on the GPU
-    def _attend(self, call, layer, block_tables, seq_lens, q, out, window, sink, stream) -> None:
-        c, dev = self.cfg, self._index
-        batch = self._tables_of(block_tables, seq_lens)
-        shape = (batch, c.num_q_heads, c.head_dim) if q.dim() == 3 else (batch, q.size(1) if q.dim() > 1 else 1, c.num_q_heads, c.head_dim)
-        _check(call(self._h.value, layer, batch, 1 if q.dim() == 3 else shape[1], block_tables.data_ptr(), seq_lens.data_ptr(),
-                    _on(dev, q, torch.bfloat16, "q", *shape), _on(dev, out, torch.bfloat16, "out", *shape), window, sink, _stream_ptr(stream, dev)))
-
     def decode_attention_window(self, layer: int, block_tables, seq_lens, q, out, *, window: int, sink: int = 0, stream=None) -> None:
         """Attention of new tokens to the last `window` tokens (their own included) and the first `sink`.
 
         q, out [batch][Hq][d], or [batch][q_len][Hq][d] with up to 8 new tokens a request."""
-        self._attend(_marshal.decode_attention_window, layer, block_tables, seq_lens, q, out, window, sink, stream)
+        _check(_marshal.decode_attention_window(self._h.value, *self._place, layer, block_tables, seq_lens, q, out, window, sink,
+                                                _stream_ptr(stream, self._index)))
 
     def pages_assign(self, block_tables, seq_lens, new_tokens, free_pages, free_count, *, lens_out, count_out, step_lens=None, new_start=None,
                      slots=None, stream=None) -> None:
@@ -477,23 +473,13 @@ class KvPool:
 
         free_pages int32 [num_pages], free_count int32 [1]; writes block_tables' new entries, lens_out (may be seq_lens), count_out
         (may be free_count) and, if wanted, step_lens [batch], new_start [batch + 1] and slots int64 (one a new token)."""
-        dev, batch = self._index, self._tables_of(block_tables, seq_lens)
-        n_slots = 0 if slots is None else slots.numel()
-        _check(_marshal.kv_pages_assign(
-            self._h.value, batch, block_tables.data_ptr(), seq_lens.data_ptr(), _on(dev, new_tokens, torch.int32, "new_tokens", batch),
-            _on(dev, free_pages, torch.int32, "free_pages", self.cfg.num_pages), _on(dev, free_count, torch.int32, "free_count", 1),
-            _on(dev, lens_out, torch.int32, "lens_out", batch), _on(dev, count_out, torch.int32, "count_out", 1),
-            None if step_lens is None else _on(dev, step_lens, torch.int32, "step_lens", batch),
-            None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
-            _on(dev, slots, torch.int64, "slots", n_slots) if n_slots else None, n_slots, _stream_ptr(stream, dev)))
+        _check(_marshal.pages_assign(self._h.value, *self._place, block_tables, seq_lens, new_tokens, free_pages, free_count, lens_out, count_out,
+                                     step_lens, new_start, slots, _stream_ptr(stream, self._index)))
 
     def pages_release(self, block_tables, seq_lens, keep_lens, free_pages, free_count, *, lens_out, count_out, stream=None) -> None:
         """Return the pages behind each request's first keep_lens tokens (0: all) to the list of free ones."""
-        dev, batch = self._index, self._tables_of(block_tables, seq_lens)
-        _check(_marshal.kv_pages_release(
-            self._h.value, batch, block_tables.data_ptr(), seq_lens.data_ptr(), _on(dev, keep_lens, torch.int32, "keep_lens", batch),
-            _on(dev, free_pages, torch.int32, "free_pages", self.cfg.num_pages), _on(dev, free_count, torch.int32, "free_count", 1),
-            _on(dev, lens_out, torch.int32, "lens_out", batch), _on(dev, count_out, torch.int32, "count_out", 1), _stream_ptr(stream, dev)))
+        _check(_marshal.pages_release(self._h.value, *self._place, block_tables, seq_lens, keep_lens, free_pages, free_count, lens_out, count_out,
+                                      _stream_ptr(stream, self._index)))
 
     def swap_image_bytes(self, n_pages: int) -> int:
         c = self.cfg
@@ -649,40 +635,20 @@ class Kv8Pool(KvPool):
                    interleaved: bool = False, scale: float = 1.0, stream=None) -> None:
         """Quantise new keys and values into their pages; with inv_freq (fp32 [rotary_dim / 2]) turn keys, and queries into
         q_out, by their positions first.  Arguments as kv_append_rope's."""
-        c, dev = self.cfg, self._index
-        batch, tokens = self._tables_of(block_tables, seq_lens), k_new.size(0)
-        q_ptr = out_ptr = None
-        q_stride = out_stride = 0
-        if (q is None) != (q_out is None):
-            raise ValueError("q and q_out go together")
-        if q is not None:
-            q_ptr, q_stride = _rows_on(dev, q, "q", tokens, c.num_q_heads, c.head_dim)
-            out_ptr, out_stride = _rows_on(dev, q_out, "q_out", tokens, c.num_q_heads, c.head_dim)
-        k_ptr, k_stride = _rows_on(dev, k_new, "k_new", tokens, c.num_kv_heads, c.head_dim)
-        v_ptr, v_stride = _rows_on(dev, v_new, "v_new", tokens, c.num_kv_heads, c.head_dim)
-        half = 0 if inv_freq is None else inv_freq.numel()
-        _check(_marshal.kv8_append(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
-                                   None if new_start is None else _on(dev, new_start, torch.int32, "new_start", batch + 1),
-                                   None if inv_freq is None else _on(dev, inv_freq, torch.float32, "inv_freq", half), 2 * half,
-                                   1 if interleaved else 0, scale, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride, out_ptr, out_stride,
-                                   _stream_ptr(stream, dev)))
+        _check(_marshal.kv8_append(self._h.value, *self._place, layer, block_tables, seq_lens, k_new, v_new, q, q_out, inv_freq, new_start,
+                                   interleaved, scale, _stream_ptr(stream, self._index)))
 
     def kv8_gather(self, layer: int, block_tables, seq_lens, k, v, *, start=None, stream=None) -> None:
         """The values of each request's last tokens: k, v bf16 [tokens][Hkv][d], tokens may lie apart.  start int32 [batch + 1]: each
         request's first row; without it every request has the same number."""
-        c, dev = self.cfg, self._index
-        batch, tokens = self._tables_of(block_tables, seq_lens), k.size(0)
-        k_ptr, k_stride = _rows_on(dev, k, "k", tokens, c.num_kv_heads, c.head_dim)
-        v_ptr, v_stride = _rows_on(dev, v, "v", tokens, c.num_kv_heads, c.head_dim)
-        _check(_marshal.kv8_gather(self._h.value, layer, batch, tokens, block_tables.data_ptr(), seq_lens.data_ptr(),
-                                   None if start is None else _on(dev, start, torch.int32, "start", batch + 1), k_ptr, k_stride, v_ptr, v_stride,
-                                   _stream_ptr(stream, dev)))
+        _check(_marshal.kv8_gather(self._h.value, *self._place, layer, block_tables, seq_lens, k, v, start, _stream_ptr(stream, self._index)))
 
     def kv8_attention(self, layer: int, block_tables, seq_lens, q, out, *, window: int = 0, sink: int = 0, stream=None) -> None:
         """Attention of new tokens over the 8-bit cache: the whole context, or the last `window` tokens and the first `sink`.
 
         q, out [batch][Hq][d], or [batch][q_len][Hq][d] with up to 8 new tokens a request."""
-        self._attend(_marshal.kv8_attention, layer, block_tables, seq_lens, q, out, window, sink, stream)
+        _check(_marshal.kv8_attention(self._h.value, *self._place, layer, block_tables, seq_lens, q, out, window, sink,
+                                      _stream_ptr(stream, self._index)))
 
 
 def decode_attention_noalloc(cfg: Config, pool: torch.Tensor, layer: int, block_tables, seq_lens, q, out,

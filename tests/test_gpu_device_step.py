@@ -150,3 +150,51 @@ def test_a_speculative_step_in_a_graph():
     assert total > 0
     plain.close()
     kp.close()
+
+
+def test_arguments_that_do_not_fit_are_named():
+    """Every tensor of every call: of another type, shape, layout or device, or none at all, it is refused by its name."""
+    B, T, H, K, P = 3, 6, 8, 2, 5
+    cfg = b.make_config(1, H, K, D, 20, P, 4)
+    pool, pool8 = b.KvPool(cfg), b.Kv8Pool(cfg)
+
+    def ints(*shape, dtype=torch.int32):
+        return torch.zeros(shape, dtype=dtype, device="cuda")
+
+    def rows(*shape):
+        return torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+
+    step = dict(block_tables=ints(B, P), seq_lens=ints(B))
+    pages = dict(step, free_pages=ints(20), free_count=ints(1), lens_out=ints(B), count_out=ints(1))
+    calls = [
+        (pool.pages_assign, dict(pages, new_tokens=ints(B), step_lens=ints(B), new_start=ints(B + 1), slots=ints(7, dtype=torch.int64)), {}),
+        (pool8.pages_release, dict(pages, keep_lens=ints(B)), {}),
+        (pool.decode_attention_window, dict(step, q=rows(B, 2, H, D), out=rows(B, 2, H, D)), dict(layer=0, window=5)),
+        (pool8.kv8_attention, dict(step, q=rows(B, H, D), out=rows(B, H, D)), dict(layer=0)),
+        (pool8.kv8_append, dict(step, k_new=rows(T, K, D), v_new=rows(T, K, D), q=rows(T, H, D), q_out=rows(T, H, D),
+                                inv_freq=torch.zeros(16, device="cuda"), new_start=ints(B + 1)), dict(layer=0)),
+        (pool8.kv8_gather, dict(step, k=rows(T, K, D), v=rows(T, K, D), start=ints(B + 1)), dict(layer=0))]
+    sparse = torch.zeros(B, device="cuda").to_sparse()
+    for call, tensors, others in calls:
+        call(**tensors, **others)
+        for name, t in tensors.items():
+            wrong = [t.cpu(), t.to(torch.float16), t[None, None], 5, "x", sparse]
+            if name not in ("slots", "inv_freq", "seq_lens", "q", "k_new", "k"):         # others follow the sizes of these
+                wrong.append(torch.cat([t, t]))
+            if name != "seq_lens" and t.numel() > 1:
+                wrong.append(torch.stack([t, t], -1)[..., 0])                            # elements apart
+            for w in wrong:
+                with pytest.raises(ValueError) as e:
+                    call(**dict(tensors, **{name: w}), **others)
+                assert "must be" in str(e.value) or "go together" in str(e.value)
+                if "must be" in str(e.value) and name not in ("seq_lens", "q", "k_new", "k"):
+                    assert str(e.value).startswith(name + " must be"), (call.__name__, name, e.value)
+        if "layer" in others:
+            with pytest.raises(OverflowError):
+                call(**tensors, **dict(others, layer=1 << 40))
+    with pytest.raises(ValueError):
+        pool8.kv8_append(0, **dict(calls[4][1], q_out=None))
+    pool.close()
+    with pytest.raises(b.CkvError):
+        pool.decode_attention_window(0, window=5, **calls[2][1])
+    torch.cuda.synchronize()
