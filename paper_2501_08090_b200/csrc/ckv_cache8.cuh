@@ -23,6 +23,9 @@ namespace ckv {
 // key), then its warps take the page's blocks, two per kv head, and after them the query rows.  A warp holds a block's
 // new rows in registers, 16 elements a lane and turn, between finding their maximum and quantising them; the first
 // block's are on their way before the page is looked up.
+//
+// Prompts are bound by HBM: 32909 tokens of 32 + 8 + 8 heads x 128 (741 MB) 120 us, 94 % of a copy's rate.  Few tokens by launch,
+// look-ups and instructions: one token 3.4 us, five of 96 requests with 64 query heads 8.0, 3.9 without queries.
 struct Append8Params {
     RopeParams rope;                // pool_layer unused; inv_freq NULL: nothing is turned; q NULL: no queries
     uint8_t *records;               // the layer's records
@@ -295,7 +298,8 @@ kv8_append_kernel(const Append8Params p)
 
 // ------------------------------------------------------------------------------------------
 // The values of each request's last tokens, as bf16 rows: exact, since n has 7 bits and the step is a power
-// of two.  A CTA per page, as in the append; a thread moves 16 elements.
+// of two.  A CTA per page, as in the append; a thread moves 16 elements.  33 000 tokens of 8 heads x 128 (203 MB): 37 us,
+// 83 % of a copy's rate, since a page's look-ups stand before 96 KB; one request's last tokens 3.5.
 // ------------------------------------------------------------------------------------------
 struct Gather8Params {
     const uint8_t *records;         // the layer's

@@ -893,6 +893,10 @@ cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
 
 // ------------------------------------------------------------------------------------------
 // A cluster of CTAs per pair and block of new tokens; q_pass: new tokens of a block.
+//
+// Windows of 2048 of 64 requests, 8 kv heads x 128: bf16 (538 MB) 78.6 us, a copy's rate and what neighbours find in L2; 8-bit
+// (270 MB) 46.5 us, 89 % of it, the rest start and fold.  Four warps a CTA instead of six: 56 us in 8 bits.  One request's
+// window of 512 in 8 bits takes 5.2 us, launch and a chain of look-ups, tiles and folds.
 // ------------------------------------------------------------------------------------------
 template <int D, bool k8>
 struct PairShape {

@@ -16,7 +16,7 @@ namespace ckv {
 // Bound by HBM: a logit is read once and a result written once.  A cluster of CTAs owns a row, a CTA a slice of it.  The
 // slice is brought into L2 by one bulk prefetch as the CTA starts, and read there twice, as pieces of 16 aligned
 // bytes: for the maximum and the sum, and for the results.  (Held in registers between, 32 tokens a thread, it cost 64
-// registers and two to four CTAs an SM: 141 us for 512 rows of 50257 tokens with everything, against 69; alone 57 against 43.)
+// registers and two to four CTAs an SM: 141 us for 512 rows of 50257 tokens with everything, against 70; alone 57 against 43.)
 // Tokens that change are few.  Meanwhile the CTA marks them, a bit each; the marks before a token give it a place in short
 // arrays in shared memory, where its occurrences are counted and its bias's last entry is found (whole numbers, and
 // the largest of entries: the order of atomics does not show), and where the CTA's threads handle them in turn.
