@@ -281,7 +281,7 @@ int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
                                           : (interleaved ? ckv::kv8_append_kernel<64, true> : ckv::kv8_append_kernel<64, false>);
     // where pages are few, several CTAs a page, as far as they fit the GPU at a time: their blocks and query rows are chains of
     // look-ups and loads (one token 4.1 us in one CTA, 3.3 in several); twice as far with query rows (five tokens of 96 requests:
-    // 8.5 us in two CTAs a page, 8.0 in four; without queries 3.9 and 4.7)
+    // 8.5 us in two CTAs a page, 7.8 in four; without queries 3.9 and 4.7)
     const unsigned pages = page_ctas(d_new_start, n_tokens, batch);
     ap.parts = 1;
     while (ap.parts < 4 && pages * 2u * ap.parts <= (d_q ? 6u : 3u) * pool->num_sms) ap.parts *= 2;
