@@ -19,7 +19,8 @@ namespace ckv {
 // mma.sync on them, the softmax in the log2 domain with a running maximum; what it has of a pair at the end is a
 // partial (m, l, O):   M = max m_i,  out = sum 2^(m_i - M) O_i / sum 2^(m_i - M) l_i.
 //   cache_attn_pair_kernel   (windows, short tables: pairs of one length, nearly)  a cluster of CTAs owns a (request, kv
-//       head), its warps take the tiles in turn; partials are folded in (distributed) shared memory.
+//       head), its warps take the tiles in turn; partials are folded in shared memory, the CTAs' pushed to
+//       the one that looks after a column.
 //   cache_attn_span_kernel   (contexts that differ a thousandfold)  the tiles of all pairs lie on one axis, kCacheCost
 //       units ahead of each pair for what a piece costs besides its tiles, and every warp takes an even span of
 //       it: no plan on the host.  A pair within one span is finished there, one within a CTA by the CTA at its end;
@@ -896,29 +897,14 @@ cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
 //
 // Windows of 2048 of 64 requests, 8 kv heads x 128: bf16 (538 MB) 78.6 us, a copy's rate and what neighbours find in L2; 8-bit
 // (270 MB) 46.5 us, 89 % of it, the rest start and fold.  Four warps a CTA instead of six: 56 us in 8 bits.  One request's
-// window of 512 in 8 bits takes 5.2 us, launch and a chain of look-ups, tiles and folds.
+// window of 512 in 8 bits takes 4.9 us, launch and a chain of look-ups, tiles and folds (5.3 while the cluster's CTAs read each
+// other's partials between two barriers, where they now push them before one).
 // ------------------------------------------------------------------------------------------
 template <int D, bool k8>
 struct PairShape {
     static constexpr int kWarps = 6, kStages = (k8 ? 2 : 1) * (D == 128 ? 1 : 2), kCtas = 2;     // CTAs resident on an SM
     using Layout = CacheAttnLayout<D, k8, kWarps, kStages>;
-    static constexpr int kCtaPartOff = Layout::kRingBytes / 2;   // the CTA's partial lies in the second half of warp 0's ring
-    static_assert(PartLayout<D>::kFloats * 4 <= Layout::kRingBytes / 2, "two partials must fit a ring");
 };
-
-__device__ __forceinline__ float4 ld_dsmem_f32x4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
-    return v;
-}
-
-__device__ __forceinline__ float ld_dsmem_f32(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr));
-    return v;
-}
 
 template <int D, bool k8>
 __global__ void __launch_bounds__(PairShape<D, k8>::kWarps * 32, PairShape<D, k8>::kCtas)
@@ -927,9 +913,12 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
     using Shape = PairShape<D, k8>;
     using Part = PartLayout<D>;
     constexpr int W = Shape::kWarps, S = Shape::kStages;
+    constexpr int kMostCtas = 16;
     extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(16) float s_fold[kMostCtas][D + 4];     // written by the cluster's CTAs: a column's partial, O, then m and l
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // waited for before others' shared memory is written
     const int rank = (int)cluster_rank(), ctas = (int)cluster_size();
     // blocks of new tokens that the columns hold at a time: neighbours, so that they meet in L2
     const int per_pass = params.q_pass, passes = (params.q_len + per_pass - 1) / per_pass;
@@ -953,6 +942,7 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
             }
             if (threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
         }
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         return;
     }
     const uint64_t policy = l2_evict_first_policy();
@@ -984,32 +974,41 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
     part.finish();
     part.store_partial((float *)(smem + warp * Shape::Layout::kRingBytes), lane, ring.alive);
     __syncthreads();
-    // ---- the CTA's fold, a column a warp
-    float *mine = (float *)(smem + Shape::kCtaPartOff);
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");          // every CTA of the cluster runs
+    // ---- the CTA's fold, a column a warp; the results go to the CTA that looks after the column, column c to CTA c % ctas
     for (int col = warp; col < ncols; col += W) {
         const FoldSum f = fold_column<D>(W, col, lane, [&](int i) -> const float * { return (const float *)(smem + i * Shape::Layout::kRingBytes); });
-        if (ctas == 1) store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
-        else store_fold_partial<D>(mine, col, f, lane);
+        if (ctas == 1) {
+            store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
+            continue;
+        }
+        const float *slot = s_fold[col / ctas * ctas + rank];
+        const int owner = col % ctas;
+        if (lane * 4 < D)
+            asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(cluster_map(smem_u32(slot + lane * 4), owner)), "f"(f.acc.x), "f"(f.acc.y), "f"(f.acc.z), "f"(f.acc.w) : "memory");
+        if (lane == 0) asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(cluster_map(smem_u32(slot + D), owner)), "f"(f.m), "f"(f.l) : "memory");
     }
     if (ctas == 1) return;
     cluster_barrier();
-    // ---- the cluster's fold: CTA c takes columns c, c + ctas, ...
+    // ---- the cluster's fold
     for (int col = rank + warp * ctas; col < ncols; col += W * ctas) {
-        const uint32_t head = smem_u32(mine) + col * 4, row = smem_u32(mine) + (Part::kHead + col * Part::kPitch + lane * 4) * 4;
-        FoldSum f = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-        for (int c = 0; c < ctas; ++c) f.m = fmaxf(f.m, ld_dsmem_f32(cluster_map(head, c)));
+        const float(*part)[D + 4] = s_fold + col / ctas * ctas;
+        FoldSum f = {lane < ctas ? part[lane][D] : -INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+        for (int x = kMostCtas / 2; x > 0; x >>= 1) f.m = fmaxf(f.m, __shfl_xor_sync(0xffffffffu, f.m, x));
+        f.m = __shfl_sync(0xffffffffu, f.m, 0);
         const float ref = f.m == -INFINITY ? 0.f : f.m;
         for (int c = 0; c < ctas; ++c) {
-            const float w = fast_exp2(ld_dsmem_f32(cluster_map(head, c)) - ref);
-            f.l += w * ld_dsmem_f32(cluster_map(head + 4 * kMaxGroup, c));
+            const float w = fast_exp2(part[c][D] - ref);
+            f.l += w * part[c][D + 1];
             if (lane * 4 < D) {
-                const float4 a = ld_dsmem_f32x4(cluster_map(row, c));
+                const float4 a = *(const float4 *)(part[c] + lane * 4);
                 f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;
             }
         }
         store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
     }
-    cluster_barrier();                            // nobody leaves while others read its partial
 }
 
 }  // namespace ckv

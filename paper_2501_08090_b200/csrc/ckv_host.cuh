@@ -157,6 +157,24 @@ cudaError_t allow(Kernel kernel, bool wide_cluster, size_t smem)
     return e;
 }
 
+// How many clusters of this size the GPU holds at a time: less than its CTAs' number says, since a cluster stays within a part
+// of the GPU.
+template <typename Kernel>
+cudaError_t resident_clusters(Kernel kernel, unsigned threads, size_t smem, unsigned cluster, int *clusters)
+{
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(cluster);
+    lc.blockDim = dim3(threads);
+    lc.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    lc.attrs = &attr;
+    lc.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(clusters, kernel, &lc);
+}
+
 // The handle of kv_pool_create and kv8_pool_create (ckv_api.cu).
 int32_t create_pool(const char *fn, const ckv_config *cfg, int bits, void *d_pool, size_t pool_bytes, void *d_workspace,
                     size_t workspace_bytes, int32_t device, ckv_pool **out_pool);

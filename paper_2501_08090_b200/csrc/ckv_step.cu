@@ -64,27 +64,33 @@ int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *s
 {
     using Span = ckv::SpanShape<D, k8>;
     using Pair = ckv::PairShape<D, k8>;
-    static thread_local int configured_device = -1;
+    static thread_local int configured_device = -1, resident[5];              // clusters of 1, 2, 4, 8, 16 CTAs
     auto span = ckv::cache_attn_span_kernel<D, k8>;
     auto pair = ckv::cache_attn_pair_kernel<D, k8>;
     if (configured_device != pool->device) {
         CKV_CUDA(allow(span, false, Span::Layout::kSmemBytes));
         CKV_CUDA(allow(pair, true, Pair::Layout::kSmemBytes));
+        for (int i = 0; i < 5; ++i) CKV_CUDA(ckv::resident_clusters(pair, Pair::kWarps * 32, Pair::Layout::kSmemBytes, 1u << i, &resident[i]));
         configured_device = pool->device;
     }
     // The most tiles that a pair can have, and the clusters that own pairs: as many CTAs as its tiles feed, while all
-    // of them fit the GPU.
+    // clusters run at once, with room for those of a call before that have not ended; without that room where a
+    // warp would have more than 5 tiles else.  Windows of 2048 of 2 requests, 8 kv heads, 8-bit: 8 CTAs a pair 6.7 us, 16, which do not all run at
+    // once, 10.3; of 4 requests, bf16: 4 CTAs (3 tiles a warp) 9.6, 8, which just do, 12.0; of 8 requests: 2 (6) 14.6, 4 14.0.
     const long long table = ap.max_pages_per_req;
     const long long cut = ((long long)ap.window + ap.q_len + ckv::kPageSize - 2) / ckv::kPageSize + 1 + ckv::pages_of(ap.sink);
     const bool windowed = ap.window > 0 && cut < table;
     const long long tiles = ((windowed ? cut : table) + ckv::kPagesPerTile - 1) / ckv::kPagesPerTile, pairs = (long long)ap.batch * ap.num_kv_heads;
     const int per_pass = std::min(ap.q_len, ckv::kMaxGroup / ap.group), passes = (ap.q_len + per_pass - 1) / per_pass;      // a launch holds 8 columns
     const long long blocks = pairs * passes;
-    unsigned cluster = 1;
-    while (cluster < 16 && (long long)cluster * Pair::kWarps < tiles && 2 * cluster * blocks <= (long long)Pair::kCtas * pool->num_sms) cluster *= 2;
+    int size = 0;
+    while (size < 4 && ((long long)Pair::kWarps << size) < tiles &&
+           (4 * blocks <= 3ll * resident[size + 1] || (blocks <= resident[size + 1] && tiles > (5ll * Pair::kWarps << size))))
+        ++size;
+    const unsigned cluster = 1u << size;
     // Pairs that a window cuts are of one length, nearly: a cluster owns each, if the clusters fill the GPU.  Otherwise that
     // pays while a warp has few tiles: the even spans cost 4 us before they win.  Measured, us, pairs against spans: windows of
-    // 2048 of 64 requests, bf16 78.9 and 88.3, 8-bit 46.4 and 51.5; one request, 8-bit, of 16384 tokens (5 tiles a warp) 15.4
+    // 2048 of 64 requests, bf16 78.9 and 88.3, 8-bit 46.4 and 51.5; one request, 8-bit, of 16384 tokens (5 tiles a warp) 14.8
     // and 16.6, of 32000 (10) 23.1 and 20.9; 64 requests of 1 to 1024 tokens (at most 5) 21.5 and 24.2, of 1 to 4096 (21)
     // 60.6 and 51.7.
     if (tiles <= 8ll * cluster * Pair::kWarps || (windowed && blocks * cluster > pool->num_sms)) {
@@ -280,7 +286,7 @@ int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
     const auto kernel = c.head_dim == 128 ? (interleaved ? ckv::kv8_append_kernel<128, true> : ckv::kv8_append_kernel<128, false>)
                                           : (interleaved ? ckv::kv8_append_kernel<64, true> : ckv::kv8_append_kernel<64, false>);
     // where pages are few, several CTAs a page, as far as they fit the GPU at a time: their blocks and query rows are chains of
-    // look-ups and loads (one token 4.1 us in one CTA, 3.3 in several); twice as far with query rows (five tokens of 96 requests:
+    // look-ups and loads (one token 3.4 us in one CTA, 2.6 in several); twice as far with query rows (five tokens of 96 requests:
     // 8.5 us in two CTAs a page, 7.8 in four; without queries 3.9 and 4.7)
     const unsigned pages = page_ctas(d_new_start, n_tokens, batch);
     ap.parts = 1;
