@@ -222,9 +222,9 @@ int32_t launch_logits(ckv::LogitsParams &lp, int32_t batch, void *stream)
     lp.pieces = (int)(slice() / E);
     lp.marked = (int)std::min(lists, slice());
     // Twice the threads where all CTAs are on their way at once with much to go through: one request's 5 rows of 128256 tokens
-    // with a history of 4096 9.3 us instead of 11.7, 64 rows of 50257 with everything 14.2 instead of 18.2, 140 of 16384 alone 5.4
+    // with a history of 4096 9.0 us instead of 11.5, 64 rows of 50257 with everything 13.8 instead of 18.0, 140 of 16384 alone 5.4
     // instead of 6.2.  With little, fewer warps meet sooner: 16 rows of 50257 with everything 10.2 and 10.3, 8 with a mask
-    // 4.2 and 5.4; and many rows go through four narrow CTAs an SM faster: 512 with everything 70 and 77.
+    // 4.2 and 5.4; and many rows go through four narrow CTAs an SM faster: 512 with everything 68 and 75.
     const bool wider = rows * cluster <= 2 * num_sms && lists + slice() >= 8192;
     CKV_CUDA(enqueue(wider ? wide : narrow, (unsigned)(rows * cluster), wider ? kWide : kNarrow, arrays * lp.marked, true, cluster, stream, lp));
     return CKV_OK;
