@@ -24,8 +24,8 @@ namespace ckv {
 // new rows in registers, 16 elements a lane and turn, between finding their maximum and quantising them; the first
 // block's are on their way before the page is looked up.
 //
-// Prompts are bound by HBM: 32909 tokens of 32 + 8 + 8 heads x 128 (741 MB) 120 us, 94 % of a copy's rate.  Few tokens by launch,
-// look-ups and instructions: one token 2.6 us, five of 96 requests with 64 query heads 7.8, 3.9 without queries.
+// Prompts are bound by HBM: 32909 tokens of 32 + 8 + 8 heads x 128 (741 MB) 118 us, 96 % of a copy's rate.  Few tokens by launch,
+// look-ups and instructions: one token 2.6 us, five of 96 requests with 64 query heads 7.5, 3.7 without queries.
 struct Append8Params {
     RopeParams rope;                // pool_layer unused; inv_freq NULL: nothing is turned; q NULL: no queries
     uint8_t *records;               // the layer's records
@@ -229,13 +229,7 @@ kv8_append_kernel(const Append8Params p)
         const bool value = item >= rp.num_kv_heads;
         const size_t block = ((size_t)page * rp.num_kv_heads + (value ? item - rp.num_kv_heads : item)) * 2 + value;
         uint8_t *rows = p.records + block * kPageSize * D;
-        // a coarser step means that older rows are requantised: they are fetched beside the step
-        constexpr int kOld = kPageSize * D / 16 / 32;            // pieces of 16 records a lane
         const float before = a > 0 ? p.steps[block] : 0.f;
-        uint4 old[kOld];
-#pragma unroll
-        for (int k = 0; k < kOld; ++k)
-            if (k * 32 + lane < a * D / 16) old[k] = ((const uint4 *)rows)[k * 32 + lane];
         uint32_t most = 0;
 #pragma unroll
         for (int k = 0; k < kTurns; ++k) {
@@ -259,12 +253,13 @@ kv8_append_kernel(const Append8Params p)
                 *(uint2 *)(rows + (a + i) * D + e1) = quantise8(x[k][1], inv);
             }
         }
-        if (a > 0 && finite && bits != __float_as_uint(before)) {                // older rows get the coarser step
+        if (a > 0 && finite && bits != __float_as_uint(before)) {                // older rows get the coarser step: seldom, so fetched only then
             const float ratio = before * inv;
-#pragma unroll
-            for (int k = 0; k < kOld; ++k)
-                if (k * 32 + lane < a * D / 16)
-                    ((uint4 *)rows)[k * 32 + lane] = make_uint4(coarser(old[k].x, ratio), coarser(old[k].y, ratio), coarser(old[k].z, ratio), coarser(old[k].w, ratio));
+#pragma unroll 1
+            for (int i = lane; i < a * D / 16; i += 32) {
+                const uint4 old = ((const uint4 *)rows)[i];
+                ((uint4 *)rows)[i] = make_uint4(coarser(old.x, ratio), coarser(old.y, ratio), coarser(old.z, ratio), coarser(old.w, ratio));
+            }
         }
         if (lane == 0) p.steps[block] = __uint_as_float(bits);
         if (item + item_step < items) fetch(item + item_step);
