@@ -293,6 +293,21 @@ def test_attention_however_the_work_is_cut(lens):
     c.kp.close()
 
 
+@pytest.mark.parametrize("batch", [1, 2, 3, 5, 9, 18, 36])
+@pytest.mark.parametrize("layout,window,q_len", [((16, 8, 128), 0, 1), ((16, 8, 128), 900, 3), ((32, 8, 64), 0, 1)])
+def test_attention_of_few_requests_and_many(batch, layout, window, q_len):
+    """Short tables and windows, from as many CTAs a pair as fit to one."""
+    lens = [40 + (577 * r) % 1100 for r in range(batch)]
+    bt, n = tables_for(lens, ref.pages(1200), 41)
+    c = Cache(layout, bt, n, seed=42)
+    q = queries(batch, q_len, c.H, c.D, 43)
+    out = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    c.kp.kv8_attention(0, c.btd, c.lens(lens), to_dev(q), out, window=window, sink=5 if window else 0)
+    c.check()
+    check_attention(c, lens, q, out, window, 5 if window else 0)
+    c.kp.close()
+
+
 def test_attention_three_dimensional_queries_and_unusable_lengths():
     lens = [40, 0, 500, -3, 16, 10 ** 9]
     bt, n = tables_for([40, 0, 500, 0, 16, 0], 32, 18)

@@ -65,6 +65,24 @@ def test_however_the_work_is_cut(lens, window, sink):
     c.kp.close()
 
 
+@pytest.mark.parametrize("batch", [1, 2, 3, 5, 9, 18, 36])
+@pytest.mark.parametrize("layout,window,q_len", [((32, 8, 128), 1500, 1), ((16, 8, 64), 700, 6)])
+def test_few_requests_and_many(batch, layout, window, q_len):
+    """Pairs of one length from as many CTAs as fit to one each; an unusable length among them."""
+    lens = [window // 2 + (577 * r) % (2 * window) for r in range(batch)]
+    bt, n = tables_for(lens, ref.pages(3 * window), 13)
+    c = Cache(layout, bt, n, seed=14)
+    q = queries(batch, q_len, c.H, c.D, 15)
+    out = c.run(lens, q, window, 20)
+    c.check(lens, q, out, window, 20)
+    assert c.kp.check_status() == 0
+    if batch > 2:
+        again = c.run(lens[:1] + [q_len - 1] + lens[2:], q, window, 20)
+        assert not again[1].any() and torch.equal(again[0], out[0]) and torch.equal(again[2:], out[2:])
+        assert c.kp.check_status(raise_on_error=False) == 1
+    c.kp.close()
+
+
 @pytest.mark.parametrize("q_len", [1, 4])
 @pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
 def test_what_a_token_does_not_see_does_not_reach_it(q_len, what):
