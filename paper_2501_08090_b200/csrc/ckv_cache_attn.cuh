@@ -39,7 +39,11 @@ namespace ckv {
 // exact).
 // V's steps: the contribution of token t to O is 2^(s_t - m) step_t n_t, so with e_t = log2(step_t) the weights
 // P_t = 2^(s_t + e_t - M), M the running maximum of s + e, are at most 2^8 whatever the steps are, and
-// l = sum_t P_t 2^-e_t.  They are rounded to fp16 (2^-11) for P V and summed unrounded in fp32.
+// l = sum_t P_t 2^-e_t.  They are rounded to fp16 (2^-11, or 2^-25 of the reference where that is more) for P V and summed unrounded in fp32.
+// A warp sums l 2^K, K the e of its first page: the factor is 2^(K - e_t), and while every |e_t - K| <= 30 what P_t loses below 2^-126
+// is 2^-66 of l.  With steps further apart it would not do: tokens of a block of zeros, whose step is 2^-106, count in l
+// as any others, and their P_t vanish beside a large step's.  From the first such page on (`far` below) l is summed against a reference r
+// of its own, the running maximum of s alone.
 // In the bf16 cache weights are rounded to bf16 as everywhere in this library (the instruction takes one type).
 //
 // Masked values.  A masked score is selected away, and a masked row of the bf16 cache too: its weight is 0, but
@@ -165,8 +169,11 @@ struct CacheAttnLayout {
     static_assert(PartLayout<D>::kFloats * 4 <= kRingBytes, "a warp's partial takes its ring's place");
 };
 
-// l is kept 2^-5 smaller than it is: with steps of 2^-106 to 2^121 it stays a normal number for 2^16 tokens and more.
-constexpr int kCacheSumBias = 5;
+// A warp's final l, against m as O is, is kept 2^-5 smaller than it is: with steps of 2^-106 to 2^121 it stays a normal number
+// for 2^16 tokens and more.
+constexpr int kCacheSumBias = 5, kCacheStepRange = 30;
+
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }       // -126 <= e <= 127
 
 template <bool k8>
 __device__ __forceinline__ float sum_bias()
@@ -275,6 +282,10 @@ struct PairPart {
     int seen_head, seen_from, seen_to;           // tiles that every column sees entirely: [0, seen_head) and [seen_from, seen_to)
     uint32_t k_off, v_off;          // ldmatrix: this lane's rows of a page's keys and values, piece 0 or 1
     float m0, m1, l0, l1;
+    static constexpr int kNoStep = 1 << 20;
+    int K;                          // 8-bit: l is 2^K times what it is against m; far: l is against r, and d = 2^(m - r)
+    bool far;
+    float r0, r1, d0, d1;
     float o[kSteps16][4];
 
     __device__ __forceinline__ void begin(const CacheAttnParams &p, const Visited &vis, int r, int h, int L, int lane)
@@ -339,6 +350,10 @@ struct PairPart {
         }
         m0 = m1 = -INFINITY;
         l0 = l1 = 0.f;
+        K = k8 ? kNoStep : 0;
+        far = false;
+        r0 = r1 = -INFINITY;
+        d0 = d1 = 0.f;
 #pragma unroll
         for (int ks = 0; ks < kSteps16; ++ks) o[ks][0] = o[ks][1] = o[ks][2] = o[ks][3] = 0.f;
     }
@@ -351,13 +366,14 @@ struct PairPart {
     // A tile in shared memory at sb, its steps at steps.
     __device__ __forceinline__ void tile(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
     {
-        if (ti < seen_head || (ti >= seen_from && ti < seen_to)) tile_as<true>(p, vis, ti, sb, steps, lane);
-        else tile_as<false>(p, vis, ti, sb, steps, lane);
+        if (!far && (ti < seen_head || (ti >= seen_from && ti < seen_to)) && tile_as<true>(p, vis, ti, sb, steps, lane)) return;
+        tile_as<false>(p, vis, ti, sb, steps, lane);
     }
 
-    // all_seen: two whole pages, which every column sees entirely.
+    // all_seen: two whole pages, which every column sees entirely.  It is `far` for the other form: false, with nothing done, where
+    // the tile's steps are far from 2^K.  (A form of its own for parts that are far cost the others 2 %.)
     template <bool all_seen>
-    __device__ __forceinline__ void tile_as(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
+    __device__ __forceinline__ bool tile_as(const CacheAttnParams &p, const Visited &vis, int ti, uint32_t sb, uint32_t steps, int lane)
     {
         constexpr int kPageBytes = 32 * D * (k8 ? 1 : 2), kHalfBytes = 32 * 128;
         const int np = all_seen ? kPagesPerTile : min(kPagesPerTile, vis.count - ti * kPagesPerTile);
@@ -404,7 +420,9 @@ struct PairPart {
             });
         }
         // ---- scores in the log2 domain, V's step among them
+        int e[kPagesPerTile] = {};               // log2 of V's step
         float wl[kPagesPerTile];                 // what a weight counts for in l
+        bool near = true;
         float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
         for (int mt = 0; mt < kPagesPerTile; ++mt) {
@@ -413,11 +431,13 @@ struct PairPart {
             if constexpr (k8) {
                 float ks, vs;
                 asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(vs) : "r"(steps + mt * 8));
-                const int e = (int)(__float_as_uint(vs) >> 23 & 255u);
+                e[mt] = (int)(__float_as_uint(vs) >> 23 & 255u) - 127;           // 128 where the block is NaN
+                if (!all_seen && mt >= np) e[mt] = e[0];         // a page that is not there, of masked tokens
                 a0 *= ks;
                 a1 *= ks;
-                add = (float)(e - 127) + (vs - vs);              // NaN where the block is
-                wl[mt] = __uint_as_float((uint32_t)max(254 - kCacheSumBias - e, 0) << 23);
+                add = (float)e[mt] + (vs - vs);
+                wl[mt] = power_of_two(K - e[mt]);
+                near = near && (unsigned)(K - e[mt] + kCacheStepRange) <= 2u * kCacheStepRange;
             }
             s[mt][0] = fmaf(s[mt][0], a0, add);
             s[mt][1] = fmaf(s[mt][1], a1, add);
@@ -435,7 +455,27 @@ struct PairPart {
         }
         // The reference that a column's exponentials are taken against moves only when a score exceeds it by
         // more than 2^8; a column with nothing above -inf so far takes them against 0: they come out 0.
-        if (__any_sync(0xffffffffu, mx0 > m0 + 8.f || mx1 > m1 + 8.f)) {
+        // (Steps that are not near are looked at here too, since a branch is taken anyway.)
+        constexpr bool may_be_far = k8 && !all_seen;
+        float lim0 = m0, lim1 = m1;
+        if (may_be_far && far) {                 // r moves too, where a score may exceed it by as much
+            const float low = (float)min(e[0], e[kPagesPerTile - 1]);
+            lim0 = fminf(lim0, r0 + low);
+            lim1 = fminf(lim1, r1 + low);
+        }
+        if (__any_sync(0xffffffffu, mx0 > lim0 + 8.f || mx1 > lim1 + 8.f || (k8 && !near))) {
+            if (k8 && !near && !(may_be_far && far)) {
+                const bool begins = K == kNoStep;
+                if (begins) K = e[0];
+                if (!begins || abs(K - e[kPagesPerTile - 1]) > kCacheStepRange) {
+                    if (all_seen) return false;
+                    far = true;
+                    r0 = m0 - (float)K;
+                    r1 = m1 - (float)K;
+                }
+#pragma unroll
+                for (int mt = 0; mt < kPagesPerTile; ++mt) wl[mt] = power_of_two(K - e[mt]);
+            }
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) {
                 mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, x));
@@ -445,8 +485,29 @@ struct PairPart {
             m0 = fmaxf(m0, mx0);
             m1 = fmaxf(m1, mx1);
             const float al0 = fast_exp2(old0 - (m0 == -INFINITY ? 0.f : m0)), al1 = fast_exp2(old1 - (m1 == -INFINITY ? 0.f : m1));
-            l0 *= al0;
-            l1 *= al1;
+            if (may_be_far && far) {
+                float t0 = -INFINITY, t1 = -INFINITY;            // the largest scores, without the steps
+#pragma unroll
+                for (int mt = 0; mt < kPagesPerTile; ++mt) {
+                    t0 = fmaxf(t0, fmaxf(s[mt][0], s[mt][2]) - (float)e[mt]);
+                    t1 = fmaxf(t1, fmaxf(s[mt][1], s[mt][3]) - (float)e[mt]);
+                }
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) {
+                    t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, x));
+                    t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, x));
+                }
+                const float was0 = r0, was1 = r1;
+                r0 = fmaxf(r0, t0);
+                r1 = fmaxf(r1, t1);
+                l0 *= fast_exp2(was0 - (r0 == -INFINITY ? 0.f : r0));
+                l1 *= fast_exp2(was1 - (r1 == -INFINITY ? 0.f : r1));
+                d0 = m0 == -INFINITY ? 0.f : fast_exp2(m0 - r0);
+                d1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - r1);
+            } else {
+                l0 *= al0;
+                l1 *= al1;
+            }
 #pragma unroll
             for (int c = 0; c < kSteps16; ++c) { o[c][0] *= al0; o[c][2] *= al0; o[c][1] *= al1; o[c][3] *= al1; }
         }
@@ -456,8 +517,22 @@ struct PairPart {
         for (int mt = 0; mt < kPagesPerTile; ++mt) {
             const float p0 = fast_exp2(s[mt][0] - ref0), p1 = fast_exp2(s[mt][1] - ref1);
             const float p2 = fast_exp2(s[mt][2] - ref0), p3 = fast_exp2(s[mt][3] - ref1);
-            l0 = fmaf(p0 + p2, wl[mt], l0);
-            l1 = fmaf(p1 + p3, wl[mt], l1);
+            if (may_be_far && far) {
+                // P 2^(m - r - e) while that factor is at most 2^64: what P loses is then 2^-62 of l.  (e at most 126 for blocks that are
+                // not finite: their tokens are masked, or make the sum NaN, and d, which may be infinite, must not meet 0.)
+                const float over = power_of_two(-min(e[mt], 126)), w0 = d0 * over, w1 = d1 * over;
+                if (fmaxf(w0, w1) <= 0x1p64f) {
+                    l0 = fmaf(p0 + p2, w0, l0);
+                    l1 = fmaf(p1 + p3, w1, l1);
+                } else {
+                    const float z0 = (float)e[mt] + (r0 == -INFINITY ? 0.f : r0), z1 = (float)e[mt] + (r1 == -INFINITY ? 0.f : r1);
+                    l0 += fast_exp2(s[mt][0] - z0) + fast_exp2(s[mt][2] - z0);
+                    l1 += fast_exp2(s[mt][1] - z1) + fast_exp2(s[mt][3] - z1);
+                }
+            } else {
+                l0 = fmaf(p0 + p2, wl[mt], l0);
+                l1 = fmaf(p1 + p3, wl[mt], l1);
+            }
             pb[mt][0] = movmatrix_trans(k8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1));          // tokens 0..7 of the page
             pb[mt][1] = movmatrix_trans(k8 ? pack_f16x2(p2, p3) : pack_bf16x2(p2, p3));          // tokens 8..15
         }
@@ -506,11 +581,20 @@ struct PairPart {
                 }
             }
         });
+        return true;
     }
 
-    // Sum l over the lanes that share a column.
+    // l against m as O is, 2^-5 of it, and summed over the lanes that share a column.
     __device__ __forceinline__ void finish()
     {
+        if constexpr (k8) {
+            // in two halves: a factor may lie below fp32's range where l lies as far above
+            const float k = K == kNoStep ? 0.f : (float)K;
+            const float h0 = fast_exp2(0.5f * ((far && m0 > -INFINITY ? r0 - m0 : -k) - (float)kCacheSumBias));
+            const float h1 = fast_exp2(0.5f * ((far && m1 > -INFINITY ? r1 - m1 : -k) - (float)kCacheSumBias));
+            l0 = l0 * h0 * h0;
+            l1 = l1 * h1 * h1;
+        }
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, x);
@@ -571,11 +655,23 @@ struct PairPart {
 struct FoldSum {
     float m, l;
     float4 acc;
+
+    // w = 2^x.  8-bit: in two halves, since a partial of small steps has an l as much larger as the factor is small; its O is small.
+    template <bool k8>
+    __device__ __forceinline__ void add_l(float l_i, float x, float w)
+    {
+        if constexpr (k8) {
+            const float half = fast_exp2(0.5f * x);
+            l += l_i * half * half;
+        } else {
+            l += w * l_i;
+        }
+    }
 };
 
 // Partial i is at(i), in shared or global memory, for i in the list: list(i) is the one behind i (>= n: none), and
 // candidates of the maximum are spread over the lanes.
-template <int D, typename At, typename Next>
+template <int D, bool k8, typename At, typename Next>
 __device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at, Next next)
 {
     using Part = PartLayout<D>;
@@ -589,7 +685,7 @@ __device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at, 
     for (int i = next(-1); i < n; i = next(i)) {
         const float *part = at(i);
         const float w = fast_exp2(part[col] - ref);
-        f.l += w * part[kMaxGroup + col];
+        f.add_l<k8>(part[kMaxGroup + col], part[col] - ref, w);
         if (lane * 4 < D) {
             const float4 a = *(const float4 *)(part + Part::kHead + col * Part::kPitch + lane * 4);
             f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;
@@ -598,10 +694,10 @@ __device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at, 
     return f;
 }
 
-template <int D, typename At>
+template <int D, bool k8, typename At>
 __device__ __forceinline__ FoldSum fold_column(int n, int col, int lane, At at)
 {
-    return fold_column<D>(n, col, lane, at, [](int i) { return i + 1; });
+    return fold_column<D, k8>(n, col, lane, at, [](int i) { return i + 1; });
 }
 
 template <int D>
@@ -846,7 +942,7 @@ cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
         float *slot = p.part + (size_t)(2 * blockIdx.x + (c.first == blockIdx.x ? 1 : 0)) * Part::kFloats;
         for (int col = 0; col < ncols; ++col) {
             if (turn++ % W != warp) continue;
-            const FoldSum f = fold_column<D>(
+            const FoldSum f = fold_column<D, k8>(
                 2 * W, col, lane,
                 [&](int i) -> const float * {
                     return i & 1 ? (const float *)(smem + i / 2 * Shape::Layout::kRingBytes) : p.part + (size_t)(2 * gridDim.x + blockIdx.x * W + i / 2) * Part::kFloats;
@@ -867,9 +963,9 @@ cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
 // ------------------------------------------------------------------------------------------
 constexpr int kFoldGroups = 4;
 
-template <int D>
+template <int D, bool k8>
 __global__ void __launch_bounds__(kMaxGroup * kFoldGroups * 32)
-cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
+cache_attn_fold_kernel(const CacheAttnParams p)
 {
     using Part = PartLayout<D>;
     __shared__ __align__(16) float s_part[kFoldGroups][Part::kFloats];
@@ -881,7 +977,7 @@ cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
     if (cut.x < 0) return;
     const int n = cut.z - first + 1;
     if (col < p.q_pass * p.group) {
-        const FoldSum f = fold_column<D>((n - group + kFoldGroups - 1) / kFoldGroups, col, lane, [&](int i) -> const float * {
+        const FoldSum f = fold_column<D, k8>((n - group + kFoldGroups - 1) / kFoldGroups, col, lane, [&](int i) -> const float * {
             const int cta = first + group + i * kFoldGroups;
             return p.part + (size_t)(2 * cta + (cta == first ? 1 : 0)) * Part::kFloats;
         });
@@ -889,7 +985,7 @@ cache_attn_fold_kernel(const CacheAttnParams p, const float bias)
     }
     __syncthreads();
     if (group == 0 && col < p.q_pass * p.group)
-        store_fold<D>(p, cut.x, cut.y, col, fold_column<D>(kFoldGroups, col, lane, [&](int i) -> const float * { return s_part[i]; }), bias, lane);
+        store_fold<D>(p, cut.x, cut.y, col, fold_column<D, k8>(kFoldGroups, col, lane, [&](int i) -> const float * { return s_part[i]; }), sum_bias<k8>(), lane);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -977,7 +1073,7 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");          // every CTA of the cluster runs
     // ---- the CTA's fold, a column a warp; the results go to the CTA that looks after the column, column c to CTA c % ctas
     for (int col = warp; col < ncols; col += W) {
-        const FoldSum f = fold_column<D>(W, col, lane, [&](int i) -> const float * { return (const float *)(smem + i * Shape::Layout::kRingBytes); });
+        const FoldSum f = fold_column<D, k8>(W, col, lane, [&](int i) -> const float * { return (const float *)(smem + i * Shape::Layout::kRingBytes); });
         if (ctas == 1) {
             store_fold<D>(p, r, h, col, f, sum_bias<k8>(), lane);
             continue;
@@ -1001,7 +1097,7 @@ cache_attn_pair_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
         const float ref = f.m == -INFINITY ? 0.f : f.m;
         for (int c = 0; c < ctas; ++c) {
             const float w = fast_exp2(part[c][D] - ref);
-            f.l += w * part[c][D + 1];
+            f.add_l<k8>(part[c][D + 1], part[c][D] - ref, w);
             if (lane * 4 < D) {
                 const float4 a = *(const float4 *)(part[c] + lane * 4);
                 f.acc.x += w * a.x; f.acc.y += w * a.y; f.acc.z += w * a.z; f.acc.w += w * a.w;

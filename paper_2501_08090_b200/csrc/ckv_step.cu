@@ -104,8 +104,7 @@ int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *s
     for (ap.q_base = 0; ap.q_base < ap.q_len; ap.q_base += per_pass) {
         ap.q_pass = std::min(per_pass, ap.q_len - ap.q_base);
         CKV_CUDA(enqueue(span, ctas, Span::kWarps * 32, Span::Layout::kSmemBytes, pool->overlap, 0, stream, pool->tmap, ap));
-        CKV_CUDA(enqueue(ckv::cache_attn_fold_kernel<D>, ctas, ckv::kMaxGroup * ckv::kFoldGroups * 32, 0, pool->overlap, 0, stream, ap,
-                         k8 ? std::ldexp(1.f, -ckv::kCacheSumBias) : 1.f));
+        CKV_CUDA(enqueue(ckv::cache_attn_fold_kernel<D, k8>, ctas, ckv::kMaxGroup * ckv::kFoldGroups * 32, 0, pool->overlap, 0, stream, ap));
         pool->launches += 2;
     }
     return CKV_OK;
