@@ -334,7 +334,8 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  *                     rows are left as they were.
  *   kv8_attention     decode_attention_multi over the 8-bit cache; window and sink as below, window 0: the whole context.
  *                     Products see the cache's values exactly; a query's elements are rounded to 2^-21 of its
- *                     largest, weights to fp16 for the product with V.  A query with an infinity or a NaN gives NaN.
+ *                     largest, a weight for the product with V to 2^-22 of it or 2^-25 of the largest weight times step among
+ *                     the tokens seen.  A query with an infinity or a NaN gives NaN.
  * Errors: CKV_EINVAL, CKV_ENOMEM, CKV_ECUDA.
  */
 size_t kv8_pool_bytes(const ckv_config *cfg);
@@ -362,6 +363,7 @@ int32_t kv8_attention(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_le
  * q_len * (num_q_heads / num_kv_heads) > 8, as there.  All inputs may come from the kernel that directly
  * precedes the call.  ckv_set_partition, ckv_profile_* and the span timeline do not apply.  The workspace belongs to
  * the handle: as with every attention call, two calls on one handle must not overlap on the GPU.
+ * Weights are rounded to 2^-15 of each for the product with V (decode_attention and its kin: to bf16).
  * Results are bit-identical from run to run.  Errors: CKV_EINVAL, CKV_ECUDA.
  */
 int32_t decode_attention_window(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_len, const int32_t *d_block_tables,

@@ -39,12 +39,16 @@ namespace ckv {
 // exact).
 // V's steps: the contribution of token t to O is 2^(s_t - m) step_t n_t, so with e_t = log2(step_t) the weights
 // P_t = 2^(s_t + e_t - M), M the running maximum of s + e, are at most 2^8 whatever the steps are, and
-// l = sum_t P_t 2^-e_t.  They are rounded to fp16 (2^-11, or 2^-25 of the reference where that is more) for P V and summed unrounded in fp32.
+// l = sum_t P_t 2^-e_t, in fp32.
 // A warp sums l 2^K, K the e of its first page: the factor is 2^(K - e_t), and while every |e_t - K| <= 30 what P_t loses below 2^-126
 // is 2^-66 of l.  With steps further apart it would not do: tokens of a block of zeros, whose step is 2^-106, count in l
 // as any others, and their P_t vanish beside a large step's.  From the first such page on (`far` below) l is summed against a reference r
 // of its own, the running maximum of s alone.
-// In the bf16 cache weights are rounded to bf16 as everywhere in this library (the instruction takes one type).
+//
+// Weights for P V.  The instruction takes them in V's type, bf16 or fp16, so each goes in as two numbers, its rounding and the rounding
+// of what that leaves, in two products: 2^-15 or 2^-22 of a weight is lost (fp16: 2^-25 of the reference where that is more), where
+// one product lost 2^-8 or 2^-11 and outputs of values that cancel were off by as much of what was summed.  It costs 1 % of
+// the bf16 windows' time and 2 to 4 % of the 8-bit cache's (64 contexts of 1024 to 16384 tokens 176.5 -> 180.6 us).
 //
 // Masked values.  A masked score is selected away, and a masked row of the bf16 cache too: its weight is 0, but
 // 0 * inf is not, so in a tile that some column does not see entirely the product is formed once a new token,
@@ -229,6 +233,25 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
     uint32_t d;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
+}
+
+// Two weights as the product with V takes them, and what that leaves of them.
+template <bool k8>
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t &weights, uint32_t &rest)
+{
+    if constexpr (k8) {
+        const uint32_t w = pack_f16x2(p0, p1);
+        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+        weights = movmatrix_trans(w);
+        rest = movmatrix_trans(pack_f16x2(p0 - x.x, p1 - x.y));
+    } else {
+        // cut, not rounded, and 2^-23 of the weight added to what is left, so that this is above 0 wherever the weight is: an infinite
+        // value that is seen has to stay infinite, which times 0 or a negative rest it would not
+        constexpr float kMore = 1.f + 0x1p-23f;
+        const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+        weights = movmatrix_trans(__byte_perm(b0, b1, 0x7632));
+        rest = movmatrix_trans(pack_bf16x2(fmaf(p0, kMore, -__uint_as_float(b0 & 0xffff0000u)), fmaf(p1, kMore, -__uint_as_float(b1 & 0xffff0000u))));
+    }
 }
 
 // ldmatrix at addr + kOffset.  Volatile: ordered behind the waits for the tile.
@@ -512,7 +535,7 @@ struct PairPart {
             for (int c = 0; c < kSteps16; ++c) { o[c][0] *= al0; o[c][2] *= al0; o[c][1] *= al1; o[c][3] *= al1; }
         }
         const float ref0 = m0 == -INFINITY ? 0.f : m0, ref1 = m1 == -INFINITY ? 0.f : m1;
-        uint32_t pb[kPagesPerTile][2];
+        uint32_t pb[kPagesPerTile][2], rest[kPagesPerTile][2];   // weights as the product takes them, and what that rounding leaves
 #pragma unroll
         for (int mt = 0; mt < kPagesPerTile; ++mt) {
             const float p0 = fast_exp2(s[mt][0] - ref0), p1 = fast_exp2(s[mt][1] - ref1);
@@ -533,8 +556,8 @@ struct PairPart {
                 l0 = fmaf(p0 + p2, wl[mt], l0);
                 l1 = fmaf(p1 + p3, wl[mt], l1);
             }
-            pb[mt][0] = movmatrix_trans(k8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1));          // tokens 0..7 of the page
-            pb[mt][1] = movmatrix_trans(k8 ? pack_f16x2(p2, p3) : pack_bf16x2(p2, p3));          // tokens 8..15
+            split_weights<k8>(p0, p1, pb[mt][0], rest[mt][0]);   // tokens 0..7 of the page
+            split_weights<k8>(p2, p3, pb[mt][1], rest[mt][1]);   // tokens 8..15
         }
         // ---- O^T += V^T P^T
         unrolled<kPagesPerTile>([&](auto page) {
@@ -548,9 +571,11 @@ struct PairPart {
                     records_to_half(x[0], lo0, hi0);
                     records_to_half(x[1], lo1, hi1);
                     mma_16816<k8>(o[c], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
+                    mma_16816<k8>(o[c], lo0, hi0, lo1, hi1, rest[mt][0], rest[mt][1]);
                     records_to_half(x[2], lo0, hi0);
                     records_to_half(x[3], lo1, hi1);
                     mma_16816<k8>(o[c + 1], lo0, hi0, lo1, hi1, pb[mt][0], pb[mt][1]);
+                    mma_16816<k8>(o[c + 1], lo0, hi0, lo1, hi1, rest[mt][0], rest[mt][1]);
                 });
             } else if constexpr (all_seen) {
                 unrolled<kSteps16>([&](auto step) {
@@ -558,6 +583,7 @@ struct PairPart {
                     uint32_t a[4];
                     ldmatrix_x4_trans_at<mt * kPageBytes + (c / 4) * kHalfBytes>(a, v_at ^ (c % 4 << 5));
                     mma_16816<k8>(o[c], a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                    mma_16816<k8>(o[c], a[0], a[1], a[2], a[3], rest[mt][0], rest[mt][1]);
                 });
             } else {
 #pragma unroll 1
@@ -575,6 +601,7 @@ struct PairPart {
                         a[0] &= keep[0]; a[1] &= keep[0]; a[2] &= keep[1]; a[3] &= keep[1];
                         float x[4] = {0.f, 0.f, 0.f, 0.f};       // other tokens' columns may hold anything
                         mma_16816<k8>(x, a[0], a[1], a[2], a[3], pb[mt][0], pb[mt][1]);
+                        mma_16816<k8>(x, a[0], a[1], a[2], a[3], rest[mt][0], rest[mt][1]);
                         if (i0 == i) { o[c][0] += x[0]; o[c][2] += x[2]; }
                         if (i1 == i) { o[c][1] += x[1]; o[c][3] += x[3]; }
                     });
