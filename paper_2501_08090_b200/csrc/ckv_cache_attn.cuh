@@ -664,7 +664,7 @@ struct PairPart {
         elements(lane, 1.f, 1.f, [&](int g, int d, float x, float y) { *(float2 *)(part + Part::kHead + g * Part::kPitch + d) = make_float2(x, y); });
     }
 
-    // To the output.
+    // To the output.  A warp that gave up leaves NaN here too.
     __device__ __forceinline__ void store_out(const CacheAttnParams &p, int r, int h, int lane, bool alive) const
     {
         const int G = p.group, heads = p.num_kv_heads * G, ncols = p.q_pass * G;
@@ -673,7 +673,7 @@ struct PairPart {
         // (O bias) / l: with the largest steps O / l alone would overflow
         elements(lane, bias, bias, [&](int g, int d, float x, float y) {
             const float inv = 1.f / ((g & 1) ? l1 : l0);
-            if (alive && g < ncols) *(uint32_t *)(rows + ((size_t)(g / G) * heads + g % G) * D + d) = pack_bf16x2(x * inv, y * inv);
+            if (g < ncols) *(uint32_t *)(rows + ((size_t)(g / G) * heads + g % G) * D + d) = alive ? pack_bf16x2(x * inv, y * inv) : 0x7fff7fffu;
         });
     }
 };
