@@ -110,12 +110,18 @@ __device__ __forceinline__ int warp_sum(int x)
     return x;
 }
 
-// The units of a span, and the first tile among them.  By one whole warp.
-__device__ __forceinline__ long long span_units(const CacheAttnParams &p, int lane)
+// The units of a span, of all spans, and whether a length is unusable; then the first tile among a span's.  By one whole warp.
+__device__ __forceinline__ long long span_units(const CacheAttnParams &p, int lane, long long &total, bool &unusable)
 {
     int sum = 0;
-    for (int r = lane; r < p.batch; r += 32) sum += units_of(visited_pages(__ldg(p.seq_lens + r), p));
-    const long long total = (long long)warp_sum(sum) * p.num_kv_heads;
+    bool none = false;
+    for (int r = lane; r < p.batch; r += 32) {
+        const int units = units_of(visited_pages(__ldg(p.seq_lens + r), p));
+        sum += units;
+        none |= units == 0;
+    }
+    unusable = __any_sync(0xffffffffu, none);
+    total = (long long)warp_sum(sum) * p.num_kv_heads;
     return max((long long)kCacheMinUnits, (total + p.num_spans - 1) / p.num_spans);
 }
 
@@ -745,19 +751,24 @@ __device__ __forceinline__ void store_fold_partial(float *part, int col, const F
     if (lane * 4 < D) *(float4 *)(part + Part::kHead + col * Part::kPitch + lane * 4) = f.acc;
 }
 
-// Requests of unusable length: rows cleared, status.  By one warp of the grid.
+// Requests of unusable length: rows cleared, status.  By all warps of the grid, a request each in turn: 4000 idle slots of 32 heads x 128
+// beside three contexts of 40000 tokens took 666 us by one warp and with requests passed over one by one, 105 so (56 without them).
 template <int D>
-__device__ __forceinline__ void clear_unusable(const CacheAttnParams &p, int lane)
+__device__ __forceinline__ void clear_unusable(const CacheAttnParams &p, int span, int lane)
 {
     const int heads = p.num_kv_heads * p.group, row_elems = p.q_pass * heads * D;
+    if (span == 0 && lane == 0) atomicOr(p.status, kStatusBadLength);
+    int upto = 0;                                // such requests before `base`
     for (int base = 0; base < p.batch; base += 32) {
         const int r = base + lane;
-        unsigned todo = __ballot_sync(0xffffffffu, r < p.batch && visited_pages(__ldg(p.seq_lens + r), p).tiles == 0);
-        if (todo && lane == 0) atomicOr(p.status, kStatusBadLength);
+        const unsigned gone = __ballot_sync(0xffffffffu, r < p.batch && visited_pages(__ldg(p.seq_lens + r), p).tiles == 0);
+        const int place = upto + __popc(gone & ((1u << lane) - 1u));
+        unsigned todo = __ballot_sync(0xffffffffu, (gone >> lane & 1u) && place % p.num_spans == span);
         for (; todo; todo &= todo - 1) {
             uint4 *row = (uint4 *)(p.out + ((size_t)(base + __ffs(todo) - 1) * p.q_len + p.q_base) * heads * D);
             for (int i = lane; i < row_elems / 8; i += 32) row[i] = make_uint4(0u, 0u, 0u, 0u);
         }
+        upto += __popc(gone);
     }
 }
 
@@ -867,8 +878,10 @@ cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
     grid_launch_dependents();
     if (threadIdx.x == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
 
-    if (span == 0) clear_unusable<D>(p, lane);
-    const long long q_units = span_units(p, lane), begin = span * q_units, end = begin + q_units;
+    long long total;
+    bool unusable;
+    const long long q_units = span_units(p, lane, total, unusable), begin = span * q_units, end = min(begin + q_units, total);
+    if (unusable) clear_unusable<D>(p, span, lane);
     TilePlace ic = span_begin(p, begin, end, lane);              // the next tile to fetch
     TilePlace cc = ic;                                           // the next to compute
 
@@ -893,11 +906,20 @@ cache_attn_span_kernel(const __grid_constant__ CUtensorMap tmap, const CacheAttn
         if (at.v >= end) return false;
         if (++at.h < p.num_kv_heads) return true;
         at.h = 0;
-        do {
-            if (++at.r >= p.batch) return false;
-            at.L = __ldg(p.seq_lens + at.r);
+        if (++at.r >= p.batch) return false;
+        at.L = __ldg(p.seq_lens + at.r);
+        at.vis = visited_pages(at.L, p);
+        while (at.vis.tiles == 0) {              // idle slots, 32 at a time
+            const int r = at.r + lane, L = r < p.batch ? __ldg(p.seq_lens + r) : 0;
+            const unsigned live = __ballot_sync(0xffffffffu, r < p.batch && visited_pages(L, p).tiles != 0);
+            if (live == 0u) {
+                if ((at.r += 32) >= p.batch) return false;
+                continue;
+            }
+            at.r += __ffs(live) - 1;
+            at.L = __shfl_sync(0xffffffffu, L, __ffs(live) - 1);
             at.vis = visited_pages(at.L, p);
-        } while (at.vis.tiles == 0);
+        }
         return true;
     };
     bool more = ic.r >= 0;
