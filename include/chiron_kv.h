@@ -415,7 +415,7 @@ int32_t kv_pages_release(ckv_pool *pool, int32_t batch, const int32_t *d_block_t
  *                a NaN or plus infinity among what is allowed makes the row NaN
  *   probs == 0:  x_v, minus infinity where excluded; the temperature is left to whoever forms probabilities
  *   d_logits, d_out   [batch][rows] rows of `vocab` (1 .. 262128), their strides (>= vocab) apart, CKV_PROBS_F32 or CKV_PROBS_BF16 each;
- *                     d_out may be d_logits (same type and stride), otherwise they do not overlap
+ *                     d_out may be d_logits (same type and stride), otherwise its rows overlap neither theirs nor another argument
  *   d_params          fp32 [batch][4]: repetition, presence, frequency, temperature; NULL: 1, 0, 0, 1
  *   d_history         int32 [batch][history_stride], all of it readable; row r holds history_lens[r] tokens (0 .. history_stride), the
  *                     first prompt_lens[r] of them the prompt.  NULL: none.  Tokens outside the vocabulary (-1) count for nothing

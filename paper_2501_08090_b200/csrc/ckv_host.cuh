@@ -4,8 +4,10 @@
 
 #include "chiron_kv.h"
 
+#include <algorithm>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <vector>
 
 #include "ckv_common.cuh"
@@ -122,6 +124,51 @@ inline bool overlap(const void *a, long long na, const void *b, long long nb)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x && y && x < y + (uintptr_t)nb * 4 && y < x + (uintptr_t)na * 4;
 }
+
+// `n` rows of `row` bytes, `stride` >= row bytes apart where there are several.  NULL: none.
+struct ByteRows {
+    const void *ptr;
+    long long row, stride, n;
+};
+
+// Whether a row of one shares a byte with a row of the other: rows of one may lie between the other's.
+inline bool overlap(const ByteRows &a, const ByteRows &b)
+{
+    if (!a.ptr || !b.ptr || a.n < 1 || b.n < 1 || a.row < 1 || b.row < 1) return false;
+    const long long at_a = (long long)reinterpret_cast<uintptr_t>(a.ptr), at_b = (long long)reinterpret_cast<uintptr_t>(b.ptr);
+    const long long step_a = a.n > 1 ? a.stride : a.row, step_b = b.n > 1 ? b.stride : b.row;
+    if (at_a + (a.n - 1) * step_a + a.row <= at_b || at_b + (b.n - 1) * step_b + b.row <= at_a) return false;
+    if (a.n > 1 && b.n > 1 && step_a == step_b) {
+        // row j of b begins at_b - at_a + (j - i) step behind row i of a: the least difference of rows that lets it begin above -b.row
+        const long long d = at_b - at_a, x = -b.row - d;
+        const long long k = std::max((x >= 0 ? x / step_a : -((-x + step_a - 1) / step_a)) + 1, 1 - a.n);
+        return k <= b.n - 1 && d + k * step_a < a.row;
+    }
+    // in order of address, from the first row that does not end before the other's begin
+    long long i = std::max(0ll, (at_b - at_a - a.row) / step_a), j = std::max(0ll, (at_a - at_b - b.row) / step_b);
+    while (i < a.n && j < b.n) {
+        const long long p = at_a + i * step_a, q = at_b + j * step_b;
+        if (p + a.row <= q) ++i;
+        else if (q + b.row <= p) ++j;
+        else return true;
+    }
+    return false;
+}
+
+// Memory that a call writes, against what it reads or writes elsewhere.
+struct NamedRows {
+    const char *name;
+    ByteRows rows;
+};
+
+inline int32_t check_apart(const char *fn, const NamedRows &written, std::initializer_list<NamedRows> others)
+{
+    for (const NamedRows &x : others)
+        if (overlap(written.rows, x.rows)) return fail(CKV_EINVAL, "%s: %s overlaps %s", fn, written.name, x.name);
+    return CKV_OK;
+}
+
+inline ByteRows whole(const void *p, long long bytes) { return {p, bytes, bytes, 1}; }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -17,7 +17,9 @@ using ckv::allow;
 using ckv::check_call;
 using ckv::enqueue;
 using ckv::fail;
+using ckv::check_apart;
 using ckv::overlap;
+using ckv::whole;
 
 namespace {
 
@@ -399,10 +401,18 @@ int32_t logits_process(int32_t batch, int32_t rows, int32_t vocab, int32_t in_dt
     const uintptr_t in_size = in_dtype == CKV_PROBS_F32 ? 4 : 2, out_size = out_dtype == CKV_PROBS_F32 ? 4 : 2;
     const uintptr_t in_at = reinterpret_cast<uintptr_t>(d_logits), out_at = reinterpret_cast<uintptr_t>(d_out);
     if (in_at % in_size != 0 || out_at % out_size != 0) return fail(CKV_EINVAL, "%s: logits or out not aligned to their type", fn);
-    const long long n = (long long)batch * rows;
-    const uintptr_t in_end = in_at + ((n - 1) * logits_stride + vocab) * in_size, out_end = out_at + ((n - 1) * out_stride + vocab) * out_size;
-    if (in_at < out_end && out_at < in_end && !(in_at == out_at && in_dtype == out_dtype && (n == 1 || logits_stride == out_stride)))
+    const long long n = (long long)batch * rows, words = (vocab + 31) / 32;
+    const ckv::NamedRows out = {"out", {d_out, (long long)(vocab * out_size), (long long)(out_stride * out_size), n}};
+    if (!(in_at == out_at && in_dtype == out_dtype && (n == 1 || logits_stride == out_stride)) &&
+        overlap(out.rows, {d_logits, (long long)(vocab * in_size), (long long)(logits_stride * in_size), n}))
         return fail(CKV_EINVAL, "%s: out overlaps the logits without being them", fn);
+    // what other blocks may still be reading
+    if (int32_t rc = check_apart(fn, out, {{"params", whole(d_params, 16ll * batch)}, {"history", whole(d_history, 4ll * batch * history_stride)},
+                                           {"prompt_lens", whole(d_history ? d_prompt_lens : nullptr, 4ll * batch)},
+                                           {"history_lens", whole(d_history ? d_history_lens : nullptr, 4ll * batch)},
+                                           {"drafts", whole(d_drafts, 4ll * batch * (rows - 1))}, {"bias_ids", whole(d_bias_ids, 4ll * batch * n_bias)},
+                                           {"bias", whole(d_bias, 4ll * batch * n_bias)}, {"mask", {d_mask, 4 * words, 4 * mask_stride, n}}}))
+        return rc;
     ckv::LogitsParams lp{};
     lp.logits = d_logits;
     lp.out = d_out;
