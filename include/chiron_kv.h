@@ -326,12 +326,13 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  *                     kv8_* calls refuse a bf16 handle: CKV_EINVAL.
  *   kv8_append        kv_append_rope into the 8-bit cache: the same arguments and rules; keys are rounded to bf16 after the
  *                     rotation, then quantised.  d_inv_freq NULL: nothing is rotated, d_q and d_q_out are NULL too.
+ *                     A d_q_out whose rows overlap another argument's (d_q, but for being it, among them): CKV_EINVAL.
  *   kv8_gather        the values of each request's last tokens, row by row as kv8_append takes them:
  *                     d_start int32 [batch + 1], request r's rows start[r] .. start[r+1] - 1 (NULL: n_tokens / batch
  *                     each) receive its tokens at positions seq_lens[r] - n_r .. seq_lens[r] - 1.  d_k, d_v: bf16 rows
  *                     [n_tokens][Hkv][head_dim], 16-byte aligned, each with its own stride.  Rows of a request of
  *                     unusable length (status bit), or of a page id outside the pool (status bit), are zero-filled; other
- *                     rows are left as they were.
+ *                     rows are left as they were.  Rows of d_k and d_v overlap neither one another nor the lists.
  *   kv8_attention     decode_attention_multi over the 8-bit cache; window and sink as below, window 0: the whole context.
  *                     Products see the cache's values exactly; a query's elements are rounded to 2^-21 of its
  *                     largest, a weight for the product with V to 2^-22 of it or 2^-25 of the largest weight times step among
@@ -358,7 +359,8 @@ int32_t kv8_attention(ckv_pool *pool, int32_t layer, int32_t batch, int32_t q_le
  * generations that keep their cost per token constant.  As decode_attention_multi, but new token i of request r,
  * at position p = seq_lens[r] - q_len + i, sees token t <= p only if t > p - window or t < sink.  Pages in which
  * no new token of a launch sees anything are not read, and their table entries neither.
- *   d_q, d_out   bf16 [batch][q_len][num_q_heads][head_dim], 16-byte aligned; 1 <= q_len <= 8; window >= 1, sink >= 0
+ *   d_q, d_out   bf16 [batch][q_len][num_q_heads][head_dim], 16-byte aligned; 1 <= q_len <= 8; window >= 1, sink >= 0.
+ *                d_out may be d_q; otherwise it overlaps neither d_q nor the tables nor the lengths (kv8_attention's likewise)
  * What a token does not see does not reach it, infinities and NaN among it.  Several launches where
  * q_len * (num_q_heads / num_kv_heads) > 8, as there.  All inputs may come from the kernel that directly
  * precedes the call.  ckv_set_partition, ckv_profile_* and the span timeline do not apply.  The workspace belongs to

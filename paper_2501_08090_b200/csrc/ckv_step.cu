@@ -121,6 +121,11 @@ int32_t cache_attention(ckv_pool *pool, const char *fn, int bits, int32_t layer,
     if (!d_block_tables || !d_seq_lens || !d_q || !d_out) return fail(CKV_EINVAL, "%s: NULL argument", fn);
     if (!aligned16(d_q) || !aligned16(d_out)) return fail(CKV_EINVAL, "%s: q/out not 16-byte aligned", fn);
     const ckv_config &c = pool->cfg;
+    const long long rows = 2ll * batch * q_len * c.num_q_heads * c.head_dim;
+    if (int32_t rc = check_apart(fn, {"out", whole(d_out, rows)},
+                                 {{"q", d_out == d_q ? ckv::ByteRows{} : whole(d_q, rows)}, {"block_tables", whole(d_block_tables, 4ll * batch * c.max_pages_per_req)},
+                                  {"seq_lens", whole(d_seq_lens, 4ll * batch)}}))
+        return rc;
     ckv::CacheAttnParams ap{};
     ap.block_tables = d_block_tables;
     ap.seq_lens = d_seq_lens;
@@ -260,6 +265,13 @@ int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
         return rc;
     if (d_q && d_q_out == d_q && n_tokens > 1 && q_out_stride != q_stride)
         return fail(CKV_EINVAL, "%s: q_out in place of q must have its stride", fn);
+    const ckv::ByteRows q_rows = {d_q, 2 * q_row, 2 * q_stride, n_tokens};
+    if (int32_t rc = check_apart(fn, {"q_out", {d_q_out, 2 * q_row, 2 * q_out_stride, n_tokens}},
+                                 {{"q", d_q_out == d_q ? ckv::ByteRows{} : q_rows}, {"k_new", {d_k_new, 2 * kv_row, 2 * k_stride, n_tokens}},
+                                  {"v_new", {d_v_new, 2 * kv_row, 2 * v_stride, n_tokens}}, {"block_tables", whole(d_block_tables, 4ll * batch * c.max_pages_per_req)},
+                                  {"seq_lens", whole(d_seq_lens, 4ll * batch)}, {"new_start", whole(d_new_start, 4ll * batch + 4)},
+                                  {"inv_freq", whole(d_inv_freq, 2ll * rotary_dim)}}))
+        return rc;
     ckv::Append8Params ap{};
     ckv::RopeParams &rp = ap.rope;
     rp.q = static_cast<const uint16_t *>(d_q);
@@ -312,6 +324,11 @@ int32_t kv8_gather(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
     if (!d_k || !d_v) return fail(CKV_EINVAL, "%s: NULL argument", fn);
     const int64_t row = (int64_t)c.num_kv_heads * c.head_dim;
     if (int32_t rc = check_rows(fn, n_tokens, {{"k", d_k, k_stride, row}, {"v", d_v, v_stride, row}})) return rc;
+    const ckv::NamedRows k_rows = {"k", {d_k, 2 * row, 2 * k_stride, n_tokens}}, v_rows = {"v", {d_v, 2 * row, 2 * v_stride, n_tokens}};
+    const ckv::NamedRows tables = {"block_tables", whole(d_block_tables, 4ll * batch * c.max_pages_per_req)}, lens = {"seq_lens", whole(d_seq_lens, 4ll * batch)},
+                         start = {"start", whole(d_start, 4ll * batch + 4)};
+    if (int32_t rc = check_apart(fn, k_rows, {v_rows, tables, lens, start})) return rc;
+    if (int32_t rc = check_apart(fn, v_rows, {tables, lens, start})) return rc;
     ckv::Gather8Params gp{};
     gp.records = layer_records(pool, layer);
     gp.steps = all_steps(pool) + layer * blocks_of(c);
