@@ -316,9 +316,15 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  *   m = max |x| of the block's new rows;  need = 2^(floor(log2 max(m, 2^-100)) - 6)
  *   a = 0: step = need;  a > 0: step = max(the block's step, need), and where it grew the records of slots 0 .. a-1 are
  *   multiplied by old / new step and rounded;  record = x / step, rounded, cut to -127 .. 127
- * (nearest, ties to even).  So |record * step - x| <= step / 2 and m / 128 < step <= m / 64, and a block's bits depend on
- * its rows and on which calls appended them, not on the launch.  An infinity or a NaN among the rows makes the
- * block's step NaN, and with it every value of the block, until slot 0 of its page is written again.
+ * (nearest, ties to even).  A block's bits depend on its rows and on which calls appended them, not on the launch.
+ * m / 128 < need <= m / 64 where m >= 2^-100; rows below that, zeros among them, need 2^-106.  The step may be above need where a > 0.
+ * |record * step - x| <= step / 2 for the rows that a call writes.  Older rows are rounded again whenever the step grows: they stay
+ * below one step off, of the step as it is then (half of each step so far, every one at most half of the next).
+ * An infinity or a NaN among the rows makes the block's step NaN, and with it every value of the block, until slot 0
+ * of its page is written again.
+ * Rows that are cut off again (rejected drafts; kv_pages_release) leave the step as they made it: larger ones have cost the rows before
+ * them in the page bits that do not come back, and one that was not finite makes these NaN too.  In a bf16 cache they are
+ * simply written over.  Where drafts are of another size than what is kept, append what is accepted, after the verification.
  *
  *   kv8_pool_create   a handle like kv_pool_create's, over d_cache (256-byte aligned, kv8_pool_bytes()) and a workspace of
  *                     kv_workspace_bytes(), of up to 2047 query heads.  It is destroyed, checked (kv_check_status), and set (ckv_set_overlap) as any
