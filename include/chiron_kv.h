@@ -324,7 +324,7 @@ int32_t draft_verify(int32_t batch, int32_t max_draft, int32_t vocab, int32_t dt
  * of its page is written again.
  * Rows that are cut off again (rejected drafts; kv_pages_release) leave the step as they made it: larger ones have cost the rows before
  * them in the page bits that do not come back, and one that was not finite makes these NaN too.  In a bf16 cache they are
- * simply written over.  Where drafts are of another size than what is kept, append what is accepted, after the verification.
+ * simply written over.
  *
  *   kv8_pool_create   a handle like kv_pool_create's, over d_cache (256-byte aligned, kv8_pool_bytes()) and a workspace of
  *                     kv_workspace_bytes(), of up to 2047 query heads.  It is destroyed, checked (kv_check_status), and set (ckv_set_overlap) as any
@@ -424,7 +424,7 @@ int32_t kv_pages_release(ckv_pool *pool, int32_t batch, const int32_t *d_block_t
  *   probs == 0:  x_v, minus infinity where excluded; the temperature is left to whoever forms probabilities
  *   d_logits, d_out   [batch][rows] rows of `vocab` (1 .. 262128), their strides (>= vocab) apart, CKV_PROBS_F32 or CKV_PROBS_BF16 each;
  *                     d_out may be d_logits (same type and stride), otherwise its rows overlap neither theirs nor another argument
- *   d_params          fp32 [batch][4]: repetition, presence, frequency, temperature; NULL: 1, 0, 0, 1
+ *   d_params          fp32 [batch][4]: repetition, presence, frequency, temperature; NULL: 1, 0, 0, 1, and no history and no drafts
  *   d_history         int32 [batch][history_stride], all of it readable; row r holds history_lens[r] tokens (0 .. history_stride), the
  *                     first prompt_lens[r] of them the prompt.  NULL: none.  Tokens outside the vocabulary (-1) count for nothing
  *   d_drafts          int32 [batch][rows - 1]; NULL: none
