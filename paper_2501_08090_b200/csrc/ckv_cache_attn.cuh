@@ -71,9 +71,10 @@ struct CacheAttnParams {
     float scale_log2;               // log2(e) / sqrt(d)
 };
 
-// Units that a piece costs besides its tiles, and the fewest that a span holds: few short contexts are not cut
-// into more partials than their tiles are worth.
-constexpr int kCacheCost = 3, kCacheMinUnits = 4;
+// Units that a piece costs besides its tiles.  Measured with 1, 2, 3, 4, 6, us, 8-bit: 64 contexts of 1 to 4096 tokens 68.9, 59.9, 57.7,
+// 56, 59; 400 of 1 to 300 62.7, 54.8, 54, 52, 54; 64 of 1024 to 16384 180 to 182.  Spans may be of one unit: held to 4, so that few short
+// contexts are cut into fewer partials, 4 contexts of 1 to 1024 tokens took 14.2 instead of 10.0.
+constexpr int kCacheCost = 4;
 
 // The pages of a context that a launch reads.
 struct Visited {
@@ -122,7 +123,7 @@ __device__ __forceinline__ long long span_units(const CacheAttnParams &p, int la
     }
     unusable = __any_sync(0xffffffffu, none);
     total = (long long)warp_sum(sum) * p.num_kv_heads;
-    return max((long long)kCacheMinUnits, (total + p.num_spans - 1) / p.num_spans);
+    return max(1ll, (total + p.num_spans - 1) / p.num_spans);
 }
 
 __device__ __forceinline__ TilePlace span_begin(const CacheAttnParams &p, long long begin, long long end, int lane)
@@ -841,9 +842,9 @@ struct TileRing {
 // Even spans of all pairs' tiles.
 //
 // Warps: what their rings hold is in flight, 128 KB an SM with eight warps of the 8-bit kernel.  More streams at once cost
-// bandwidth: 64 contexts of 8700 tokens (1.14 GB) take 177 us with eight warps of two stages (99 % of a copy's rate), 180
-// with eight of three, 189 with ten of two, 193 with twelve of two, 220 with six of two.  In long runs the GPU's power limit
-// holds them at 184 to 199 us.
+// bandwidth: 64 contexts of 8700 tokens (1.14 GB) take 181 us with eight warps of two stages (97 % of a copy's rate), 180
+// with eight of three (contexts of 1024 to 16384 181 and 182), 190 with ten of two, 191 with twelve of two, 240 with six of two.  In
+// long runs the GPU's power limit holds them at 195 to 214 us.
 // ------------------------------------------------------------------------------------------
 template <int D, bool k8>
 struct SpanShape {
@@ -1040,10 +1041,10 @@ cache_attn_fold_kernel(const CacheAttnParams p)
 // ------------------------------------------------------------------------------------------
 // A cluster of CTAs per pair and block of new tokens; q_pass: new tokens of a block.
 //
-// Windows of 2048 of 64 requests, 8 kv heads x 128: bf16 (538 MB) 78.6 us, a copy's rate and what neighbours find in L2; 8-bit
-// (270 MB) 46.5 us, 89 % of it, the rest start and fold.  Four warps a CTA instead of six: 56 us in 8 bits.  One request's
-// window of 512 in 8 bits takes 4.9 us, launch and a chain of look-ups, tiles and folds (5.3 while the cluster's CTAs read each
-// other's partials between two barriers, where they now push them before one).
+// Windows of 2048 of 64 requests, 8 kv heads x 128: bf16 (538 MB) 78.7 us, a copy's rate and what neighbours find in L2; 8-bit
+// (270 MB) 48.6 us, 85 % of it, the rest start and fold.  Four warps a CTA instead of six: 81.9 and 52.5.  One request's
+// window of 512 in 8 bits takes 5.1 us, launch and a chain of look-ups, tiles and folds (with the cluster's CTAs reading each
+// other's partials between two barriers, where they push them before one, 0.4 more).
 // ------------------------------------------------------------------------------------------
 template <int D, bool k8>
 struct PairShape {

@@ -77,8 +77,9 @@ int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *s
     }
     // The most tiles that a pair can have, and the clusters that own pairs: as many CTAs as its tiles feed, while all
     // clusters run at once, with room for those of a call before that have not ended; without that room where a
-    // warp would have more than 5 tiles else.  Windows of 2048 of 2 requests, 8 kv heads, 8-bit: 8 CTAs a pair 6.7 us, 16, which do not all run at
-    // once, 10.3; of 4 requests, bf16: 4 CTAs (3 tiles a warp) 9.6, 8, which just do, 12.0; of 8 requests: 2 (6) 14.6, 4 14.0.
+    // warp would have more than 5 tiles else.  Windows of 2048, 8 kv heads, with 1, 2, 4, 8, 16 CTAs a pair, us: 2 requests, 8-bit, 10.7, 11.6, 8.0,
+    // 7.2, 10.8 (16 do not all run at once); 4 requests, bf16, 13.4, 12.4, 10.0 (3 tiles a warp), 11.6, 16.8; 8 requests, bf16, 17.8,
+    // 15.0, 14.4, 20.9, 27.9; 16 requests, 8-bit, 21.7, 17.3, 22.6, 32.8, 51.5.  Taken: 8, 4, 4, 2.
     const long long table = ap.max_pages_per_req;
     const long long cut = ((long long)ap.window + ap.q_len + ckv::kPageSize - 2) / ckv::kPageSize + 1 + ckv::pages_of(ap.sink);
     const bool windowed = ap.window > 0 && cut < table;
@@ -92,9 +93,11 @@ int32_t launch_cache_attention(ckv_pool *pool, ckv::CacheAttnParams &ap, void *s
     const unsigned cluster = 1u << size;
     // Pairs that a window cuts are of one length, nearly: a cluster owns each, if the clusters fill the GPU.  Otherwise that
     // pays while a warp has few tiles: the even spans cost 4 us before they win.  Measured, us, pairs against spans: windows of
-    // 2048 of 64 requests, bf16 78.9 and 88.3, 8-bit 46.4 and 51.5; one request, 8-bit, of 16384 tokens (5 tiles a warp) 14.8
-    // and 16.6, of 32000 (10) 23.1 and 20.9; 64 requests of 1 to 1024 tokens (at most 5) 21.5 and 24.2, of 1 to 4096 (21)
-    // 60.6 and 51.7.
+    // 2048 of 64 requests, bf16 78.9 and 90.1, 8-bit 48.8 and 54.6; one request, 8-bit, of 16384 tokens (5 tiles a warp) 15.4
+    // and 17.2, of 32000 (10) 23.7 and 21.8; 64 requests of 1 to 1024 tokens (at most 5) 23.4 and 24.7, of 1 to 2048 (11)
+    // 37.4 and 35.1; 400 of 1 to 300 57.3 and 52.7 (bf16 57.7 and 53.9), where the rule is on the wrong side.
+    // The host knows the table's width and not the lengths: under one of 8192 pages, 64 requests of 1 to 1024 tokens take
+    // the spans (25.1), and 4 of them 10.0 instead of 6.5.
     if (tiles <= 8ll * cluster * Pair::kWarps || (windowed && blocks * cluster > pool->num_sms)) {
         ap.q_pass = per_pass;
         CKV_CUDA(enqueue(pair, (unsigned)(blocks * cluster), Pair::kWarps * 32, Pair::Layout::kSmemBytes, pool->overlap, cluster, stream, pool->tmap, ap));
