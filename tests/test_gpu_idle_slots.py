@@ -46,6 +46,25 @@ def test_rows_of_idle_slots(kind, layout, q_len, idle):
 
 
 @pytest.mark.parametrize("kind", [test_gpu_cache8.Cache, test_gpu_window.Cache])
+@pytest.mark.parametrize("batch,lens", [(1, [0]), (70, [0]), (2000, [0, -1]), (65, [0] * 64 + [1]), (65, [1] + [0] * 64)])
+def test_all_slots_idle_or_all_but_one(kind, batch, lens):
+    lens = (lens * batch)[:batch]
+    bt, n = tables_for(lens, 9000, 7)
+    c = kind((8, 2, 64), bt, n, seed=8)
+    q = torch.zeros(batch, 8, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 5.0)
+    before = c.kp.launch_count()
+    attend(c, torch.tensor(lens, dtype=torch.int32, device="cuda"), q, out)
+    assert c.kp.launch_count() - before == 2 and c.kp.check_status(raise_on_error=False) == c.b.STATUS_BAD_LENGTH
+    live = torch.tensor(lens) == 1
+    assert not out[~live.cuda()].any()
+    for r in torch.nonzero(live).flatten().tolist():         # one token: its value
+        v = c.values(r, 1)[0, :, 1] if kind is test_gpu_cache8.Cache else c.pool[bt[r, 0], :, 1, 0]
+        assert torch.equal(out[r].double().cpu(), torch.from_numpy(v).repeat_interleave(4, 0))
+    c.kp.close()
+
+
+@pytest.mark.parametrize("kind", [test_gpu_cache8.Cache, test_gpu_window.Cache])
 def test_time_of_idle_slots(kind):
     """4000 of them, 32 heads x 128: 33 MB of zeros, 5 us at the memory's rate; one warp took 500."""
     B = 4003
