@@ -216,7 +216,7 @@ kv8_append_kernel(const Append8Params p)
         for (int f = lane; f < half; f += 32) {
             const double turns = (double)(column * kPageSize + a + i) * (double)__ldg(rp.inv_freq + f) * 0.15915494309189533577;     // 1 / (2 pi)
             float c, s;
-            sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+            cosine_sine(turns, c, s);
             s_cos[i][f] = c * rp.scale;
             s_sin[i][f] = s * rp.scale;
         }

@@ -12,8 +12,8 @@ namespace ckv {
 //
 // The angle grows with the position: in 32 bits t * inv_freq loses 2^-24 of up to 10^5 radians.  So
 // the product is formed in 64 bits, in whole turns, and its fraction (within half a turn) goes to
-// sincospif as fp32: the cosine's error stays near 2^-23 at any position.  Each product is rounded
-// once to bf16.
+// sincospif as fp32, what that rounding leaves by one step of the sums of angles: both stay within a few 2^-24 of themselves at any
+// position, where they are near 0 too (without that step they were 2^-24 off in absolute terms).  Each product is rounded once to bf16.
 //
 // Layout of the work.  A CTA owns kTokens consecutive tokens: one where they are few, four in long
 // prompts, where finding each token's request, page and sines would otherwise hold up its loads.  A
@@ -57,6 +57,17 @@ __device__ __forceinline__ int request_of_token(const int32_t *__restrict__ new_
 
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+
+// Of an angle in whole turns.
+__device__ __forceinline__ void cosine_sine(double turns, float &c, float &s)
+{
+    const double halves = 2. * (turns - rint(turns));
+    const float x = (float)halves, rest = (float)(halves - (double)x) * 3.14159265f;
+    float sine, cosine;
+    sincospif(x, &sine, &cosine);
+    c = fmaf(-rest, sine, cosine);
+    s = fmaf(rest, cosine, sine);
+}
 
 template <int D, bool kInterleaved, int kTokens>
 __global__ void __launch_bounds__(256, kTokens == 1 ? 4 : 5)
@@ -125,7 +136,7 @@ kv_append_rope_kernel(const RopeParams p)
         const int tok = kTokens == 1 ? 0 : j / half, f = kTokens == 1 ? j : j % half;
         const double turns = (double)max(s_pos[tok], 0) * (double)__ldg(p.inv_freq + f) * 0.15915494309189533577;     // 1 / (2 pi)
         float c, s;
-        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+        cosine_sine(turns, c, s);
         s_cos[tok][f] = c * p.scale;
         s_sin[tok][f] = s * p.scale;
     }
