@@ -25,7 +25,7 @@ namespace ckv {
 // block's are on their way before the page is looked up.
 //
 // Prompts are bound by HBM: 32909 tokens of 32 + 8 + 8 heads x 128 (741 MB) 118 us, 96 % of a copy's rate.  Few tokens by launch,
-// look-ups and instructions: one token 2.6 us, five of 96 requests with 64 query heads 7.5, 3.7 without queries.
+// look-ups and instructions: one token 2.7 us, five of 96 requests with 64 query heads 7.5, 3.7 without queries.
 struct Append8Params {
     RopeParams rope;                // pool_layer unused; inv_freq NULL: nothing is turned; q NULL: no queries
     uint8_t *records;               // the layer's records
@@ -176,7 +176,7 @@ kv8_append_kernel(const Append8Params p)
     const int u = lane % U, half = rp.inv_freq != nullptr ? rp.rotary / 2 : 0;
     const bool turned = 8 * u < half;
     const int e0 = kInterleaved || !turned ? 16 * u : 8 * u, e1 = kInterleaved || !turned ? 16 * u + 8 : half + 8 * u;
-    // who takes query rows: from the last warp on, since the first ones have blocks before (one token 2.6 us instead of 3.3)
+    // who takes query rows: from the last warp on, since the first ones have blocks before (one token 2.7 us instead of 3.3)
     const int row_threads = p.parts * kAppend8Warps * kRows, row_thread = row_threads - 1 - (part * kAppend8Warps * 32 + (int)threadIdx.x) / U;
     if (tiles_of_length(t.L, rp.max_pages_per_req, t.n) == 0) {  // unusable: the request's rows of q_out are cleared, 16 a page's CTAs
         if (threadIdx.x == 0) atomicOr(rp.status, kStatusBadLength);

@@ -302,7 +302,7 @@ int32_t kv8_append(ckv_pool *pool, int32_t layer, int32_t batch, int32_t n_token
     const auto kernel = c.head_dim == 128 ? (interleaved ? ckv::kv8_append_kernel<128, true> : ckv::kv8_append_kernel<128, false>)
                                           : (interleaved ? ckv::kv8_append_kernel<64, true> : ckv::kv8_append_kernel<64, false>);
     // where pages are few, several CTAs a page, as far as they fit the GPU at a time: their blocks and query rows are chains of
-    // look-ups and loads (one token 3.4 us in one CTA, 2.6 in several); twice as far with query rows (five tokens of 96 requests:
+    // look-ups and loads (one token 3.4 us in one CTA, 2.7 in several); twice as far with query rows (five tokens of 96 requests:
     // 8.5 us in two CTAs a page, 7.8 in four; without queries 3.9 and 4.7)
     const unsigned pages = page_ctas(d_new_start, n_tokens, batch);
     ap.parts = 1;
